@@ -38,7 +38,8 @@
  *   - Beyond the four stage calls there are: whole-path calls (msa_prefill_forward,
  *     msa_prefill_forward_varlen, msa_decode_forward and their *_host forms), the fused
  *     Eq. 6 + Eq. 7 call msa_index_topk_fused (top_k <= 16), and the index branch's
- *     log-sum-exp msa_index_lse_prefill (Section 4.3).
+ *     log-sum-exp msa_index_lse_prefill (Section 4.3).  Around the path: msa_qk_norm_rope and
+ *     its backward, msa_paged_append, msa_paged_attn.
  */
 #ifndef MSA_H_
 #define MSA_H_
@@ -400,6 +401,100 @@ msa_status_t msa_decode_forward_host(const msa_shape_t* shape, const void* q_hos
                                      void* out_host, void* workspace, size_t workspace_bytes,
                                      msa_stream_t stream);
 
+/* ------------------------------------------------------------------------------------
+ * Around the path (the paper takes finished Q, K, V and describes no cache layout): norms of
+ * queries and keys with the position rotation, a paged K/V cache, and dense attention of new
+ * tokens over it - what Eq. 8 computes when k * B_k covers the context.
+ *
+ * Rotation.  Pair i < rot_dim/2 of a head (elements i and i + rot_dim/2, or 2i and 2i+1 with
+ * interleaved = 1) turns by the angle position * freqs[i]; elements from rot_dim on stay.
+ * freqs holds rot_dim/2 fp64 values in DEVICE memory, so any scaling rule for long contexts is
+ * a matter of its values; mscale multiplies the rotated elements.  Angles are reduced in 64 bits.
+ * rot_dim is a multiple of 16 (8 when interleaved) and at most the head size; 0 = no rotation.
+ */
+typedef struct {
+    const double* freqs;
+    int32_t rot_dim;
+    int32_t interleaved;
+    float mscale;
+} msa_rope_t;
+
+/*
+ * For every token t and head h (d = head_dim elements, multiple of 8, at most 256):
+ *   n = x * rsqrt(mean(x^2) + eps) * weight     (weight NULL: n = x)
+ *   out = the rotation of n by positions[t]     (rope NULL: out = n)
+ * q rows of n_q_heads * d bf16 start every q_stride elements (a multiple of 8, at least
+ * n_q_heads * d: slices of a fused projection need no copy), likewise k; outputs are dense.
+ * Weights are d bf16, or d fp32 with weight_fp32 = 1.  Sums and products are fp32, rounded once.
+ * positions: int64 [n_tokens], any value (NULL allowed when nothing rotates).  Either tensor
+ * may be absent (0 heads).  An output may be its own input when that one is dense.
+ */
+msa_status_t msa_qk_norm_rope(const msa_rope_t* rope, const void* q, int64_t q_stride, int32_t n_q_heads,
+                              const void* q_weight, const void* k, int64_t k_stride, int32_t n_k_heads,
+                              const void* k_weight, int32_t head_dim, int32_t weight_fp32, float eps,
+                              const int64_t* positions, int64_t n_tokens, void* q_out, void* k_out,
+                              msa_stream_t stream);
+
+/*
+ * Gradients of msa_qk_norm_rope: dq_out, dk_out (rows every dq_stride / dk_stride elements) are
+ * the gradients of its outputs; dq, dk (bf16, dense) those of its inputs; dq_weight, dk_weight
+ * (fp32 [d]; may be NULL, and untouched without a weight) those of its weights, summed over
+ * tokens and heads in a fixed order (equal calls give equal bits).  q and k are read only where
+ * there is a weight.  dq may be dq_out when that one is dense.
+ * workspace >= msa_qk_norm_rope_backward_workspace_bytes (0 bytes without weights).
+ */
+msa_status_t msa_qk_norm_rope_backward(const msa_rope_t* rope, const void* dq_out, int64_t dq_stride,
+                                       const void* dk_out, int64_t dk_stride, const void* q, int64_t q_stride,
+                                       int32_t n_q_heads, const void* q_weight, const void* k, int64_t k_stride,
+                                       int32_t n_k_heads, const void* k_weight, int32_t head_dim,
+                                       int32_t weight_fp32, float eps, const int64_t* positions,
+                                       int64_t n_tokens, void* dq, void* dk, float* dq_weight, float* dk_weight,
+                                       void* workspace, size_t workspace_bytes, msa_stream_t stream);
+msa_status_t msa_qk_norm_rope_backward_workspace_bytes(int32_t head_dim, int64_t n_tokens, size_t* min_bytes);
+
+/*
+ * A paged cache and the batch that uses it.  k and v are pools [n_pages, page_size, n_kv_heads,
+ * head_dim] of bf16, or fp8 E4M3 with fp8 = 1 (decoded exactly, as everywhere in this library).
+ * Token t of sequence s lives in row t mod page_size of page page_table[s * max_pages + t /
+ * page_size].  The new tokens of the call are packed rows: those of sequence s are rows
+ * [cu_q[s], cu_q[s+1]) (cu_q int32 [batch+1], not decreasing, cu_q[0] = 0) and the last tokens of
+ * its kv_lens[s] (int32 [batch], the new ones included).  All index arrays are in DEVICE
+ * memory, so a captured graph follows their values.  Rows from cu_q[batch] on (a padded batch)
+ * are left as they are in every output.  With pages in order a sequence is the contiguous cache
+ * of msa_decode_forward (row offset = first page * page_size).
+ * A page outside [0, n_pages), a length beyond max_pages * page_size or a new token in front of
+ * position 0 is reported through the async status as a bad index and never followed.
+ */
+typedef struct {
+    void* k;
+    void* v;
+    const int32_t* page_table;
+    const int32_t* kv_lens;
+    const int32_t* cu_q;
+    int32_t batch;
+    int32_t max_pages;
+    int32_t n_pages;
+    int32_t page_size;
+    int32_t n_kv_heads;
+    int32_t head_dim;
+    int32_t fp8;
+} msa_paged_cache_t;
+
+/*
+ * Writes the new tokens' keys (norm with k_weight, rotation by their positions in the sequence;
+ * either may be absent as in msa_qk_norm_rope) and values (as they are) to their places in the
+ * cache, and the new tokens' queries, treated like the keys, to q_out [n_tokens, n_q_heads, d]
+ * bf16.  One launch.  fp8 caches take the nearest E4M3 value (beyond the range: the largest).
+ * n_tokens >= cu_q[batch] rows of q, k, v with strides as in msa_qk_norm_rope; n_q_heads = 0: no
+ * queries.  v and cache->v may both be NULL (a cache of index keys: one head, no values).
+ * Two new tokens must not share a place (page tables that alias the written pages): which one
+ * stays is then undefined.  A token without a valid place is not stored; its query is still written.
+ */
+msa_status_t msa_paged_append(const msa_paged_cache_t* cache, const msa_rope_t* rope, const void* q,
+                              int64_t q_stride, int32_t n_q_heads, const void* q_weight, const void* k,
+                              int64_t k_stride, const void* k_weight, const void* v, int64_t v_stride,
+                              int32_t weight_fp32, float eps, int64_t n_tokens, void* q_out, msa_stream_t stream);
+
 /*
  * Test hook for the device-side bounded waits (the paper has no counterpart).  Every wait of a
  * kernel on an mbarrier gives up after a limit of SM cycles (about two seconds by default),
@@ -419,7 +514,7 @@ int64_t msa_launch_count(void);
  * Optional per-stage timing for benchmarks (the paper has no counterpart).  Between
  * msa_profile_begin() and msa_profile_end() every kernel launch of the library is
  * bracketed by CUDA events on its stream; msa_profile_end() synchronises the device and
- * returns, per stage, the summed device time in milliseconds and the number of launches
+ * returns, per stage of the path, the summed device time in milliseconds and the number of launches
  * (arrays of 9: 0 index scoring, 1 top-k, 2 reverse index/schedule, 3 prefill attention,
  * 4 combine, 5 decode index scoring, 6 decode attention, 7 decode combine, 8 index-branch
  * log-sum-exp).  The first

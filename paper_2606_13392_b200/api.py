@@ -1,9 +1,10 @@
 """Convenience layer over the binding: allocates outputs/workspaces with torch and calls the
-C ABI.  No arithmetic happens here."""
+C ABI.  No arithmetic happens here (but for the table of frequencies of rope_frequencies)."""
 
 from __future__ import annotations
 
-from typing import Dict, Optional
+import math
+from typing import Dict, NamedTuple, Optional
 
 import torch
 
@@ -123,3 +124,97 @@ def decode_forward(cfg: MSAConfig, x: Dict[str, torch.Tensor]):
                          x["k_cache"].shape[0], x["seq_offsets"], x["seq_lens"], batch, max_len,
                          scores, ld, block_idx, out, lse, ws)
     return out, lse, block_idx, scores
+
+
+# ------------------------------------------------------------------ around the path
+class Rope(NamedTuple):
+    """A position rotation: fp64 radians per position of each pair (on the device), the pairs' layout (elements i and
+    i + n, or 2i and 2i+1), and a factor on the rotated elements."""
+    freqs: torch.Tensor
+    interleaved: bool = False
+    mscale: float = 1.0
+
+
+class PagedCache(NamedTuple):
+    """Pools [pages, page size, KV heads, d] (bf16 or float8_e4m3fn; v may be None), the pages of each sequence int32
+    [batch, pages], its length with the new tokens int32 [batch], and the first new row of each int32 [batch + 1]."""
+    k: torch.Tensor
+    v: Optional[torch.Tensor]
+    page_table: torch.Tensor
+    kv_lens: torch.Tensor
+    cu_q: torch.Tensor
+
+
+_NO_ROPE = Rope(None)
+
+
+def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                     original_len: int = 4096, low: float = 1.0, high: float = 32.0, device="cuda") -> torch.Tensor:
+    """fp64 frequencies base^(-2i/rot_dim) of a rotation of rot_dim elements, stretched for contexts `factor` times
+    the original length: "linear" divides all by factor; "base" raises the base so that the slowest pair turns factor
+    times slower and the fastest as before; "bands" keeps pairs that turn more than `high` times within original_len,
+    divides those that turn fewer than `low` times, and blends linearly in the number of turns between."""
+    i = torch.arange(rot_dim // 2, dtype=torch.float64)
+    if scaling == "base":
+        if rot_dim > 2:
+            base = base * factor ** (rot_dim / (rot_dim - 2))
+    elif scaling not in ("none", "linear", "bands"):
+        raise ValueError("unknown scaling %r" % scaling)
+    f = base ** (-2.0 * i / rot_dim)
+    if scaling == "linear":
+        f = f / factor
+    elif scaling == "bands":
+        keep = ((original_len * f / (2 * math.pi) - low) / (high - low)).clamp(0.0, 1.0)
+        f = f * keep + f / factor * (1 - keep)
+    return f.to(device)
+
+
+def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: Optional[torch.Tensor],
+                 rope: Optional[Rope] = None, q_weight: Optional[torch.Tensor] = None,
+                 k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, q_out: Optional[torch.Tensor] = None,
+                 k_out: Optional[torch.Tensor] = None):
+    """Norm of each head (where there is a weight) and position rotation of q and k [rows, heads, d], which may be
+    slices of one projection; either may be None -> (q_out, k_out), dense."""
+    if q_out is None and q is not None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if k_out is None and k is not None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    freqs, interleaved, mscale = rope or _NO_ROPE
+    B.msa_qk_norm_rope(freqs, interleaved, mscale, q, q_weight, k, k_weight, eps, positions, q_out, k_out)
+    return q_out, k_out
+
+
+def qk_norm_rope_backward(dq_out: Optional[torch.Tensor], dk_out: Optional[torch.Tensor], q: Optional[torch.Tensor],
+                          k: Optional[torch.Tensor], positions: Optional[torch.Tensor], rope: Optional[Rope] = None,
+                          q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+                          eps: float = 1e-6):
+    """Gradients of qk_norm_rope's inputs for those of its outputs -> (dq, dk, dq_weight, dk_weight); the weights'
+    are fp32, None without a weight."""
+    dy = dq_out if dq_out is not None else dk_out
+    dev, d = dy.device, dy.shape[2]
+    dq = None if dq_out is None else torch.empty(dq_out.shape, dtype=torch.bfloat16, device=dev)
+    dk = None if dk_out is None else torch.empty(dk_out.shape, dtype=torch.bfloat16, device=dev)
+    dwq = None if q_weight is None else torch.empty(d, dtype=torch.float32, device=dev)
+    dwk = None if k_weight is None else torch.empty(d, dtype=torch.float32, device=dev)
+    ws = None
+    if dwq is not None or dwk is not None:
+        with torch.cuda.device(dev):
+            ws = B.alloc_workspace(B.msa_qk_norm_rope_backward_workspace_bytes(d, dy.shape[0]), dev)
+    freqs, interleaved, mscale = rope or _NO_ROPE
+    B.msa_qk_norm_rope_backward(freqs, interleaved, mscale, dq_out, dk_out, q, q_weight, k, k_weight, eps, positions, dq, dk,
+                                dwq, dwk, ws)
+    return dq, dk, dwq, dwk
+
+
+def paged_append(cache: PagedCache, k: torch.Tensor, v: Optional[torch.Tensor], q: Optional[torch.Tensor] = None,
+                 rope: Optional[Rope] = None, q_weight: Optional[torch.Tensor] = None,
+                 k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, q_out: Optional[torch.Tensor] = None):
+    """Writes the new tokens' keys (normed, turned) and values into the cache and returns their queries, treated like
+    the keys (None without queries).  Rows behind the last sequence are left as they are (uninitialised in a q_out
+    made here)."""
+    if q_out is None and q is not None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    freqs, interleaved, mscale = rope or _NO_ROPE
+    B.msa_paged_append(cache.k, cache.v, cache.page_table, cache.kv_lens, cache.cu_q, freqs, interleaved, mscale, q, q_weight, k,
+                       k_weight, v, eps, q_out)
+    return q_out

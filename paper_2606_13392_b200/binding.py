@@ -33,6 +33,7 @@ EXPORTS = [
     "msa_prefill_forward_varlen_workspace_bytes", "msa_prefill_forward_host",
     "msa_prefill_forward_host_workspace_bytes", "msa_decode_forward", "msa_decode_forward_host",
     "msa_launch_count", "msa_profile_begin", "msa_profile_end", "msa_index_scores_plan", "msa_debug_set_wait",
+    "msa_qk_norm_rope", "msa_qk_norm_rope_backward", "msa_qk_norm_rope_backward_workspace_bytes", "msa_paged_append",
 ]
 
 
@@ -41,6 +42,16 @@ class MsaShape(ctypes.Structure):
                 ("idx_dim", c_i32), ("block_size", c_i32), ("top_k", c_i32),
                 ("softmax_scale", ctypes.c_float), ("index_scale", ctypes.c_float),
                 ("idx_fp8", c_i32), ("kv_fp8", c_i32), ("q_fp8", c_i32), ("score_runs", c_i32)]
+
+
+class MsaRope(ctypes.Structure):
+    _fields_ = [("freqs", c_vp), ("rot_dim", c_i32), ("interleaved", c_i32), ("mscale", ctypes.c_float)]
+
+
+class MsaPagedCache(ctypes.Structure):
+    _fields_ = [("k", c_vp), ("v", c_vp), ("page_table", c_vp), ("kv_lens", c_vp), ("cu_q", c_vp), ("batch", c_i32),
+                ("max_pages", c_i32), ("n_pages", c_i32), ("page_size", c_i32), ("n_kv_heads", c_i32),
+                ("head_dim", c_i32), ("fp8", c_i32)]
 
 
 class MsaError(RuntimeError):
@@ -360,6 +371,167 @@ def msa_decode_forward_host(shape, q_host, q_idx_host, q_dev, q_idx_dev, k_cache
                                          _dev(out_dev), _host(out_host), _dev(workspace),
                                          c_sz(workspace.numel() * workspace.element_size()),
                                          _stream(stream)), "msa_decode_forward_host")
+
+
+# ------------------------------------------------------------------ around the path
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _launch(device: torch.device, name: str, *args, stream=None) -> None:
+    """Calls the library with `device` current (the tensors' own, whatever the caller's is) on its current stream."""
+    fn = getattr(lib(), name)
+    if device.index != torch.cuda.current_device():
+        with torch.cuda.device(device):
+            _check(fn(*args, _stream(stream)), name)
+    else:
+        _check(fn(*args, _stream(stream)), name)
+
+
+def _heads(t: torch.Tensor, what: str, head_dim: int, rows: int, device: torch.device, dense: bool = False) -> int:
+    """A bf16 tensor [rows, heads, head_dim] whose heads are dense; returns its row stride."""
+    _need(t.dtype == torch.bfloat16 and t.device == device, "%s must be bf16 on %s" % (what, device))
+    _need(t.dim() == 3 and t.shape[0] == rows and t.shape[2] == head_dim,
+          "%s must be [%d, heads, %d], got %s" % (what, rows, head_dim, tuple(t.shape)))
+    s, width = t.stride(), t.shape[1] * head_dim
+    # (strides of dimensions with fewer than two entries say nothing)
+    _need((t.shape[2] < 2 or s[2] == 1) and (t.shape[1] < 2 or s[1] == head_dim),
+          "the last two dimensions of %s must be dense" % what)
+    if rows < 2:
+        return width
+    _need(s[0] == width or not dense, "%s must be contiguous" % what)
+    return s[0]
+
+
+def _weights(head_dim: int, device: torch.device, *weights) -> int:
+    """Checks the weights of the norms (None: no norm); 1 if they are fp32, 0 if bf16."""
+    kinds = {w.dtype for w in weights if w is not None}
+    _need(len(kinds) < 2 and kinds <= {torch.bfloat16, torch.float32}, "norm weights must be all bf16 or all fp32")
+    for w in weights:
+        _need(w is None or (w.shape == (head_dim,) and w.is_contiguous() and w.device == device),
+              "norm weights must be contiguous vectors of head_dim values on %s" % device)
+    return 1 if torch.float32 in kinds else 0
+
+
+def _rope(freqs, interleaved, mscale, device: torch.device):
+    if freqs is None:
+        return None
+    _need(freqs.dtype == torch.float64 and freqs.dim() == 1 and freqs.is_contiguous() and freqs.device == device,
+          "frequencies must be a contiguous fp64 vector on %s" % device)
+    return MsaRope(freqs.data_ptr(), 2 * freqs.shape[0], 1 if interleaved else 0, mscale)
+
+
+def _positions(positions, rows: int, device: torch.device):
+    if positions is not None:
+        _need(positions.dtype == torch.int64 and positions.shape == (rows,) and positions.is_contiguous() and
+              positions.device == device, "positions must be a contiguous int64 vector, one for each row, on %s" % device)
+    return c_vp(None if positions is None else positions.data_ptr())
+
+
+def _at(t: Optional[torch.Tensor]) -> c_vp:
+    return c_vp(None if t is None else t.data_ptr())
+
+
+def _ref(s):
+    return None if s is None else ctypes.byref(s)
+
+
+def msa_qk_norm_rope(freqs, interleaved, mscale, q, q_weight, k, k_weight, eps, positions, q_out, k_out, stream=None):
+    """q, k: bf16 [rows, heads, d], rows may be strided; either may be None.  freqs None: no rotation."""
+    x = q if q is not None else k
+    _need(x is not None and x.is_cuda, "a tensor on a CUDA device is needed")
+    dev, rows, d = x.device, x.shape[0], x.shape[2] if x.dim() == 3 else 0
+    qs = ks = 0
+    if q is not None:
+        qs = _heads(q, "q", d, rows, dev)
+        _need(q_out.shape == q.shape, "q_out must have q's shape")
+        _heads(q_out, "q_out", d, rows, dev, dense=True)
+    if k is not None:
+        ks = _heads(k, "k", d, rows, dev)
+        _need(k_out.shape == k.shape, "k_out must have k's shape")
+        _heads(k_out, "k_out", d, rows, dev, dense=True)
+    w32 = _weights(d, dev, q_weight, k_weight)
+    rope = _rope(freqs, interleaved, mscale, dev)
+    _launch(dev, "msa_qk_norm_rope", _ref(rope), _at(q), c_i64(qs), c_i32(q.shape[1] if q is not None else 0), _at(q_weight),
+            _at(k), c_i64(ks), c_i32(k.shape[1] if k is not None else 0), _at(k_weight), c_i32(d), c_i32(w32),
+            ctypes.c_float(eps), _positions(positions, rows, dev), c_i64(rows), _at(q_out), _at(k_out), stream=stream)
+
+
+def msa_qk_norm_rope_backward_workspace_bytes(head_dim: int, n_tokens: int) -> int:
+    mn = c_sz(0)
+    _check(lib().msa_qk_norm_rope_backward_workspace_bytes(c_i32(head_dim), c_i64(n_tokens), ctypes.byref(mn)),
+           "msa_qk_norm_rope_backward_workspace_bytes")
+    return int(mn.value)
+
+
+def msa_qk_norm_rope_backward(freqs, interleaved, mscale, dq_out, dk_out, q, q_weight, k, k_weight, eps, positions, dq,
+                              dk, dq_weight, dk_weight, workspace, stream=None):
+    """q / k are needed where there is a weight (else None is fine); dq, dk bf16 dense, weight gradients fp32 [d]."""
+    x = dq_out if dq_out is not None else dk_out
+    _need(x is not None and x.is_cuda, "a tensor on a CUDA device is needed")
+    dev, rows, d = x.device, x.shape[0], x.shape[2] if x.dim() == 3 else 0
+    strides = []
+    for n, dy, t, w, dx, dw in (("q", dq_out, q, q_weight, dq, dq_weight), ("k", dk_out, k, k_weight, dk, dk_weight)):
+        if dy is None:
+            strides += [0, 0]
+            continue
+        strides.append(_heads(dy, "d%s_out" % n, d, rows, dev))
+        _need(w is None or t is not None, "%s is needed for the gradients of its norm" % n)
+        strides.append(0 if t is None else _heads(t, n, d, rows, dev))
+        _need((t is None or t.shape == dy.shape) and dx.shape == dy.shape, "%s and its gradients must have one shape" % n)
+        _heads(dx, "d%s" % n, d, rows, dev, dense=True)
+        _need(dw is None or (dw.dtype == torch.float32 and dw.shape == (d,) and dw.is_contiguous() and dw.device == dev),
+              "d%s_weight must be a contiguous fp32 vector of head_dim values on %s" % (n, dev))
+    w32 = _weights(d, dev, q_weight, k_weight)
+    rope = _rope(freqs, interleaved, mscale, dev)
+    _need(workspace is None or (workspace.is_contiguous() and workspace.device == dev), "workspace must be on %s" % dev)
+    _launch(dev, "msa_qk_norm_rope_backward", _ref(rope), _at(dq_out), c_i64(strides[0]), _at(dk_out), c_i64(strides[2]), _at(q),
+            c_i64(strides[1]), c_i32(dq_out.shape[1] if dq_out is not None else 0), _at(q_weight), _at(k), c_i64(strides[3]),
+            c_i32(dk_out.shape[1] if dk_out is not None else 0), _at(k_weight), c_i32(d), c_i32(w32), ctypes.c_float(eps),
+            _positions(positions, rows, dev), c_i64(rows), _at(dq), _at(dk), _at(dq_weight), _at(dk_weight), _at(workspace),
+            c_sz(0 if workspace is None else workspace.numel() * workspace.element_size()), stream=stream)
+
+
+def _paged(k_pool, v_pool, page_table, kv_lens, cu_q):
+    """The cache structure of checked tensors."""
+    _need(k_pool.is_cuda and k_pool.dim() == 4 and k_pool.is_contiguous() and
+          k_pool.dtype in (torch.bfloat16, torch.float8_e4m3fn),
+          "the key pool must be a contiguous [pages, page size, KV heads, head_dim] tensor of bf16 or float8_e4m3fn on a CUDA device")
+    dev = k_pool.device
+    _need(v_pool is None or (v_pool.shape == k_pool.shape and v_pool.dtype == k_pool.dtype and v_pool.is_contiguous() and
+                             v_pool.device == dev), "the value pool must be like the key pool")
+    _need(page_table.dim() == 2 and kv_lens.dim() == 1 and cu_q.dim() == 1 and kv_lens.shape[0] == page_table.shape[0] and
+          cu_q.shape[0] == kv_lens.shape[0] + 1, "page_table [batch, pages], kv_lens [batch] and cu_q [batch + 1] must agree")
+    for n, t in (("page_table", page_table), ("kv_lens", kv_lens), ("cu_q", cu_q)):
+        _need(t.dtype == torch.int32 and t.is_contiguous() and t.device == dev, "%s must be contiguous int32 on %s" % (n, dev))
+    pages, size, heads, d = k_pool.shape
+    return MsaPagedCache(k_pool.data_ptr(), 0 if v_pool is None else v_pool.data_ptr(), page_table.data_ptr(),
+                         kv_lens.data_ptr(), cu_q.data_ptr(), kv_lens.shape[0], page_table.shape[1], pages, size, heads, d,
+                         1 if k_pool.dtype == torch.float8_e4m3fn else 0)
+
+
+def msa_paged_append(k_pool, v_pool, page_table, kv_lens, cu_q, freqs, interleaved, mscale, q, q_weight, k, k_weight, v,
+                     eps, q_out, stream=None):
+    """k, v (and q): bf16 [rows, heads, d], rows may be strided; q None: no queries; v None: a cache without values."""
+    cache = _paged(k_pool, v_pool, page_table, kv_lens, cu_q)
+    dev, d, rows = k_pool.device, k_pool.shape[3], k.shape[0]
+    ks = _heads(k, "k", d, rows, dev)
+    _need(k.shape[1] == cache.n_kv_heads, "k must have the cache's heads")
+    vs = qs = 0
+    _need((v is None) == (v_pool is None), "values and a value pool come together")
+    if v is not None:
+        vs = _heads(v, "v", d, rows, dev)
+        _need(v.shape[1] == cache.n_kv_heads, "v must have the cache's heads")
+    if q is not None:
+        qs = _heads(q, "q", d, rows, dev)
+        _need(q_out.shape == q.shape, "q_out must have q's shape")
+        _heads(q_out, "q_out", d, rows, dev, dense=True)
+    w32 = _weights(d, dev, q_weight, k_weight)
+    rope = _rope(freqs, interleaved, mscale, dev)
+    _launch(dev, "msa_paged_append", ctypes.byref(cache), _ref(rope), _at(q), c_i64(qs), c_i32(q.shape[1] if q is not None else 0),
+            _at(q_weight), _at(k), c_i64(ks), _at(k_weight), _at(v), c_i64(vs), c_i32(w32), ctypes.c_float(eps), c_i64(rows),
+            _at(q_out), stream=stream)
 
 
 # ------------------------------------------------------------------ allocation helpers

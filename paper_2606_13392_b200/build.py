@@ -12,7 +12,7 @@ LIB_PATH = os.path.join(_HERE, "libmsa_b200.so")
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-    "--shared", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",
+    "--shared", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr", "--threads", "0",
 ]
 
 

@@ -86,9 +86,11 @@ __device__ __forceinline__ float warp_sum(float v) {
 inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 int* async_status_ptr();  // device address of the status word of the current device
+bool paged_set_wait(long long limit, long long late);  // msa_debug_set_wait for the kernels of paged.cu
 
 // Stages of the path, for launch counting and the optional per-stage timing.
 enum Stage : int {
+    kStageNone = -1,      // counted, not timed (what stands around the path)
     kStageIndex = 0,      // Eq. 6, prefill
     kStageTopk = 1,       // Eq. 7
     kStageSchedule = 2,   // reverse index + work list (KV-outer prefill)

@@ -28,7 +28,7 @@ static bool g_prof_created = false;
 
 StageScope::StageScope(int stage, cudaStream_t st) : slot_(-1), st_(st) {
     g_launches.fetch_add(1, std::memory_order_relaxed);
-    if (g_prof_on && g_prof_used < kProfSlots) {
+    if (stage >= 0 && g_prof_on && g_prof_used < kProfSlots) {
         slot_ = g_prof_used++;
         g_prof_stage[slot_] = stage;
         cudaEventRecord(g_prof_ev[slot_][0], st_);
@@ -940,7 +940,7 @@ msa_status_t msa_debug_set_wait(int64_t wait_limit_cycles, int64_t producer_dela
     if (producer_delay_cycles > 100000000LL) return MSA_ERR_INVALID_ARG;  // 50 ms
     const long long late = (long long)producer_delay_cycles;
     if (cudaMemcpyToSymbol(g_wait_limit_cycles, &limit, sizeof(limit)) != cudaSuccess ||
-        cudaMemcpyToSymbol(g_debug_producer_delay, &late, sizeof(late)) != cudaSuccess)
+        cudaMemcpyToSymbol(g_debug_producer_delay, &late, sizeof(late)) != cudaSuccess || !paged_set_wait(limit, late))
         return MSA_ERR_CUDA;
     return MSA_OK;
 }

@@ -1,0 +1,251 @@
+// C ABI of what stands around the sparse path (see include/msa.h): norms of queries and keys with the position
+// rotation and their gradients, the paged K/V cache, attention of new tokens over it.  Argument validation,
+// launch shapes and dispatch; the arithmetic is in the kernels included below.
+#include <algorithm>
+#include <cmath>
+
+#include "norm_rope.cuh"
+#include "tc_common.cuh"
+
+namespace msa {
+
+bool paged_set_wait(long long limit, long long late) {
+    return cudaMemcpyToSymbol(g_wait_limit_cycles, &limit, sizeof(limit)) == cudaSuccess &&
+           cudaMemcpyToSymbol(g_debug_producer_delay, &late, sizeof(late)) == cudaSuccess;
+}
+
+static bool aligned_to(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+static int current_device() {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) dev = 0;
+    return dev;
+}
+
+static int sm_count() {
+    static int n[64] = {0};  // per device
+    const int dev = current_device();
+    if (n[dev] == 0 && cudaDeviceGetAttribute(&n[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) n[dev] = 148;
+    return n[dev];
+}
+
+static msa_status_t launch_status() { return cudaPeekAtLastError() == cudaSuccess ? MSA_OK : MSA_ERR_CUDA; }
+
+// ---------------------------------------------------------------------- norm and rotation
+static msa_status_t resolve_rope(const msa_rope_t* rope, int d, RopeArgs& rp) {
+    rp = RopeArgs{nullptr, 0, 0, 1.f};
+    if (d <= 0) return MSA_ERR_INVALID_ARG;
+    if (d % 8 != 0 || d > 256) return MSA_ERR_UNSUPPORTED;
+    if (rope == nullptr) return MSA_OK;
+    if (rope->rot_dim < 0 || rope->rot_dim > d || (rope->interleaved != 0 && rope->interleaved != 1)) return MSA_ERR_INVALID_ARG;
+    if (!std::isfinite(rope->mscale)) return MSA_ERR_INVALID_ARG;
+    if (rope->rot_dim == 0) return MSA_OK;
+    if (rope->freqs == nullptr || !aligned_to(rope->freqs, 8)) return MSA_ERR_INVALID_ARG;
+    if (rope->rot_dim % (rope->interleaved ? 8 : 16) != 0) return MSA_ERR_UNSUPPORTED;
+    rp = RopeArgs{rope->freqs, rope->rot_dim, rope->interleaved, rope->mscale};
+    return MSA_OK;
+}
+
+// Rows of n_heads*d bf16 every `stride` elements.
+static bool rows_ok(const void* x, int64_t stride, int64_t n_heads, int d) {
+    return x != nullptr && aligned_to(x, 16) && stride % 8 == 0 && stride >= n_heads * d;
+}
+static bool weight_ok(const void* w, bool w32) { return w == nullptr || aligned_to(w, w32 ? 4 : 2); }
+
+constexpr int kMaxRopeHeads = 1024;
+
+// Lanes reserved for a head.
+static int lanes_per_head(int d) { return d <= 64 ? 8 : (d <= 128 ? 16 : 32); }
+
+template <int LPH, bool APPEND, bool F8>
+static void launch_norm_rope(const RopeArgs& rp, const RopeHeads& q, const RopeHeads& k, const RopeHeads& v, int64_t n,
+                             int d, float eps, bool w32, const int64_t* positions, const PagedView& cache, void* k_pool,
+                             void* v_pool, cudaStream_t st) {
+    // Many tokens: eight a CTA, so that 256 threads have about one angle each and all warps have items.  Few: one a
+    // CTA, its items spread over CTAs until the machine has four CTAs per SM (each repeats the token's angles).
+    const int run = 4 * (32 / LPH);
+    const int items = (q.n_heads + run - 1) / run + (k.n_heads + run - 1) / run + (v.n_heads + run - 1) / run;
+    const int64_t want = 4LL * sm_count();
+    int tile = kRopeMaxTile;
+    while (tile > 1 && ceil_div64(n, tile) < want) tile /= 2;
+    const int64_t tiles = ceil_div64(n, tile);
+    const int parts = tiles >= want ? 1 : (int)std::min<int64_t>(items, ceil_div64(want, tiles));
+    const int per = (items + parts - 1) / parts;
+    const dim3 grid((unsigned)std::min<int64_t>(tiles, 8LL * sm_count()), (items + per - 1) / per);
+    const size_t smem = (size_t)tile * 2 * LPH * 16 * sizeof(float);
+    StageScope sc(kStageNone, st);
+    norm_rope_kernel<LPH, APPEND, F8><<<grid, kRopeThreads, smem, st>>>(rp, q, k, v, n, d, eps, w32, positions, tile, per, cache,
+                                                                      k_pool, v_pool, APPEND ? async_status_ptr() : nullptr);
+}
+
+template <bool APPEND, bool F8>
+static msa_status_t run_norm_rope(const RopeArgs& rp, const RopeHeads& q, const RopeHeads& k, const RopeHeads& v,
+                                  int64_t n, int d, float eps, bool w32, const int64_t* positions,
+                                  const PagedView& cache, void* k_pool, void* v_pool, cudaStream_t st) {
+    switch (lanes_per_head(d)) {
+        case 8: launch_norm_rope<8, APPEND, F8>(rp, q, k, v, n, d, eps, w32, positions, cache, k_pool, v_pool, st); break;
+        case 16: launch_norm_rope<16, APPEND, F8>(rp, q, k, v, n, d, eps, w32, positions, cache, k_pool, v_pool, st); break;
+        default: launch_norm_rope<32, APPEND, F8>(rp, q, k, v, n, d, eps, w32, positions, cache, k_pool, v_pool, st); break;
+    }
+    return launch_status();
+}
+
+// CTAs of the gradient kernel = rows of weight gradients it leaves.
+static int64_t grad_tiles(int64_t n, int& tile) {
+    tile = kRopeMaxTile;
+    while (tile > 1 && ceil_div64(n, tile) < 4LL * sm_count()) tile /= 2;
+    return std::min<int64_t>(ceil_div64(n, tile), 4LL * sm_count());
+}
+
+template <int LPH>
+static void launch_norm_rope_grad(const RopeArgs& rp, const RopeHeads& q, const RopeHeads& k, const RopeGrads& gq,
+                                  const RopeGrads& gk, int64_t n, int d, float eps, bool w32, const int64_t* positions,
+                                  float* dw_rows, cudaStream_t st) {
+    int tile;
+    const int64_t grid = grad_tiles(n, tile);
+    const size_t smem = std::max((size_t)tile * LPH * 16, (size_t)kRopeWarps * 2 * LPH * 8) * sizeof(float);
+    StageScope sc(kStageNone, st);
+    norm_rope_grad_kernel<LPH><<<(unsigned)grid, kRopeThreads, smem, st>>>(rp, q, k, gq, gk, n, d, eps, w32, positions, tile, dw_rows);
+}
+
+// ---------------------------------------------------------------------- the paged cache
+static msa_status_t resolve_cache(const msa_paged_cache_t* c, int64_t n_tokens, PagedView& v) {
+    if (c == nullptr || n_tokens < 0 || n_tokens > 2147483647LL) return MSA_ERR_INVALID_ARG;
+    if (c->batch < 0 || c->max_pages < 0 || c->n_pages < 0 || c->page_size <= 0 || c->n_kv_heads <= 0 || c->head_dim <= 0)
+        return MSA_ERR_INVALID_ARG;
+    if (c->fp8 != 0 && c->fp8 != 1) return MSA_ERR_INVALID_ARG;
+    if (c->head_dim % 8 != 0 || c->head_dim > 256 || c->n_kv_heads > kMaxRopeHeads) return MSA_ERR_UNSUPPORTED;
+    v = PagedView{c->cu_q, c->kv_lens, c->page_table, c->batch, c->max_pages, c->n_pages, c->page_size, c->n_kv_heads};
+    if (c->batch == 0 || n_tokens == 0) return MSA_OK;
+    if (!c->cu_q || !c->kv_lens || !aligned_to(c->cu_q, 4) || !aligned_to(c->kv_lens, 4)) return MSA_ERR_INVALID_ARG;
+    if (c->max_pages > 0 && (!c->page_table || !aligned_to(c->page_table, 4))) return MSA_ERR_INVALID_ARG;
+    if (c->n_pages > 0 && (!c->k || !aligned_to(c->k, 16) || !aligned_to(c->v, 16))) return MSA_ERR_INVALID_ARG;
+    return MSA_OK;
+}
+
+}  // namespace msa
+
+using namespace msa;
+
+extern "C" {
+
+msa_status_t msa_qk_norm_rope(const msa_rope_t* rope, const void* q, int64_t q_stride, int32_t n_q_heads,
+                              const void* q_weight, const void* k, int64_t k_stride, int32_t n_k_heads,
+                              const void* k_weight, int32_t head_dim, int32_t weight_fp32, float eps,
+                              const int64_t* positions, int64_t n_tokens, void* q_out, void* k_out,
+                              msa_stream_t stream) {
+    RopeArgs rp;
+    const msa_status_t s = resolve_rope(rope, head_dim, rp);
+    if (s != MSA_OK) return s;
+    if (n_tokens < 0 || n_q_heads < 0 || n_k_heads < 0 || !(eps >= 0.f) || !std::isfinite(eps)) return MSA_ERR_INVALID_ARG;
+    if (weight_fp32 != 0 && weight_fp32 != 1) return MSA_ERR_INVALID_ARG;
+    if (n_q_heads > kMaxRopeHeads || n_k_heads > kMaxRopeHeads) return MSA_ERR_UNSUPPORTED;
+    if (n_tokens == 0 || n_q_heads + n_k_heads == 0) return MSA_OK;
+    const bool w32 = weight_fp32 == 1;
+    if (n_q_heads > 0 && (!rows_ok(q, q_stride, n_q_heads, head_dim) || !rows_ok(q_out, (int64_t)n_q_heads * head_dim, n_q_heads, head_dim)))
+        return MSA_ERR_INVALID_ARG;
+    if (n_k_heads > 0 && (!rows_ok(k, k_stride, n_k_heads, head_dim) || !rows_ok(k_out, (int64_t)n_k_heads * head_dim, n_k_heads, head_dim)))
+        return MSA_ERR_INVALID_ARG;
+    if (!weight_ok(q_weight, w32) || !weight_ok(k_weight, w32)) return MSA_ERR_INVALID_ARG;
+    if (rp.rot > 0 && (positions == nullptr || !aligned_to(positions, 8))) return MSA_ERR_INVALID_ARG;
+    const RopeHeads qh{(const __nv_bfloat16*)q, q_stride, n_q_heads, q_weight, (__nv_bfloat16*)q_out};
+    const RopeHeads kh{(const __nv_bfloat16*)k, k_stride, n_k_heads, k_weight, (__nv_bfloat16*)k_out};
+    return run_norm_rope<false, false>(rp, qh, kh, RopeHeads{}, n_tokens, head_dim, eps, w32, positions, PagedView{}, nullptr,
+                                       nullptr, (cudaStream_t)stream);
+}
+
+msa_status_t msa_qk_norm_rope_backward_workspace_bytes(int32_t head_dim, int64_t n_tokens, size_t* min_bytes) {
+    if (head_dim <= 0 || n_tokens < 0 || min_bytes == nullptr) return MSA_ERR_INVALID_ARG;
+    if (head_dim % 8 != 0 || head_dim > 256) return MSA_ERR_UNSUPPORTED;
+    int tile;
+    *min_bytes = (size_t)grad_tiles(n_tokens, tile) * 2 * head_dim * sizeof(float);
+    return MSA_OK;
+}
+
+msa_status_t msa_qk_norm_rope_backward(const msa_rope_t* rope, const void* dq_out, int64_t dq_stride,
+                                       const void* dk_out, int64_t dk_stride, const void* q, int64_t q_stride,
+                                       int32_t n_q_heads, const void* q_weight, const void* k, int64_t k_stride,
+                                       int32_t n_k_heads, const void* k_weight, int32_t head_dim,
+                                       int32_t weight_fp32, float eps, const int64_t* positions, int64_t n_tokens,
+                                       void* dq, void* dk, float* dq_weight, float* dk_weight, void* workspace,
+                                       size_t workspace_bytes, msa_stream_t stream) {
+    RopeArgs rp;
+    const msa_status_t s = resolve_rope(rope, head_dim, rp);
+    if (s != MSA_OK) return s;
+    if (n_tokens < 0 || n_q_heads < 0 || n_k_heads < 0 || !(eps >= 0.f) || !std::isfinite(eps)) return MSA_ERR_INVALID_ARG;
+    if (weight_fp32 != 0 && weight_fp32 != 1) return MSA_ERR_INVALID_ARG;
+    if (n_q_heads > kMaxRopeHeads || n_k_heads > kMaxRopeHeads) return MSA_ERR_UNSUPPORTED;
+    const bool w32 = weight_fp32 == 1;
+    const bool some = n_tokens > 0;
+    if (some && n_q_heads > 0 &&
+        (!rows_ok(dq_out, dq_stride, n_q_heads, head_dim) || !rows_ok(dq, (int64_t)n_q_heads * head_dim, n_q_heads, head_dim) ||
+         (q_weight && !rows_ok(q, q_stride, n_q_heads, head_dim))))
+        return MSA_ERR_INVALID_ARG;
+    if (some && n_k_heads > 0 &&
+        (!rows_ok(dk_out, dk_stride, n_k_heads, head_dim) || !rows_ok(dk, (int64_t)n_k_heads * head_dim, n_k_heads, head_dim) ||
+         (k_weight && !rows_ok(k, k_stride, n_k_heads, head_dim))))
+        return MSA_ERR_INVALID_ARG;
+    if (!weight_ok(q_weight, w32) || !weight_ok(k_weight, w32)) return MSA_ERR_INVALID_ARG;
+    if (some && rp.rot > 0 && (positions == nullptr || !aligned_to(positions, 8))) return MSA_ERR_INVALID_ARG;
+    float* dwq = q_weight != nullptr ? dq_weight : nullptr;
+    float* dwk = k_weight != nullptr ? dk_weight : nullptr;
+    if (!aligned_to(dwq, 4) || !aligned_to(dwk, 4)) return MSA_ERR_INVALID_ARG;
+    const bool want = dwq != nullptr || dwk != nullptr;
+    int tile;
+    const int64_t rows = grad_tiles(n_tokens, tile);
+    if (want && some) {
+        if (workspace == nullptr || !aligned_to(workspace, 16)) return MSA_ERR_INVALID_ARG;
+        if (workspace_bytes < (size_t)rows * 2 * head_dim * sizeof(float)) return MSA_ERR_WORKSPACE;
+    }
+    cudaStream_t st = (cudaStream_t)stream;
+    if (some && n_q_heads + n_k_heads > 0) {
+        const RopeHeads qh{(const __nv_bfloat16*)q, q_stride, n_q_heads, q_weight, nullptr};
+        const RopeHeads kh{(const __nv_bfloat16*)k, k_stride, n_k_heads, k_weight, nullptr};
+        const RopeGrads gq{(const __nv_bfloat16*)dq_out, dq_stride, (__nv_bfloat16*)dq};
+        const RopeGrads gk{(const __nv_bfloat16*)dk_out, dk_stride, (__nv_bfloat16*)dk};
+        float* dw = want ? (float*)workspace : nullptr;
+        switch (lanes_per_head(head_dim)) {
+            case 8: launch_norm_rope_grad<8>(rp, qh, kh, gq, gk, n_tokens, head_dim, eps, w32, positions, dw, st); break;
+            case 16: launch_norm_rope_grad<16>(rp, qh, kh, gq, gk, n_tokens, head_dim, eps, w32, positions, dw, st); break;
+            default: launch_norm_rope_grad<32>(rp, qh, kh, gq, gk, n_tokens, head_dim, eps, w32, positions, dw, st); break;
+        }
+    }
+    if (want) {
+        const int n_rows = some && n_q_heads + n_k_heads > 0 ? (int)rows : 0;  // no rows: the gradients are zeros
+        StageScope sc(kStageNone, st);
+        norm_rope_dw_kernel<<<(2 * head_dim + 31) / 32, 1024, 0, st>>>((const float*)workspace, n_rows, head_dim, dwq, dwk);
+    }
+    return launch_status();
+}
+
+msa_status_t msa_paged_append(const msa_paged_cache_t* cache, const msa_rope_t* rope, const void* q, int64_t q_stride,
+                              int32_t n_q_heads, const void* q_weight, const void* k, int64_t k_stride,
+                              const void* k_weight, const void* v, int64_t v_stride, int32_t weight_fp32, float eps,
+                              int64_t n_tokens, void* q_out, msa_stream_t stream) {
+    PagedView view;
+    msa_status_t s = resolve_cache(cache, n_tokens, view);
+    if (s != MSA_OK) return s;
+    const int d = cache->head_dim, H = cache->n_kv_heads;
+    RopeArgs rp;
+    if ((s = resolve_rope(rope, d, rp)) != MSA_OK) return s;
+    if (n_q_heads < 0 || !(eps >= 0.f) || !std::isfinite(eps)) return MSA_ERR_INVALID_ARG;
+    if (weight_fp32 != 0 && weight_fp32 != 1) return MSA_ERR_INVALID_ARG;
+    if (n_q_heads > kMaxRopeHeads) return MSA_ERR_UNSUPPORTED;
+    if (n_tokens == 0 || cache->batch == 0) return MSA_OK;
+    const bool w32 = weight_fp32 == 1;
+    if (n_q_heads > 0 && (!rows_ok(q, q_stride, n_q_heads, d) || !rows_ok(q_out, (int64_t)n_q_heads * d, n_q_heads, d)))
+        return MSA_ERR_INVALID_ARG;
+    if (!rows_ok(k, k_stride, H, d)) return MSA_ERR_INVALID_ARG;
+    if ((v == nullptr) != (cache->v == nullptr)) return MSA_ERR_INVALID_ARG;
+    if (v != nullptr && !rows_ok(v, v_stride, H, d)) return MSA_ERR_INVALID_ARG;
+    if (!weight_ok(q_weight, w32) || !weight_ok(k_weight, w32)) return MSA_ERR_INVALID_ARG;
+    if (async_status_ptr() == nullptr) return MSA_ERR_CUDA;
+    const RopeHeads qh{(const __nv_bfloat16*)q, q_stride, n_q_heads, q_weight, (__nv_bfloat16*)q_out};
+    const RopeHeads kh{(const __nv_bfloat16*)k, k_stride, H, k_weight, nullptr};
+    const RopeHeads vh{(const __nv_bfloat16*)v, v_stride, v != nullptr ? H : 0, nullptr, nullptr};
+    if (cache->fp8)
+        return run_norm_rope<true, true>(rp, qh, kh, vh, n_tokens, d, eps, w32, nullptr, view, cache->k, cache->v, (cudaStream_t)stream);
+    return run_norm_rope<true, false>(rp, qh, kh, vh, n_tokens, d, eps, w32, nullptr, view, cache->k, cache->v, (cudaStream_t)stream);
+}
+
+}  // extern "C"
