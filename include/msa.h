@@ -496,6 +496,27 @@ msa_status_t msa_paged_append(const msa_paged_cache_t* cache, const msa_rope_t* 
                               int32_t weight_fp32, float eps, int64_t n_tokens, void* q_out, msa_stream_t stream);
 
 /*
+ * Dense causal attention of the new tokens over the cache, which already holds their own keys and
+ * values (msa_paged_append): query head h of new token i of sequence s uses KV head h / G and sees
+ * tokens 0 .. kv_lens[s] - (cu_q[s+1] - cu_q[s]) + i.  q, out [n_tokens, n_q_heads, d] bf16 dense,
+ * lse [n_tokens, n_q_heads] fp32 or NULL (natural log).  softmax_scale 0 = 1/sqrt(d).  A token that
+ * sees nothing gets zeros and -inf.  K and V of visible tokens must be finite (a value that is not
+ * would reach other tokens of its 128-key tile); what the pages hold behind kv_lens[s] is not read
+ * into the result.  Sequences may be ragged and mixed, from one token on a long cache to long
+ * chunks: work is split evenly over the device and split tiles are merged in a fixed order, so equal
+ * calls give equal bits.  Bad pages or lengths are reported as a bad index; the outputs of that
+ * sequence are then unspecified.
+ * head_dim = 128 with pages of a multiple of 8 tokens runs on the tensor cores (P is rounded to
+ * bf16 before P V, as in Eq. 8's calls), other shapes on a generic kernel.
+ * workspace (256-byte aligned) >= msa_paged_attn_workspace_bytes.  Of `cache`, that query reads the
+ * sizes only.
+ */
+msa_status_t msa_paged_attn(const msa_paged_cache_t* cache, const void* q, int32_t n_q_heads, int64_t n_tokens,
+                            float softmax_scale, void* out, float* lse, void* workspace,
+                            size_t workspace_bytes, msa_stream_t stream);
+msa_status_t msa_paged_attn_workspace_bytes(const msa_paged_cache_t* cache, int32_t n_q_heads, size_t* min_bytes);
+
+/*
  * Test hook for the device-side bounded waits (the paper has no counterpart).  Every wait of a
  * kernel on an mbarrier gives up after a limit of SM cycles (about two seconds by default),
  * raises MSA_ERR_TIMEOUT in the async status and lets the kernel unwind and return.

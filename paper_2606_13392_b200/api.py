@@ -148,6 +148,20 @@ class PagedCache(NamedTuple):
 _NO_ROPE = Rope(None)
 
 
+def _empty(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
+    return None if t is None else torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
+def _workspace(t: torch.Tensor, size, *args) -> torch.Tensor:
+    """A workspace of size(*args) bytes on t's device (the size may depend on the device)."""
+    if t.get_device() == torch.cuda.current_device():
+        n = size(*args)
+    else:
+        with torch.cuda.device(t.device):
+            n = size(*args)
+    return B.alloc_workspace(n, t.device)
+
+
 def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
                      original_len: int = 4096, low: float = 1.0, high: float = 32.0, device="cuda") -> torch.Tensor:
     """fp64 frequencies base^(-2i/rot_dim) of a rotation of rot_dim elements, stretched for contexts `factor` times
@@ -175,10 +189,8 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions
                  k_out: Optional[torch.Tensor] = None):
     """Norm of each head (where there is a weight) and position rotation of q and k [rows, heads, d], which may be
     slices of one projection; either may be None -> (q_out, k_out), dense."""
-    if q_out is None and q is not None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    if k_out is None and k is not None:
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    q_out = _empty(q) if q_out is None else q_out
+    k_out = _empty(k) if k_out is None else k_out
     freqs, interleaved, mscale = rope or _NO_ROPE
     B.msa_qk_norm_rope(freqs, interleaved, mscale, q, q_weight, k, k_weight, eps, positions, q_out, k_out)
     return q_out, k_out
@@ -191,15 +203,13 @@ def qk_norm_rope_backward(dq_out: Optional[torch.Tensor], dk_out: Optional[torch
     """Gradients of qk_norm_rope's inputs for those of its outputs -> (dq, dk, dq_weight, dk_weight); the weights'
     are fp32, None without a weight."""
     dy = dq_out if dq_out is not None else dk_out
-    dev, d = dy.device, dy.shape[2]
-    dq = None if dq_out is None else torch.empty(dq_out.shape, dtype=torch.bfloat16, device=dev)
-    dk = None if dk_out is None else torch.empty(dk_out.shape, dtype=torch.bfloat16, device=dev)
+    dev, d = dy.device, dy.shape[-1]
+    dq, dk = _empty(dq_out), _empty(dk_out)
     dwq = None if q_weight is None else torch.empty(d, dtype=torch.float32, device=dev)
     dwk = None if k_weight is None else torch.empty(d, dtype=torch.float32, device=dev)
     ws = None
     if dwq is not None or dwk is not None:
-        with torch.cuda.device(dev):
-            ws = B.alloc_workspace(B.msa_qk_norm_rope_backward_workspace_bytes(d, dy.shape[0]), dev)
+        ws = _workspace(dy, B.msa_qk_norm_rope_backward_workspace_bytes, d, dy.shape[0])
     freqs, interleaved, mscale = rope or _NO_ROPE
     B.msa_qk_norm_rope_backward(freqs, interleaved, mscale, dq_out, dk_out, q, q_weight, k, k_weight, eps, positions, dq, dk,
                                 dwq, dwk, ws)
@@ -212,9 +222,20 @@ def paged_append(cache: PagedCache, k: torch.Tensor, v: Optional[torch.Tensor], 
     """Writes the new tokens' keys (normed, turned) and values into the cache and returns their queries, treated like
     the keys (None without queries).  Rows behind the last sequence are left as they are (uninitialised in a q_out
     made here)."""
-    if q_out is None and q is not None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    q_out = _empty(q) if q_out is None else q_out
     freqs, interleaved, mscale = rope or _NO_ROPE
     B.msa_paged_append(cache.k, cache.v, cache.page_table, cache.kv_lens, cache.cu_q, freqs, interleaved, mscale, q, q_weight, k,
                        k_weight, v, eps, q_out)
     return q_out
+
+
+def paged_attn(cache: PagedCache, q: torch.Tensor, softmax_scale: float = 0.0, out: Optional[torch.Tensor] = None,
+               want_lse: bool = True, workspace: Optional[torch.Tensor] = None):
+    """Dense causal attention of the new tokens q [rows, heads, d] over the cache, which already holds their keys and
+    values -> (out, lse).  Rows behind the last sequence are left as they are (uninitialised in outputs made here)."""
+    out = _empty(q) if out is None else out
+    lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if want_lse else None
+    if workspace is None:
+        workspace = _workspace(q, B.msa_paged_attn_workspace_bytes, cache.k, q.shape[1])
+    B.msa_paged_attn(cache.k, cache.v, cache.page_table, cache.kv_lens, cache.cu_q, q, softmax_scale, out, lse, workspace)
+    return out, lse

@@ -34,6 +34,7 @@ EXPORTS = [
     "msa_prefill_forward_host_workspace_bytes", "msa_decode_forward", "msa_decode_forward_host",
     "msa_launch_count", "msa_profile_begin", "msa_profile_end", "msa_index_scores_plan", "msa_debug_set_wait",
     "msa_qk_norm_rope", "msa_qk_norm_rope_backward", "msa_qk_norm_rope_backward_workspace_bytes", "msa_paged_append",
+    "msa_paged_attn", "msa_paged_attn_workspace_bytes",
 ]
 
 
@@ -374,88 +375,126 @@ def msa_decode_forward_host(shape, q_host, q_idx_host, q_dev, q_idx_dev, k_cache
 
 
 # ------------------------------------------------------------------ around the path
-def _need(ok: bool, what: str) -> None:
-    if not ok:
-        raise ValueError(what)
+# (These run in a decode step, where a call's own cost counts: checks format their message only when they fail, and
+# the argument types are declared once.)
+_F32 = ctypes.c_float
+_ARGTYPES = {
+    "msa_qk_norm_rope": [c_vp, c_vp, c_i64, c_i32, c_vp, c_vp, c_i64, c_i32, c_vp, c_i32, c_i32, _F32, c_vp, c_i64, c_vp, c_vp,
+                         c_vp],
+    "msa_qk_norm_rope_backward": [c_vp, c_vp, c_i64, c_vp, c_i64, c_vp, c_i64, c_i32, c_vp, c_vp, c_i64, c_i32, c_vp, c_i32,
+                                  c_i32, _F32, c_vp, c_i64, c_vp, c_vp, c_vp, c_vp, c_vp, c_sz, c_vp],
+    "msa_paged_attn": [c_vp, c_vp, c_i32, c_i64, _F32, c_vp, c_vp, c_vp, c_sz, c_vp],
+    "msa_paged_append": [c_vp, c_vp, c_vp, c_i64, c_i32, c_vp, c_vp, c_i64, c_vp, c_vp, c_i64, c_i32, _F32, c_i64, c_vp, c_vp],
+}
+_fns = {}
 
 
-def _launch(device: torch.device, name: str, *args, stream=None) -> None:
-    """Calls the library with `device` current (the tensors' own, whatever the caller's is) on its current stream."""
-    fn = getattr(lib(), name)
-    if device.index != torch.cuda.current_device():
-        with torch.cuda.device(device):
-            _check(fn(*args, _stream(stream)), name)
+def _fn(name: str):
+    fn = _fns.get(name)
+    if fn is None:
+        fn = getattr(lib(), name)
+        fn.argtypes = _ARGTYPES[name]
+        _fns[name] = fn
+    return fn
+
+
+def _launch(index: int, name: str, *args) -> None:
+    """Calls the library with the tensors' device current (whatever the caller's is), on that device's current stream."""
+    if index == torch.cuda.current_device():
+        code = _fn(name)(*args, torch._C._cuda_getCurrentRawStream(index))
     else:
-        _check(fn(*args, _stream(stream)), name)
+        with torch.cuda.device(index):
+            code = _fn(name)(*args, torch._C._cuda_getCurrentRawStream(index))
+    if code != 0:
+        raise MsaError(code, name)
 
 
-def _heads(t: torch.Tensor, what: str, head_dim: int, rows: int, device: torch.device, dense: bool = False) -> int:
+def _heads(t: torch.Tensor, what: str, head_dim: int, rows: int, index: int, dense: bool = False) -> int:
     """A bf16 tensor [rows, heads, head_dim] whose heads are dense; returns its row stride."""
-    _need(t.dtype == torch.bfloat16 and t.device == device, "%s must be bf16 on %s" % (what, device))
-    _need(t.dim() == 3 and t.shape[0] == rows and t.shape[2] == head_dim,
-          "%s must be [%d, heads, %d], got %s" % (what, rows, head_dim, tuple(t.shape)))
-    s, width = t.stride(), t.shape[1] * head_dim
+    shape = t.shape
+    if t.dtype != torch.bfloat16 or t.get_device() != index:
+        raise ValueError("%s must be bf16 on cuda:%d, got %s on %s" % (what, index, t.dtype, t.device))
+    if len(shape) != 3 or shape[0] != rows or shape[2] != head_dim:
+        raise ValueError("%s must be [%d, heads, %d], got %s" % (what, rows, head_dim, tuple(shape)))
+    s, width = t.stride(), shape[1] * head_dim
     # (strides of dimensions with fewer than two entries say nothing)
-    _need((t.shape[2] < 2 or s[2] == 1) and (t.shape[1] < 2 or s[1] == head_dim),
-          "the last two dimensions of %s must be dense" % what)
+    if (head_dim > 1 and s[2] != 1) or (shape[1] > 1 and s[1] != head_dim):
+        raise ValueError("the last two dimensions of %s must be dense, got strides %s" % (what, s))
     if rows < 2:
         return width
-    _need(s[0] == width or not dense, "%s must be contiguous" % what)
+    if dense and s[0] != width:
+        raise ValueError("%s must be contiguous, got strides %s" % (what, s))
     return s[0]
 
 
-def _weights(head_dim: int, device: torch.device, *weights) -> int:
+def _like(t: torch.Tensor, other: torch.Tensor, what: str, head_dim: int, rows: int, index: int) -> None:
+    """A dense bf16 tensor of another's shape."""
+    if t.shape != other.shape:
+        raise ValueError("%s must be %s, got %s" % (what, tuple(other.shape), tuple(t.shape)))
+    _heads(t, what, head_dim, rows, index, dense=True)
+
+
+def _weights(head_dim: int, index: int, *weights) -> int:
     """Checks the weights of the norms (None: no norm); 1 if they are fp32, 0 if bf16."""
-    kinds = {w.dtype for w in weights if w is not None}
-    _need(len(kinds) < 2 and kinds <= {torch.bfloat16, torch.float32}, "norm weights must be all bf16 or all fp32")
+    kind = None
     for w in weights:
-        _need(w is None or (w.shape == (head_dim,) and w.is_contiguous() and w.device == device),
-              "norm weights must be contiguous vectors of head_dim values on %s" % device)
-    return 1 if torch.float32 in kinds else 0
+        if w is None:
+            continue
+        if (w.dtype not in (torch.bfloat16, torch.float32) or kind not in (None, w.dtype) or w.shape != (head_dim,) or
+                not w.is_contiguous() or w.get_device() != index):
+            raise ValueError("norm weights must be contiguous vectors of %d values, all bf16 or all fp32, on cuda:%d"
+                             % (head_dim, index))
+        kind = w.dtype
+    return 1 if kind == torch.float32 else 0
 
 
-def _rope(freqs, interleaved, mscale, device: torch.device):
+def _rope(freqs, interleaved, mscale, index: int):
     if freqs is None:
         return None
-    _need(freqs.dtype == torch.float64 and freqs.dim() == 1 and freqs.is_contiguous() and freqs.device == device,
-          "frequencies must be a contiguous fp64 vector on %s" % device)
+    if freqs.dtype != torch.float64 or freqs.dim() != 1 or not freqs.is_contiguous() or freqs.get_device() != index:
+        raise ValueError("frequencies must be a contiguous fp64 vector on cuda:%d" % index)
     return MsaRope(freqs.data_ptr(), 2 * freqs.shape[0], 1 if interleaved else 0, mscale)
 
 
-def _positions(positions, rows: int, device: torch.device):
-    if positions is not None:
-        _need(positions.dtype == torch.int64 and positions.shape == (rows,) and positions.is_contiguous() and
-              positions.device == device, "positions must be a contiguous int64 vector, one for each row, on %s" % device)
-    return c_vp(None if positions is None else positions.data_ptr())
+def _positions(positions, rows: int, index: int):
+    if positions is None:
+        return None
+    if (positions.dtype != torch.int64 or positions.shape != (rows,) or not positions.is_contiguous() or
+            positions.get_device() != index):
+        raise ValueError("positions must be a contiguous int64 vector, one for each of %d rows, on cuda:%d" % (rows, index))
+    return positions.data_ptr()
 
 
-def _at(t: Optional[torch.Tensor]) -> c_vp:
-    return c_vp(None if t is None else t.data_ptr())
+def _device_of(t: Optional[torch.Tensor], what: str) -> int:
+    if t is None or not t.is_cuda:
+        raise ValueError("%s must be a tensor on a CUDA device" % what)
+    return t.get_device()
+
+
+def _at(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
 
 
 def _ref(s):
     return None if s is None else ctypes.byref(s)
 
 
-def msa_qk_norm_rope(freqs, interleaved, mscale, q, q_weight, k, k_weight, eps, positions, q_out, k_out, stream=None):
+def msa_qk_norm_rope(freqs, interleaved, mscale, q, q_weight, k, k_weight, eps, positions, q_out, k_out):
     """q, k: bf16 [rows, heads, d], rows may be strided; either may be None.  freqs None: no rotation."""
-    x = q if q is not None else k
-    _need(x is not None and x.is_cuda, "a tensor on a CUDA device is needed")
-    dev, rows, d = x.device, x.shape[0], x.shape[2] if x.dim() == 3 else 0
-    qs = ks = 0
+    x = k if q is None else q
+    index = _device_of(x, "q or k")
+    rows, d = x.shape[0], x.shape[-1]
+    qs = ks = hq = hk = 0
     if q is not None:
-        qs = _heads(q, "q", d, rows, dev)
-        _need(q_out.shape == q.shape, "q_out must have q's shape")
-        _heads(q_out, "q_out", d, rows, dev, dense=True)
+        qs, hq = _heads(q, "q", d, rows, index), q.shape[1]
+        _like(q_out, q, "q_out", d, rows, index)
     if k is not None:
-        ks = _heads(k, "k", d, rows, dev)
-        _need(k_out.shape == k.shape, "k_out must have k's shape")
-        _heads(k_out, "k_out", d, rows, dev, dense=True)
-    w32 = _weights(d, dev, q_weight, k_weight)
-    rope = _rope(freqs, interleaved, mscale, dev)
-    _launch(dev, "msa_qk_norm_rope", _ref(rope), _at(q), c_i64(qs), c_i32(q.shape[1] if q is not None else 0), _at(q_weight),
-            _at(k), c_i64(ks), c_i32(k.shape[1] if k is not None else 0), _at(k_weight), c_i32(d), c_i32(w32),
-            ctypes.c_float(eps), _positions(positions, rows, dev), c_i64(rows), _at(q_out), _at(k_out), stream=stream)
+        ks, hk = _heads(k, "k", d, rows, index), k.shape[1]
+        _like(k_out, k, "k_out", d, rows, index)
+    w32 = _weights(d, index, q_weight, k_weight)
+    rope = _rope(freqs, interleaved, mscale, index)
+    _launch(index, "msa_qk_norm_rope", _ref(rope), _at(q), qs, hq, _at(q_weight), _at(k), ks, hk, _at(k_weight), d, w32, eps,
+            _positions(positions, rows, index), rows, _at(q_out), _at(k_out))
 
 
 def msa_qk_norm_rope_backward_workspace_bytes(head_dim: int, n_tokens: int) -> int:
@@ -465,73 +504,108 @@ def msa_qk_norm_rope_backward_workspace_bytes(head_dim: int, n_tokens: int) -> i
     return int(mn.value)
 
 
+def _workspace(ws: Optional[torch.Tensor], index: int) -> int:
+    """Checks a workspace and returns its bytes."""
+    if ws is None:
+        return 0
+    if not ws.is_contiguous() or ws.get_device() != index:
+        raise ValueError("the workspace must be contiguous on cuda:%d" % index)
+    return ws.numel() * ws.element_size()
+
+
 def msa_qk_norm_rope_backward(freqs, interleaved, mscale, dq_out, dk_out, q, q_weight, k, k_weight, eps, positions, dq,
-                              dk, dq_weight, dk_weight, workspace, stream=None):
+                              dk, dq_weight, dk_weight, workspace):
     """q / k are needed where there is a weight (else None is fine); dq, dk bf16 dense, weight gradients fp32 [d]."""
-    x = dq_out if dq_out is not None else dk_out
-    _need(x is not None and x.is_cuda, "a tensor on a CUDA device is needed")
-    dev, rows, d = x.device, x.shape[0], x.shape[2] if x.dim() == 3 else 0
-    strides = []
+    x = dk_out if dq_out is None else dq_out
+    index = _device_of(x, "dq_out or dk_out")
+    rows, d = x.shape[0], x.shape[-1]
+    at = []
     for n, dy, t, w, dx, dw in (("q", dq_out, q, q_weight, dq, dq_weight), ("k", dk_out, k, k_weight, dk, dk_weight)):
         if dy is None:
-            strides += [0, 0]
+            at.append((0, 0, 0))
             continue
-        strides.append(_heads(dy, "d%s_out" % n, d, rows, dev))
-        _need(w is None or t is not None, "%s is needed for the gradients of its norm" % n)
-        strides.append(0 if t is None else _heads(t, n, d, rows, dev))
-        _need((t is None or t.shape == dy.shape) and dx.shape == dy.shape, "%s and its gradients must have one shape" % n)
-        _heads(dx, "d%s" % n, d, rows, dev, dense=True)
-        _need(dw is None or (dw.dtype == torch.float32 and dw.shape == (d,) and dw.is_contiguous() and dw.device == dev),
-              "d%s_weight must be a contiguous fp32 vector of head_dim values on %s" % (n, dev))
-    w32 = _weights(d, dev, q_weight, k_weight)
-    rope = _rope(freqs, interleaved, mscale, dev)
-    _need(workspace is None or (workspace.is_contiguous() and workspace.device == dev), "workspace must be on %s" % dev)
-    _launch(dev, "msa_qk_norm_rope_backward", _ref(rope), _at(dq_out), c_i64(strides[0]), _at(dk_out), c_i64(strides[2]), _at(q),
-            c_i64(strides[1]), c_i32(dq_out.shape[1] if dq_out is not None else 0), _at(q_weight), _at(k), c_i64(strides[3]),
-            c_i32(dk_out.shape[1] if dk_out is not None else 0), _at(k_weight), c_i32(d), c_i32(w32), ctypes.c_float(eps),
-            _positions(positions, rows, dev), c_i64(rows), _at(dq), _at(dk), _at(dq_weight), _at(dk_weight), _at(workspace),
-            c_sz(0 if workspace is None else workspace.numel() * workspace.element_size()), stream=stream)
+        ys, ts = _heads(dy, "the gradient of %s_out" % n, d, rows, index), 0
+        if t is not None:
+            ts = _heads(t, n, d, rows, index)
+            if t.shape != dy.shape:
+                raise ValueError("%s must be %s, got %s" % (n, tuple(dy.shape), tuple(t.shape)))
+        elif w is not None:
+            raise ValueError("%s is needed for the gradients of its norm" % n)
+        _like(dx, dy, "the gradient of %s" % n, d, rows, index)
+        if dw is not None and (dw.dtype != torch.float32 or dw.shape != (d,) or not dw.is_contiguous() or dw.get_device() != index):
+            raise ValueError("the gradient of %s_weight must be a contiguous fp32 vector of %d values on cuda:%d" % (n, d, index))
+        at.append((ys, ts, dy.shape[1]))
+    w32 = _weights(d, index, q_weight, k_weight)
+    rope = _rope(freqs, interleaved, mscale, index)
+    _launch(index, "msa_qk_norm_rope_backward", _ref(rope), _at(dq_out), at[0][0], _at(dk_out), at[1][0], _at(q), at[0][1],
+            at[0][2], _at(q_weight), _at(k), at[1][1], at[1][2], _at(k_weight), d, w32, eps, _positions(positions, rows, index),
+            rows, _at(dq), _at(dk), _at(dq_weight), _at(dk_weight), _at(workspace), _workspace(workspace, index))
 
 
 def _paged(k_pool, v_pool, page_table, kv_lens, cu_q):
     """The cache structure of checked tensors."""
-    _need(k_pool.is_cuda and k_pool.dim() == 4 and k_pool.is_contiguous() and
-          k_pool.dtype in (torch.bfloat16, torch.float8_e4m3fn),
-          "the key pool must be a contiguous [pages, page size, KV heads, head_dim] tensor of bf16 or float8_e4m3fn on a CUDA device")
-    dev = k_pool.device
-    _need(v_pool is None or (v_pool.shape == k_pool.shape and v_pool.dtype == k_pool.dtype and v_pool.is_contiguous() and
-                             v_pool.device == dev), "the value pool must be like the key pool")
-    _need(page_table.dim() == 2 and kv_lens.dim() == 1 and cu_q.dim() == 1 and kv_lens.shape[0] == page_table.shape[0] and
-          cu_q.shape[0] == kv_lens.shape[0] + 1, "page_table [batch, pages], kv_lens [batch] and cu_q [batch + 1] must agree")
-    for n, t in (("page_table", page_table), ("kv_lens", kv_lens), ("cu_q", cu_q)):
-        _need(t.dtype == torch.int32 and t.is_contiguous() and t.device == dev, "%s must be contiguous int32 on %s" % (n, dev))
-    pages, size, heads, d = k_pool.shape
-    return MsaPagedCache(k_pool.data_ptr(), 0 if v_pool is None else v_pool.data_ptr(), page_table.data_ptr(),
-                         kv_lens.data_ptr(), cu_q.data_ptr(), kv_lens.shape[0], page_table.shape[1], pages, size, heads, d,
-                         1 if k_pool.dtype == torch.float8_e4m3fn else 0)
+    index = _device_of(k_pool, "the key pool")
+    kind, shape = k_pool.dtype, k_pool.shape
+    if len(shape) != 4 or kind not in (torch.bfloat16, torch.float8_e4m3fn) or not k_pool.is_contiguous():
+        raise ValueError("the key pool must be a contiguous [pages, page size, KV heads, head_dim] tensor of bf16 or "
+                         "float8_e4m3fn, got %s %s" % (kind, tuple(shape)))
+    if v_pool is not None and (v_pool.shape != shape or v_pool.dtype != kind or not v_pool.is_contiguous() or
+                               v_pool.get_device() != index):
+        raise ValueError("the value pool must be like the key pool")
+    batch = kv_lens.shape[0]
+    if page_table.dim() != 2 or kv_lens.dim() != 1 or page_table.shape[0] != batch or cu_q.shape != (batch + 1,):
+        raise ValueError("page_table [batch, pages], kv_lens [batch] and cu_q [batch + 1] must agree")
+    for t in (page_table, kv_lens, cu_q):
+        if t.dtype != torch.int32 or not t.is_contiguous() or t.get_device() != index:
+            raise ValueError("page_table, kv_lens and cu_q must be contiguous int32 on cuda:%d" % index)
+    return index, MsaPagedCache(k_pool.data_ptr(), _at(v_pool), page_table.data_ptr(), kv_lens.data_ptr(), cu_q.data_ptr(), batch,
+                                page_table.shape[1], shape[0], shape[1], shape[2], shape[3], 0 if kind == torch.bfloat16 else 1)
 
 
 def msa_paged_append(k_pool, v_pool, page_table, kv_lens, cu_q, freqs, interleaved, mscale, q, q_weight, k, k_weight, v,
-                     eps, q_out, stream=None):
+                     eps, q_out):
     """k, v (and q): bf16 [rows, heads, d], rows may be strided; q None: no queries; v None: a cache without values."""
-    cache = _paged(k_pool, v_pool, page_table, kv_lens, cu_q)
-    dev, d, rows = k_pool.device, k_pool.shape[3], k.shape[0]
-    ks = _heads(k, "k", d, rows, dev)
-    _need(k.shape[1] == cache.n_kv_heads, "k must have the cache's heads")
-    vs = qs = 0
-    _need((v is None) == (v_pool is None), "values and a value pool come together")
+    index, cache = _paged(k_pool, v_pool, page_table, kv_lens, cu_q)
+    d, rows = cache.head_dim, k.shape[0]
+    vs = qs = hq = 0
+    ks = _heads(k, "k", d, rows, index)
+    if (v is None) != (v_pool is None):
+        raise ValueError("values and a value pool come together")
     if v is not None:
-        vs = _heads(v, "v", d, rows, dev)
-        _need(v.shape[1] == cache.n_kv_heads, "v must have the cache's heads")
+        vs = _heads(v, "v", d, rows, index)
+    if k.shape[1] != cache.n_kv_heads or (v is not None and v.shape[1] != cache.n_kv_heads):
+        raise ValueError("k and v must have the cache's %d heads" % cache.n_kv_heads)
     if q is not None:
-        qs = _heads(q, "q", d, rows, dev)
-        _need(q_out.shape == q.shape, "q_out must have q's shape")
-        _heads(q_out, "q_out", d, rows, dev, dense=True)
-    w32 = _weights(d, dev, q_weight, k_weight)
-    rope = _rope(freqs, interleaved, mscale, dev)
-    _launch(dev, "msa_paged_append", ctypes.byref(cache), _ref(rope), _at(q), c_i64(qs), c_i32(q.shape[1] if q is not None else 0),
-            _at(q_weight), _at(k), c_i64(ks), _at(k_weight), _at(v), c_i64(vs), c_i32(w32), ctypes.c_float(eps), c_i64(rows),
-            _at(q_out), stream=stream)
+        qs, hq = _heads(q, "q", d, rows, index), q.shape[1]
+        _like(q_out, q, "q_out", d, rows, index)
+    w32 = _weights(d, index, q_weight, k_weight)
+    rope = _rope(freqs, interleaved, mscale, index)
+    _launch(index, "msa_paged_append", ctypes.byref(cache), _ref(rope), _at(q), qs, hq, _at(q_weight), _at(k), ks, _at(k_weight),
+            _at(v), vs, w32, eps, rows, _at(q_out))
+
+
+def msa_paged_attn_workspace_bytes(k_pool, n_q_heads: int) -> int:
+    pages, size, heads, d = k_pool.shape
+    cache = MsaPagedCache(n_pages=pages, page_size=size, n_kv_heads=heads, head_dim=d, fp8=0 if k_pool.dtype == torch.bfloat16 else 1)
+    mn = c_sz(0)
+    _check(lib().msa_paged_attn_workspace_bytes(ctypes.byref(cache), c_i32(n_q_heads), ctypes.byref(mn)),
+           "msa_paged_attn_workspace_bytes")
+    return int(mn.value)
+
+
+def msa_paged_attn(k_pool, v_pool, page_table, kv_lens, cu_q, q, softmax_scale, out, lse, workspace):
+    """q, out: bf16 [rows, heads, d] dense; lse fp32 [rows, heads] or None."""
+    index, cache = _paged(k_pool, v_pool, page_table, kv_lens, cu_q)
+    d, rows = cache.head_dim, q.shape[0]
+    if v_pool is None:
+        raise ValueError("attention needs a value pool")
+    _heads(q, "q", d, rows, index, dense=True)
+    _like(out, q, "out", d, rows, index)
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous() or
+                            lse.get_device() != index):
+        raise ValueError("lse must be contiguous fp32 %s on cuda:%d" % (tuple(q.shape[:2]), index))
+    _launch(index, "msa_paged_attn", ctypes.byref(cache), q.data_ptr(), q.shape[1], rows, softmax_scale, out.data_ptr(), _at(lse),
+            _at(workspace), _workspace(workspace, index))
 
 
 # ------------------------------------------------------------------ allocation helpers

@@ -5,6 +5,7 @@
 #include <cmath>
 
 #include "norm_rope.cuh"
+#include "paged_attn.cuh"
 #include "tc_common.cuh"
 
 namespace msa {
@@ -121,6 +122,70 @@ static msa_status_t resolve_cache(const msa_paged_cache_t* c, int64_t n_tokens, 
     if (c->max_pages > 0 && (!c->page_table || !aligned_to(c->page_table, 4))) return MSA_ERR_INVALID_ARG;
     if (c->n_pages > 0 && (!c->k || !aligned_to(c->k, 16) || !aligned_to(c->v, 16))) return MSA_ERR_INVALID_ARG;
     return MSA_OK;
+}
+
+// ---------------------------------------------------------------------- attention over the cache
+// Workspace: the CTAs' ends, then the partials.
+struct PagedWorkspace { size_t ends, ml, o, bytes; };
+static PagedWorkspace paged_workspace() {
+    const size_t n = sm_count(), rows = 2 * n * kPagedSlotRows;
+    PagedWorkspace w;
+    w.ends = 0;
+    w.ml = (n * 32 + 255) / 256 * 256;
+    w.o = w.ml + rows * sizeof(float2);
+    w.bytes = w.o + rows * 128 * sizeof(float);
+    return w;
+}
+
+static int common_divisor(int a, int b) { return b == 0 ? a : common_divisor(b, a % b); }
+
+// Shapes of the tensor-core kernel: one 128-wide head row, a group that fits 128 rows, pages that are whole
+// 1 KB operand atoms (8 keys), coordinates in 32 bits.
+static bool paged_tc_ok(const msa_paged_cache_t& c, int G) {
+    return c.head_dim == 128 && G <= 128 && c.page_size % 8 == 0 && c.n_pages > 0 &&
+           (int64_t)c.n_pages * c.page_size < 2147483647LL - 128;
+}
+
+template <bool F8>
+static msa_status_t launch_paged_attn(const PagedAttnArgs& a, const msa_paged_cache_t& c, const void* q, cudaStream_t st) {
+    CUtensorMap tm_q, tm_q1, tm_k, tm_v;
+    const uint64_t H_q = (uint64_t)a.c.H_kv * a.G, H = (uint64_t)a.c.H_kv, rows = (uint64_t)c.n_pages * c.page_size;
+    const int box = common_divisor(c.page_size, kPagedKeys);
+    const uint64_t qd[3] = {128, H_q, (uint64_t)a.n_tokens}, qs[2] = {256, H_q * 256};
+    const uint32_t qb[3] = {64, (uint32_t)a.G, (uint32_t)a.TPT}, qb1[3] = {64, (uint32_t)a.G, 1};
+    bool ok = encode_tmap_bf16(&tm_q, q, 3, qd, qs, qb) && encode_tmap_bf16(&tm_q1, q, 3, qd, qs, qb1);
+    if constexpr (F8) {  // (128 bytes of a key as 64 two-byte elements: only bytes move)
+        const uint64_t kd[3] = {64, H, rows}, ks[2] = {128, H * 128};
+        const uint32_t kb[3] = {64, 1, (uint32_t)box};
+        ok = ok && encode_tmap_bf16(&tm_k, c.k, 3, kd, ks, kb, true) && encode_tmap_bf16(&tm_v, c.v, 3, kd, ks, kb, true);
+    } else {  // 64 of d, 8 keys, the two halves of d, head, groups of 8 keys: a box is a run of operand atoms
+        const uint64_t kd[5] = {64, 8, 2, H, rows / 8}, ks[4] = {H * 256, 128, 256, H * 2048};
+        const uint32_t kb[5] = {64, 8, 2, 1, (uint32_t)box / 8};
+        ok = ok && encode_tmap_bf16(&tm_k, c.k, 5, kd, ks, kb) && encode_tmap_bf16(&tm_v, c.v, 5, kd, ks, kb);
+    }
+    int* status = async_status_ptr();
+    if (!ok || status == nullptr) return MSA_ERR_CUDA;
+    const size_t smem = sizeof(PagedSmem) + 1024;
+    static bool attr_set[64] = {false};  // per device
+    const int dev = current_device(), grid = sm_count();
+    if (!attr_set[dev]) {
+        if (cudaFuncSetAttribute(paged_attn_tc_kernel<F8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+            return MSA_ERR_CUDA;
+        attr_set[dev] = true;
+    }
+    // K and V of one (sequence, head) beyond a third of L2: CTAs on different tiles of it should read in step
+    const int64_t snap = (int64_t)40e6 / (F8 ? 256 : 512);
+    {
+        StageScope sc(kStageNone, st);
+        paged_attn_tc_kernel<F8><<<grid, paged_threads(F8), smem, st>>>(tm_q, tm_q1, tm_k, tm_v, a, box, snap, status);
+    }
+    if (cudaPeekAtLastError() != cudaSuccess) return MSA_ERR_CUDA;
+    {   // a cut tile has at most 256 rows: up to 16 CTAs of four rows at a time, as far as the call has rows
+        const int64_t most = std::min<int64_t>(kPagedSlotRows, (int64_t)a.n_tokens * a.G);
+        StageScope sc(kStageNone, st);
+        paged_combine_kernel<<<dim3(grid, (unsigned)std::min<int64_t>(16, ceil_div64(most, 4))), 128, 0, st>>>(a, grid);
+    }
+    return launch_status();
 }
 
 }  // namespace msa
@@ -246,6 +311,59 @@ msa_status_t msa_paged_append(const msa_paged_cache_t* cache, const msa_rope_t* 
     if (cache->fp8)
         return run_norm_rope<true, true>(rp, qh, kh, vh, n_tokens, d, eps, w32, nullptr, view, cache->k, cache->v, (cudaStream_t)stream);
     return run_norm_rope<true, false>(rp, qh, kh, vh, n_tokens, d, eps, w32, nullptr, view, cache->k, cache->v, (cudaStream_t)stream);
+}
+
+msa_status_t msa_paged_attn_workspace_bytes(const msa_paged_cache_t* cache, int32_t n_q_heads, size_t* min_bytes) {
+    PagedView view;
+    const msa_status_t s = resolve_cache(cache, 0, view);
+    if (s != MSA_OK) return s;
+    if (n_q_heads <= 0 || n_q_heads % cache->n_kv_heads != 0 || min_bytes == nullptr) return MSA_ERR_INVALID_ARG;
+    *min_bytes = paged_tc_ok(*cache, n_q_heads / cache->n_kv_heads) ? paged_workspace().bytes : 0;
+    return MSA_OK;
+}
+
+msa_status_t msa_paged_attn(const msa_paged_cache_t* cache, const void* q, int32_t n_q_heads, int64_t n_tokens,
+                            float softmax_scale, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                            msa_stream_t stream) {
+    PagedView view;
+    const msa_status_t s = resolve_cache(cache, n_tokens, view);
+    if (s != MSA_OK) return s;
+    const int d = cache->head_dim;
+    if (n_q_heads <= 0 || n_q_heads % cache->n_kv_heads != 0) return MSA_ERR_INVALID_ARG;
+    if (!(softmax_scale >= 0.f) || !std::isfinite(softmax_scale)) return MSA_ERR_INVALID_ARG;
+    if (n_q_heads > kMaxRopeHeads) return MSA_ERR_UNSUPPORTED;
+    if (n_tokens == 0 || cache->batch == 0) return MSA_OK;
+    if (!rows_ok(q, (int64_t)n_q_heads * d, n_q_heads, d) || !rows_ok(out, (int64_t)n_q_heads * d, n_q_heads, d)) return MSA_ERR_INVALID_ARG;
+    if (!aligned_to(lse, 4) || (cache->n_pages > 0 && cache->v == nullptr)) return MSA_ERR_INVALID_ARG;
+    const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)d);
+    PagedAttnArgs a{};
+    a.c = view;
+    a.G = n_q_heads / cache->n_kv_heads;
+    a.n_tokens = (int)n_tokens;
+    a.scale_log2e = scale * 1.4426950408889634f;
+    a.out = (__nv_bfloat16*)out;
+    a.lse = lse;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (paged_tc_ok(*cache, a.G)) {
+        const PagedWorkspace w = paged_workspace();
+        if (workspace == nullptr || !aligned_to(workspace, 256)) return MSA_ERR_INVALID_ARG;
+        if (workspace_bytes < w.bytes) return MSA_ERR_WORKSPACE;
+        a.TPT = 128 / a.G;
+        a.ends = (int4*)((char*)workspace + w.ends);
+        a.part_ml = (float2*)((char*)workspace + w.ml);
+        a.part_o = (float*)((char*)workspace + w.o);
+        return cache->fp8 ? launch_paged_attn<true>(a, *cache, q, st) : launch_paged_attn<false>(a, *cache, q, st);
+    }
+    const int64_t grid = ceil_div64(n_tokens * n_q_heads, 4);
+    if (grid > 2147483647LL) return MSA_ERR_UNSUPPORTED;
+    int* status = async_status_ptr();
+    if (status == nullptr) return MSA_ERR_CUDA;
+    {
+        StageScope sc(kStageNone, st);
+        if (cache->fp8) paged_attn_generic_kernel<true><<<(unsigned)grid, 128, 0, st>>>(a, (const __nv_bfloat16*)q, cache->k, cache->v, d, status);
+        else paged_attn_generic_kernel<false><<<(unsigned)grid, 128, 0, st>>>(a, (const __nv_bfloat16*)q, cache->k, cache->v, d, status);
+    }
+    return launch_status();
 }
 
 }  // extern "C"

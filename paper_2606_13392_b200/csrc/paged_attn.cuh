@@ -1,0 +1,793 @@
+// Softmax attention of new tokens over a paged cache (include/msa.h: msa_paged_attn):
+//   out[t, h] = sum_{j <= pos(t)} softmax_j(scale <q[t, h], k_j>) v_j,   lse = log sum_j exp(scale <q, k_j>)
+//
+// Unit of work: 128 keys against one tile of query rows of a (sequence, KV head).  A row is a (token, head of the
+// group) pair, so the G heads of a group share every K/V tile: a context holds TPT = 128 / G tokens.  Sequences of
+// more new tokens than that give a CTA two contexts of consecutive tokens that share the K/V tiles (256 rows per
+// 64 KB); short ones (decode) put both contexts on the same rows, taking key tiles in turn, and merge at the end.
+//
+// The units of all tiles form one line (sequence, head, tile, key tile) and every CTA takes an equal stretch of it:
+// ragged batches balance to one unit whatever their lengths.  A tile that a stretch boundary cuts leaves fp32
+// partials (at most two per CTA), merged by paged_combine_kernel; all others are written directly.
+#pragma once
+
+#include "norm_rope.cuh"
+#include "tc_common.cuh"
+
+namespace msa {
+
+constexpr int kPagedKeys = 128;   // keys of a tile
+constexpr int kPagedKStages = 2, kPagedVStages = 3;  // (V waits for the softmax, K does not)
+constexpr int kPagedSlotRows = 256;                  // rows of a partial: two contexts
+
+struct PagedAttnArgs {
+    PagedView c;
+    int G, TPT;          // query heads per KV head; tokens per context
+    int n_tokens;
+    float scale_log2e;
+    __nv_bfloat16* out;  // [n_tokens, H_kv*G, 128]
+    float* lse;          // [n_tokens, H_kv*G] or null
+    // partials: CTA i owns slots 2i (a tile begun by an earlier CTA) and 2i+1 (a tile that a later one ends)
+    float* part_o;       // [slot][kPagedSlotRows][128], not normalised
+    float2* part_ml;     // [slot][kPagedSlotRows] reference maximum (log2 units) and sum
+    int4* ends;          // [CTA][2]: see PagedEnds
+};
+
+// What paged_combine_kernel has to know about a CTA.
+//   first: 0 no work; 1 its first tile came from an earlier CTA and goes on in a later one; 2 came from an earlier
+//          one and ends here; 3 begins here
+//   open:  its last tile begins here and ends in a later CTA; q_row, tokens, head describe it
+struct PagedEnds { int first, open, q_row, tokens, head, pad[3]; };
+static_assert(sizeof(PagedEnds) == 32, "two int4");
+
+// ---------------------------------------------------------------- the line of units
+struct PagedSeq { int q_row, q_len, kv, base, tile_tokens, n_tiles; };
+
+__host__ __device__ __forceinline__ int64_t paged_cap(const PagedView& c) { return (int64_t)c.max_pages * c.page_size; }
+
+__host__ __device__ __forceinline__ PagedSeq paged_seq(const PagedAttnArgs& a, int s) {
+    PagedSeq q;
+    const int lo = max(a.c.cu_q[s], 0), hi = min(a.c.cu_q[s + 1], a.n_tokens);
+    q.q_row = lo;
+    q.q_len = max(hi - lo, 0);
+    q.kv = (int)min((int64_t)max(a.c.kv_lens[s], 0), paged_cap(a.c));
+    q.base = q.kv - q.q_len;  // position of the first new token
+    q.tile_tokens = q.q_len <= a.TPT ? a.TPT : 2 * a.TPT;
+    q.n_tiles = (q.q_len + q.tile_tokens - 1) / q.tile_tokens;
+    return q;
+}
+
+// Key tiles of query tile t: up to its last token's position (at least one: a tile of rows that see nothing is
+// visited too, to write their zeros).
+__host__ __device__ __forceinline__ int paged_blocks(const PagedSeq& q, int t) {
+    const int64_t last = (int64_t)max(q.base, 0) + min((int64_t)(t + 1) * q.tile_tokens, (int64_t)q.q_len);
+    return (int)((last + kPagedKeys - 1) / kPagedKeys);
+}
+
+// sum over i < n of floor((a i + b) / m), a, b >= 0: Euclid's steps on (a, m).
+__host__ __device__ inline int64_t floor_sum(int64_t n, int64_t m, int64_t a, int64_t b) {
+    int64_t sum = 0;
+    while (n > 0) {
+        sum += n * (n - 1) / 2 * (a / m) + n * (b / m);
+        a %= m;
+        b %= m;
+        const int64_t y = a * n + b;
+        n = y / m;
+        b = y % m;
+        const int64_t t = m;
+        m = a;
+        a = t;
+        if (m == 0) break;
+    }
+    return sum;
+}
+
+// Units of the first t query tiles of one head.
+__host__ __device__ inline int64_t paged_units_before(const PagedSeq& q, int t) {
+    if (t <= 0) return 0;
+    const int full = min(t, q.n_tiles - 1);  // (the last tile may be short)
+    int64_t u = floor_sum(full, kPagedKeys, q.tile_tokens, (int64_t)max(q.base, 0) + q.tile_tokens + kPagedKeys - 1);
+    if (t >= q.n_tiles) u += paged_blocks(q, q.n_tiles - 1);
+    return u;
+}
+
+// A place on the line; seq = batch: its end.
+struct PagedPlace { int seq, head, tile, blk; };
+
+// Unit `u` of sequence s.  snap: places inside long tiles move to the nearest eighth of the tile, so that CTAs that
+// read the same long K/V do it in step (see launch_paged_attn).
+__host__ __device__ inline PagedPlace paged_place(const PagedAttnArgs& a, int s, int64_t u, int64_t snap_keys) {
+    const PagedSeq q = paged_seq(a, s);
+    const int64_t per_head = paged_units_before(q, q.n_tiles);
+    PagedPlace p;
+    p.seq = s;
+    p.head = (int)(u / per_head);
+    u -= p.head * per_head;
+    int lo = 0, hi = q.n_tiles;  // units_before(lo) <= u < units_before(hi)
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (paged_units_before(q, mid) <= u) lo = mid; else hi = mid;
+    }
+    p.tile = lo;
+    p.blk = (int)(u - paged_units_before(q, lo));
+    if (q.n_tiles > 1 && q.kv > snap_keys) {
+        const int nb = paged_blocks(q, lo), step = (nb + 7) / 8;
+        p.blk = min(nb, (p.blk + step / 2) / step * step);
+    }
+    return p;
+}
+
+struct PagedItem {
+    int seq, head, q_row, n0, n1;  // tokens of the two contexts; n1 = 0: both contexts on the first's rows
+    int lo, hi, nb;                // key tiles [lo, hi) of nb
+    int pos, kv;                   // position of the first token; visible keys of the sequence
+    __host__ __device__ bool dual() const { return n1 == 0; }
+    // key tiles that context j takes
+    __host__ __device__ int steps(int j) const { return n1 == 0 ? (hi - lo + 1 - j) / 2 : hi - lo; }
+    __host__ __device__ int block(int j, int n) const { return n1 == 0 ? lo + 2 * n + j : lo + n; }
+    __host__ __device__ bool partial() const { return lo > 0 || hi < nb; }
+};
+
+// Walks the items of a stretch; every role of a CTA walks the same ones.
+struct PagedWalk {
+    PagedPlace at, end;
+    PagedSeq q;
+    int loaded;
+    __host__ __device__ PagedWalk(const PagedPlace& from, const PagedPlace& to) : at(from), end(to), loaded(-1) {}
+    __host__ __device__ bool next(const PagedAttnArgs& a, PagedItem& it) {
+        while (at.seq < a.c.batch) {
+            if (loaded != at.seq) { q = paged_seq(a, at.seq); loaded = at.seq; }
+            if (at.tile >= q.n_tiles) {
+                at.tile = 0;
+                if (++at.head >= a.c.H_kv || q.n_tiles == 0) {
+                    if (at.seq >= end.seq) { at.seq = a.c.batch; return false; }
+                    at.head = 0;
+                    ++at.seq;
+                }
+                continue;
+            }
+            const int nb = paged_blocks(q, at.tile);
+            const bool last = at.seq == end.seq && at.head == end.head && at.tile == end.tile;
+            const int lo = at.blk, hi = last ? end.blk : nb, tile = at.tile, head = at.head, seq = at.seq;
+            at.blk = 0;
+            ++at.tile;
+            if (last) at.seq = a.c.batch;
+            if (lo >= hi) continue;
+            const int first = tile * q.tile_tokens, n = min(q.tile_tokens, q.q_len - first);
+            it.seq = seq; it.head = head;
+            it.q_row = q.q_row + first;
+            it.n0 = min(n, a.TPT); it.n1 = n - it.n0;
+            it.lo = lo; it.hi = hi; it.nb = nb;
+            it.pos = q.base + first; it.kv = q.kv;
+            return true;
+        }
+        return false;
+    }
+};
+
+// ---------------------------------------------------------------- the kernel
+struct PagedSmem {
+    alignas(1024) uint8_t q[2][128 * 256];  // [context][d half][row][64 bf16]
+    alignas(1024) uint8_t k[kPagedKStages][kPagedKeys * 256];  // [8 keys][d half][key][64 bf16]
+    alignas(1024) uint8_t v[kPagedVStages][kPagedKeys * 256];
+    float2 ml[128];                          // the second context's maxima and sums on their way to the first
+    alignas(8) uint64_t q_full[2], q_empty[2];
+    uint64_t k_full[kPagedKStages], k_empty[kPagedKStages], k_land[kPagedKStages];
+    uint64_t v_full[kPagedVStages], v_empty[kPagedVStages], v_land[kPagedVStages];
+    uint64_t s_full[2], p_full[2], o_full[2], o_empty[2];
+    uint64_t v_tail, ml_full, ml_empty, drain;
+    int64_t scan[16], targets[2];
+    PagedPlace place[2];
+    uint32_t tmem_base;
+    int abort;
+};
+
+constexpr int paged_threads(bool f8) { return f8 ? 512 : 384; }
+
+// Barriers among the four widening warps only.
+__device__ __forceinline__ void conv_barrier() { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ bool conv_agree(bool mine) {
+    uint32_t all;
+    asm volatile(
+        "{\n\t.reg .pred p, r;\n\t"
+        "setp.ne.u32 p, %1, 0;\n\t"
+        "barrier.cta.red.and.pred r, 2, 128, p;\n\t"
+        "selp.u32 %0, 1, 0, r;\n\t}"
+        : "=r"(all)
+        : "r"((uint32_t)mine)
+        : "memory");
+    return all != 0;
+}
+
+// Warps: 0-3 / 4-7 softmax of context 0 / 1 (thread = row), 8 loads K, 9 loads V, 10 issues the MMAs, 11 loads Q,
+// 12-15 (fp8 caches) widen the tiles to bf16.
+template <bool F8>
+__global__ void __launch_bounds__(paged_threads(F8), 1)
+paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_q1,
+                     const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                     const PagedAttnArgs a, int box_keys, int64_t snap_keys, int* status) {
+    constexpr uint32_t TILE = F8 ? kPagedKeys * 128 : kPagedKeys * 256;  // bytes of a K or V tile in the cache
+    extern __shared__ uint8_t smem_raw[];
+    PagedSmem& sm = *reinterpret_cast<PagedSmem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    volatile int* abort = &sm.abort;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&sm.q_full[i], 1); mbar_init(&sm.q_empty[i], 1);
+            mbar_init(&sm.s_full[i], 1); mbar_init(&sm.p_full[i], 4);
+            mbar_init(&sm.o_full[i], 1); mbar_init(&sm.o_empty[i], 4);
+        }
+        for (int i = 0; i < kPagedKStages; ++i) {
+            mbar_init(&sm.k_full[i], F8 ? 4 : 1); mbar_init(&sm.k_empty[i], 1); mbar_init(&sm.k_land[i], 1);
+        }
+        for (int i = 0; i < kPagedVStages; ++i) {
+            mbar_init(&sm.v_full[i], F8 ? 4 : 1); mbar_init(&sm.v_empty[i], 1); mbar_init(&sm.v_land[i], 1);
+        }
+        mbar_init(&sm.v_tail, 1); mbar_init(&sm.ml_full, 4); mbar_init(&sm.ml_empty, 4); mbar_init(&sm.drain, 1);
+        sm.abort = 0;
+        sm.targets[0] = sm.targets[1] = -1;
+        fence_mbar_init();
+        tma_prefetch_desc(&tm_q); tma_prefetch_desc(&tm_q1);
+        tma_prefetch_desc(&tm_k); tma_prefetch_desc(&tm_v);
+    }
+    if (warp == 10) tmem_alloc(&sm.tmem_base, 512);
+
+    // ---- this CTA's stretch: units of all sequences summed up, the boundaries looked up
+    {
+        const int per = (a.c.batch + blockDim.x - 1) / blockDim.x;
+        const int s_lo = min((int)threadIdx.x * per, a.c.batch), s_hi = min(s_lo + per, a.c.batch);
+        int64_t mine = 0;
+        for (int s = s_lo; s < s_hi; ++s) {
+            const PagedSeq q = paged_seq(a, s);
+            mine += (int64_t)a.c.H_kv * paged_units_before(q, q.n_tiles);
+            if (blockIdx.x == 0 && (a.c.kv_lens[s] < 0 || a.c.kv_lens[s] > paged_cap(a.c)))
+                report_async(status, kAsyncBadIndex, 0x601);
+        }
+        int64_t upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t below = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += below;
+        }
+        if (lane == 31) sm.scan[warp] = upto;
+        __syncthreads();
+        int64_t total = 0;
+        for (int w = 0; w < (int)blockDim.x / 32; ++w) {
+            if (w < warp) upto += sm.scan[w];
+            total += sm.scan[w];
+        }
+        for (int e = 0; e < 2; ++e) {
+            const int64_t target = total / gridDim.x * (blockIdx.x + e) + total % gridDim.x * (blockIdx.x + e) / gridDim.x;
+            if (target >= upto - mine && target < upto) {  // (one thread, unless target = total)
+                int64_t before = upto - mine;
+                for (int s = s_lo; s < s_hi; ++s) {
+                    const PagedSeq q = paged_seq(a, s);
+                    const int64_t u = (int64_t)a.c.H_kv * paged_units_before(q, q.n_tiles);
+                    if (target < before + u) {
+                        sm.place[e] = paged_place(a, s, target - before, snap_keys);
+                        break;
+                    }
+                    before += u;
+                }
+                sm.targets[e] = target;
+            }
+        }
+        __syncthreads();
+        if (threadIdx.x < 2 && sm.targets[threadIdx.x] < 0) sm.place[threadIdx.x] = PagedPlace{a.c.batch, 0, 0, 0};
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sm.tmem_base;
+    PagedWalk walk(sm.place[0], sm.place[1]);
+    PagedItem it{};
+
+    if (warp == 8 || warp == 9) {
+        // ---------------- K / V producer: one box per page (or 128 keys of a larger one), a lane each
+        const bool is_v = warp == 9;
+        const int stages = is_v ? kPagedVStages : kPagedKStages;
+        const int boxes = kPagedKeys / box_keys;
+        const CUtensorMap* tm = is_v ? &tm_v : &tm_k;
+        const int nowhere = F8 ? a.c.n_pages * a.c.page_size : a.c.n_pages * a.c.page_size / 8;  // reads as zeros
+        bool ok = true;
+        int t = 0;
+        uint32_t tails = 0;
+        if (const long long late = g_debug_producer_delay; late > 0) spin_cycles(late);  // tests only
+        // coordinate of this lane's box of key tile b: its page's row, or outside the pool
+        auto place_of = [&](int b) {
+            const int64_t key = (int64_t)b * kPagedKeys + lane * box_keys;
+            if (lane >= boxes || key >= it.kv) return nowhere;
+            const int page = a.c.table[(int64_t)it.seq * a.c.max_pages + key / a.c.page_size];
+            if (page < 0 || page >= a.c.n_pages) {
+                report_async(status, kAsyncBadIndex, 0x602);
+                return nowhere;
+            }
+            const int row = page * a.c.page_size + (int)(key % a.c.page_size);
+            return F8 ? row : row / 8;
+        };
+        while (ok && walk.next(a, it)) {
+            int where = place_of(it.lo);
+            for (int b = it.lo; b < it.hi; ++b, ++t) {
+                const int where_next = b + 1 < it.hi ? place_of(b + 1) : 0;
+                const int st = t % stages;
+                const uint32_t use = t / stages;
+                uint64_t* empty = is_v ? &sm.v_empty[st] : &sm.k_empty[st];
+                uint64_t* full = is_v ? &sm.v_full[st] : &sm.k_full[st];
+                uint64_t* land = is_v ? &sm.v_land[st] : &sm.k_land[st];
+                uint8_t* dst = is_v ? sm.v[st] : sm.k[st];
+                if (use > 0 && !mbar_wait(empty, (use - 1) & 1, abort)) {
+                    if (lane == 0) report_async(status, kAsyncTimeout, 0x611);
+                    ok = false;
+                    break;
+                }
+                // The last tile's V rows behind the end may hold anything, and 0 * NaN is NaN: they are overwritten
+                // with zeros before the MMA sees the tile (fp8: by the widening warps).
+                const int rows = it.kv - b * kPagedKeys;  // rows inside the sequence
+                const bool tail = !F8 && is_v && rows < kPagedKeys;
+                uint64_t* bar = F8 ? land : (tail ? &sm.v_tail : full);
+                if (lane == 0) mbar_arrive_expect_tx(bar, TILE);
+                __syncwarp();
+                if (lane < boxes) {
+                    if constexpr (F8) tma_load_3d(dst + TILE + lane * box_keys * 128, tm, 0, it.head, where, bar);
+                    else tma_load_5d(dst + lane * box_keys * 256, tm, 0, 0, 0, it.head, where, bar);
+                }
+                if (tail) {
+                    if (!mbar_wait(&sm.v_tail, tails & 1, abort)) {
+                        if (lane == 0) report_async(status, kAsyncTimeout, 0x612);
+                        ok = false;
+                        break;
+                    }
+                    ++tails;
+                    for (int i = max(rows, 0) * 16 + lane; i < kPagedKeys * 16; i += 32) {
+                        const int key = i >> 4, c = i & 15;
+                        *reinterpret_cast<uint4*>(dst + (key >> 3) * 2048 + (c >> 3) * 1024 + (key & 7) * 128 + (c & 7) * 16) =
+                            make_uint4(0u, 0u, 0u, 0u);
+                    }
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(full);
+                }
+                where = where_next;
+            }
+        }
+        if (*abort != 0) spin_cycles(200000);
+    } else if (warp == 11) {
+        // ---------------- Q producer, and the note for the merge
+        PagedEnds e{};
+        bool ok = true;
+        uint32_t used[2] = {0, 0};
+        while (walk.next(a, it)) {
+            if (e.first == 0) e.first = it.lo == 0 ? 3 : (it.hi < it.nb ? 1 : 2);
+            e.open = it.lo == 0 && it.hi < it.nb;
+            e.q_row = it.q_row; e.tokens = it.n0 + it.n1; e.head = it.head;
+            for (int j = 0; j < 2 && ok; ++j) {
+                const int n = j == 0 ? it.n0 : it.n1;
+                if (n == 0) continue;
+                if (used[j] > 0 && !mbar_wait(&sm.q_empty[j], (used[j] - 1) & 1, abort)) {
+                    if (lane == 0) report_async(status, kAsyncTimeout, 0x621);
+                    ok = false;
+                    break;
+                }
+                ++used[j];
+                const int row = it.q_row + j * a.TPT, head = it.head * a.G;
+                // Few tokens: their own boxes (rows behind them keep what they held: no row reads another's).  All: one
+                // box for each half of d; tokens of the next sequence come along, tokens that are not there read as zeros.
+                const bool few = n * 2 <= 16 && n < a.TPT && a.G % 8 == 0;
+                if (lane == 0) mbar_arrive_expect_tx(&sm.q_full[j], (uint32_t)((few ? n : a.TPT) * a.G * 256));
+                __syncwarp();
+                if (few) {
+                    if (lane < 2 * n)
+                        tma_load_3d(sm.q[j] + (lane & 1) * 16384 + (lane >> 1) * a.G * 128, &tm_q1, (lane & 1) * 64, head, row + (lane >> 1),
+                                    &sm.q_full[j]);
+                } else if (lane < 2) {
+                    tma_load_3d(sm.q[j] + lane * 16384, &tm_q, lane * 64, head, row, &sm.q_full[j]);
+                }
+            }
+        }
+        if (lane == 0) {
+            a.ends[blockIdx.x * 2] = make_int4(e.first, e.open, e.q_row, e.tokens);
+            a.ends[blockIdx.x * 2 + 1] = make_int4(e.head, 0, 0, 0);
+        }
+        if (*abort != 0) spin_cycles(200000);
+    } else if (warp == 10) {
+        // ---------------- MMA issuer: S_j(n) = Q_j K^T, then, once P_j(n) is written, O_j += P_j(n) V.  MMAs run in
+        // issue order: S_j(n) may overwrite P_j(n-1) because O_j += P_j(n-1) V was issued before it, and the barrier
+        // that says S_j(n) is there says as well that O_j holds everything up to n-1.
+        if (lane == 0) {
+            constexpr uint32_t idesc_s = make_idesc_bf16(128, kPagedKeys, false, false);
+            constexpr uint32_t idesc_o = make_idesc_bf16(128, 128, false, true);
+            uint32_t n_p[2] = {0, 0}, n_o[2] = {0, 0}, n_q[2] = {0, 0};
+            int kt = 0, vt = 0;
+            bool ok = true;
+            while (ok && walk.next(a, it)) {
+                const bool dual = it.dual();
+                const int st[2] = {it.steps(0), it.steps(1)};
+                for (int n = 0; ok && n <= st[0]; ++n) {
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const uint32_t ts = tmem + j * 128, to = tmem + 256 + j * 128;
+                        if (n >= 1 && n - 1 < st[j]) {
+                            const int v_tile = vt + (dual ? 2 * (n - 1) + j : n - 1), vs = v_tile % kPagedVStages;
+                            if (!mbar_wait(&sm.p_full[j], n_p[j]++ & 1, abort) ||
+                                !mbar_wait(&sm.v_full[vs], (v_tile / kPagedVStages) & 1, abort) ||
+                                (n == 1 && n_o[j] > 0 && !mbar_wait(&sm.o_empty[j], (n_o[j] - 1) & 1, abort))) {
+                                report_async(status, kAsyncTimeout, 0x631);
+                                ok = false;
+                                break;
+                            }
+                            tc_fence_after();
+                            // V as the MN-major B operand: 8-key groups 2 KB apart, the other 64 columns of d 1 KB away
+                            const uint64_t vd = make_smem_desc(smem_u32(sm.v[vs]), 1024, 2048);
+#pragma unroll
+                            for (int kk = 0; kk < kPagedKeys / 16; ++kk)
+                                mma_bf16_ts(to, ts + kk * 8, vd + (uint64_t)(kk * 4096 / 16), idesc_o, n > 1 || kk > 0);
+                            if (dual || j == 1) mma_commit(&sm.v_empty[vs]);
+                            if (n == st[j]) { mma_commit(&sm.o_full[j]); ++n_o[j]; }
+                        }
+                        if (n < st[j]) {
+                            const int qb = dual ? 0 : j;
+                            const int k_tile = kt + (dual ? 2 * n + j : n), ks = k_tile % kPagedKStages;
+                            if (!mbar_wait(&sm.q_full[qb], n_q[qb] & 1, abort) ||
+                                !mbar_wait(&sm.k_full[ks], (k_tile / kPagedKStages) & 1, abort)) {
+                                report_async(status, kAsyncTimeout, 0x632);
+                                ok = false;
+                                break;
+                            }
+                            tc_fence_after();
+                            const uint64_t qd = make_smem_desc(smem_u32(sm.q[qb]), 16, 1024);
+                            const uint64_t kd = make_smem_desc(smem_u32(sm.k[ks]), 16, 2048);
+#pragma unroll
+                            for (int kk = 0; kk < 8; ++kk)  // 16 of d each; second half of Q 16 KB on, of K 1 KB
+                                mma_bf16_ss(ts, qd + (uint64_t)((kk >> 2) * 1024 + 2 * (kk & 3)),
+                                            kd + (uint64_t)((kk >> 2) * 64 + 2 * (kk & 3)), idesc_s, kk > 0);
+                            mma_commit(&sm.s_full[j]);
+                            if (dual || j == 1) mma_commit(&sm.k_empty[ks]);
+                            if (dual ? 2 * n + j == it.hi - it.lo - 1 : n == st[j] - 1) mma_commit(&sm.q_empty[qb]);
+                        }
+                    }
+                }
+                kt += it.hi - it.lo; vt += it.hi - it.lo;
+                ++n_q[0];
+                if (!dual) ++n_q[1];
+            }
+            if (*abort != 0) {
+                mma_commit(&sm.drain);
+                mbar_wait_quiet(&sm.drain, 0, 20000000);
+            }
+        }
+    } else if (warp >= 12) {
+        // ---------------- widening (fp8): a tile lands in the upper half of its stage (row = key, 128 bytes, chunks
+        // swizzled by key mod 8); all threads read their row before any writes the bf16 tile over it.
+        if constexpr (F8) {
+            const int key = threadIdx.x - 384, sw = key & 7;
+            int t = 0;
+            bool ok = true;
+            while (ok && walk.next(a, it)) {
+                for (int b = it.lo; ok && b < it.hi; ++b, ++t)
+                    for (int kv = 0; kv < 2; ++kv) {
+                        const int stages = kv == 0 ? kPagedKStages : kPagedVStages, st = t % stages;
+                        uint64_t* land = kv == 0 ? &sm.k_land[st] : &sm.v_land[st];
+                        uint64_t* full = kv == 0 ? &sm.k_full[st] : &sm.v_full[st];
+                        uint8_t* tile = kv == 0 ? sm.k[st] : sm.v[st];
+                        // (a wait may run out in one warp and not in another: all four go on or none)
+                        const bool landed = mbar_wait(land, (t / stages) & 1, abort);
+                        if (!conv_agree(landed)) {
+                            if (lane == 0) report_async(status, kAsyncTimeout, 0x641);
+                            ok = false;
+                            break;
+                        }
+                        const bool inside = kv == 0 || (int64_t)b * kPagedKeys + key < it.kv;
+                        uint4 x[8];
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) {
+                            x[c] = make_uint4(0u, 0u, 0u, 0u);
+                            if (inside) x[c] = *reinterpret_cast<const uint4*>(tile + TILE + key * 128 + ((c ^ sw) << 4));
+                        }
+                        conv_barrier();
+                        uint8_t* row = tile + (key >> 3) * 2048 + sw * 128;
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) {
+                            const uint32_t w[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
+                            uint32_t o[8];
+                            e4m3x16_to_bf16x16(w, o);
+                            const int cc = 2 * (c & 3);
+                            uint8_t* to = row + (c >> 2) * 1024;
+                            *reinterpret_cast<uint4*>(to + ((cc ^ sw) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+                            *reinterpret_cast<uint4*>(to + (((cc + 1) ^ sw) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+                        }
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(full);
+                    }
+            }
+        }
+    } else {
+        // ---------------- softmax and epilogue: thread = row (TMEM lane)
+        const int j = warp >> 2, quarter = warp & 3;
+        const int row = quarter * 32 + lane, tok = row / a.G, g = row - tok * a.G;
+        const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
+        const uint32_t tmem_s = tmem + lane_base + j * 128, tmem_o = tmem + lane_base + 256 + j * 128;
+        const int H_q = a.c.H_kv * a.G;
+        uint32_t n_s = 0, n_o[2] = {0, 0}, n_ml = 0;
+        bool ok = true;
+        while (ok && walk.next(a, it)) {
+            const bool dual = it.dual();
+            const int steps = it.steps(j);
+            const int tokens = dual || j == 0 ? it.n0 : it.n1;
+            const bool warp_on = quarter * 32 < tokens * a.G;  // some row of the warp is a query's
+            const bool row_on = tok < tokens;
+            const int first = dual || j == 0 ? 0 : a.TPT;
+            const int64_t pos = (int64_t)it.pos + first + tok;
+            float m_ref = -INFINITY, l = 0.f;
+            for (int n = 0; n < steps; ++n) {
+                if (!mbar_wait(&sm.s_full[j], n_s++ & 1, abort)) {
+                    if (lane == 0) report_async(status, kAsyncTimeout, 0x651);
+                    ok = false;
+                    break;
+                }
+                if (warp_on) {
+                    tc_fence_after();
+                    uint32_t sv[4][32];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) tmem_ld_32x32(tmem_s + c * 32, sv[c]);
+                    tmem_wait_ld();
+                    const int64_t lim = pos - (int64_t)it.block(j, n) * kPagedKeys;  // keys 0..lim of the tile are visible
+                    if (lim < kPagedKeys - 1) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (c * 32 + e > lim) sv[c][e] = 0xFF800000u;  // -inf
+                    }
+                    const float mx = fmaxf(fmaxf(tree_max32(sv[0]), tree_max32(sv[1])), fmaxf(tree_max32(sv[2]), tree_max32(sv[3])));
+                    // The reference maximum moves only when a row's maximum has outgrown it by 2^8: P then stays below
+                    // 2^8 (bf16 keeps its relative precision) and O is hardly ever rescaled.
+                    const float m_new = fmaxf(m_ref, mx);
+                    if (n == 0) {
+                        m_ref = m_new;
+                    } else if (__any_sync(0xffffffffu, row_on && (m_new - m_ref) * a.scale_log2e > 8.f)) {
+                        const float corr = m_new == -INFINITY ? 1.f : ex2_approx((m_ref - m_new) * a.scale_log2e);
+                        m_ref = m_new;
+                        l *= corr;
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            uint32_t ov[32];
+                            tmem_ld_32x32(tmem_o + c * 32, ov);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * corr);
+                            tmem_st_32x32(tmem_o + c * 32, ov);
+                        }
+                    }
+                    const float mc = m_ref == -INFINITY ? 0.f : m_ref * a.scale_log2e;
+                    float l4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int c2 = 0; c2 < 2; ++c2) {
+                        uint32_t pk[32];
+#pragma unroll
+                        for (int w = 0; w < 32; ++w) {
+                            const int col = c2 * 64 + 2 * w;
+                            const float p0 = ex2_approx(fmaf(__uint_as_float(sv[col >> 5][col & 31]), a.scale_log2e, -mc));
+                            const float p1 = ex2_approx(fmaf(__uint_as_float(sv[col >> 5][(col & 31) + 1]), a.scale_log2e, -mc));
+                            l4[w & 3] += p0 + p1;
+                            pk[w] = pack2(p0, p1);
+                        }
+                        tmem_st_32x32(tmem_s + c2 * 32, pk);
+                    }
+                    l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
+                    tmem_wait_st();
+                    tc_fence_before();
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sm.p_full[j]);
+            }
+            if (!ok) break;
+            const float m_log2 = m_ref == -INFINITY ? -INFINITY : m_ref * a.scale_log2e;
+            const int other = dual ? it.steps(1) : 0;  // steps of the context to be merged in
+            if (dual && j == 1) {
+                // hand the row's maximum and sum to the first context, which reads O_1 as well
+                if (steps == 0) continue;
+                if (n_ml > 0 && !mbar_wait(&sm.ml_empty, (n_ml - 1) & 1, abort)) {
+                    if (lane == 0) report_async(status, kAsyncTimeout, 0x652);
+                    break;
+                }
+                ++n_ml;
+                sm.ml[row] = make_float2(m_log2, l);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sm.ml_full);
+                ++n_o[1];
+                continue;
+            }
+            if (j == 0 && !dual) ++n_o[1];  // (the second context's own accumulator of this item)
+            float w0 = 1.f, w1 = 0.f, m_all = m_log2;
+            if (!mbar_wait(&sm.o_full[j], n_o[j]++ & 1, abort)) {
+                if (lane == 0) report_async(status, kAsyncTimeout, 0x653);
+                break;
+            }
+            if (other > 0) {
+                if (!mbar_wait(&sm.o_full[1], n_o[1]++ & 1, abort) || !mbar_wait(&sm.ml_full, n_ml & 1, abort)) {
+                    if (lane == 0) report_async(status, kAsyncTimeout, 0x654);
+                    break;
+                }
+                ++n_ml;
+                const float2 ml = sm.ml[row];
+                m_all = fmaxf(m_log2, ml.x);
+                w0 = m_log2 == -INFINITY ? 0.f : ex2_approx(m_log2 - m_all);
+                w1 = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - m_all);
+                l = w0 * l + w1 * ml.y;
+            }
+            tc_fence_after();
+            if (warp_on) {
+                const bool partial = it.partial();
+                const int64_t out_row = ((int64_t)it.q_row + first + tok) * H_q + it.head * a.G + g;
+                const int64_t slot_row = ((int64_t)blockIdx.x * 2 + (it.lo > 0 ? 0 : 1)) * kPagedSlotRows + (first > 0 ? 128 : 0) + row;
+                if (!partial) {
+                    const float inv = l == 0.f ? 0.f : 1.f / l;  // (a row that sees nothing is zero)
+                    w0 *= inv; w1 *= inv;
+                }
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t ov[32];
+                    tmem_ld_32x32(tmem_o + c * 32, ov);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * w0);
+                    if (other > 0) {
+                        uint32_t o1[32];
+                        tmem_ld_32x32(tmem_o + 128 + c * 32, o1);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(fmaf(__uint_as_float(o1[e]), w1, __uint_as_float(ov[e])));
+                    }
+                    if (row_on && partial) {
+                        float4* to = reinterpret_cast<float4*>(a.part_o + slot_row * 128 + c * 32);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            to[e] = make_float4(__uint_as_float(ov[4 * e]), __uint_as_float(ov[4 * e + 1]), __uint_as_float(ov[4 * e + 2]),
+                                                __uint_as_float(ov[4 * e + 3]));
+                    } else if (row_on) {
+                        uint4* to = reinterpret_cast<uint4*>(a.out + out_row * 128 + c * 32);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            float f[8];
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(ov[8 * e + i]);
+                            to[e] = pack8(f);
+                        }
+                    }
+                    __syncwarp();
+                }
+                if (row_on) {
+                    if (partial) a.part_ml[slot_row] = make_float2(m_all, l);
+                    else if (a.lse != nullptr) a.lse[out_row] = l == 0.f ? -INFINITY : (m_all + log2f(l)) * 0.6931471805599453f;
+                }
+                tc_fence_before();
+            }
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(&sm.o_empty[j]);
+                if (other > 0) { mbar_arrive(&sm.o_empty[1]); mbar_arrive(&sm.ml_empty); }
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 10) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// Merges the partials of tiles that stretch boundaries cut: CTA (i, .) the tile that attention CTA i left open, a warp
+// per row.  With M the largest reference maximum, O = sum 2^(m - M) O_p, l likewise; out = O / l.  The order of the
+// parts is that of the line, so equal calls give equal bits.
+__global__ void __launch_bounds__(128)
+paged_combine_kernel(const PagedAttnArgs a, int n_ctas) {
+    const int c0 = blockIdx.x;
+    const int4 e = a.ends[c0 * 2];
+    if (e.y == 0) return;
+    const int head = a.ends[c0 * 2 + 1].x, tokens = e.w, lane = threadIdx.x & 31;
+    __shared__ int s_slot[512];  // parts: at most one for each CTA
+    __shared__ int s_n;
+    if (threadIdx.x < 32) {
+        int n = 1;
+        if (lane == 0) s_slot[0] = 2 * c0 + 1;
+        for (int c = c0 + 1; c < n_ctas; c += 32) {
+            const int first = c + lane < n_ctas ? a.ends[(c + lane) * 2].x : 3;
+            const unsigned stop = __ballot_sync(0xffffffffu, first >= 2);  // 2: the last part, 3: none of this tile's
+            const int upto = stop ? __ffs(stop) - 1 : 32;
+            const bool part = (lane < upto && first == 1) || (lane == upto && first == 2);
+            const unsigned parts = __ballot_sync(0xffffffffu, part);
+            if (part) s_slot[n + __popc(parts & ((1u << lane) - 1))] = 2 * (c + lane);
+            n += __popc(parts);
+            if (stop) break;
+        }
+        if (lane == 0) s_n = n;
+    }
+    __syncthreads();
+    const int n = s_n, rows = tokens * a.G, H_q = a.c.H_kv * a.G;
+    for (int r = blockIdx.y * 4 + (threadIdx.x >> 5); r < rows; r += gridDim.y * 4) {
+        const int tok = r / a.G, g = r - tok * a.G;
+        const int in_slot = tok < a.TPT ? r : 128 + (tok - a.TPT) * a.G + g;
+        float M = -INFINITY;
+        for (int p = lane; p < n; p += 32) M = fmaxf(M, a.part_ml[(int64_t)s_slot[p] * kPagedSlotRows + in_slot].x);
+        M = warp_max(M);
+        float L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+        for (int p = 0; p < n; ++p) {
+            const int64_t at = (int64_t)s_slot[p] * kPagedSlotRows + in_slot;
+            const float2 ml = a.part_ml[at];
+            const float4 x = *reinterpret_cast<const float4*>(a.part_o + at * 128 + lane * 4);
+            const float w = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - M);
+            L = fmaf(w, ml.y, L);
+            o[0] = fmaf(w, x.x, o[0]); o[1] = fmaf(w, x.y, o[1]); o[2] = fmaf(w, x.z, o[2]); o[3] = fmaf(w, x.w, o[3]);
+        }
+        const float inv = L == 0.f ? 0.f : 1.f / L;
+        const int64_t row = ((int64_t)e.z + tok) * H_q + head * a.G + g;
+        *reinterpret_cast<uint2*>(a.out + row * 128 + lane * 4) = make_uint2(pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv));
+        if (lane == 0 && a.lse != nullptr) a.lse[row] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+    }
+}
+
+// ---------------------------------------------------------------- other shapes
+// Head sizes, page sizes and group sizes the kernel above does not take: a warp per (token, query head), 32 keys at a
+// time (a lane each for the products, then all lanes on d for the values).  fp32 throughout.
+template <bool F8>
+__global__ void __launch_bounds__(128)
+paged_attn_generic_kernel(PagedAttnArgs a, const __nv_bfloat16* __restrict__ q, const void* __restrict__ k_pool,
+                          const void* __restrict__ v_pool, int d, int* status) {
+    __shared__ float qs[4][256];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int H_q = a.c.H_kv * a.G;
+    const int64_t unit = (int64_t)blockIdx.x * 4 + warp;
+    if (unit >= (int64_t)a.n_tokens * H_q) return;
+    const int i = (int)(unit / H_q), h = (int)(unit - (int64_t)i * H_q), hk = h / a.G;
+    const int s = paged_seq_of(a.c, i);
+    if (s < 0) return;
+    const int64_t cap = paged_cap(a.c);
+    const int len = a.c.kv_lens[s];
+    if ((len < 0 || len > cap) && lane == 0) report_async(status, kAsyncBadIndex, 0x601);
+    const int64_t kv = min((int64_t)max(len, 0), cap);
+    const int64_t pos = kv - (min(a.c.cu_q[s + 1], a.n_tokens) - i);
+    for (int c = lane; c < d; c += 32) qs[warp][c] = __bfloat162float(q[unit * d + c]) * a.scale_log2e;
+    __syncwarp();
+    float m = -INFINITY, l = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int64_t j0 = 0; j0 <= pos; j0 += 32) {
+        const int64_t key = j0 + lane;
+        int64_t row = -1;
+        if (key <= pos) {
+            const int page = a.c.table[(int64_t)s * a.c.max_pages + key / a.c.page_size];
+            if (page >= 0 && page < a.c.n_pages) row = ((int64_t)page * a.c.page_size + key % a.c.page_size) * a.c.H_kv + hk;
+            else report_async(status, kAsyncBadIndex, 0x602);
+        }
+        float x = -INFINITY;
+        if (row >= 0) {
+            x = 0.f;
+            for (int c = 0; c < d; ++c) x = fmaf(qs[warp][c], idx_elem<F8>(static_cast<const uint8_t*>(k_pool) + row * d * (F8 ? 1 : 2), c), x);
+        }
+        const float m_new = fmaxf(m, warp_max(x));
+        const float m_use = m_new == -INFINITY ? 0.f : m_new;
+        const float corr = m == -INFINITY ? 0.f : exp2f(m - m_use);
+        const float p = row >= 0 ? exp2f(x - m_use) : 0.f;
+        l = l * corr + warp_sum(p);
+        m = m_new;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) o[c] *= corr;
+        for (int t = 0; t < 32; ++t) {
+            const int64_t rt = __shfl_sync(0xffffffffu, row, t);
+            const float pt = __shfl_sync(0xffffffffu, p, t);
+            if (rt < 0) continue;
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+                if (lane + 32 * c < d) o[c] = fmaf(pt, idx_elem<F8>(static_cast<const uint8_t*>(v_pool) + rt * d * (F8 ? 1 : 2), lane + 32 * c), o[c]);
+        }
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+        if (lane + 32 * c < d) a.out[unit * d + lane + 32 * c] = __float2bfloat16(o[c] * inv);
+    if (lane == 0 && a.lse != nullptr) a.lse[unit] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+}
+
+}  // namespace msa
