@@ -280,9 +280,15 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = sm.tmem_base;
+    // Registers: the softmax warps hold a row of S (128) and more, the others little.  The shares stay within what the
+    // block was launched with: 384 x 168 >= 256 x 200 + 128 x 104, 512 x 128 >= 256 x 168 + 128 x 88 + 128 x 80.
+    // (Set at the head of each role: where roles share code the smallest share would rule.)
+    constexpr int kRegsSoftmax = F8 ? 168 : 200, kRegsIssue = F8 ? 88 : 104, kRegsWiden = 80;
     PagedWalk walk(sm.place[0], sm.place[1]);
     PagedItem it{};
 
+    if (warp >= 8 && warp < 12) {
+    reg_release<kRegsIssue>();
     if (warp == 8 || warp == 9) {
         // ---------------- K / V producer: one box per page (or 128 keys of a larger one), a lane each
         const bool is_v = warp == 9;
@@ -456,10 +462,12 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 mbar_wait_quiet(&sm.drain, 0, 20000000);
             }
         }
+    }
     } else if (warp >= 12) {
         // ---------------- widening (fp8): a tile lands in the upper half of its stage (row = key, 128 bytes, chunks
         // swizzled by key mod 8); all threads read their row before any writes the bf16 tile over it.
         if constexpr (F8) {
+            reg_release<kRegsWiden>();
             const int key = threadIdx.x - 384, sw = key & 7;
             int t = 0;
             bool ok = true;
@@ -503,6 +511,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             }
         }
     } else {
+        reg_acquire<kRegsSoftmax>();
         // ---------------- softmax and epilogue: thread = row (TMEM lane)
         const int j = warp >> 2, quarter = warp & 3;
         const int row = quarter * 32 + lane, tok = row / a.G, g = row - tok * a.G;
@@ -532,7 +541,8 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
 #pragma unroll
                     for (int c = 0; c < 4; ++c) tmem_ld_32x32(tmem_s + c * 32, sv[c]);
                     tmem_wait_ld();
-                    const int64_t lim = pos - (int64_t)it.block(j, n) * kPagedKeys;  // keys 0..lim of the tile are visible
+                    // keys 0..lim of the tile are visible
+                    const int lim = (int)max(min(pos - (int64_t)it.block(j, n) * kPagedKeys, (int64_t)kPagedKeys), (int64_t)-1);
                     if (lim < kPagedKeys - 1) {
 #pragma unroll
                         for (int c = 0; c < 4; ++c)
@@ -550,14 +560,14 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                         const float corr = m_new == -INFINITY ? 1.f : ex2_approx((m_ref - m_new) * a.scale_log2e);
                         m_ref = m_new;
                         l *= corr;
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            uint32_t ov[32];
-                            tmem_ld_32x32(tmem_o + c * 32, ov);
+#pragma unroll 1
+                        for (int c = 0; c < 8; ++c) {
+                            uint32_t ov[16];
+                            tmem_ld_32x16(tmem_o + c * 16, ov);
                             tmem_wait_ld();
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * corr);
-                            tmem_st_32x32(tmem_o + c * 32, ov);
+                            for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * corr);
+                            tmem_st_32x16(tmem_o + c * 16, ov);
                         }
                     }
                     const float mc = m_ref == -INFINITY ? 0.f : m_ref * a.scale_log2e;
