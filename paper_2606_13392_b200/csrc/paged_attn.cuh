@@ -400,67 +400,75 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         // ---------------- MMA issuer: S_j(n) = Q_j K^T, then, once P_j(n) is written, O_j += P_j(n) V.  MMAs run in
         // issue order: S_j(n) may overwrite P_j(n-1) because O_j += P_j(n-1) V was issued before it, and the barrier
         // that says S_j(n) is there says as well that O_j holds everything up to n-1.
-        if (lane == 0) {
-            constexpr uint32_t idesc_s = make_idesc_bf16(128, kPagedKeys, false, false);
-            constexpr uint32_t idesc_o = make_idesc_bf16(128, 128, false, true);
-            uint32_t n_p[2] = {0, 0}, n_o[2] = {0, 0}, n_q[2] = {0, 0};
-            int kt = 0, vt = 0;
-            bool ok = true;
-            while (ok && walk.next(a, it)) {
-                const bool dual = it.dual();
-                const int st[2] = {it.steps(0), it.steps(1)};
-                for (int n = 0; ok && n <= st[0]; ++n) {
+        // The whole warp walks and waits, one elected lane issues: descriptors then stay in uniform registers.
+        constexpr uint32_t idesc_s = make_idesc_bf16(128, kPagedKeys, false, false);
+        constexpr uint32_t idesc_o = make_idesc_bf16(128, 128, false, true);
+        const uint64_t q_desc = make_smem_desc(smem_u32(sm.q[0]), 16, 1024), k_desc = make_smem_desc(smem_u32(sm.k[0]), 16, 2048);
+        // V as the MN-major B operand: 8-key groups 2 KB apart, the other 64 columns of d 1 KB away
+        const uint64_t v_desc = make_smem_desc(smem_u32(sm.v[0]), 1024, 2048);
+        uint32_t n_p[2] = {0, 0}, n_o[2] = {0, 0}, n_q[2] = {0, 0};
+        uint32_t ks = 0, k_phase = 0, vs = 0, v_phase = 0;  // stage of the next K / V tile and its use's parity
+        bool ok = true;
+        while (ok && walk.next(a, it)) {
+            const bool dual = it.dual();
+            const int st[2] = {it.steps(0), it.steps(1)};
+            for (int n = 0; ok && n <= st[0]; ++n) {
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const uint32_t ts = tmem + j * 128, to = tmem + 256 + j * 128;
-                        if (n >= 1 && n - 1 < st[j]) {
-                            const int v_tile = vt + (dual ? 2 * (n - 1) + j : n - 1), vs = v_tile % kPagedVStages;
-                            if (!mbar_wait(&sm.p_full[j], n_p[j]++ & 1, abort) ||
-                                !mbar_wait(&sm.v_full[vs], (v_tile / kPagedVStages) & 1, abort) ||
-                                (n == 1 && n_o[j] > 0 && !mbar_wait(&sm.o_empty[j], (n_o[j] - 1) & 1, abort))) {
-                                report_async(status, kAsyncTimeout, 0x631);
-                                ok = false;
-                                break;
-                            }
-                            tc_fence_after();
-                            // V as the MN-major B operand: 8-key groups 2 KB apart, the other 64 columns of d 1 KB away
-                            const uint64_t vd = make_smem_desc(smem_u32(sm.v[vs]), 1024, 2048);
+                for (int j = 0; j < 2; ++j) {
+                    const uint32_t ts = tmem + j * 128, to = tmem + 256 + j * 128;
+                    const bool last_user = dual || j == 1;  // of a K or V tile
+                    if (n >= 1 && n - 1 < st[j]) {
+                        if (!mbar_wait(&sm.v_full[vs], v_phase, abort) ||
+                            (n == 1 && n_o[j] > 0 && !mbar_wait(&sm.o_empty[j], (n_o[j] - 1) & 1, abort)) ||
+                            !mbar_wait(&sm.p_full[j], n_p[j]++ & 1, abort)) {
+                            if (lane == 0) report_async(status, kAsyncTimeout, 0x631);
+                            ok = false;
+                            break;
+                        }
+                        tc_fence_after();
+                        if (elect_one()) {
+                            const uint64_t vd = v_desc + vs * (kPagedKeys * 256 / 16);
 #pragma unroll
                             for (int kk = 0; kk < kPagedKeys / 16; ++kk)
                                 mma_bf16_ts(to, ts + kk * 8, vd + (uint64_t)(kk * 4096 / 16), idesc_o, n > 1 || kk > 0);
-                            if (dual || j == 1) mma_commit(&sm.v_empty[vs]);
-                            if (n == st[j]) { mma_commit(&sm.o_full[j]); ++n_o[j]; }
+                            if (last_user) mma_commit(&sm.v_empty[vs]);
+                            if (n == st[j]) mma_commit(&sm.o_full[j]);
                         }
-                        if (n < st[j]) {
-                            const int qb = dual ? 0 : j;
-                            const int k_tile = kt + (dual ? 2 * n + j : n), ks = k_tile % kPagedKStages;
-                            if (!mbar_wait(&sm.q_full[qb], n_q[qb] & 1, abort) ||
-                                !mbar_wait(&sm.k_full[ks], (k_tile / kPagedKStages) & 1, abort)) {
-                                report_async(status, kAsyncTimeout, 0x632);
-                                ok = false;
-                                break;
-                            }
-                            tc_fence_after();
-                            const uint64_t qd = make_smem_desc(smem_u32(sm.q[qb]), 16, 1024);
-                            const uint64_t kd = make_smem_desc(smem_u32(sm.k[ks]), 16, 2048);
+                        __syncwarp();
+                        n_o[j] += n == st[j];
+                        if (last_user && ++vs == kPagedVStages) { vs = 0; v_phase ^= 1; }
+                    }
+                    if (n < st[j]) {
+                        const int qb = dual ? 0 : j;
+                        if ((n == 0 && !mbar_wait(&sm.q_full[qb], n_q[qb] & 1, abort)) || !mbar_wait(&sm.k_full[ks], k_phase, abort)) {
+                            if (lane == 0) report_async(status, kAsyncTimeout, 0x632);
+                            ok = false;
+                            break;
+                        }
+                        tc_fence_after();
+                        const bool q_done = dual ? 2 * n + j == it.hi - it.lo - 1 : n == st[j] - 1;
+                        if (elect_one()) {
+                            const uint64_t qd = q_desc + qb * (128 * 256 / 16), kd = k_desc + ks * (kPagedKeys * 256 / 16);
 #pragma unroll
                             for (int kk = 0; kk < 8; ++kk)  // 16 of d each; second half of Q 16 KB on, of K 1 KB
                                 mma_bf16_ss(ts, qd + (uint64_t)((kk >> 2) * 1024 + 2 * (kk & 3)),
                                             kd + (uint64_t)((kk >> 2) * 64 + 2 * (kk & 3)), idesc_s, kk > 0);
                             mma_commit(&sm.s_full[j]);
-                            if (dual || j == 1) mma_commit(&sm.k_empty[ks]);
-                            if (dual ? 2 * n + j == it.hi - it.lo - 1 : n == st[j] - 1) mma_commit(&sm.q_empty[qb]);
+                            if (last_user) mma_commit(&sm.k_empty[ks]);
+                            if (q_done) mma_commit(&sm.q_empty[qb]);
                         }
+                        __syncwarp();
+                        if (last_user && ++ks == kPagedKStages) { ks = 0; k_phase ^= 1; }
                     }
                 }
-                kt += it.hi - it.lo; vt += it.hi - it.lo;
-                ++n_q[0];
-                if (!dual) ++n_q[1];
             }
-            if (*abort != 0) {
-                mma_commit(&sm.drain);
-                mbar_wait_quiet(&sm.drain, 0, 20000000);
-            }
+            ++n_q[0];
+            n_q[1] += !dual;
+        }
+        if (*abort != 0) {
+            if (elect_one()) mma_commit(&sm.drain);
+            __syncwarp();
+            mbar_wait_quiet(&sm.drain, 0, 20000000);
         }
     }
     } else if (warp >= 12) {
