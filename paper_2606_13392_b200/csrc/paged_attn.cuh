@@ -122,9 +122,9 @@ struct PagedItem {
     int lo, hi, nb;                // key tiles [lo, hi) of nb
     int pos, kv;                   // position of the first token; visible keys of the sequence
     __host__ __device__ bool dual() const { return n1 == 0; }
-    // key tiles that context j takes
+    // key tiles that context j takes: all, or every other one where both contexts have the same rows
     __host__ __device__ int steps(int j) const { return n1 == 0 ? (hi - lo + 1 - j) / 2 : hi - lo; }
-    __host__ __device__ int block(int j, int n) const { return n1 == 0 ? lo + 2 * n + j : lo + n; }
+    __host__ __device__ int tile(int j, int i) const { return n1 == 0 ? lo + 2 * i + j : lo + i; }
     __host__ __device__ bool partial() const { return lo > 0 || hi < nb; }
 };
 
@@ -174,7 +174,7 @@ struct PagedSmem {
     alignas(8) uint64_t q_full[2], q_empty[2];
     uint64_t k_full[kPagedKStages], k_empty[kPagedKStages], k_land[kPagedKStages];
     uint64_t v_full[kPagedVStages], v_empty[kPagedVStages], v_land[kPagedVStages];
-    uint64_t s_full[2], p_full[2], o_full[2], o_empty[2];
+    uint64_t s_full[2], p_full[2][2], o_full[2], o_empty[2];  // [context], P: [half]
     uint64_t v_tail, ml_full, ml_empty, drain;
     int64_t scan[16], targets[2];
     PagedPlace place[2];
@@ -215,7 +215,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(&sm.q_full[i], 1); mbar_init(&sm.q_empty[i], 1);
-            mbar_init(&sm.s_full[i], 1); mbar_init(&sm.p_full[i], 4);
+            mbar_init(&sm.s_full[i], 1); mbar_init(&sm.p_full[i][0], 4); mbar_init(&sm.p_full[i][1], 4);
             mbar_init(&sm.o_full[i], 1); mbar_init(&sm.o_empty[i], 4);
         }
         for (int i = 0; i < kPagedKStages; ++i) {
@@ -281,9 +281,9 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     tc_fence_after();
     const uint32_t tmem = sm.tmem_base;
     // Registers: the softmax warps hold a row of S (128) and more, the others little.  The shares stay within what the
-    // block was launched with: 384 x 168 >= 256 x 200 + 128 x 104, 512 x 128 >= 256 x 168 + 128 x 88 + 128 x 80.
+    // block was launched with: 384 x 168 >= 256 x 192 + 128 x 120, 512 x 128 >= 256 x 168 + 128 x 88 + 128 x 80.
     // (Set at the head of each role: where roles share code the smallest share would rule.)
-    constexpr int kRegsSoftmax = F8 ? 168 : 200, kRegsIssue = F8 ? 88 : 104, kRegsWiden = 80;
+    constexpr int kRegsSoftmax = F8 ? 168 : 192, kRegsIssue = F8 ? 88 : 120, kRegsWiden = 80;
     PagedWalk walk(sm.place[0], sm.place[1]);
     PagedItem it{};
 
@@ -397,62 +397,77 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         }
         if (*abort != 0) spin_cycles(200000);
     } else if (warp == 10) {
-        // ---------------- MMA issuer: S_j(n) = Q_j K^T, then, once P_j(n) is written, O_j += P_j(n) V.  MMAs run in
-        // issue order: S_j(n) may overwrite P_j(n-1) because O_j += P_j(n-1) V was issued before it, and the barrier
-        // that says S_j(n) is there says as well that O_j holds everything up to n-1.
+        // ---------------- MMA issuer: S_j(i) = Q_j K^T, then, once P_j(i) is written over it, O_j += P_j(i) V.
+        // S_j(i+1) is issued right behind O_j += P_j(i) V: MMAs run in issue order, so it may overwrite P_j(i), it runs
+        // while the other context's softmax is at work, and the barrier that says S_j(i) is there says as well that O_j
+        // holds all steps before.  P comes in halves, so that the product starts on the first.  (S in two 64-key
+        // buffers, one product ahead, was slower: 64-key products read Q twice as often, and shared memory is what the
+        // MMAs run short of; 128-row chunk 4.8 against 4.3 ms.)
         // The whole warp walks and waits, one elected lane issues: descriptors then stay in uniform registers.
-        constexpr uint32_t idesc_s = make_idesc_bf16(128, kPagedKeys, false, false);
-        constexpr uint32_t idesc_o = make_idesc_bf16(128, 128, false, true);
+        constexpr uint32_t idesc = make_idesc_bf16(128, 128, false, false), idesc_o = make_idesc_bf16(128, 128, false, true);
+        constexpr uint32_t kTile = kPagedKeys * 256 / 16;  // in descriptor units of 16 bytes
         const uint64_t q_desc = make_smem_desc(smem_u32(sm.q[0]), 16, 1024), k_desc = make_smem_desc(smem_u32(sm.k[0]), 16, 2048);
         // V as the MN-major B operand: 8-key groups 2 KB apart, the other 64 columns of d 1 KB away
         const uint64_t v_desc = make_smem_desc(smem_u32(sm.v[0]), 1024, 2048);
-        uint32_t n_p[2] = {0, 0}, n_o[2] = {0, 0}, n_q[2] = {0, 0};
-        uint32_t ks = 0, k_phase = 0, vs = 0, v_phase = 0;  // stage of the next K / V tile and its use's parity
+        uint32_t n_p[2] = {0, 0}, n_o[2] = {0, 0}, n_q[2] = {0, 0};  // P's, items and uses of Q so far
+        uint32_t ks = 0, k_phase = 0, vs = 0, v_phase = 0;            // stage of the next K / V tile and its use's parity
         bool ok = true;
         while (ok && walk.next(a, it)) {
             const bool dual = it.dual();
             const int st[2] = {it.steps(0), it.steps(1)};
-            for (int n = 0; ok && n <= st[0]; ++n) {
+            for (int i = -1; ok && i < st[0]; ++i) {
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const uint32_t ts = tmem + j * 128, to = tmem + 256 + j * 128;
-                    const bool last_user = dual || j == 1;  // of a K or V tile
-                    if (n >= 1 && n - 1 < st[j]) {
-                        if (!mbar_wait(&sm.v_full[vs], v_phase, abort) ||
-                            (n == 1 && n_o[j] > 0 && !mbar_wait(&sm.o_empty[j], (n_o[j] - 1) & 1, abort)) ||
-                            !mbar_wait(&sm.p_full[j], n_p[j]++ & 1, abort)) {
+                    const bool first_user = dual || j == 0, last_user = dual || j == 1;  // of a K or V tile
+                    // (K is waited for behind the product with V: where loads are the limit, V's stage is free sooner)
+                    if (i >= 0 && i < st[j]) {
+                        if ((first_user && !mbar_wait(&sm.v_full[vs], v_phase, abort)) ||
+                            (i == 0 && n_o[j] > 0 && !mbar_wait(&sm.o_empty[j], (n_o[j] - 1) & 1, abort)) ||
+                            !mbar_wait(&sm.p_full[j][0], n_p[j] & 1, abort)) {
                             if (lane == 0) report_async(status, kAsyncTimeout, 0x631);
                             ok = false;
                             break;
                         }
                         tc_fence_after();
+                        const uint64_t vd = v_desc + vs * kTile;
                         if (elect_one()) {
-                            const uint64_t vd = v_desc + vs * (kPagedKeys * 256 / 16);
 #pragma unroll
-                            for (int kk = 0; kk < kPagedKeys / 16; ++kk)
-                                mma_bf16_ts(to, ts + kk * 8, vd + (uint64_t)(kk * 4096 / 16), idesc_o, n > 1 || kk > 0);
-                            if (last_user) mma_commit(&sm.v_empty[vs]);
-                            if (n == st[j]) mma_commit(&sm.o_full[j]);
+                            for (int kk = 0; kk < 4; ++kk) mma_bf16_ts(to, ts + kk * 8, vd + (uint64_t)(kk * 256), idesc_o, i > 0 || kk > 0);
                         }
                         __syncwarp();
-                        n_o[j] += n == st[j];
-                        if (last_user && ++vs == kPagedVStages) { vs = 0; v_phase ^= 1; }
-                    }
-                    if (n < st[j]) {
-                        const int qb = dual ? 0 : j;
-                        if ((n == 0 && !mbar_wait(&sm.q_full[qb], n_q[qb] & 1, abort)) || !mbar_wait(&sm.k_full[ks], k_phase, abort)) {
+                        if (!mbar_wait(&sm.p_full[j][1], n_p[j]++ & 1, abort)) {
                             if (lane == 0) report_async(status, kAsyncTimeout, 0x632);
                             ok = false;
                             break;
                         }
                         tc_fence_after();
-                        const bool q_done = dual ? 2 * n + j == it.hi - it.lo - 1 : n == st[j] - 1;
                         if (elect_one()) {
-                            const uint64_t qd = q_desc + qb * (128 * 256 / 16), kd = k_desc + ks * (kPagedKeys * 256 / 16);
+#pragma unroll
+                            for (int kk = 4; kk < 8; ++kk) mma_bf16_ts(to, ts + kk * 8, vd + (uint64_t)(kk * 256), idesc_o, true);
+                            if (last_user) mma_commit(&sm.v_empty[vs]);
+                            if (i == st[j] - 1) mma_commit(&sm.o_full[j]);
+                        }
+                        __syncwarp();
+                        n_o[j] += i == st[j] - 1;
+                        if (last_user && ++vs == kPagedVStages) { vs = 0; v_phase ^= 1; }
+                    }
+                    if (i + 1 < st[j]) {
+                        const int qb = dual ? 0 : j;
+                        if ((first_user && !mbar_wait(&sm.k_full[ks], k_phase, abort)) ||
+                            (i == -1 && (!dual || j == 0) && !mbar_wait(&sm.q_full[qb], n_q[qb] & 1, abort))) {
+                            if (lane == 0) report_async(status, kAsyncTimeout, 0x633);
+                            ok = false;
+                            break;
+                        }
+                        tc_fence_after();
+                        const bool q_done = dual ? 2 * (i + 1) + j == it.hi - it.lo - 1 : i + 2 == st[j];
+                        if (elect_one()) {
+                            const uint64_t qd = q_desc + qb * (128 * 256 / 16), kd = k_desc + ks * kTile;
 #pragma unroll
                             for (int kk = 0; kk < 8; ++kk)  // 16 of d each; second half of Q 16 KB on, of K 1 KB
                                 mma_bf16_ss(ts, qd + (uint64_t)((kk >> 2) * 1024 + 2 * (kk & 3)),
-                                            kd + (uint64_t)((kk >> 2) * 64 + 2 * (kk & 3)), idesc_s, kk > 0);
+                                            kd + (uint64_t)((kk >> 2) * 64 + 2 * (kk & 3)), idesc, kk > 0);
                             mma_commit(&sm.s_full[j]);
                             if (last_user) mma_commit(&sm.k_empty[ks]);
                             if (q_done) mma_commit(&sm.q_empty[qb]);
@@ -526,7 +541,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         const uint32_t lane_base = (uint32_t)(quarter * 32) << 16;
         const uint32_t tmem_s = tmem + lane_base + j * 128, tmem_o = tmem + lane_base + 256 + j * 128;
         const int H_q = a.c.H_kv * a.G;
-        uint32_t n_s = 0, n_o[2] = {0, 0}, n_ml = 0;
+        uint32_t n_s = 0, n_o[2] = {0, 0}, n_ml = 0;  // steps, accumulators of the two contexts, merges so far
         bool ok = true;
         while (ok && walk.next(a, it)) {
             const bool dual = it.dual();
@@ -537,94 +552,96 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             const int first = dual || j == 0 ? 0 : a.TPT;
             const int64_t pos = (int64_t)it.pos + first + tok;
             float m_ref = -INFINITY, l = 0.f;
-            for (int n = 0; n < steps; ++n) {
+            for (int i = 0; i < steps; ++i) {
                 if (!mbar_wait(&sm.s_full[j], n_s++ & 1, abort)) {
                     if (lane == 0) report_async(status, kAsyncTimeout, 0x651);
                     ok = false;
                     break;
                 }
-                if (warp_on) {
-                    tc_fence_after();
-                    uint32_t sv[4][32];
+                if (!warp_on) {
+                    if (lane < 2) mbar_arrive(&sm.p_full[j][lane]);
+                    continue;
+                }
+                tc_fence_after();
+                uint32_t sv[4][32];
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) tmem_ld_32x32(tmem_s + c * 32, sv[c]);
-                    tmem_wait_ld();
-                    // keys 0..lim of the tile are visible
-                    const int lim = (int)max(min(pos - (int64_t)it.block(j, n) * kPagedKeys, (int64_t)kPagedKeys), (int64_t)-1);
-                    if (lim < kPagedKeys - 1) {
+                for (int c = 0; c < 4; ++c) tmem_ld_32x32(tmem_s + c * 32, sv[c]);
+                tmem_wait_ld();
+                // keys 0..lim of the tile are visible
+                const int lim = (int)max(min(pos - (int64_t)it.tile(j, i) * kPagedKeys, (int64_t)kPagedKeys), (int64_t)-1);
+                if (lim < kPagedKeys - 1) {
 #pragma unroll
-                        for (int c = 0; c < 4; ++c)
+                    for (int c = 0; c < 4; ++c)
 #pragma unroll
-                            for (int e = 0; e < 32; ++e)
-                                if (c * 32 + e > lim) sv[c][e] = 0xFF800000u;  // -inf
-                    }
-                    const float mx = fmaxf(fmaxf(tree_max32(sv[0]), tree_max32(sv[1])), fmaxf(tree_max32(sv[2]), tree_max32(sv[3])));
-                    // The reference maximum moves only when a row's maximum has outgrown it by 2^8: P then stays below
-                    // 2^8 (bf16 keeps its relative precision) and O is hardly ever rescaled.
-                    const float m_new = fmaxf(m_ref, mx);
-                    if (n == 0) {
-                        m_ref = m_new;
-                    } else if (__any_sync(0xffffffffu, row_on && (m_new - m_ref) * a.scale_log2e > 8.f)) {
-                        const float corr = m_new == -INFINITY ? 1.f : ex2_approx((m_ref - m_new) * a.scale_log2e);
-                        m_ref = m_new;
-                        l *= corr;
+                        for (int e = 0; e < 32; ++e)
+                            if (c * 32 + e > lim) sv[c][e] = 0xFF800000u;  // -inf
+                }
+                const float mx = fmaxf(fmaxf(tree_max32(sv[0]), tree_max32(sv[1])), fmaxf(tree_max32(sv[2]), tree_max32(sv[3])));
+                // The reference maximum moves only when a row's maximum has outgrown it by 2^8: P then stays below 2^8
+                // (bf16 keeps its relative precision) and O is hardly ever rescaled.
+                const float m_new = fmaxf(m_ref, mx);
+                if (i == 0) {
+                    m_ref = m_new;
+                } else if (__any_sync(0xffffffffu, row_on && (m_new - m_ref) * a.scale_log2e > 8.f)) {
+                    const float corr = m_new == -INFINITY ? 1.f : ex2_approx((m_ref - m_new) * a.scale_log2e);
+                    m_ref = m_new;
+                    l *= corr;
 #pragma unroll 1
-                        for (int c = 0; c < 8; ++c) {
-                            uint32_t ov[16];
-                            tmem_ld_32x16(tmem_o + c * 16, ov);
-                            tmem_wait_ld();
+                    for (int c = 0; c < 8; ++c) {
+                        uint32_t ov[16];
+                        tmem_ld_32x16(tmem_o + c * 16, ov);
+                        tmem_wait_ld();
 #pragma unroll
-                            for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * corr);
-                            tmem_st_32x16(tmem_o + c * 16, ov);
-                        }
+                        for (int e = 0; e < 16; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * corr);
+                        tmem_st_32x16(tmem_o + c * 16, ov);
                     }
-                    const float mc = m_ref == -INFINITY ? 0.f : m_ref * a.scale_log2e;
-                    float l4[4] = {0.f, 0.f, 0.f, 0.f};
+                }
+                const float mc = m_ref == -INFINITY ? 0.f : m_ref * a.scale_log2e;
+                const float2 sc2 = make_float2(a.scale_log2e, a.scale_log2e), mc2 = make_float2(-mc, -mc);
+                float2 l2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-                    for (int c2 = 0; c2 < 2; ++c2) {
-                        uint32_t pk[32];
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t pk[32];
 #pragma unroll
-                        for (int w = 0; w < 32; ++w) {
-                            const int col = c2 * 64 + 2 * w;
-                            const float p0 = ex2_approx(fmaf(__uint_as_float(sv[col >> 5][col & 31]), a.scale_log2e, -mc));
-                            const float p1 = ex2_approx(fmaf(__uint_as_float(sv[col >> 5][(col & 31) + 1]), a.scale_log2e, -mc));
-                            l4[w & 3] += p0 + p1;
-                            pk[w] = pack2(p0, p1);
-                        }
-                        tmem_st_32x32(tmem_s + c2 * 32, pk);
+                    for (int w = 0; w < 32; ++w) {
+                        const uint32_t* from = &sv[2 * h + (w >> 4)][2 * (w & 15)];
+                        const float2 x = __ffma2_rn(make_float2(__uint_as_float(from[0]), __uint_as_float(from[1])), sc2, mc2);
+                        const float2 p = make_float2(ex2_approx(x.x), ex2_approx(x.y));
+                        l2[w & 1] = __fadd2_rn(l2[w & 1], p);
+                        pk[w] = pack2(p.x, p.y);
                     }
-                    l += (l4[0] + l4[1]) + (l4[2] + l4[3]);
+                    tmem_st_32x32(tmem_s + h * 32, pk);
                     tmem_wait_st();
                     tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&sm.p_full[j][h]);
                 }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sm.p_full[j]);
+                l += (l2[0].x + l2[0].y) + (l2[1].x + l2[1].y);
             }
             if (!ok) break;
             const float m_log2 = m_ref == -INFINITY ? -INFINITY : m_ref * a.scale_log2e;
-            const int other = dual ? it.steps(1) : 0;  // steps of the context to be merged in
+            const bool merge = dual && it.steps(1) > 0;
             if (dual && j == 1) {
                 // hand the row's maximum and sum to the first context, which reads O_1 as well
-                if (steps == 0) continue;
+                if (!merge) continue;
                 if (n_ml > 0 && !mbar_wait(&sm.ml_empty, (n_ml - 1) & 1, abort)) {
                     if (lane == 0) report_async(status, kAsyncTimeout, 0x652);
                     break;
                 }
-                ++n_ml;
+                ++n_ml; ++n_o[1];
                 sm.ml[row] = make_float2(m_log2, l);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sm.ml_full);
-                ++n_o[1];
                 continue;
             }
-            if (j == 0 && !dual) ++n_o[1];  // (the second context's own accumulator of this item)
             float w0 = 1.f, w1 = 0.f, m_all = m_log2;
-            if (!mbar_wait(&sm.o_full[j], n_o[j]++ & 1, abort)) {
+            if (!mbar_wait(&sm.o_full[j], n_o[j] & 1, abort)) {
                 if (lane == 0) report_async(status, kAsyncTimeout, 0x653);
                 break;
             }
-            if (other > 0) {
-                if (!mbar_wait(&sm.o_full[1], n_o[1]++ & 1, abort) || !mbar_wait(&sm.ml_full, n_ml & 1, abort)) {
+            if (merge) {
+                // (O_1 of the item before was complete before this item's first S was issued: the parity is this item's)
+                if (!mbar_wait(&sm.o_full[1], n_o[1] & 1, abort) || !mbar_wait(&sm.ml_full, n_ml & 1, abort)) {
                     if (lane == 0) report_async(status, kAsyncTimeout, 0x654);
                     break;
                 }
@@ -635,6 +652,8 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 w1 = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - m_all);
                 l = w0 * l + w1 * ml.y;
             }
+            n_o[0] += 1;
+            n_o[1] += !dual || merge;
             tc_fence_after();
             if (warp_on) {
                 const bool partial = it.partial();
@@ -651,7 +670,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     tmem_wait_ld();
 #pragma unroll
                     for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(__uint_as_float(ov[e]) * w0);
-                    if (other > 0) {
+                    if (merge) {
                         uint32_t o1[32];
                         tmem_ld_32x32(tmem_o + 128 + c * 32, o1);
                         tmem_wait_ld();
@@ -685,7 +704,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             __syncwarp();
             if (lane == 0) {
                 mbar_arrive(&sm.o_empty[j]);
-                if (other > 0) { mbar_arrive(&sm.o_empty[1]); mbar_arrive(&sm.ml_empty); }
+                if (merge) { mbar_arrive(&sm.o_empty[1]); mbar_arrive(&sm.ml_empty); }
             }
         }
     }
