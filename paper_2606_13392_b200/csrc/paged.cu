@@ -165,7 +165,7 @@ static msa_status_t launch_paged_attn(const PagedAttnArgs& a, const msa_paged_ca
     }
     int* status = async_status_ptr();
     if (!ok || status == nullptr) return MSA_ERR_CUDA;
-    const size_t smem = sizeof(PagedSmem) + 1024;
+    const size_t smem = sizeof(PagedSmem);
     static bool attr_set[64] = {false};  // per device
     const int dev = current_device(), grid = sm_count();
     if (!attr_set[dev]) {

@@ -171,7 +171,8 @@ struct PagedSmem {
     alignas(1024) uint8_t k[kPagedKStages][kPagedKeys * 256];  // [8 keys][d half][key][64 bf16]
     alignas(1024) uint8_t v[kPagedVStages][kPagedKeys * 256];
     float2 ml[128];                          // the second context's maxima and sums on their way to the first
-    alignas(8) uint64_t q_full[2], q_empty[2];
+    int8_t q_exp[2][2][128];                 // fp8: [item parity][context][row] power of two taken out of a row of Q
+    alignas(8) uint64_t q_full[2], q_empty[2], q_land[2];
     uint64_t k_full[kPagedKStages], k_empty[kPagedKStages], k_land[kPagedKStages];
     uint64_t v_full[kPagedVStages], v_empty[kPagedVStages], v_land[kPagedVStages];
     uint64_t s_full[2], p_full[2][2], o_full[2], o_empty[2];  // [context], P: [half]
@@ -184,14 +185,18 @@ struct PagedSmem {
 
 constexpr int paged_threads(bool f8) { return f8 ? 512 : 384; }
 
-// Barriers among the four widening warps only.
-__device__ __forceinline__ void conv_barrier() { asm volatile("barrier.cta.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ uint32_t pack2_f16(float a, float b) {
+    const __half2 v = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// Barrier among the four widening warps only; true if `mine` is in all threads.
 __device__ __forceinline__ bool conv_agree(bool mine) {
     uint32_t all;
     asm volatile(
         "{\n\t.reg .pred p, r;\n\t"
         "setp.ne.u32 p, %1, 0;\n\t"
-        "barrier.cta.red.and.pred r, 2, 128, p;\n\t"
+        "barrier.cta.red.and.pred r, 1, 128, p;\n\t"
         "selp.u32 %0, 1, 0, r;\n\t}"
         : "=r"(all)
         : "r"((uint32_t)mine)
@@ -207,14 +212,18 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                      const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                      const PagedAttnArgs a, int box_keys, int64_t snap_keys, int* status) {
     constexpr uint32_t TILE = F8 ? kPagedKeys * 128 : kPagedKeys * 256;  // bytes of a K or V tile in the cache
-    extern __shared__ uint8_t smem_raw[];
-    PagedSmem& sm = *reinterpret_cast<PagedSmem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    extern __shared__ __align__(1024) uint8_t paged_smem[];  // (no room to round the base up)
+    PagedSmem& sm = *reinterpret_cast<PagedSmem*>(paged_smem);
+    if ((smem_u32(paged_smem) & 1023) != 0) {  // swizzled tiles need it; the same for every thread
+        if (threadIdx.x == 0) report_async(status, kAsyncBadIndex, 0x6FF);
+        return;
+    }
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int* abort = &sm.abort;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
-            mbar_init(&sm.q_full[i], 1); mbar_init(&sm.q_empty[i], 1);
+            mbar_init(&sm.q_full[i], F8 ? 4 : 1); mbar_init(&sm.q_empty[i], 1); mbar_init(&sm.q_land[i], 1);
             mbar_init(&sm.s_full[i], 1); mbar_init(&sm.p_full[i][0], 4); mbar_init(&sm.p_full[i][1], 4);
             mbar_init(&sm.o_full[i], 1); mbar_init(&sm.o_empty[i], 4);
         }
@@ -281,9 +290,9 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     tc_fence_after();
     const uint32_t tmem = sm.tmem_base;
     // Registers: the softmax warps hold a row of S (128) and more, the others little.  The shares stay within what the
-    // block was launched with: 384 x 168 >= 256 x 192 + 128 x 120, 512 x 128 >= 256 x 168 + 128 x 88 + 128 x 80.
+    // block was launched with: 384 x 168 >= 256 x 192 + 128 x 120, 512 x 128 >= 256 x 176 + 2 x 128 x 80.
     // (Set at the head of each role: where roles share code the smallest share would rule.)
-    constexpr int kRegsSoftmax = F8 ? 168 : 192, kRegsIssue = F8 ? 88 : 120, kRegsWiden = 80;
+    constexpr int kRegsSoftmax = F8 ? 176 : 192, kRegsIssue = F8 ? 80 : 120, kRegsWiden = 80;
     PagedWalk walk(sm.place[0], sm.place[1]);
     PagedItem it{};
 
@@ -380,14 +389,15 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 // Few tokens: their own boxes (rows behind them keep what they held: no row reads another's).  All: one
                 // box for each half of d; tokens of the next sequence come along, tokens that are not there read as zeros.
                 const bool few = n * 2 <= 16 && n < a.TPT && a.G % 8 == 0;
-                if (lane == 0) mbar_arrive_expect_tx(&sm.q_full[j], (uint32_t)((few ? n : a.TPT) * a.G * 256));
+                uint64_t* bar = F8 ? &sm.q_land[j] : &sm.q_full[j];
+                if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)((few ? n : a.TPT) * a.G * 256));
                 __syncwarp();
                 if (few) {
                     if (lane < 2 * n)
                         tma_load_3d(sm.q[j] + (lane & 1) * 16384 + (lane >> 1) * a.G * 128, &tm_q1, (lane & 1) * 64, head, row + (lane >> 1),
-                                    &sm.q_full[j]);
+                                    bar);
                 } else if (lane < 2) {
-                    tma_load_3d(sm.q[j] + lane * 16384, &tm_q, lane * 64, head, row, &sm.q_full[j]);
+                    tma_load_3d(sm.q[j] + lane * 16384, &tm_q, lane * 64, head, row, bar);
                 }
             }
         }
@@ -404,7 +414,8 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         // buffers, one product ahead, was slower: 64-key products read Q twice as often, and shared memory is what the
         // MMAs run short of; 128-row chunk 4.8 against 4.3 ms.)
         // The whole warp walks and waits, one elected lane issues: descriptors then stay in uniform registers.
-        constexpr uint32_t idesc = make_idesc_bf16(128, 128, false, false), idesc_o = make_idesc_bf16(128, 128, false, true);
+        constexpr uint32_t idesc = F8 ? make_idesc_f16(128, 128, false, false) : make_idesc_bf16(128, 128, false, false);
+        constexpr uint32_t idesc_o = F8 ? make_idesc_f16(128, 128, false, true) : make_idesc_bf16(128, 128, false, true);
         constexpr uint32_t kTile = kPagedKeys * 256 / 16;  // in descriptor units of 16 bytes
         const uint64_t q_desc = make_smem_desc(smem_u32(sm.q[0]), 16, 1024), k_desc = make_smem_desc(smem_u32(sm.k[0]), 16, 2048);
         // V as the MN-major B operand: 8-key groups 2 KB apart, the other 64 columns of d 1 KB away
@@ -487,50 +498,84 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         }
     }
     } else if (warp >= 12) {
-        // ---------------- widening (fp8): a tile lands in the upper half of its stage (row = key, 128 bytes, chunks
-        // swizzled by key mod 8); all threads read their row before any writes the bf16 tile over it.
+        // ---------------- widening (fp8): K and V become fp16, which holds every E4M3 value and takes one conversion
+        // for two elements (bf16 takes four operations).  A tile lands in the upper half of its stage (row = key, 128
+        // bytes, chunks swizzled by key mod 8); all threads have read their row before any writes the fp16 tile over it.
+        // Q becomes fp16 as well, with a power of two taken out of each row so that any bf16 row fits: what is rounded
+        // off is below 2^-38 of the row's largest element.  The softmax warps put it back into the scale.
         if constexpr (F8) {
             reg_release<kRegsWiden>();
             const int key = threadIdx.x - 384, sw = key & 7;
-            int t = 0;
+            uint32_t t = 0, n_q[2] = {0, 0}, item = 0;
             bool ok = true;
             while (ok && walk.next(a, it)) {
-                for (int b = it.lo; ok && b < it.hi; ++b, ++t)
+                for (int b = it.lo; ok && b < it.hi; ++b, ++t) {
                     for (int kv = 0; kv < 2; ++kv) {
-                        const int stages = kv == 0 ? kPagedKStages : kPagedVStages, st = t % stages;
-                        uint64_t* land = kv == 0 ? &sm.k_land[st] : &sm.v_land[st];
-                        uint64_t* full = kv == 0 ? &sm.k_full[st] : &sm.v_full[st];
+                        const uint32_t stages = kv == 0 ? kPagedKStages : kPagedVStages, st = t % stages;
                         uint8_t* tile = kv == 0 ? sm.k[st] : sm.v[st];
-                        // (a wait may run out in one warp and not in another: all four go on or none)
-                        const bool landed = mbar_wait(land, (t / stages) & 1, abort);
-                        if (!conv_agree(landed)) {
-                            if (lane == 0) report_async(status, kAsyncTimeout, 0x641);
-                            ok = false;
-                            break;
-                        }
-                        const bool inside = kv == 0 || (int64_t)b * kPagedKeys + key < it.kv;
+                        const bool landed = mbar_wait(kv == 0 ? &sm.k_land[st] : &sm.v_land[st], (t / stages) & 1, abort);
+                        // (rows behind the end may hold anything, and 0 * NaN is NaN: V's become zeros)
+                        const bool inside = landed && (kv == 0 || (int64_t)b * kPagedKeys + key < it.kv);
                         uint4 x[8];
 #pragma unroll
                         for (int c = 0; c < 8; ++c) {
                             x[c] = make_uint4(0u, 0u, 0u, 0u);
                             if (inside) x[c] = *reinterpret_cast<const uint4*>(tile + TILE + key * 128 + ((c ^ sw) << 4));
                         }
-                        conv_barrier();
+                        if (!conv_agree(landed)) {  // (a wait may run out in one warp and not in another: all go on or none)
+                            if (lane == 0) report_async(status, kAsyncTimeout, 0x641);
+                            ok = false;
+                            break;
+                        }
                         uint8_t* row = tile + (key >> 3) * 2048 + sw * 128;
 #pragma unroll
                         for (int c = 0; c < 8; ++c) {
-                            const uint32_t w[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
-                            uint32_t o[8];
-                            e4m3x16_to_bf16x16(w, o);
+                            uint4 lo, hi;
+                            e4m3x4_to_f16x2x2(x[c].x, lo.x, lo.y); e4m3x4_to_f16x2x2(x[c].y, lo.z, lo.w);
+                            e4m3x4_to_f16x2x2(x[c].z, hi.x, hi.y); e4m3x4_to_f16x2x2(x[c].w, hi.z, hi.w);
                             const int cc = 2 * (c & 3);
                             uint8_t* to = row + (c >> 2) * 1024;
-                            *reinterpret_cast<uint4*>(to + ((cc ^ sw) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
-                            *reinterpret_cast<uint4*>(to + (((cc + 1) ^ sw) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
+                            *reinterpret_cast<uint4*>(to + ((cc ^ sw) << 4)) = lo;
+                            *reinterpret_cast<uint4*>(to + (((cc + 1) ^ sw) << 4)) = hi;
                         }
                         fence_proxy_async_smem();
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(full);
+                        if (lane == 0) mbar_arrive(kv == 0 ? &sm.k_full[st] : &sm.v_full[st]);
                     }
+                    for (int j = 0; ok && b == it.lo && j < (it.dual() ? 1 : 2); ++j) {  // Q, behind the first tile
+                        if (!conv_agree(mbar_wait(&sm.q_land[j], n_q[j]++ & 1, abort))) {
+                            if (lane == 0) report_async(status, kAsyncTimeout, 0x642);
+                            ok = false;
+                            break;
+                        }
+                        uint8_t* row = sm.q[j] + key * 128;  // thread = row: two halves of 128 bytes
+                        uint32_t most = 0;
+#pragma unroll
+                        for (int c = 0; c < 16; ++c) {
+                            const uint4 v = *reinterpret_cast<const uint4*>(row + (c >> 3) * 16384 + (((c & 7) ^ sw) << 4));
+                            most = max(max(max(most, v.x & 0x7FFF0000u), max(v.y & 0x7FFF0000u, v.z & 0x7FFF0000u)), v.w & 0x7FFF0000u);
+                            most = max(max(max(most, v.x << 17 >> 1), max(v.y << 17 >> 1, v.z << 17 >> 1)), v.w << 17 >> 1);
+                        }
+                        // the largest element goes to [2^14, 2^15): beyond, for rows below 2^-98, as far as 2^112 takes it
+                        const int e = most == 0 ? 0 : max((int)(most >> 23) - 127 - 14, -112);
+                        const float f = __uint_as_float((uint32_t)(127 - e) << 23);
+                        sm.q_exp[item & 1][j][key] = (int8_t)e;
+#pragma unroll
+                        for (int c = 0; c < 16; ++c) {
+                            uint4* at = reinterpret_cast<uint4*>(row + (c >> 3) * 16384 + (((c & 7) ^ sw) << 4));
+                            float y[8];
+                            unpack8(*at, y);
+                            uint32_t o[4];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) o[i] = pack2_f16(y[2 * i] * f, y[2 * i + 1] * f);
+                            *at = make_uint4(o[0], o[1], o[2], o[3]);
+                        }
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&sm.q_full[j]);
+                    }
+                }
+                ++item;
             }
         }
     } else {
@@ -543,7 +588,8 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         const int H_q = a.c.H_kv * a.G;
         uint32_t n_s = 0, n_o[2] = {0, 0}, n_ml = 0;  // steps, accumulators of the two contexts, merges so far
         bool ok = true;
-        while (ok && walk.next(a, it)) {
+        uint32_t n_item = 0;
+        for (; ok && walk.next(a, it); ++n_item) {
             const bool dual = it.dual();
             const int steps = it.steps(j);
             const int tokens = dual || j == 0 ? it.n0 : it.n1;
@@ -551,7 +597,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             const bool row_on = tok < tokens;
             const int first = dual || j == 0 ? 0 : a.TPT;
             const int64_t pos = (int64_t)it.pos + first + tok;
-            float m_ref = -INFINITY, l = 0.f;
+            float m_ref = -INFINITY, l = 0.f, scale = a.scale_log2e;
             for (int i = 0; i < steps; ++i) {
                 if (!mbar_wait(&sm.s_full[j], n_s++ & 1, abort)) {
                     if (lane == 0) report_async(status, kAsyncTimeout, 0x651);
@@ -563,6 +609,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     continue;
                 }
                 tc_fence_after();
+                if (F8 && i == 0) scale *= __uint_as_float((uint32_t)(127 + sm.q_exp[n_item & 1][dual ? 0 : j][row]) << 23);
                 uint32_t sv[4][32];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tmem_ld_32x32(tmem_s + c * 32, sv[c]);
@@ -577,13 +624,15 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                             if (c * 32 + e > lim) sv[c][e] = 0xFF800000u;  // -inf
                 }
                 const float mx = fmaxf(fmaxf(tree_max32(sv[0]), tree_max32(sv[1])), fmaxf(tree_max32(sv[2]), tree_max32(sv[3])));
-                // The reference maximum moves only when a row's maximum has outgrown it by 2^8: P then stays below 2^8
-                // (bf16 keeps its relative precision) and O is hardly ever rescaled.
+                // The reference maximum moves only when a row's maximum has outgrown it by 2^kPGrow, so that O is hardly
+                // ever rescaled.  bf16 P keeps its relative precision at any size.  fp16 P is held 2^10 up, which leaves
+                // 2^5 to grow below its largest value and rounds by 2^-11 of the value or 2^-35 of the row's largest.
+                constexpr float kPGrow = F8 ? 5.f : 8.f, kPShift = F8 ? 10.f : 0.f;
                 const float m_new = fmaxf(m_ref, mx);
                 if (i == 0) {
                     m_ref = m_new;
-                } else if (__any_sync(0xffffffffu, row_on && (m_new - m_ref) * a.scale_log2e > 8.f)) {
-                    const float corr = m_new == -INFINITY ? 1.f : ex2_approx((m_ref - m_new) * a.scale_log2e);
+                } else if (__any_sync(0xffffffffu, row_on && (m_new - m_ref) * scale > kPGrow)) {
+                    const float corr = m_new == -INFINITY ? 1.f : ex2_approx((m_ref - m_new) * scale);
                     m_ref = m_new;
                     l *= corr;
 #pragma unroll 1
@@ -596,8 +645,8 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                         tmem_st_32x16(tmem_o + c * 16, ov);
                     }
                 }
-                const float mc = m_ref == -INFINITY ? 0.f : m_ref * a.scale_log2e;
-                const float2 sc2 = make_float2(a.scale_log2e, a.scale_log2e), mc2 = make_float2(-mc, -mc);
+                const float mc = m_ref == -INFINITY ? 0.f : fmaf(m_ref, scale, -kPShift);
+                const float2 sc2 = make_float2(scale, scale), mc2 = make_float2(-mc, -mc);
                 float2 l2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -608,7 +657,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                         const float2 x = __ffma2_rn(make_float2(__uint_as_float(from[0]), __uint_as_float(from[1])), sc2, mc2);
                         const float2 p = make_float2(ex2_approx(x.x), ex2_approx(x.y));
                         l2[w & 1] = __fadd2_rn(l2[w & 1], p);
-                        pk[w] = pack2(p.x, p.y);
+                        pk[w] = F8 ? pack2_f16(p.x, p.y) : pack2(p.x, p.y);
                     }
                     tmem_st_32x32(tmem_s + h * 32, pk);
                     tmem_wait_st();
@@ -619,7 +668,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 l += (l2[0].x + l2[0].y) + (l2[1].x + l2[1].y);
             }
             if (!ok) break;
-            const float m_log2 = m_ref == -INFINITY ? -INFINITY : m_ref * a.scale_log2e;
+            const float m_log2 = m_ref == -INFINITY ? -INFINITY : fmaf(m_ref, scale, F8 ? -10.f : -0.f);
             const bool merge = dual && it.steps(1) > 0;
             if (dual && j == 1) {
                 // hand the row's maximum and sum to the first context, which reads O_1 as well

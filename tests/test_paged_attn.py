@@ -5,6 +5,10 @@ products: off by at most d steps of 2^-24 of sum |q_i k_i|, and the scaled maxim
 itself; a probability is off by that factor, delta.  The tensor-core kernel rounds P to bf16 (half a step, 2^-8 of the
 value) before P V, sums in fp32 (2^-14 of A is over 500 steps), and the result is rounded to bf16 once:
     |out - ref| <= 2^-8 |ref| + (2^-8 + 2 delta + 2^-14) A
+On fp8 caches P is rounded to fp16 instead, held 2^10 up: half a step is 2^-11 of the value or, among its subnormal
+numbers, 2^-25, that is 2^-35 of the row's largest probability (which is at least that of its reference maximum, so the
+sum it is divided by is no smaller): where the large probabilities meet values that are exactly zero, A does not cover
+that, and 2^-35 sum_j |v_j| is added.
     |lse - ref| <= delta + 2^-15 + 2^-21 |ref|        (the sum of p: at most 500 additions; its logarithm)"""
 
 import ctypes
@@ -74,6 +78,8 @@ def check(cache, q, out, lse, scale=None):
             most = (x.abs() @ k[:, h].abs().T * scale).masked_fill(hidden[:, None], 0.0).amax(-1) if kv[s] else torch.zeros_like(ref_lse)
             delta = d * 2.0 ** -24 * most + 2.0 ** -23 * most
             tol = 2.0 ** -8 * ref.abs() + (2.0 ** -8 + 2 * delta[..., None] + 2.0 ** -14) * size
+            if cache.k.dtype == torch.float8_e4m3fn:
+                tol = tol + 2.0 ** -35 * v[:, h].abs().sum(0)
             err = (out[rows, heads].double() - ref).abs()
             assert err.le(tol).all(), (s, h, float((err - tol).max()))
             if lse is not None:
@@ -184,6 +190,19 @@ def test_growing_maxima_and_large_scores():
     falling = cache._replace(k=cache.k.neg())
     out, lse = api.paged_attn(falling, q)
     check(falling, q, out, lse)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fp8", [False, True])
+def test_queries_of_any_size(fp8):
+    # rows of one tile that are powers of two apart, beyond what fp16 holds (fp8 caches multiply in fp16)
+    cache = make([(3, 900), (60, 300)], 16, 2, 128, fp8)
+    q = queries(63, 16, 128)
+    size = torch.tensor([2.0 ** e for e in (-140, -100, -40, -17, 0, 12, 17, 30)], device=DEV).repeat(63 * 2).view(63, 16, 1)
+    q = (q.float() * size).bfloat16()
+    for scale in (2.0 ** -21, 2.0 ** -34):
+        out, lse = api.paged_attn(cache, q, scale)
+        check(cache, q, out, lse, scale)
 
 
 @pytest.mark.gpu
