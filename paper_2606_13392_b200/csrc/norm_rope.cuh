@@ -5,12 +5,12 @@
 //   y = rotation of the pairs of n's first `rot` elements by the angle p f_i, times mscale; the rest unchanged
 //
 // Bound by HBM (about 2 flop per byte), so the design is about bytes in flight and about doing the per-token work
-// once.  A head is 16 bytes for each of d/8 lanes (a power of two reserved: 8, 16 or 32), a warp loads U heads per
-// lane group before it computes.  Both outputs of a pair need both inputs: in the half layout the partner sits
-// rot/16 lanes away and its raw bf16 come by shuffle (four registers for eight elements), in the interleaved
-// layout it is in the same register.  Angles are formed in 64 bits as turns, p (f / 2 pi) minus the nearest whole
+// once.  A head is 16 bytes for each of d/8 lanes (a power of two reserved: 8, 16 or 32); a warp of the forward kernel
+// loads four heads per lane group before it computes.  Both outputs of a pair need both inputs: in the half layout the partner sits rot/16 lanes away and its raw bf16 come by shuffle (four registers
+// for eight elements), in the interleaved layout it is in the same register.
+// Angles are formed in 64 bits as turns, p (f / 2 pi) minus the nearest whole
 // number, because a 32-bit angle at position 10^6 is off by 0.03 rad; sine and cosine of the remainder are 32-bit.
-// A CTA computes them once per (token, pair) into shared memory, as coefficients of the partner form
+// The forward kernel's CTAs compute them once per (token, pair) into shared memory, as coefficients of the partner form
 //   y_e = rstd (x_e A_e + x_partner B_e),   A_e = w_e cos, B_e = -+ w_partner sin
 // which holds for the elements behind `rot` too (A = w, B = 0).
 // Sums of squares and all products are 32-bit; the one rounding is the store (bf16, or E4M3 saturating).
@@ -67,14 +67,26 @@ __device__ __forceinline__ uint4 pack8(const float (&f)[8]) {
     return make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7]));
 }
 
-// Eight floats -> eight E4M3 (nearest, beyond the range the largest).
-__device__ __forceinline__ uint2 pack8_e4m3(const float (&f)[8]) {
+// Eight bf16 as four pairs of floats, and back: packed two-float arithmetic halves the instructions, which is what
+// bounds these kernels next to the bytes.
+struct F8v { float2 v[4]; };
+__device__ __forceinline__ F8v widen8(const uint4& u) {
+    return F8v{{bf16x2_to_float2(u.x), bf16x2_to_float2(u.y), bf16x2_to_float2(u.z), bf16x2_to_float2(u.w)}};
+}
+__device__ __forceinline__ uint4 narrow8(const F8v& f) {
+    return make_uint4(pack2(f.v[0].x, f.v[0].y), pack2(f.v[1].x, f.v[1].y), pack2(f.v[2].x, f.v[2].y), pack2(f.v[3].x, f.v[3].y));
+}
+__device__ __forceinline__ uint2 narrow8_e4m3(const F8v& f) {  // nearest, beyond the range the largest
     uint32_t h[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        h[i] = __nv_cvt_float2_to_fp8x2(make_float2(f[2 * i], f[2 * i + 1]), __NV_SATFINITE, __NV_E4M3);
+    for (int i = 0; i < 4; ++i) h[i] = __nv_cvt_float2_to_fp8x2(f.v[i], __NV_SATFINITE, __NV_E4M3);
     return make_uint2(h[0] | (h[1] << 16), h[2] | (h[3] << 16));
 }
+__device__ __forceinline__ F8v load8(const float* p) {
+    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+    return F8v{{make_float2(a.x, a.y), make_float2(a.z, a.w), make_float2(b.x, b.y), make_float2(b.z, b.w)}};
+}
+__device__ __forceinline__ float2 twice(float a) { return make_float2(a, a); }
 
 template <int LPH>
 __device__ __forceinline__ float group_sum(float v) {
@@ -125,11 +137,14 @@ __device__ __forceinline__ int paged_seq_of(const PagedView& c, int i) {
     return lo;
 }
 
+// (Warps on their own with asynchronous copies, the gradient kernel's form, were slower here: 250 against 212 us for 32768
+// tokens of 64 + 8 heads.  One reduction and half the bytes per output leave the independent heads of an item enough.)
 // Forward (APPEND = false: q and k to q.out and k.out; true: k and v to the cache, q to q.out).
 // Coefficients in shared memory: [token][set 0 = q, 1 = k][lane of the head][A 0..7, B 0..7].
-template <int LPH, bool APPEND, bool F8>
+// EXACT: a head fills its lanes (d = 8 LPH).
+template <int LPH, bool EXACT, bool APPEND, bool F8>
 __global__ void __launch_bounds__(kRopeThreads)
-norm_rope_kernel(RopeArgs rp, RopeHeads q, RopeHeads k, RopeHeads v, int64_t n_tokens, int d, float eps, bool w32,
+norm_rope_kernel(RopeArgs rp, RopeHeads q, RopeHeads k, RopeHeads v, int64_t n_tokens, int d_arg, float eps, bool w32,
                  const int64_t* __restrict__ positions, int tile, int heads_per_cta, PagedView cache,
                  void* __restrict__ k_pool, void* __restrict__ v_pool, int* status) {
     constexpr int HPW = 32 / LPH;                // heads a warp holds side by side
@@ -138,7 +153,9 @@ norm_rope_kernel(RopeArgs rp, RopeHeads q, RopeHeads k, RopeHeads v, int64_t n_t
     __shared__ int64_t s_pos[kRopeMaxTile], s_row[kRopeMaxTile];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int j = lane % LPH, sub = lane / LPH;
-    const bool active = j * 8 < d;
+    const int d = EXACT ? LPH * 8 : d_arg;
+    const float inv_d = 1.0f / (float)d;
+    const bool active = EXACT || j * 8 < d;
     const int half = rp.rot / 2;
     const bool turned = rp.freqs != nullptr && j * 8 < rp.rot;
     const int partner = sub * LPH + (j * 8 < half ? j + half / 8 : j - half / 8);
@@ -208,45 +225,41 @@ norm_rope_kernel(RopeArgs rp, RopeHeads q, RopeHeads k, RopeHeads v, int64_t n_t
         // One item: U loads per lane group in flight, then head after head.
         auto heads = [&](const RopeHeads& hs, auto set_c, int t, int item, void* to, int64_t to_row) {
             constexpr int set = decltype(set_c)::value;
-            const __nv_bfloat16* src = hs.x + (t0 + t) * hs.stride;
+            const int h0 = item * run + sub, left = hs.n_heads - item * run;  // this lane group's first head; heads of the item
+            const __nv_bfloat16* src = hs.x + (t0 + t) * hs.stride + (int64_t)h0 * d + j * 8;
             uint4 x[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int h = item * run + u * HPW + sub;
                 x[u] = make_uint4(0u, 0u, 0u, 0u);
-                if (active && h < hs.n_heads) x[u] = *reinterpret_cast<const uint4*>(src + (int64_t)h * d + j * 8);
+                if (active && (left >= run || h0 + u * HPW < hs.n_heads)) x[u] = *reinterpret_cast<const uint4*>(src + u * HPW * d);
             }
-            float A[8], B[8];
+            F8v A, B;
             if constexpr (set < 2) {
-                const float4* from = reinterpret_cast<const float4*>(coef + (t * 2 + set) * (LPH * 16) + j * 16);
-                float4 a0 = make_float4(0.f, 0.f, 0.f, 0.f), a1 = a0, b0 = a0, b1 = a0;
-                if (active) { a0 = from[0]; a1 = from[1]; b0 = from[2]; b1 = from[3]; }
-                A[0] = a0.x; A[1] = a0.y; A[2] = a0.z; A[3] = a0.w; A[4] = a1.x; A[5] = a1.y; A[6] = a1.z; A[7] = a1.w;
-                B[0] = b0.x; B[1] = b0.y; B[2] = b0.z; B[3] = b0.w; B[4] = b1.x; B[5] = b1.y; B[6] = b1.z; B[7] = b1.w;
+                const float* from = coef + (t * 2 + set) * (LPH * 16) + j * 16;
+                A = load8(from);
+                B = load8(from + 8);
             }
+            const int64_t at0 = (to_row * hs.n_heads + h0) * d + j * 8;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int h = item * run + u * HPW + sub;
-                if (item * run + u * HPW >= hs.n_heads) break;  // (the same for the whole warp)
-                float y[8];
-                unpack8(x[u], y);
+                if (left < run && u * HPW >= left) break;  // (the same for the whole warp)
+                F8v y = widen8(x[u]);
                 if constexpr (set < 2) {
-                    float r = 1.f;
+                    float2 r = twice(1.f);
                     if (hs.w != nullptr) {
-                        float ss = 0.f;
+                        float2 ss = __fmul2_rn(y.v[0], y.v[0]);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) ss = fmaf(y[e], y[e], ss);
-                        r = rsqrtf(group_sum<LPH>(ss) / (float)d + eps);
+                        for (int e = 1; e < 4; ++e) ss = __ffma2_rn(y.v[e], y.v[e], ss);
+                        r = twice(rsqrtf(fmaf(group_sum<LPH>(ss.x + ss.y), inv_d, eps)));
                     }
-                    float xp[8];
-                    unpack8(rope_partner(x[u], partner, turned, rp.interleaved), xp);
+                    const F8v p = widen8(rope_partner(x[u], partner, turned, rp.interleaved));
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) y[e] = r * fmaf(y[e], A[e], xp[e] * B[e]);
+                    for (int e = 0; e < 4; ++e) y.v[e] = __fmul2_rn(r, __ffma2_rn(y.v[e], A.v[e], __fmul2_rn(p.v[e], B.v[e])));
                 }
-                if (!active || h >= hs.n_heads) continue;
-                const int64_t at = (to_row * hs.n_heads + h) * d + j * 8;
-                if constexpr (F8 && set > 0) *reinterpret_cast<uint2*>(static_cast<uint8_t*>(to) + at) = pack8_e4m3(y);
-                else *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(to) + at) = pack8(y);
+                if (!active || (left < run && h0 + u * HPW >= hs.n_heads)) continue;
+                const int64_t at = at0 + u * HPW * d;
+                if constexpr (F8 && set > 0) *reinterpret_cast<uint2*>(static_cast<uint8_t*>(to) + at) = narrow8_e4m3(y);
+                else *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(to) + at) = narrow8(y);
             }
         };
         for (int it = warp; it < nt * item_n; it += kRopeWarps) {
@@ -267,12 +280,29 @@ norm_rope_kernel(RopeArgs rp, RopeHeads q, RopeHeads k, RopeHeads v, int64_t n_t
     }
 }
 
+// 16 bytes to shared memory without registers or waiting.
+__device__ __forceinline__ void copy16_async(void* dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+
 // Gradients.  With g = (the transposed rotation of dy) and xh = x rstd:
 //   dw = sum over tokens and heads of g xh,   dx = rstd (g w - xh mean(g w xh))      (w = none: dx = g)
-// rstd is computed again from x: that is cheaper than keeping it.  A lane accumulates its eight elements of dw of
-// both sets in registers over all its items; lanes and warps of a CTA join in a fixed order, CTAs leave a row each
-// in the workspace and norm_rope_dw_kernel adds the rows in order, so equal calls give equal bits.
-// Shared memory: [token][lane of the head][cos 0..7, signed sin 0..7].
+// rstd is computed again from x: that is cheaper than keeping it.  Two tensors in, one out, and two reductions per head:
+// what it takes is bytes in flight, and registers do not hold enough of them.  So warps work alone, without CTA barriers:
+// a step is the heads that fit a warp side by side, and every warp takes an equal run of the steps of all tokens; it
+// computes a token's angles into a table of its own, and its lanes copy their 16 bytes of x and dy of the next
+// kGradStages - 1 steps to shared memory asynchronously (each lane reads back only what it copied).  The first q_ctas
+// CTAs do the queries, the others the keys (one set of weights and sums in registers).  A lane accumulates its eight elements of dw over all its steps; lanes and warps of a CTA join in
+// a fixed order, CTAs leave a row each in the workspace and norm_rope_dw_kernel adds the rows in order, so equal calls
+// give equal bits.
+// Table: [lane of the head][cos 0..7, signed sin 0..7].
+constexpr int kGradThreads = 128, kGradWarps = kGradThreads / 32;
+constexpr int kGradCtas = 4;    // per SM
+constexpr int kGradStages = 4;  // steps of 32 lanes x 16 bytes of x and of dy
 struct RopeGrads {
     const __nv_bfloat16* dy;  // rows of n_heads*d, at dy + token*stride
     int64_t stride;
@@ -280,146 +310,157 @@ struct RopeGrads {
 };
 
 template <int LPH>
-__global__ void __launch_bounds__(kRopeThreads)
-norm_rope_grad_kernel(RopeArgs rp, RopeHeads q, RopeHeads k, RopeGrads gq, RopeGrads gk, int64_t n_tokens, int d,
-                      float eps, bool w32, const int64_t* __restrict__ positions, int tile, float* __restrict__ dw_rows) {
-    constexpr int HPW = 32 / LPH, U = 2;
-    extern __shared__ __align__(16) float coef[];  // [tile][LPH][16], then reused: [warps][2][LPH*8]
-    __shared__ int64_t s_pos[kRopeMaxTile];
+constexpr size_t grad_smem() {
+    return (size_t)kGradWarps * (kGradStages * 2 * 32 * sizeof(uint4) + LPH * 16 * sizeof(float));
+}
+
+template <int LPH, bool EXACT>
+__global__ void __launch_bounds__(kGradThreads, kGradCtas)
+norm_rope_grad_kernel(RopeArgs rp, RopeHeads q, RopeHeads k, RopeGrads gq, RopeGrads gk, int64_t n_tokens, int d_arg,
+                      float eps, bool w32, const int64_t* __restrict__ positions, int q_ctas,
+                      float* __restrict__ dw_rows) {
+    constexpr int HPW = 32 / LPH;  // heads of a step, side by side
+    extern __shared__ __align__(16) uint8_t grad_raw[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint4* ring = reinterpret_cast<uint4*>(grad_raw) + warp * (kGradStages * 64) + lane;  // [stage][x, dy][lane]
+    float* table = reinterpret_cast<float*>(grad_raw + (size_t)kGradWarps * kGradStages * 64 * sizeof(uint4)) + warp * (LPH * 16);
+    const bool is_k = (int)blockIdx.x >= q_ctas;
+    const RopeHeads& hs = is_k ? k : q;
+    const RopeGrads& gs = is_k ? gk : gq;
+    const int64_t mine = (is_k ? blockIdx.x - q_ctas : blockIdx.x) * kGradWarps + warp;  // of `warps`
+    const int64_t warps = (is_k ? gridDim.x - q_ctas : q_ctas) * kGradWarps;
     const int j = lane % LPH, sub = lane / LPH;
-    const bool active = j * 8 < d;
+    const int d = EXACT ? LPH * 8 : d_arg;
+    const float inv_d = 1.0f / (float)d;
+    const bool active = EXACT || j * 8 < d;
     const int half = rp.rot / 2;
     const bool turned = rp.freqs != nullptr && j * 8 < rp.rot;
     const int partner = sub * LPH + (j * 8 < half ? j + half / 8 : j - half / 8);
-    const int run = U * HPW;
-    const int n_q = (q.n_heads + run - 1) / run, n_k = (k.n_heads + run - 1) / run, n_all = n_q + n_k;
+    const bool norm = hs.w != nullptr;
     const int first_plain = rp.freqs != nullptr ? rp.rot : 0;
-    float w[2][8], dw[2][8];
+    const int groups = (hs.n_heads + HPW - 1) / HPW;  // steps of a token
+    const int64_t steps = n_tokens * groups, lo = steps / warps * mine + min(mine, steps % warps);
+    int64_t left = steps / warps + (mine < steps % warps);
+    F8v w, dw;
 #pragma unroll
-    for (int set = 0; set < 2; ++set)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const void* from = set == 0 ? q.w : k.w;
-            w[set][e] = active && from != nullptr ? weight_at(from, j * 8 + e, w32) : 1.f;
-            dw[set][e] = 0.f;
-        }
-    for (int64_t t0 = (int64_t)blockIdx.x * tile; t0 < n_tokens; t0 += (int64_t)gridDim.x * tile) {
-        const int nt = (int)min((int64_t)tile, n_tokens - t0);
-        if (threadIdx.x < nt) s_pos[threadIdx.x] = positions != nullptr ? positions[t0 + threadIdx.x] : 0;
-        __syncthreads();
-        if (rp.freqs != nullptr)
-            for (int e = threadIdx.x; e < nt * half; e += kRopeThreads) {
-                const int t = e / half, i = e - t * half;
-                float c, s;
-                rope_angle(rp, s_pos[t], i, c, s);
-                const int a = rope_first(rp, i), b = rope_second(rp, i);
-                float* to = coef + t * (LPH * 16);
-                to[(a >> 3) * 16 + (a & 7)] = c;
-                to[(a >> 3) * 16 + 8 + (a & 7)] = s;
-                to[(b >> 3) * 16 + (b & 7)] = c;
-                to[(b >> 3) * 16 + 8 + (b & 7)] = -s;
-            }
-        for (int e = threadIdx.x; e < nt * (d - first_plain); e += kRopeThreads) {
-            const int t = e / (d - first_plain), c = first_plain + e - t * (d - first_plain);
-            float* to = coef + t * (LPH * 16) + (c >> 3) * 16 + (c & 7);
-            to[0] = 1.f;
-            to[8] = 0.f;
-        }
-        __syncthreads();
-        auto heads = [&](const RopeHeads& hs, const RopeGrads& gs, const float (&w)[8], float (&dw)[8], int t, int item) {
-            const bool norm = hs.w != nullptr;
-            uint4 xv[U], gv[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int h = item * run + u * HPW + sub;
-                xv[u] = gv[u] = make_uint4(0u, 0u, 0u, 0u);
-                if (active && h < hs.n_heads) {
-                    gv[u] = *reinterpret_cast<const uint4*>(gs.dy + (t0 + t) * gs.stride + (int64_t)h * d + j * 8);
-                    if (norm) xv[u] = *reinterpret_cast<const uint4*>(hs.x + (t0 + t) * hs.stride + (int64_t)h * d + j * 8);
-                }
-            }
-            float c[8], s[8];
-            {
-                const float4* from = reinterpret_cast<const float4*>(coef + t * (LPH * 16) + j * 16);
-                float4 c0 = make_float4(0.f, 0.f, 0.f, 0.f), c1 = c0, s0 = c0, s1 = c0;
-                if (active) { c0 = from[0]; c1 = from[1]; s0 = from[2]; s1 = from[3]; }
-                c[0] = c0.x; c[1] = c0.y; c[2] = c0.z; c[3] = c0.w; c[4] = c1.x; c[5] = c1.y; c[6] = c1.z; c[7] = c1.w;
-                s[0] = s0.x; s[1] = s0.y; s[2] = s0.z; s[3] = s0.w; s[4] = s1.x; s[5] = s1.y; s[6] = s1.z; s[7] = s1.w;
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (item * run + u * HPW >= hs.n_heads) break;  // (the same for the whole warp)
-                const int h = item * run + u * HPW + sub;
-                float g[8], gp[8];
-                unpack8(gv[u], g);
-                unpack8(rope_partner(gv[u], partner, turned, rp.interleaved), gp);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) g[e] = fmaf(g[e], c[e], gp[e] * s[e]);
-                if (norm) {
-                    float x[8], ss = 0.f, dot = 0.f;
-                    unpack8(xv[u], x);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        ss = fmaf(x[e], x[e], ss);
-                        dot = fmaf(g[e] * w[e], x[e], dot);
-                    }
-                    ss = group_sum<LPH>(ss);
-                    dot = group_sum<LPH>(dot);
-                    const float r = rsqrtf(ss / (float)d + eps);
-                    const float m = dot / (float)d * r * r;  // times x = xh mean(g w xh)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        if (h < hs.n_heads) dw[e] = fmaf(g[e], x[e] * r, dw[e]);  // (eps = 0: r of an absent head is infinite)
-                        g[e] = r * (g[e] * w[e] - x[e] * m);
-                    }
-                }
-                if (active && h < hs.n_heads)
-                    *reinterpret_cast<uint4*>(gs.dx + ((t0 + t) * hs.n_heads + h) * d + j * 8) = pack8(g);
-            }
-        };
-        for (int it = warp; it < nt * n_all; it += kRopeWarps) {
-            const int t = it / n_all;
-            const int item = it - t * n_all;
-            if (item < n_q) heads(q, gq, w[0], dw[0], t, item);
-            else heads(k, gk, w[1], dw[1], t, item - n_q);
-        }
-        __syncthreads();
+    for (int e = 0; e < 4; ++e) {
+        w.v[e] = active && norm ? make_float2(weight_at(hs.w, j * 8 + 2 * e, w32), weight_at(hs.w, j * 8 + 2 * e + 1, w32)) : twice(1.f);
+        dw.v[e] = twice(0.f);
     }
-    if (dw_rows == nullptr) return;
-#pragma unroll
-    for (int set = 0; set < 2; ++set)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-#pragma unroll
-            for (int o = 16; o >= LPH; o >>= 1) dw[set][e] += __shfl_xor_sync(0xffffffffu, dw[set][e], o);
-            if (sub == 0) coef[(warp * 2 + set) * (LPH * 8) + j * 8 + e] = dw[set][e];
+    int64_t t = groups > 0 ? lo / groups : 0;
+    int g0 = (int)(lo - t * groups);
+    // the copies' place in the run, kGradStages - 1 steps ahead
+    int64_t ahead = left, ahead_t = t;
+    int ahead_g = g0, put = 0;
+    auto copy_next = [&]() {
+        if (ahead > 0) {
+            const int h = ahead_g * HPW + sub;
+            if (active && h < hs.n_heads) {
+                const int64_t at = (int64_t)h * d + j * 8;
+                if (norm) copy16_async(ring + put * 64, hs.x + ahead_t * hs.stride + at);
+                copy16_async(ring + put * 64 + 32, gs.dy + ahead_t * gs.stride + at);
+            }
+            --ahead;
+            if (++ahead_g == groups) { ahead_g = 0; ++ahead_t; }
         }
+        put = put + 1 == kGradStages ? 0 : put + 1;
+        copy_async_commit();  // (an empty group at the end keeps the count)
+    };
+    for (int i = 0; i < kGradStages - 1; ++i) copy_next();
+    int get = 0;
+    for (; left > 0; ++t, g0 = 0) {
+        const int g_hi = (int)min((int64_t)groups, g0 + left);
+        left -= g_hi - g0;
+        const int64_t pos = positions != nullptr ? positions[t] : 0;
+        __syncwarp();
+        if (rp.freqs != nullptr)
+            for (int i = lane; i < half; i += 32) {
+                float c, s;
+                rope_angle(rp, pos, i, c, s);
+                const int a = rope_first(rp, i), b = rope_second(rp, i);
+                table[(a >> 3) * 16 + (a & 7)] = c;
+                table[(a >> 3) * 16 + 8 + (a & 7)] = s;
+                table[(b >> 3) * 16 + (b & 7)] = c;
+                table[(b >> 3) * 16 + 8 + (b & 7)] = -s;
+            }
+        for (int c = first_plain + lane; c < LPH * 8; c += 32) {
+            table[(c >> 3) * 16 + (c & 7)] = c < d ? 1.f : 0.f;  // (lanes without elements add zeros to the sums)
+            table[(c >> 3) * 16 + 8 + (c & 7)] = 0.f;
+        }
+        __syncwarp();
+        const F8v c = load8(table + j * 16), s = load8(table + j * 16 + 8);
+        __nv_bfloat16* to = gs.dx + (t * hs.n_heads + g0 * HPW + sub) * d + j * 8;
+        for (int gi = g0; gi < g_hi; ++gi, to += HPW * d) {
+            copy_async_wait<kGradStages - 2>();
+            const bool here = active && gi * HPW + sub < hs.n_heads;
+            const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+            const uint4 xv = here && norm ? ring[get * 64] : none, gv = here ? ring[get * 64 + 32] : none;
+            get = get + 1 == kGradStages ? 0 : get + 1;
+            copy_next();
+            F8v g = widen8(gv);
+            const F8v gp = widen8(rope_partner(gv, partner, turned, rp.interleaved));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) g.v[e] = __ffma2_rn(g.v[e], c.v[e], __fmul2_rn(gp.v[e], s.v[e]));
+            if (norm) {
+                const F8v x = widen8(xv);
+                F8v gw;
+                float2 ss = twice(0.f), dot = twice(0.f);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    gw.v[e] = __fmul2_rn(g.v[e], w.v[e]);
+                    ss = __ffma2_rn(x.v[e], x.v[e], ss);
+                    dot = __ffma2_rn(gw.v[e], x.v[e], dot);
+                }
+                const float sum = group_sum<LPH>(ss.x + ss.y), prod = group_sum<LPH>(dot.x + dot.y);
+                const float r = rsqrtf(fmaf(sum, inv_d, eps));
+                const float m = -(prod * inv_d * r * r);  // times x = -xh mean(g w xh)
+                // (an absent head adds nothing; with eps = 0 its r is infinite)
+                const float2 r2 = twice(r), m2 = twice(m), rd = twice(here ? r : 0.f);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    dw.v[e] = __ffma2_rn(g.v[e], __fmul2_rn(x.v[e], rd), dw.v[e]);
+                    g.v[e] = __fmul2_rn(r2, __ffma2_rn(x.v[e], m2, gw.v[e]));
+                }
+            }
+            if (here) *reinterpret_cast<uint4*>(to) = narrow8(g);
+        }
+    }
+    copy_async_wait<0>();
+    if (dw_rows == nullptr) return;
     __syncthreads();
-    for (int e = threadIdx.x; e < 2 * d; e += kRopeThreads) {
-        const int set = e / d, c = e - set * d;
+    float* join = reinterpret_cast<float*>(grad_raw);  // [warp][LPH * 8]
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        float sum = e & 1 ? dw.v[e >> 1].y : dw.v[e >> 1].x;
+#pragma unroll
+        for (int o = 16; o >= LPH; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (sub == 0) join[warp * (LPH * 8) + j * 8 + e] = sum;
+    }
+    __syncthreads();
+    for (int c = threadIdx.x; c < d; c += kGradThreads) {
         float sum = 0.f;
-        for (int i = 0; i < kRopeWarps; ++i) sum += coef[(i * 2 + set) * (LPH * 8) + c];
-        dw_rows[(int64_t)blockIdx.x * 2 * d + e] = sum;
+        for (int i = 0; i < kGradWarps; ++i) sum += join[i * (LPH * 8) + c];
+        dw_rows[(int64_t)blockIdx.x * d + c] = sum;
     }
 }
 
-// dw[e] = sum over the CTAs' rows, 32 columns per CTA: 32 x 32 threads, each row class in order, then a tree.
+// dw[c] = sum over the rows of the q CTAs (blockIdx.y = 0) or the k CTAs, 32 columns per CTA: 32 x 32 threads, each row
+// class in order, then a tree.
 __global__ void __launch_bounds__(1024)
-norm_rope_dw_kernel(const float* __restrict__ rows, int n_rows, int d, float* __restrict__ dwq, float* __restrict__ dwk) {
+norm_rope_dw_kernel(const float* __restrict__ rows, int q_rows, int n_rows, int d, float* __restrict__ dwq, float* __restrict__ dwk) {
     __shared__ float s[32][33];
+    float* to = blockIdx.y == 0 ? dwq : dwk;
+    if (to == nullptr) return;
+    const int first = blockIdx.y == 0 ? 0 : q_rows, last = blockIdx.y == 0 ? q_rows : n_rows;
     const int c = blockIdx.x * 32 + (threadIdx.x & 31), r0 = threadIdx.x >> 5;
     float sum = 0.f;
-    if (c < 2 * d)
-        for (int r = r0; r < n_rows; r += 32) sum += rows[(int64_t)r * 2 * d + c];
+    if (c < d)
+        for (int r = first + r0; r < last; r += 32) sum += rows[(int64_t)r * d + c];
     s[r0][threadIdx.x & 31] = sum;
     __syncthreads();
     const float total = warp_sum(s[threadIdx.x & 31][r0]);  // warp r0 owns column r0 of the 32
     const int col = blockIdx.x * 32 + r0;
-    if ((threadIdx.x & 31) == 0 && col < 2 * d) {
-        if (col < d) { if (dwq != nullptr) dwq[col] = total; }
-        else if (dwk != nullptr) dwk[col - d] = total;
-    }
+    if ((threadIdx.x & 31) == 0 && col < d) to[col] = total;
 }
 
 }  // namespace msa

@@ -58,12 +58,13 @@ constexpr int kMaxRopeHeads = 1024;
 // Lanes reserved for a head.
 static int lanes_per_head(int d) { return d <= 64 ? 8 : (d <= 128 ? 16 : 32); }
 
-template <int LPH, bool APPEND, bool F8>
+template <int LPH, bool EXACT, bool APPEND, bool F8>
 static void launch_norm_rope(const RopeArgs& rp, const RopeHeads& q, const RopeHeads& k, const RopeHeads& v, int64_t n,
                              int d, float eps, bool w32, const int64_t* positions, const PagedView& cache, void* k_pool,
                              void* v_pool, cudaStream_t st) {
-    // Many tokens: eight a CTA, so that 256 threads have about one angle each and all warps have items.  Few: one a
-    // CTA, its items spread over CTAs until the machine has four CTAs per SM (each repeats the token's angles).
+    // Many tokens: eight a CTA at a time, so that 256 threads have an angle or two each and all warps have items.  Few: one
+    // a CTA, its items spread over CTAs until the machine has four CTAs per SM (each repeats the token's angles).  Twice
+    // the CTAs that are resident: the second half evens out the rounds.
     const int run = 4 * (32 / LPH);
     const int items = (q.n_heads + run - 1) / run + (k.n_heads + run - 1) / run + (v.n_heads + run - 1) / run;
     const int64_t want = 4LL * sm_count();
@@ -72,41 +73,46 @@ static void launch_norm_rope(const RopeArgs& rp, const RopeHeads& q, const RopeH
     const int64_t tiles = ceil_div64(n, tile);
     const int parts = tiles >= want ? 1 : (int)std::min<int64_t>(items, ceil_div64(want, tiles));
     const int per = (items + parts - 1) / parts;
-    const dim3 grid((unsigned)std::min<int64_t>(tiles, 8LL * sm_count()), (items + per - 1) / per);
+    const dim3 grid((unsigned)std::min<int64_t>(tiles, 2 * want), (items + per - 1) / per);
     const size_t smem = (size_t)tile * 2 * LPH * 16 * sizeof(float);
     StageScope sc(kStageNone, st);
-    norm_rope_kernel<LPH, APPEND, F8><<<grid, kRopeThreads, smem, st>>>(rp, q, k, v, n, d, eps, w32, positions, tile, per, cache,
-                                                                      k_pool, v_pool, APPEND ? async_status_ptr() : nullptr);
+    norm_rope_kernel<LPH, EXACT, APPEND, F8><<<grid, kRopeThreads, smem, st>>>(rp, q, k, v, n, d, eps, w32, positions, tile, per, cache,
+                                                                             k_pool, v_pool, APPEND ? async_status_ptr() : nullptr);
 }
 
 template <bool APPEND, bool F8>
 static msa_status_t run_norm_rope(const RopeArgs& rp, const RopeHeads& q, const RopeHeads& k, const RopeHeads& v,
                                   int64_t n, int d, float eps, bool w32, const int64_t* positions,
                                   const PagedView& cache, void* k_pool, void* v_pool, cudaStream_t st) {
-    switch (lanes_per_head(d)) {
-        case 8: launch_norm_rope<8, APPEND, F8>(rp, q, k, v, n, d, eps, w32, positions, cache, k_pool, v_pool, st); break;
-        case 16: launch_norm_rope<16, APPEND, F8>(rp, q, k, v, n, d, eps, w32, positions, cache, k_pool, v_pool, st); break;
-        default: launch_norm_rope<32, APPEND, F8>(rp, q, k, v, n, d, eps, w32, positions, cache, k_pool, v_pool, st); break;
-    }
+#define MSA_ROPE(LPH, EXACT) launch_norm_rope<LPH, EXACT, APPEND, F8>(rp, q, k, v, n, d, eps, w32, positions, cache, k_pool, v_pool, st)
+    const int lanes = lanes_per_head(d);
+    if (d == 64) MSA_ROPE(8, true);
+    else if (d == 128) MSA_ROPE(16, true);
+    else if (lanes == 8) MSA_ROPE(8, false);
+    else if (lanes == 16) MSA_ROPE(16, false);
+    else MSA_ROPE(32, false);
+#undef MSA_ROPE
     return launch_status();
 }
 
-// CTAs of the gradient kernel = rows of weight gradients it leaves.
-static int64_t grad_tiles(int64_t n, int& tile) {
-    tile = kRopeMaxTile;
-    while (tile > 1 && ceil_div64(n, tile) < 4LL * sm_count()) tile /= 2;
-    return std::min<int64_t>(ceil_div64(n, tile), 4LL * sm_count());
+// CTAs of the gradient kernel, each leaving a row of weight gradients: all that are resident at once, shared out by
+// heads (the angles, which both kinds compute, cost a warp about as much as four heads).
+struct GradGrid { int64_t ctas, q_ctas; };
+static GradGrid grad_grid(int H_q, int H_k) {
+    GradGrid g;
+    g.ctas = (int64_t)kGradCtas * sm_count();
+    g.q_ctas = H_k == 0 ? g.ctas : (H_q == 0 ? 0 : std::min<int64_t>(g.ctas - 1, std::max<int64_t>(1, g.ctas * (H_q + 4) / (H_q + H_k + 8))));
+    return g;
 }
 
-template <int LPH>
+template <int LPH, bool EXACT>
 static void launch_norm_rope_grad(const RopeArgs& rp, const RopeHeads& q, const RopeHeads& k, const RopeGrads& gq,
                                   const RopeGrads& gk, int64_t n, int d, float eps, bool w32, const int64_t* positions,
-                                  float* dw_rows, cudaStream_t st) {
-    int tile;
-    const int64_t grid = grad_tiles(n, tile);
-    const size_t smem = std::max((size_t)tile * LPH * 16, (size_t)kRopeWarps * 2 * LPH * 8) * sizeof(float);
+                                  const GradGrid& g, float* dw_rows, cudaStream_t st) {
+    const size_t smem = std::max(grad_smem<LPH>(), (size_t)kGradWarps * LPH * 8 * sizeof(float));
     StageScope sc(kStageNone, st);
-    norm_rope_grad_kernel<LPH><<<(unsigned)grid, kRopeThreads, smem, st>>>(rp, q, k, gq, gk, n, d, eps, w32, positions, tile, dw_rows);
+    norm_rope_grad_kernel<LPH, EXACT><<<(unsigned)g.ctas, kGradThreads, smem, st>>>(rp, q, k, gq, gk, n, d, eps, w32, positions,
+                                                                                   (int)g.q_ctas, dw_rows);
 }
 
 // ---------------------------------------------------------------------- the paged cache
@@ -222,8 +228,7 @@ msa_status_t msa_qk_norm_rope(const msa_rope_t* rope, const void* q, int64_t q_s
 msa_status_t msa_qk_norm_rope_backward_workspace_bytes(int32_t head_dim, int64_t n_tokens, size_t* min_bytes) {
     if (head_dim <= 0 || n_tokens < 0 || min_bytes == nullptr) return MSA_ERR_INVALID_ARG;
     if (head_dim % 8 != 0 || head_dim > 256) return MSA_ERR_UNSUPPORTED;
-    int tile;
-    *min_bytes = (size_t)grad_tiles(n_tokens, tile) * 2 * head_dim * sizeof(float);
+    *min_bytes = (size_t)grad_grid(1, 1).ctas * head_dim * sizeof(float);
     return MSA_OK;
 }
 
@@ -256,11 +261,10 @@ msa_status_t msa_qk_norm_rope_backward(const msa_rope_t* rope, const void* dq_ou
     float* dwk = k_weight != nullptr ? dk_weight : nullptr;
     if (!aligned_to(dwq, 4) || !aligned_to(dwk, 4)) return MSA_ERR_INVALID_ARG;
     const bool want = dwq != nullptr || dwk != nullptr;
-    int tile;
-    const int64_t rows = grad_tiles(n_tokens, tile);
+    const GradGrid g = grad_grid(n_q_heads, n_k_heads);
     if (want && some) {
         if (workspace == nullptr || !aligned_to(workspace, 16)) return MSA_ERR_INVALID_ARG;
-        if (workspace_bytes < (size_t)rows * 2 * head_dim * sizeof(float)) return MSA_ERR_WORKSPACE;
+        if (workspace_bytes < (size_t)g.ctas * head_dim * sizeof(float)) return MSA_ERR_WORKSPACE;
     }
     cudaStream_t st = (cudaStream_t)stream;
     if (some && n_q_heads + n_k_heads > 0) {
@@ -269,16 +273,20 @@ msa_status_t msa_qk_norm_rope_backward(const msa_rope_t* rope, const void* dq_ou
         const RopeGrads gq{(const __nv_bfloat16*)dq_out, dq_stride, (__nv_bfloat16*)dq};
         const RopeGrads gk{(const __nv_bfloat16*)dk_out, dk_stride, (__nv_bfloat16*)dk};
         float* dw = want ? (float*)workspace : nullptr;
-        switch (lanes_per_head(head_dim)) {
-            case 8: launch_norm_rope_grad<8>(rp, qh, kh, gq, gk, n_tokens, head_dim, eps, w32, positions, dw, st); break;
-            case 16: launch_norm_rope_grad<16>(rp, qh, kh, gq, gk, n_tokens, head_dim, eps, w32, positions, dw, st); break;
-            default: launch_norm_rope_grad<32>(rp, qh, kh, gq, gk, n_tokens, head_dim, eps, w32, positions, dw, st); break;
-        }
+#define MSA_GRAD(LPH, EXACT) launch_norm_rope_grad<LPH, EXACT>(rp, qh, kh, gq, gk, n_tokens, head_dim, eps, w32, positions, g, dw, st)
+        const int lanes = lanes_per_head(head_dim);
+        if (head_dim == 64) MSA_GRAD(8, true);
+        else if (head_dim == 128) MSA_GRAD(16, true);
+        else if (lanes == 8) MSA_GRAD(8, false);
+        else if (lanes == 16) MSA_GRAD(16, false);
+        else MSA_GRAD(32, false);
+#undef MSA_GRAD
     }
     if (want) {
-        const int n_rows = some && n_q_heads + n_k_heads > 0 ? (int)rows : 0;  // no rows: the gradients are zeros
+        const bool any = some && n_q_heads + n_k_heads > 0;  // no rows: the gradients are zeros
         StageScope sc(kStageNone, st);
-        norm_rope_dw_kernel<<<(2 * head_dim + 31) / 32, 1024, 0, st>>>((const float*)workspace, n_rows, head_dim, dwq, dwk);
+        norm_rope_dw_kernel<<<dim3((head_dim + 31) / 32, 2), 1024, 0, st>>>((const float*)workspace, any ? (int)g.q_ctas : 0,
+                                                                            any ? (int)g.ctas : 0, head_dim, dwq, dwk);
     }
     return launch_status();
 }
