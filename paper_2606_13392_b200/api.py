@@ -159,7 +159,7 @@ def _workspace(t: torch.Tensor, size, *args) -> torch.Tensor:
     else:
         with torch.cuda.device(t.device):
             n = size(*args)
-    return B.alloc_workspace(n, t.device)
+    return t.new_empty(max(n, 256), dtype=torch.uint8)
 
 
 def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
@@ -203,10 +203,10 @@ def qk_norm_rope_backward(dq_out: Optional[torch.Tensor], dk_out: Optional[torch
     """Gradients of qk_norm_rope's inputs for those of its outputs -> (dq, dk, dq_weight, dk_weight); the weights'
     are fp32, None without a weight."""
     dy = dq_out if dq_out is not None else dk_out
-    dev, d = dy.device, dy.shape[-1]
+    d = dy.shape[-1]
     dq, dk = _empty(dq_out), _empty(dk_out)
-    dwq = None if q_weight is None else torch.empty(d, dtype=torch.float32, device=dev)
-    dwk = None if k_weight is None else torch.empty(d, dtype=torch.float32, device=dev)
+    dwq = None if q_weight is None else dy.new_empty(d, dtype=torch.float32)
+    dwk = None if k_weight is None else dy.new_empty(d, dtype=torch.float32)
     ws = None
     if dwq is not None or dwk is not None:
         ws = _workspace(dy, B.msa_qk_norm_rope_backward_workspace_bytes, d, dy.shape[0])
@@ -234,7 +234,7 @@ def paged_attn(cache: PagedCache, q: torch.Tensor, softmax_scale: float = 0.0, o
     """Dense causal attention of the new tokens q [rows, heads, d] over the cache, which already holds their keys and
     values -> (out, lse).  Rows behind the last sequence are left as they are (uninitialised in outputs made here)."""
     out = _empty(q) if out is None else out
-    lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if want_lse else None
+    lse = q.new_empty(q.shape[:2], dtype=torch.float32) if want_lse else None
     if workspace is None:
         workspace = _workspace(q, B.msa_paged_attn_workspace_bytes, cache.k, q.shape[1])
     B.msa_paged_attn(cache.k, cache.v, cache.page_table, cache.kv_lens, cache.cu_q, q, softmax_scale, out, lse, workspace)

@@ -383,10 +383,12 @@ _ARGTYPES = {
                          c_vp],
     "msa_qk_norm_rope_backward": [c_vp, c_vp, c_i64, c_vp, c_i64, c_vp, c_i64, c_i32, c_vp, c_vp, c_i64, c_i32, c_vp, c_i32,
                                   c_i32, _F32, c_vp, c_i64, c_vp, c_vp, c_vp, c_vp, c_vp, c_sz, c_vp],
+    "msa_paged_attn_workspace_bytes": [c_vp, c_i32, c_vp],
     "msa_paged_attn": [c_vp, c_vp, c_i32, c_i64, _F32, c_vp, c_vp, c_vp, c_sz, c_vp],
     "msa_paged_append": [c_vp, c_vp, c_vp, c_i64, c_i32, c_vp, c_vp, c_i64, c_vp, c_vp, c_i64, c_i32, _F32, c_i64, c_vp, c_vp],
 }
 _fns = {}
+_POOL_TYPES = {torch.bfloat16: 0, torch.float8_e4m3fn: 1}  # msa_paged_cache_t.fp8
 
 
 def _fn(name: str):
@@ -546,20 +548,20 @@ def _paged(k_pool, v_pool, page_table, kv_lens, cu_q):
     """The cache structure of checked tensors."""
     index = _device_of(k_pool, "the key pool")
     kind, shape = k_pool.dtype, k_pool.shape
-    if len(shape) != 4 or kind not in (torch.bfloat16, torch.float8_e4m3fn) or not k_pool.is_contiguous():
+    if len(shape) != 4 or kind not in _POOL_TYPES or not k_pool.is_contiguous():
         raise ValueError("the key pool must be a contiguous [pages, page size, KV heads, head_dim] tensor of bf16 or "
                          "float8_e4m3fn, got %s %s" % (kind, tuple(shape)))
     if v_pool is not None and (v_pool.shape != shape or v_pool.dtype != kind or not v_pool.is_contiguous() or
                                v_pool.get_device() != index):
         raise ValueError("the value pool must be like the key pool")
-    batch = kv_lens.shape[0]
-    if page_table.dim() != 2 or kv_lens.dim() != 1 or page_table.shape[0] != batch or cu_q.shape != (batch + 1,):
+    table, lens = page_table.shape, kv_lens.shape
+    if len(table) != 2 or len(lens) != 1 or table[0] != lens[0] or cu_q.shape != (lens[0] + 1,):
         raise ValueError("page_table [batch, pages], kv_lens [batch] and cu_q [batch + 1] must agree")
     for t in (page_table, kv_lens, cu_q):
         if t.dtype != torch.int32 or not t.is_contiguous() or t.get_device() != index:
             raise ValueError("page_table, kv_lens and cu_q must be contiguous int32 on cuda:%d" % index)
-    return index, MsaPagedCache(k_pool.data_ptr(), _at(v_pool), page_table.data_ptr(), kv_lens.data_ptr(), cu_q.data_ptr(), batch,
-                                page_table.shape[1], shape[0], shape[1], shape[2], shape[3], 0 if kind == torch.bfloat16 else 1)
+    return index, MsaPagedCache(k_pool.data_ptr(), _at(v_pool), page_table.data_ptr(), kv_lens.data_ptr(), cu_q.data_ptr(), lens[0],
+                                table[1], *shape, _POOL_TYPES[kind])
 
 
 def msa_paged_append(k_pool, v_pool, page_table, kv_lens, cu_q, freqs, interleaved, mscale, q, q_weight, k, k_weight, v,
@@ -588,9 +590,10 @@ def msa_paged_attn_workspace_bytes(k_pool, n_q_heads: int) -> int:
     pages, size, heads, d = k_pool.shape
     cache = MsaPagedCache(n_pages=pages, page_size=size, n_kv_heads=heads, head_dim=d, fp8=0 if k_pool.dtype == torch.bfloat16 else 1)
     mn = c_sz(0)
-    _check(lib().msa_paged_attn_workspace_bytes(ctypes.byref(cache), c_i32(n_q_heads), ctypes.byref(mn)),
-           "msa_paged_attn_workspace_bytes")
-    return int(mn.value)
+    code = _fn("msa_paged_attn_workspace_bytes")(ctypes.byref(cache), n_q_heads, ctypes.byref(mn))
+    if code != 0:
+        raise MsaError(code, "msa_paged_attn_workspace_bytes")
+    return mn.value
 
 
 def msa_paged_attn(k_pool, v_pool, page_table, kv_lens, cu_q, q, softmax_scale, out, lse, workspace):

@@ -30,6 +30,14 @@ static int sm_count() {
     return n[dev];
 }
 
+// The status word of the current device; its address is looked up once per device.
+static int* status_word() {
+    static int* word[64] = {nullptr};
+    const int dev = current_device();
+    if (word[dev] == nullptr) word[dev] = async_status_ptr();
+    return word[dev];
+}
+
 static msa_status_t launch_status() { return cudaPeekAtLastError() == cudaSuccess ? MSA_OK : MSA_ERR_CUDA; }
 
 // ---------------------------------------------------------------------- norm and rotation
@@ -77,7 +85,7 @@ static void launch_norm_rope(const RopeArgs& rp, const RopeHeads& q, const RopeH
     const size_t smem = (size_t)tile * 2 * LPH * 16 * sizeof(float);
     StageScope sc(kStageNone, st);
     norm_rope_kernel<LPH, EXACT, APPEND, F8><<<grid, kRopeThreads, smem, st>>>(rp, q, k, v, n, d, eps, w32, positions, tile, per, cache,
-                                                                             k_pool, v_pool, APPEND ? async_status_ptr() : nullptr);
+                                                                             k_pool, v_pool, APPEND ? status_word() : nullptr);
 }
 
 template <bool APPEND, bool F8>
@@ -169,7 +177,7 @@ static msa_status_t launch_paged_attn(const PagedAttnArgs& a, const msa_paged_ca
         const uint32_t kb[5] = {64, 8, 2, 1, (uint32_t)box / 8};
         ok = ok && encode_tmap_bf16(&tm_k, c.k, 5, kd, ks, kb) && encode_tmap_bf16(&tm_v, c.v, 5, kd, ks, kb);
     }
-    int* status = async_status_ptr();
+    int* status = status_word();
     if (!ok || status == nullptr) return MSA_ERR_CUDA;
     const size_t smem = sizeof(PagedSmem);
     static bool attr_set[64] = {false};  // per device
@@ -183,13 +191,23 @@ static msa_status_t launch_paged_attn(const PagedAttnArgs& a, const msa_paged_ca
     const int64_t snap = (int64_t)40e6 / (F8 ? 256 : 512);
     {
         StageScope sc(kStageNone, st);
-        paged_attn_tc_kernel<F8><<<grid, paged_threads(F8), smem, st>>>(tm_q, tm_q1, tm_k, tm_v, a, box, snap, status);
+        paged_attn_tc_kernel<F8><<<grid, paged_threads(F8), smem, st>>>(tm_q, tm_q1, tm_k, tm_v, a, box, snap, 1.0 / grid, status);
     }
     if (cudaPeekAtLastError() != cudaSuccess) return MSA_ERR_CUDA;
     {   // a cut tile has at most 256 rows: up to 16 CTAs of four rows at a time, as far as the call has rows
         const int64_t most = std::min<int64_t>(kPagedSlotRows, (int64_t)a.n_tokens * a.G);
+        // (its launch overlaps the attention kernel's end; it waits there before it reads)
+        cudaLaunchAttribute early;
+        early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        early.val.programmaticStreamSerializationAllowed = 1;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(grid, (unsigned)std::min<int64_t>(16, ceil_div64(most, 4)));
+        cfg.blockDim = dim3(128);
+        cfg.stream = st;
+        cfg.attrs = &early;
+        cfg.numAttrs = 1;
         StageScope sc(kStageNone, st);
-        paged_combine_kernel<<<dim3(grid, (unsigned)std::min<int64_t>(16, ceil_div64(most, 4))), 128, 0, st>>>(a, grid);
+        if (cudaLaunchKernelEx(&cfg, paged_combine_kernel, a, grid) != cudaSuccess) return MSA_ERR_CUDA;
     }
     return launch_status();
 }
@@ -312,7 +330,7 @@ msa_status_t msa_paged_append(const msa_paged_cache_t* cache, const msa_rope_t* 
     if ((v == nullptr) != (cache->v == nullptr)) return MSA_ERR_INVALID_ARG;
     if (v != nullptr && !rows_ok(v, v_stride, H, d)) return MSA_ERR_INVALID_ARG;
     if (!weight_ok(q_weight, w32) || !weight_ok(k_weight, w32)) return MSA_ERR_INVALID_ARG;
-    if (async_status_ptr() == nullptr) return MSA_ERR_CUDA;
+    if (status_word() == nullptr) return MSA_ERR_CUDA;
     const RopeHeads qh{(const __nv_bfloat16*)q, q_stride, n_q_heads, q_weight, (__nv_bfloat16*)q_out};
     const RopeHeads kh{(const __nv_bfloat16*)k, k_stride, H, k_weight, nullptr};
     const RopeHeads vh{(const __nv_bfloat16*)v, v_stride, v != nullptr ? H : 0, nullptr, nullptr};
@@ -364,7 +382,7 @@ msa_status_t msa_paged_attn(const msa_paged_cache_t* cache, const void* q, int32
     }
     const int64_t grid = ceil_div64(n_tokens * n_q_heads, 4);
     if (grid > 2147483647LL) return MSA_ERR_UNSUPPORTED;
-    int* status = async_status_ptr();
+    int* status = status_word();
     if (status == nullptr) return MSA_ERR_CUDA;
     {
         StageScope sc(kStageNone, st);

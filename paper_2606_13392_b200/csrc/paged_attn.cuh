@@ -91,6 +91,12 @@ __host__ __device__ inline int64_t paged_units_before(const PagedSeq& q, int t) 
     return u;
 }
 
+// Units of a sequence.
+__host__ __device__ inline int64_t paged_units(const PagedAttnArgs& a, const PagedSeq& q) {
+    if (q.n_tiles <= 1) return q.n_tiles == 0 ? 0 : (int64_t)a.c.H_kv * paged_blocks(q, 0);
+    return (int64_t)a.c.H_kv * paged_units_before(q, q.n_tiles);
+}
+
 // A place on the line; seq = batch: its end.
 struct PagedPlace { int seq, head, tile, blk; };
 
@@ -98,11 +104,16 @@ struct PagedPlace { int seq, head, tile, blk; };
 // read the same long K/V do it in step (see launch_paged_attn).
 __host__ __device__ inline PagedPlace paged_place(const PagedAttnArgs& a, int s, int64_t u, int64_t snap_keys) {
     const PagedSeq q = paged_seq(a, s);
-    const int64_t per_head = paged_units_before(q, q.n_tiles);
+    const int64_t per_head = q.n_tiles == 1 ? paged_blocks(q, 0) : paged_units_before(q, q.n_tiles);
     PagedPlace p;
     p.seq = s;
-    p.head = (int)(u / per_head);
+    p.head = (u >> 31) == 0 && (per_head >> 31) == 0 ? (int)((uint32_t)u / (uint32_t)per_head) : (int)(u / per_head);
     u -= p.head * per_head;
+    if (q.n_tiles == 1) {
+        p.tile = 0;
+        p.blk = (int)u;
+        return p;
+    }
     int lo = 0, hi = q.n_tiles;  // units_before(lo) <= u < units_before(hi)
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
@@ -210,7 +221,7 @@ template <bool F8>
 __global__ void __launch_bounds__(paged_threads(F8), 1)
 paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_q1,
                      const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
-                     const PagedAttnArgs a, int box_keys, int64_t snap_keys, int* status) {
+                     const PagedAttnArgs a, int box_keys, int64_t snap_keys, double inv_grid, int* status) {
     constexpr uint32_t TILE = F8 ? kPagedKeys * 128 : kPagedKeys * 256;  // bytes of a K or V tile in the cache
     extern __shared__ __align__(1024) uint8_t paged_smem[];  // (no room to round the base up)
     PagedSmem& sm = *reinterpret_cast<PagedSmem*>(paged_smem);
@@ -242,48 +253,56 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     }
     if (warp == 10) tmem_alloc(&sm.tmem_base, 512);
 
-    // ---- this CTA's stretch: units of all sequences summed up, the boundaries looked up
+    // ---- this CTA's stretch: units of all sequences summed up, the boundaries looked up.  (A third of a short call's
+    // time once: no 64-bit divisions where the numbers are small, warps without sequences stay out, the two places are
+    // worked out side by side.)
     {
         const int per = (a.c.batch + blockDim.x - 1) / blockDim.x;
         const int s_lo = min((int)threadIdx.x * per, a.c.batch), s_hi = min(s_lo + per, a.c.batch);
-        int64_t mine = 0;
-        for (int s = s_lo; s < s_hi; ++s) {
-            const PagedSeq q = paged_seq(a, s);
-            mine += (int64_t)a.c.H_kv * paged_units_before(q, q.n_tiles);
-            if (blockIdx.x == 0 && (a.c.kv_lens[s] < 0 || a.c.kv_lens[s] > paged_cap(a.c)))
-                report_async(status, kAsyncBadIndex, 0x601);
-        }
-        int64_t upto = mine;
+        const int busy = (a.c.batch + 32 * per - 1) / max(32 * per, 1);  // warps that have sequences
+        int64_t mine = 0, upto = 0;
+        if (warp < busy) {
+            for (int s = s_lo; s < s_hi; ++s) {
+                mine += paged_units(a, paged_seq(a, s));
+                if (blockIdx.x == 0 && (a.c.kv_lens[s] < 0 || a.c.kv_lens[s] > paged_cap(a.c)))
+                    report_async(status, kAsyncBadIndex, 0x601);
+            }
+            upto = mine;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int64_t below = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += below;
+            for (int o = 1; o < 32; o <<= 1) {
+                const int64_t below = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += below;
+            }
+            if (lane == 31) sm.scan[warp] = upto;
         }
-        if (lane == 31) sm.scan[warp] = upto;
         __syncthreads();
-        int64_t total = 0;
-        for (int w = 0; w < (int)blockDim.x / 32; ++w) {
-            if (w < warp) upto += sm.scan[w];
-            total += sm.scan[w];
-        }
-        for (int e = 0; e < 2; ++e) {
-            const int64_t target = total / gridDim.x * (blockIdx.x + e) + total % gridDim.x * (blockIdx.x + e) / gridDim.x;
-            if (target >= upto - mine && target < upto) {  // (one thread, unless target = total)
-                int64_t before = upto - mine;
-                for (int s = s_lo; s < s_hi; ++s) {
-                    const PagedSeq q = paged_seq(a, s);
-                    const int64_t u = (int64_t)a.c.H_kv * paged_units_before(q, q.n_tiles);
-                    if (target < before + u) {
-                        sm.place[e] = paged_place(a, s, target - before, snap_keys);
-                        break;
+        if (warp < busy) {
+            int64_t total = 0;
+            for (int w = 0; w < busy; ++w) {
+                if (w < warp) upto += sm.scan[w];
+                total += sm.scan[w];
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                // (the same rounding in every CTA, not decreasing; the last one is the end whatever it says)
+                const int64_t target = (int64_t)((double)total * (double)(blockIdx.x + e) * inv_grid);
+                if (blockIdx.x + e < gridDim.x && target >= upto - mine && target < upto) {  // (one thread)
+                    int64_t before = upto - mine;
+                    int s = s_lo;
+                    for (; s < s_hi - 1; ++s) {
+                        const int64_t u = paged_units(a, paged_seq(a, s));
+                        if (target < before + u) break;
+                        before += u;
                     }
-                    before += u;
+                    sm.targets[e] = target - before;
+                    sm.place[e].seq = s;
                 }
-                sm.targets[e] = target;
             }
         }
         __syncthreads();
-        if (threadIdx.x < 2 && sm.targets[threadIdx.x] < 0) sm.place[threadIdx.x] = PagedPlace{a.c.batch, 0, 0, 0};
+        if (lane == 0 && warp < 2)
+            sm.place[warp] = sm.targets[warp] < 0 ? PagedPlace{a.c.batch, 0, 0, 0}
+                                                  : paged_place(a, sm.place[warp].seq, sm.targets[warp], snap_keys);
     }
     tc_fence_before();
     __syncthreads();
@@ -311,14 +330,15 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         if (const long long late = g_debug_producer_delay; late > 0) spin_cycles(late);  // tests only
         // coordinate of this lane's box of key tile b: its page's row, or outside the pool
         auto place_of = [&](int b) {
-            const int64_t key = (int64_t)b * kPagedKeys + lane * box_keys;
-            if (lane >= boxes || key >= it.kv) return nowhere;
-            const int page = a.c.table[(int64_t)it.seq * a.c.max_pages + key / a.c.page_size];
+            const uint32_t key = (uint32_t)b * kPagedKeys + lane * box_keys, size = a.c.page_size;  // (below 2^31 + 128)
+            if (lane >= boxes || key >= (uint32_t)it.kv) return nowhere;
+            const uint32_t slot = key / size;
+            const int page = a.c.table[(int64_t)it.seq * a.c.max_pages + slot];
             if (page < 0 || page >= a.c.n_pages) {
                 report_async(status, kAsyncBadIndex, 0x602);
                 return nowhere;
             }
-            const int row = page * a.c.page_size + (int)(key % a.c.page_size);
+            const int row = page * a.c.page_size + (int)(key - slot * size);
             return F8 ? row : row / 8;
         };
         while (ok && walk.next(a, it)) {
@@ -771,6 +791,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
 __global__ void __launch_bounds__(128)
 paged_combine_kernel(const PagedAttnArgs a, int n_ctas) {
     const int c0 = blockIdx.x;
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // launched early: what the attention kernel wrote is there after this
     const int4 e = a.ends[c0 * 2];
     if (e.y == 0) return;
     const int head = a.ends[c0 * 2 + 1].x, tokens = e.w, lane = threadIdx.x & 31;
