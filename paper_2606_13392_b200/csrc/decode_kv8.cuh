@@ -28,19 +28,6 @@ struct DecKv8Smem {
     int abort;
 };
 
-// 16-byte chunk `chunk` (0..7: d = 16 chunk .. 16 chunk + 15) of key row `key` inside a swizzled fp8 tile.
-__device__ __forceinline__ uint32_t dec_kv8_addr(uint32_t tile_base, int key, int chunk) {
-    return tile_base + (uint32_t)(key * 128 + ((chunk ^ (key & 7)) << 4));
-}
-
-__device__ __forceinline__ void mma_m16n8k16_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
-                                                 uint32_t b0, uint32_t b1) {
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-
 // Two bf16 (lower half first) -> two f16, round to nearest.
 __device__ __forceinline__ uint32_t bf16x2_to_f16x2(uint32_t two) {
     const float2 f = bf16x2_to_float2(two);

@@ -6,6 +6,7 @@
 
 #include "norm_rope.cuh"
 #include "paged_attn.cuh"
+#include "paged_few8.cuh"
 #include "tc_common.cuh"
 
 namespace msa {
@@ -142,10 +143,11 @@ static msa_status_t resolve_cache(const msa_paged_cache_t* c, int64_t n_tokens, 
 // Workspace: the CTAs' ends, then the partials.
 struct PagedWorkspace { size_t ends, ml, o, bytes; };
 static PagedWorkspace paged_workspace() {
-    const size_t n = sm_count(), rows = 2 * n * kPagedSlotRows;
+    const size_t n = sm_count(), rows = 2 * n * kPagedSlotRows;  // (more than the small tiles of kFewCtas * n CTAs take)
+    static_assert(kFewCtas * kFewRows <= kPagedSlotRows, "workspace");
     PagedWorkspace w;
     w.ends = 0;
-    w.ml = (n * 32 + 255) / 256 * 256;
+    w.ml = (kFewCtas * n * sizeof(PagedEnds) + 255) / 256 * 256;
     w.o = w.ml + rows * sizeof(float2);
     w.bytes = w.o + rows * 128 * sizeof(float);
     return w;
@@ -160,11 +162,64 @@ static bool paged_tc_ok(const msa_paged_cache_t& c, int G) {
            (int64_t)c.n_pages * c.page_size < 2147483647LL - 128;
 }
 
+// Merges the tiles that the boundaries between `ctas` CTAs cut.
+static msa_status_t launch_paged_combine(const PagedAttnArgs& a, int ctas, cudaStream_t st) {
+    // a cut tile has at most slot_rows rows: up to 16 CTAs of four rows at a time, as far as the call has rows
+    const int64_t most = std::min<int64_t>(a.slot_rows, (int64_t)a.n_tokens * a.G);
+    // (the launch overlaps the attention kernel's end; the kernel waits there before it reads)
+    cudaLaunchAttribute early;
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(ctas, (unsigned)std::min<int64_t>(16, ceil_div64(most, 4)));
+    cfg.blockDim = dim3(128);
+    cfg.stream = st;
+    cfg.attrs = &early;
+    cfg.numAttrs = 1;
+    StageScope sc(kStageNone, st);
+    return cudaLaunchKernelEx(&cfg, paged_combine_kernel, a, ctas) == cudaSuccess ? MSA_OK : MSA_ERR_CUDA;
+}
+
+// Calls of a token or so per sequence on fp8 caches, groups of at most 16: see paged_few8.cuh.  (The rule goes by what the
+// host knows; a longer sequence among the others is right all the same, in tiles of its own.)
+static bool paged_few8_ok(const PagedAttnArgs& a, const msa_paged_cache_t& c) {
+    return c.fp8 == 1 && a.G <= kFewRows && a.n_tokens <= c.batch;
+}
+
+template <int HG>
+static msa_status_t launch_paged_few8(PagedAttnArgs a, const msa_paged_cache_t& c, const void* q, cudaStream_t st) {
+    a.TPT = a.tile_tokens = HG * 8 / a.G;
+    a.slot_rows = kFewRows;
+    CUtensorMap tm_k, tm_v;
+    const uint64_t H = (uint64_t)a.c.H_kv, rows = (uint64_t)c.n_pages * c.page_size;
+    const int box = common_divisor(c.page_size, kPagedKeys);
+    const uint64_t kd[3] = {64, H, rows}, ks[2] = {128, H * 128};  // (128 bytes of a key as 64 two-byte elements)
+    const uint32_t kb[3] = {64, 1, (uint32_t)box};
+    int* status = status_word();
+    if (!encode_tmap_bf16(&tm_k, c.k, 3, kd, ks, kb, true) || !encode_tmap_bf16(&tm_v, c.v, 3, kd, ks, kb, true) || status == nullptr)
+        return MSA_ERR_CUDA;
+    const size_t smem = sizeof(FewSmem<HG>);
+    static_assert(sizeof(FewSmem<HG>) <= 113 * 1024, "two CTAs per SM");
+    static bool attr_set[64] = {false};  // per device
+    const int dev = current_device(), grid = kFewCtas * sm_count();
+    if (!attr_set[dev]) {
+        if (cudaFuncSetAttribute(paged_few8_kernel<HG>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+            return MSA_ERR_CUDA;
+        attr_set[dev] = true;
+    }
+    {
+        StageScope sc(kStageNone, st);
+        paged_few8_kernel<HG><<<grid, kFewThreads, smem, st>>>(tm_k, tm_v, a, (const __nv_bfloat16*)q, box, 1.0 / grid, status);
+    }
+    if (cudaPeekAtLastError() != cudaSuccess) return MSA_ERR_CUDA;
+    return launch_paged_combine(a, grid, st);
+}
+
 template <bool F8>
 static msa_status_t launch_paged_attn(const PagedAttnArgs& a, const msa_paged_cache_t& c, const void* q, cudaStream_t st) {
     CUtensorMap tm_q, tm_q1, tm_k, tm_v;
     const uint64_t H_q = (uint64_t)a.c.H_kv * a.G, H = (uint64_t)a.c.H_kv, rows = (uint64_t)c.n_pages * c.page_size;
-    const int box = common_divisor(c.page_size, kPagedKeys);
+    const int box = std::min(common_divisor(c.page_size, kPagedKeys), F8 ? 32 : kPagedKeys);  // keys of a copy
     const uint64_t qd[3] = {128, H_q, (uint64_t)a.n_tokens}, qs[2] = {256, H_q * 256};
     const uint32_t qb[3] = {64, (uint32_t)a.G, (uint32_t)a.TPT}, qb1[3] = {64, (uint32_t)a.G, 1};
     bool ok = encode_tmap_bf16(&tm_q, q, 3, qd, qs, qb) && encode_tmap_bf16(&tm_q1, q, 3, qd, qs, qb1);
@@ -194,22 +249,7 @@ static msa_status_t launch_paged_attn(const PagedAttnArgs& a, const msa_paged_ca
         paged_attn_tc_kernel<F8><<<grid, paged_threads(F8), smem, st>>>(tm_q, tm_q1, tm_k, tm_v, a, box, snap, 1.0 / grid, status);
     }
     if (cudaPeekAtLastError() != cudaSuccess) return MSA_ERR_CUDA;
-    {   // a cut tile has at most 256 rows: up to 16 CTAs of four rows at a time, as far as the call has rows
-        const int64_t most = std::min<int64_t>(kPagedSlotRows, (int64_t)a.n_tokens * a.G);
-        // (its launch overlaps the attention kernel's end; it waits there before it reads)
-        cudaLaunchAttribute early;
-        early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        early.val.programmaticStreamSerializationAllowed = 1;
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3(grid, (unsigned)std::min<int64_t>(16, ceil_div64(most, 4)));
-        cfg.blockDim = dim3(128);
-        cfg.stream = st;
-        cfg.attrs = &early;
-        cfg.numAttrs = 1;
-        StageScope sc(kStageNone, st);
-        if (cudaLaunchKernelEx(&cfg, paged_combine_kernel, a, grid) != cudaSuccess) return MSA_ERR_CUDA;
-    }
-    return launch_status();
+    return launch_paged_combine(a, grid, st);
 }
 
 }  // namespace msa
@@ -375,9 +415,12 @@ msa_status_t msa_paged_attn(const msa_paged_cache_t* cache, const void* q, int32
         if (workspace == nullptr || !aligned_to(workspace, 256)) return MSA_ERR_INVALID_ARG;
         if (workspace_bytes < w.bytes) return MSA_ERR_WORKSPACE;
         a.TPT = 128 / a.G;
+        a.tile_tokens = 2 * a.TPT;
+        a.slot_rows = kPagedSlotRows;
         a.ends = (int4*)((char*)workspace + w.ends);
         a.part_ml = (float2*)((char*)workspace + w.ml);
         a.part_o = (float*)((char*)workspace + w.o);
+        if (paged_few8_ok(a, *cache)) return a.G <= 8 ? launch_paged_few8<1>(a, *cache, q, st) : launch_paged_few8<2>(a, *cache, q, st);
         return cache->fp8 ? launch_paged_attn<true>(a, *cache, q, st) : launch_paged_attn<false>(a, *cache, q, st);
     }
     const int64_t grid = ceil_div64(n_tokens * n_q_heads, 4);

@@ -23,13 +23,15 @@ constexpr int kPagedSlotRows = 256;                  // rows of a partial: two c
 struct PagedAttnArgs {
     PagedView c;
     int G, TPT;          // query heads per KV head; tokens per context
+    int tile_tokens;     // tokens of a query tile of a sequence with more than TPT: two contexts, or one
+    int slot_rows;       // rows of a partial
     int n_tokens;
     float scale_log2e;
     __nv_bfloat16* out;  // [n_tokens, H_kv*G, 128]
     float* lse;          // [n_tokens, H_kv*G] or null
     // partials: CTA i owns slots 2i (a tile begun by an earlier CTA) and 2i+1 (a tile that a later one ends)
-    float* part_o;       // [slot][kPagedSlotRows][128], not normalised
-    float2* part_ml;     // [slot][kPagedSlotRows] reference maximum (log2 units) and sum
+    float* part_o;       // [slot][slot_rows][128], not normalised
+    float2* part_ml;     // [slot][slot_rows] reference maximum (log2 units) and sum
     int4* ends;          // [CTA][2]: see PagedEnds
 };
 
@@ -52,7 +54,7 @@ __host__ __device__ __forceinline__ PagedSeq paged_seq(const PagedAttnArgs& a, i
     q.q_len = max(hi - lo, 0);
     q.kv = (int)min((int64_t)max(a.c.kv_lens[s], 0), paged_cap(a.c));
     q.base = q.kv - q.q_len;  // position of the first new token
-    q.tile_tokens = q.q_len <= a.TPT ? a.TPT : 2 * a.TPT;
+    q.tile_tokens = q.q_len <= a.TPT ? a.TPT : a.tile_tokens;
     q.n_tiles = (q.q_len + q.tile_tokens - 1) / q.tile_tokens;
     return q;
 }
@@ -176,6 +178,65 @@ struct PagedWalk {
     }
 };
 
+// This CTA's stretch of the line into p.place: units of all sequences summed up, the boundaries looked up.  All threads
+// call it; places are there after the caller's next __syncthreads.  (A third of a short call's time once: no 64-bit
+// divisions where the numbers are small, warps without sequences stay out, the two places are worked out side by side.)
+struct PagedPlan {
+    int64_t scan[16], targets[2];
+    PagedPlace place[2];
+};
+
+__device__ inline void paged_stretch(const PagedAttnArgs& a, PagedPlan& p, int64_t snap_keys, double inv_grid, int* status) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) p.targets[0] = p.targets[1] = -1;
+    const int per = (a.c.batch + blockDim.x - 1) / blockDim.x;
+    const int s_lo = min((int)threadIdx.x * per, a.c.batch), s_hi = min(s_lo + per, a.c.batch);
+    const int busy = (a.c.batch + 32 * per - 1) / max(32 * per, 1);  // warps that have sequences
+    int64_t mine = 0, upto = 0;
+    if (warp < busy) {
+        for (int s = s_lo; s < s_hi; ++s) {
+            mine += paged_units(a, paged_seq(a, s));
+            if (blockIdx.x == 0 && (a.c.kv_lens[s] < 0 || a.c.kv_lens[s] > paged_cap(a.c)))
+                report_async(status, kAsyncBadIndex, 0x601);
+        }
+        upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t below = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += below;
+        }
+        if (lane == 31) p.scan[warp] = upto;
+    }
+    __syncthreads();
+    if (warp < busy) {
+        int64_t total = 0;
+        for (int w = 0; w < busy; ++w) {
+            if (w < warp) upto += p.scan[w];
+            total += p.scan[w];
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            // (the same rounding in every CTA, not decreasing; the last one is the end whatever it says)
+            const int64_t target = (int64_t)((double)total * (double)(blockIdx.x + e) * inv_grid);
+            if (blockIdx.x + e < gridDim.x && target >= upto - mine && target < upto) {  // (one thread)
+                int64_t before = upto - mine;
+                int s = s_lo;
+                for (; s < s_hi - 1; ++s) {
+                    const int64_t u = paged_units(a, paged_seq(a, s));
+                    if (target < before + u) break;
+                    before += u;
+                }
+                p.targets[e] = target - before;
+                p.place[e].seq = s;
+            }
+        }
+    }
+    __syncthreads();
+    if (lane == 0 && warp < 2)
+        p.place[warp] = p.targets[warp] < 0 ? PagedPlace{a.c.batch, 0, 0, 0}
+                                              : paged_place(a, p.place[warp].seq, p.targets[warp], snap_keys);
+}
+
 // ---------------------------------------------------------------- the kernel
 struct PagedSmem {
     alignas(1024) uint8_t q[2][128 * 256];  // [context][d half][row][64 bf16]
@@ -188,8 +249,7 @@ struct PagedSmem {
     uint64_t v_full[kPagedVStages], v_empty[kPagedVStages], v_land[kPagedVStages];
     uint64_t s_full[2], p_full[2][2], o_full[2], o_empty[2];  // [context], P: [half]
     uint64_t v_tail, ml_full, ml_empty, drain;
-    int64_t scan[16], targets[2];
-    PagedPlace place[2];
+    PagedPlan plan;
     uint32_t tmem_base;
     int abort;
 };
@@ -199,20 +259,6 @@ constexpr int paged_threads(bool f8) { return f8 ? 512 : 384; }
 __device__ __forceinline__ uint32_t pack2_f16(float a, float b) {
     const __half2 v = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&v);
-}
-
-// Barrier among the four widening warps only; true if `mine` is in all threads.
-__device__ __forceinline__ bool conv_agree(bool mine) {
-    uint32_t all;
-    asm volatile(
-        "{\n\t.reg .pred p, r;\n\t"
-        "setp.ne.u32 p, %1, 0;\n\t"
-        "barrier.cta.red.and.pred r, 1, 128, p;\n\t"
-        "selp.u32 %0, 1, 0, r;\n\t}"
-        : "=r"(all)
-        : "r"((uint32_t)mine)
-        : "memory");
-    return all != 0;
 }
 
 // Warps: 0-3 / 4-7 softmax of context 0 / 1 (thread = row), 8 loads K, 9 loads V, 10 issues the MMAs, 11 loads Q,
@@ -246,64 +292,13 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         }
         mbar_init(&sm.v_tail, 1); mbar_init(&sm.ml_full, 4); mbar_init(&sm.ml_empty, 4); mbar_init(&sm.drain, 1);
         sm.abort = 0;
-        sm.targets[0] = sm.targets[1] = -1;
         fence_mbar_init();
         tma_prefetch_desc(&tm_q); tma_prefetch_desc(&tm_q1);
         tma_prefetch_desc(&tm_k); tma_prefetch_desc(&tm_v);
     }
     if (warp == 10) tmem_alloc(&sm.tmem_base, 512);
 
-    // ---- this CTA's stretch: units of all sequences summed up, the boundaries looked up.  (A third of a short call's
-    // time once: no 64-bit divisions where the numbers are small, warps without sequences stay out, the two places are
-    // worked out side by side.)
-    {
-        const int per = (a.c.batch + blockDim.x - 1) / blockDim.x;
-        const int s_lo = min((int)threadIdx.x * per, a.c.batch), s_hi = min(s_lo + per, a.c.batch);
-        const int busy = (a.c.batch + 32 * per - 1) / max(32 * per, 1);  // warps that have sequences
-        int64_t mine = 0, upto = 0;
-        if (warp < busy) {
-            for (int s = s_lo; s < s_hi; ++s) {
-                mine += paged_units(a, paged_seq(a, s));
-                if (blockIdx.x == 0 && (a.c.kv_lens[s] < 0 || a.c.kv_lens[s] > paged_cap(a.c)))
-                    report_async(status, kAsyncBadIndex, 0x601);
-            }
-            upto = mine;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int64_t below = __shfl_up_sync(0xffffffffu, upto, o);
-                if (lane >= o) upto += below;
-            }
-            if (lane == 31) sm.scan[warp] = upto;
-        }
-        __syncthreads();
-        if (warp < busy) {
-            int64_t total = 0;
-            for (int w = 0; w < busy; ++w) {
-                if (w < warp) upto += sm.scan[w];
-                total += sm.scan[w];
-            }
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                // (the same rounding in every CTA, not decreasing; the last one is the end whatever it says)
-                const int64_t target = (int64_t)((double)total * (double)(blockIdx.x + e) * inv_grid);
-                if (blockIdx.x + e < gridDim.x && target >= upto - mine && target < upto) {  // (one thread)
-                    int64_t before = upto - mine;
-                    int s = s_lo;
-                    for (; s < s_hi - 1; ++s) {
-                        const int64_t u = paged_units(a, paged_seq(a, s));
-                        if (target < before + u) break;
-                        before += u;
-                    }
-                    sm.targets[e] = target - before;
-                    sm.place[e].seq = s;
-                }
-            }
-        }
-        __syncthreads();
-        if (lane == 0 && warp < 2)
-            sm.place[warp] = sm.targets[warp] < 0 ? PagedPlace{a.c.batch, 0, 0, 0}
-                                                  : paged_place(a, sm.place[warp].seq, sm.targets[warp], snap_keys);
-    }
+    paged_stretch(a, sm.plan, snap_keys, inv_grid, status);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -312,7 +307,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     // block was launched with: 384 x 168 >= 256 x 192 + 128 x 120, 512 x 128 >= 256 x 176 + 2 x 128 x 80.
     // (Set at the head of each role: where roles share code the smallest share would rule.)
     constexpr int kRegsSoftmax = F8 ? 176 : 192, kRegsIssue = F8 ? 80 : 120, kRegsWiden = 80;
-    PagedWalk walk(sm.place[0], sm.place[1]);
+    PagedWalk walk(sm.plan.place[0], sm.plan.place[1]);
     PagedItem it{};
 
     if (warp >= 8 && warp < 12) {
@@ -364,7 +359,8 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 if (lane == 0) mbar_arrive_expect_tx(bar, TILE);
                 __syncwarp();
                 if (lane < boxes) {
-                    if constexpr (F8) tma_load_3d(dst + TILE + lane * box_keys * 128, tm, 0, it.head, where, bar);
+                    // (fp8: 32 keys into the upper half of the 8 KB of their fp16)
+                    if constexpr (F8) tma_load_3d(dst + (lane * box_keys >> 5) * 8192 + 4096 + (lane * box_keys & 31) * 128, tm, 0, it.head, where, bar);
                     else tma_load_5d(dst + lane * box_keys * 256, tm, 0, 0, 0, it.head, where, bar);
                 }
                 if (tail) {
@@ -519,51 +515,65 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     }
     } else if (warp >= 12) {
         // ---------------- widening (fp8): K and V become fp16, which holds every E4M3 value and takes one conversion
-        // for two elements (bf16 takes four operations).  A tile lands in the upper half of its stage (row = key, 128
-        // bytes, chunks swizzled by key mod 8); all threads have read their row before any writes the fp16 tile over it.
+        // for two elements (bf16 takes four operations).  Warp w widens keys 32w .. 32w+31 of every tile: their 4 KB (row =
+        // key, 128 bytes, chunks swizzled by key mod 8) land in the upper half of the 8 KB that their fp16 will fill, so
+        // that a warp overwrites only what it has read itself.  The fence that shows a tile to the MMAs waits for the
+        // warp's stores, hundreds of cycles; it comes behind the next tile's loads unless that tile is late.
         // Q becomes fp16 as well, with a power of two taken out of each row so that any bf16 row fits: what is rounded
         // off is below 2^-38 of the row's largest element.  The softmax warps put it back into the scale.
         if constexpr (F8) {
             reg_release<kRegsWiden>();
-            const int key = threadIdx.x - 384, sw = key & 7;
+            const int w = warp - 12, key = w * 32 + lane, sw = lane & 7;
+            const uint32_t from = w * 8192 + 4096 + lane * 128, into = w * 8192 + (lane >> 3) * 2048 + sw * 128;
             uint32_t t = 0, n_q[2] = {0, 0}, item = 0;
+            uint64_t* written = nullptr;  // the barrier of the tile that is written and not yet shown
+            auto show = [&]() {
+                if (written == nullptr) return;
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(written);
+                written = nullptr;
+            };
             bool ok = true;
             while (ok && walk.next(a, it)) {
                 for (int b = it.lo; ok && b < it.hi; ++b, ++t) {
                     for (int kv = 0; kv < 2; ++kv) {
                         const uint32_t stages = kv == 0 ? kPagedKStages : kPagedVStages, st = t % stages;
                         uint8_t* tile = kv == 0 ? sm.k[st] : sm.v[st];
-                        const bool landed = mbar_wait(kv == 0 ? &sm.k_land[st] : &sm.v_land[st], (t / stages) & 1, abort);
+                        uint64_t* land = kv == 0 ? &sm.k_land[st] : &sm.v_land[st];
+                        if (!__all_sync(0xffffffffu, mbar_try_wait(land, (t / stages) & 1))) {
+                            show();  // (what has to be seen for this tile to come)
+                            if (!mbar_wait(land, (t / stages) & 1, abort)) {
+                                if (lane == 0) report_async(status, kAsyncTimeout, 0x641);
+                                ok = false;
+                                break;
+                            }
+                        }
                         // (rows behind the end may hold anything, and 0 * NaN is NaN: V's become zeros)
-                        const bool inside = landed && (kv == 0 || (int64_t)b * kPagedKeys + key < it.kv);
+                        const bool inside = kv == 0 || (int64_t)b * kPagedKeys + key < it.kv;
                         uint4 x[8];
 #pragma unroll
                         for (int c = 0; c < 8; ++c) {
                             x[c] = make_uint4(0u, 0u, 0u, 0u);
-                            if (inside) x[c] = *reinterpret_cast<const uint4*>(tile + TILE + key * 128 + ((c ^ sw) << 4));
+                            if (inside) x[c] = *reinterpret_cast<const uint4*>(tile + from + ((c ^ sw) << 4));
                         }
-                        if (!conv_agree(landed)) {  // (a wait may run out in one warp and not in another: all go on or none)
-                            if (lane == 0) report_async(status, kAsyncTimeout, 0x641);
-                            ok = false;
-                            break;
-                        }
-                        uint8_t* row = tile + (key >> 3) * 2048 + sw * 128;
+                        show();
+                        __syncwarp();  // (every lane has read its row)
 #pragma unroll
                         for (int c = 0; c < 8; ++c) {
                             uint4 lo, hi;
                             e4m3x4_to_f16x2x2(x[c].x, lo.x, lo.y); e4m3x4_to_f16x2x2(x[c].y, lo.z, lo.w);
                             e4m3x4_to_f16x2x2(x[c].z, hi.x, hi.y); e4m3x4_to_f16x2x2(x[c].w, hi.z, hi.w);
                             const int cc = 2 * (c & 3);
-                            uint8_t* to = row + (c >> 2) * 1024;
+                            uint8_t* to = tile + into + (c >> 2) * 1024;
                             *reinterpret_cast<uint4*>(to + ((cc ^ sw) << 4)) = lo;
                             *reinterpret_cast<uint4*>(to + (((cc + 1) ^ sw) << 4)) = hi;
                         }
-                        fence_proxy_async_smem();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(kv == 0 ? &sm.k_full[st] : &sm.v_full[st]);
+                        written = kv == 0 ? &sm.k_full[st] : &sm.v_full[st];
                     }
                     for (int j = 0; ok && b == it.lo && j < (it.dual() ? 1 : 2); ++j) {  // Q, behind the first tile
-                        if (!conv_agree(mbar_wait(&sm.q_land[j], n_q[j]++ & 1, abort))) {
+                        show();
+                        if (!mbar_wait(&sm.q_land[j], n_q[j]++ & 1, abort)) {
                             if (lane == 0) report_async(status, kAsyncTimeout, 0x642);
                             ok = false;
                             break;
@@ -583,20 +593,17 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
 #pragma unroll
                         for (int c = 0; c < 16; ++c) {
                             uint4* at = reinterpret_cast<uint4*>(row + (c >> 3) * 16384 + (((c & 7) ^ sw) << 4));
-                            float y[8];
-                            unpack8(*at, y);
-                            uint32_t o[4];
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) o[i] = pack2_f16(y[2 * i] * f, y[2 * i + 1] * f);
-                            *at = make_uint4(o[0], o[1], o[2], o[3]);
+                            const F8v y = widen8(*at);
+                            *at = make_uint4(pack2_f16(y.v[0].x * f, y.v[0].y * f), pack2_f16(y.v[1].x * f, y.v[1].y * f),
+                                             pack2_f16(y.v[2].x * f, y.v[2].y * f), pack2_f16(y.v[3].x * f, y.v[3].y * f));
                         }
-                        fence_proxy_async_smem();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&sm.q_full[j]);
+                        written = &sm.q_full[j];
+                        show();
                     }
                 }
                 ++item;
             }
+            show();
         }
     } else {
         reg_acquire<kRegsSoftmax>();
@@ -727,7 +734,7 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             if (warp_on) {
                 const bool partial = it.partial();
                 const int64_t out_row = ((int64_t)it.q_row + first + tok) * H_q + it.head * a.G + g;
-                const int64_t slot_row = ((int64_t)blockIdx.x * 2 + (it.lo > 0 ? 0 : 1)) * kPagedSlotRows + (first > 0 ? 128 : 0) + row;
+                const int64_t slot_row = ((int64_t)blockIdx.x * 2 + (it.lo > 0 ? 0 : 1)) * a.slot_rows + (first > 0 ? 128 : 0) + row;
                 if (!partial) {
                     const float inv = l == 0.f ? 0.f : 1.f / l;  // (a row that sees nothing is zero)
                     w0 *= inv; w1 *= inv;
@@ -818,12 +825,12 @@ paged_combine_kernel(const PagedAttnArgs a, int n_ctas) {
         const int tok = r / a.G, g = r - tok * a.G;
         const int in_slot = tok < a.TPT ? r : 128 + (tok - a.TPT) * a.G + g;
         float M = -INFINITY;
-        for (int p = lane; p < n; p += 32) M = fmaxf(M, a.part_ml[(int64_t)s_slot[p] * kPagedSlotRows + in_slot].x);
+        for (int p = lane; p < n; p += 32) M = fmaxf(M, a.part_ml[(int64_t)s_slot[p] * a.slot_rows + in_slot].x);
         M = warp_max(M);
         float L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
         for (int p = 0; p < n; ++p) {
-            const int64_t at = (int64_t)s_slot[p] * kPagedSlotRows + in_slot;
+            const int64_t at = (int64_t)s_slot[p] * a.slot_rows + in_slot;
             const float2 ml = a.part_ml[at];
             const float4 x = *reinterpret_cast<const float4*>(a.part_o + at * 128 + lane * 4);
             const float w = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - M);

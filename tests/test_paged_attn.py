@@ -103,6 +103,13 @@ CASES = [  # lens (new, old), page, query heads per KV head, KV heads, d, fp8
     ([(1, 5000), (1, 3), (1, 0), (1, 777), (1, 12345)], 64, 8, 4, 128, False),
     ([(1, 5000), (1, 3), (1, 0), (1, 777), (1, 12345)], 128, 16, 4, 128, True),
     ([(1, 300 + 7 * i) for i in range(70)], 32, 16, 2, 128, False),
+    ([(1, 300 + 7 * i) for i in range(70)], 32, 16, 2, 128, True),
+    ([(1, 2046)], 64, 8, 8, 128, True),
+    ([(1, 9000), (1, 0), (0, 70), (1, 127)], 16, 1, 2, 128, True),
+    ([(1, 500), (1, 129), (1, 128)], 48, 5, 3, 128, True),
+    ([(1, 500), (1, 129), (1, 4000)], 256, 12, 2, 128, True),
+    ([(3, 40), (0, 9), (2, 700), (0, 0), (0, 3)], 24, 4, 2, 128, True),   # no more tokens than sequences, not one each
+    ([(5, 300)] + [(0, 4)] * 4, 64, 16, 1, 128, True),
     ([(3, 40), (0, 9), (7, 1000), (16, 0), (1, 64), (0, 0), (17, 512)], 16, 8, 2, 128, False),
     ([(3, 40), (0, 9), (7, 1000), (16, 0), (1, 64), (0, 0), (17, 512)], 48, 8, 2, 128, True),
     ([(32, 0)], 64, 8, 1, 128, False),                                 # both contexts full
@@ -196,19 +203,21 @@ def test_growing_maxima_and_large_scores():
 @pytest.mark.parametrize("fp8", [False, True])
 def test_queries_of_any_size(fp8):
     # rows of one tile that are powers of two apart, beyond what fp16 holds (fp8 caches multiply in fp16)
-    cache = make([(3, 900), (60, 300)], 16, 2, 128, fp8)
-    q = queries(63, 16, 128)
-    size = torch.tensor([2.0 ** e for e in (-140, -100, -40, -17, 0, 12, 17, 30)], device=DEV).repeat(63 * 2).view(63, 16, 1)
-    q = (q.float() * size).bfloat16()
-    for scale in (2.0 ** -21, 2.0 ** -34):
-        out, lse = api.paged_attn(cache, q, scale)
-        check(cache, q, out, lse, scale)
+    for lens in ([(3, 900), (60, 300)], [(1, 900), (1, 300)]):
+        cache = make(lens, 16, 2, 128, fp8)
+        n = sum(x for x, _ in lens)
+        q = queries(n, 16, 128)
+        size = torch.tensor([2.0 ** e for e in (-140, -100, -40, -17, 0, 12, 17, 30)], device=DEV).repeat(n * 2).view(n, 16, 1)
+        q = (q.float() * size).bfloat16()
+        for scale in (2.0 ** -21, 2.0 ** -34):
+            out, lse = api.paged_attn(cache, q, scale)
+            check(cache, q, out, lse, scale)
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("lens", [[(1, 700), (1, 90)], [(70, 700), (1, 3000)]])
-def test_graphs_and_streams(lens):
-    cache = make(lens, 16, 2, 128, False)
+@pytest.mark.parametrize("lens,fp8", [([(1, 700), (1, 90)], False), ([(70, 700), (1, 3000)], False), ([(1, 700), (1, 90)], True)])
+def test_graphs_and_streams(lens, fp8):
+    cache = make(lens, 16, 2, 128, fp8)
     n = sum(x for x, _ in lens)
     q = queries(n, 16, 128)
     want = api.paged_attn(cache, q)
@@ -230,7 +239,7 @@ def test_graphs_and_streams(lens):
     want = api.paged_attn(cache, q)
     assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
     # two calls in flight on two streams have a workspace each
-    other = make(lens, 16, 2, 128, False, seed=9)
+    other = make(lens, 16, 2, 128, fp8, seed=9)
     with torch.cuda.stream(side):
         a = [api.paged_attn(other, q) for _ in range(5)]
     b = [api.paged_attn(cache, q) for _ in range(5)]
@@ -244,8 +253,8 @@ def test_graphs_and_streams(lens):
 def test_bad_pages_and_lengths_are_reported(d):
     # the kernels check a page against the pool before they form an address, and a length against the table; the other
     # sequences' results stay right
-    for change in ("page", "negative page", "length", "negative length"):
-        cache = make([(2, 500), (1, 300)], 16, 1, d, False)
+    for change, fp8 in [(c, f) for c in ("page", "negative page", "length", "negative length") for f in (False, True)]:
+        cache = make([(2, 500), (1, 300)] + [(0, 1)] * fp8, 16, 1, d, fp8)
         if change == "page":
             cache.page_table[0, 3] = cache.k.shape[0]
         elif change == "negative page":
@@ -257,7 +266,7 @@ def test_bad_pages_and_lengths_are_reported(d):
         q = queries(3, 8, d)
         out, lse = api.paged_attn(cache, q)
         assert B.check_async_status()[0] == 6, change
-        rest = api.PagedCache(cache.k, cache.v, cache.page_table[1:].contiguous(), cache.kv_lens[1:].clone(),
+        rest = api.PagedCache(cache.k, cache.v, cache.page_table[1:2].contiguous(), cache.kv_lens[1:2].clone(),
                               torch.tensor([0, 1], dtype=torch.int32, device=DEV))
         check(rest, q[2:], out[2:], lse[2:])
     assert B.check_async_status() == (0, 0)
@@ -277,9 +286,10 @@ def test_guard_bands():
 
 
 @pytest.mark.gpu
-def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_right():
-    cache = make([(40, 3000), (1, 900)], 16, 2, 128, False)
-    q = queries(41, 16, 128)
+@pytest.mark.parametrize("lens,fp8", [([(40, 3000), (1, 900)], False), ([(40, 3000), (1, 900)], True), ([(1, 3000), (1, 900)], True)])
+def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_right(lens, fp8):
+    cache = make(lens, 16, 2, 128, fp8)
+    q = queries(sum(n for n, _ in lens), 16, 128)
     try:
         B.msa_debug_set_wait(20000, 2000000)  # 10 us against a copy role that is 1 ms late
         api.paged_attn(cache, q)
