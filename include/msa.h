@@ -506,8 +506,10 @@ msa_status_t msa_paged_append(const msa_paged_cache_t* cache, const msa_rope_t* 
  * chunks: work is split evenly over the device and split tiles are merged in a fixed order, so equal
  * calls give equal bits.  Bad pages or lengths are reported as a bad index; the outputs of that
  * sequence are then unspecified.
- * head_dim = 128 with pages of a multiple of 8 tokens runs on the tensor cores (P is rounded to
- * bf16 before P V, as in Eq. 8's calls), other shapes on a generic kernel.
+ * head_dim = 128 with pages of a multiple of 8 tokens and groups of at most 128 heads runs on the
+ * tensor cores: P is rounded to bf16 before P V, as in Eq. 8's calls; on fp8 caches the products run
+ * in fp16 (K and V exact, any Q, P to 2^-11 of itself or 2^-35 of its row's largest).  Other shapes
+ * run on a generic kernel in fp32.
  * workspace (256-byte aligned) >= msa_paged_attn_workspace_bytes.  Of `cache`, that query reads the
  * sizes only.
  */

@@ -148,9 +148,6 @@ class PagedCache(NamedTuple):
 _NO_ROPE = Rope(None)
 
 
-def _empty(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
-    return None if t is None else torch.empty_like(t, memory_format=torch.contiguous_format)
-
 
 def _workspace(t: torch.Tensor, size, *args) -> torch.Tensor:
     """A workspace of size(*args) bytes on t's device (the size may depend on the device)."""
@@ -189,11 +186,8 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions
                  k_out: Optional[torch.Tensor] = None):
     """Norm of each head (where there is a weight) and position rotation of q and k [rows, heads, d], which may be
     slices of one projection; either may be None -> (q_out, k_out), dense."""
-    q_out = _empty(q) if q_out is None else q_out
-    k_out = _empty(k) if k_out is None else k_out
     freqs, interleaved, mscale = rope or _NO_ROPE
-    B.msa_qk_norm_rope(freqs, interleaved, mscale, q, q_weight, k, k_weight, eps, positions, q_out, k_out)
-    return q_out, k_out
+    return B.msa_qk_norm_rope(freqs, interleaved, mscale, q, q_weight, k, k_weight, eps, positions, q_out, k_out)
 
 
 def qk_norm_rope_backward(dq_out: Optional[torch.Tensor], dk_out: Optional[torch.Tensor], q: Optional[torch.Tensor],
@@ -204,15 +198,14 @@ def qk_norm_rope_backward(dq_out: Optional[torch.Tensor], dk_out: Optional[torch
     are fp32, None without a weight."""
     dy = dq_out if dq_out is not None else dk_out
     d = dy.shape[-1]
-    dq, dk = _empty(dq_out), _empty(dk_out)
     dwq = None if q_weight is None else dy.new_empty(d, dtype=torch.float32)
     dwk = None if k_weight is None else dy.new_empty(d, dtype=torch.float32)
     ws = None
     if dwq is not None or dwk is not None:
         ws = _workspace(dy, B.msa_qk_norm_rope_backward_workspace_bytes, d, dy.shape[0])
     freqs, interleaved, mscale = rope or _NO_ROPE
-    B.msa_qk_norm_rope_backward(freqs, interleaved, mscale, dq_out, dk_out, q, q_weight, k, k_weight, eps, positions, dq, dk,
-                                dwq, dwk, ws)
+    dq, dk = B.msa_qk_norm_rope_backward(freqs, interleaved, mscale, dq_out, dk_out, q, q_weight, k, k_weight, eps, positions,
+                                         None, None, dwq, dwk, ws)
     return dq, dk, dwq, dwk
 
 
@@ -222,20 +215,17 @@ def paged_append(cache: PagedCache, k: torch.Tensor, v: Optional[torch.Tensor], 
     """Writes the new tokens' keys (normed, turned) and values into the cache and returns their queries, treated like
     the keys (None without queries).  Rows behind the last sequence are left as they are (uninitialised in a q_out
     made here)."""
-    q_out = _empty(q) if q_out is None else q_out
     freqs, interleaved, mscale = rope or _NO_ROPE
-    B.msa_paged_append(cache.k, cache.v, cache.page_table, cache.kv_lens, cache.cu_q, freqs, interleaved, mscale, q, q_weight, k,
-                       k_weight, v, eps, q_out)
-    return q_out
+    return B.msa_paged_append(cache.k, cache.v, cache.page_table, cache.kv_lens, cache.cu_q, freqs, interleaved, mscale, q,
+                              q_weight, k, k_weight, v, eps, q_out)
 
 
 def paged_attn(cache: PagedCache, q: torch.Tensor, softmax_scale: float = 0.0, out: Optional[torch.Tensor] = None,
                want_lse: bool = True, workspace: Optional[torch.Tensor] = None):
     """Dense causal attention of the new tokens q [rows, heads, d] over the cache, which already holds their keys and
     values -> (out, lse).  Rows behind the last sequence are left as they are (uninitialised in outputs made here)."""
-    out = _empty(q) if out is None else out
     lse = q.new_empty(q.shape[:2], dtype=torch.float32) if want_lse else None
     if workspace is None:
         workspace = _workspace(q, B.msa_paged_attn_workspace_bytes, cache.k, q.shape[1])
-    B.msa_paged_attn(cache.k, cache.v, cache.page_table, cache.kv_lens, cache.cu_q, q, softmax_scale, out, lse, workspace)
+    out = B.msa_paged_attn(cache.k, cache.v, cache.page_table, cache.kv_lens, cache.cu_q, q, softmax_scale, out, lse, workspace)
     return out, lse

@@ -400,13 +400,15 @@ def _fn(name: str):
     return fn
 
 
-def _launch(index: int, name: str, *args) -> None:
-    """Calls the library with the tensors' device current (whatever the caller's is), on that device's current stream."""
+def _launch(index: int, name: str, *args, stream=None) -> None:
+    """Calls the library with the tensors' device current (whatever the caller's is), on `stream` or that device's
+    current stream."""
+    raw = torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
     if index == torch.cuda.current_device():
-        code = _fn(name)(*args, torch._C._cuda_getCurrentRawStream(index))
+        code = _fn(name)(*args, raw)
     else:
         with torch.cuda.device(index):
-            code = _fn(name)(*args, torch._C._cuda_getCurrentRawStream(index))
+            code = _fn(name)(*args, raw)
     if code != 0:
         raise MsaError(code, name)
 
@@ -429,11 +431,14 @@ def _heads(t: torch.Tensor, what: str, head_dim: int, rows: int, index: int, den
     return s[0]
 
 
-def _like(t: torch.Tensor, other: torch.Tensor, what: str, head_dim: int, rows: int, index: int) -> None:
-    """A dense bf16 tensor of another's shape."""
+def _output(t: Optional[torch.Tensor], other: torch.Tensor, what: str, head_dim: int, rows: int, index: int) -> torch.Tensor:
+    """An output of another's shape: dense bf16, made here if there is none."""
+    if t is None:
+        return torch.empty_like(other, memory_format=torch.contiguous_format)
     if t.shape != other.shape:
         raise ValueError("%s must be %s, got %s" % (what, tuple(other.shape), tuple(t.shape)))
     _heads(t, what, head_dim, rows, index, dense=True)
+    return t
 
 
 def _weights(head_dim: int, index: int, *weights) -> int:
@@ -481,22 +486,24 @@ def _ref(s):
     return None if s is None else ctypes.byref(s)
 
 
-def msa_qk_norm_rope(freqs, interleaved, mscale, q, q_weight, k, k_weight, eps, positions, q_out, k_out):
-    """q, k: bf16 [rows, heads, d], rows may be strided; either may be None.  freqs None: no rotation."""
+def msa_qk_norm_rope(freqs, interleaved, mscale, q, q_weight, k, k_weight, eps, positions, q_out, k_out, stream=None):
+    """q, k: bf16 [rows, heads, d], rows may be strided; either may be None.  freqs None: no rotation.
+    -> (q_out, k_out); outputs that are not given are made."""
     x = k if q is None else q
     index = _device_of(x, "q or k")
     rows, d = x.shape[0], x.shape[-1]
     qs = ks = hq = hk = 0
     if q is not None:
         qs, hq = _heads(q, "q", d, rows, index), q.shape[1]
-        _like(q_out, q, "q_out", d, rows, index)
+        q_out = _output(q_out, q, "q_out", d, rows, index)
     if k is not None:
         ks, hk = _heads(k, "k", d, rows, index), k.shape[1]
-        _like(k_out, k, "k_out", d, rows, index)
+        k_out = _output(k_out, k, "k_out", d, rows, index)
     w32 = _weights(d, index, q_weight, k_weight)
     rope = _rope(freqs, interleaved, mscale, index)
     _launch(index, "msa_qk_norm_rope", _ref(rope), _at(q), qs, hq, _at(q_weight), _at(k), ks, hk, _at(k_weight), d, w32, eps,
-            _positions(positions, rows, index), rows, _at(q_out), _at(k_out))
+            _positions(positions, rows, index), rows, _at(q_out), _at(k_out), stream=stream)
+    return q_out, k_out
 
 
 def msa_qk_norm_rope_backward_workspace_bytes(head_dim: int, n_tokens: int) -> int:
@@ -516,15 +523,17 @@ def _workspace(ws: Optional[torch.Tensor], index: int) -> int:
 
 
 def msa_qk_norm_rope_backward(freqs, interleaved, mscale, dq_out, dk_out, q, q_weight, k, k_weight, eps, positions, dq,
-                              dk, dq_weight, dk_weight, workspace):
-    """q / k are needed where there is a weight (else None is fine); dq, dk bf16 dense, weight gradients fp32 [d]."""
+                              dk, dq_weight, dk_weight, workspace, stream=None):
+    """q / k are needed where there is a weight (else None is fine); dq, dk bf16 dense, weight gradients fp32 [d].
+    -> (dq, dk); those that are not given are made."""
     x = dk_out if dq_out is None else dq_out
     index = _device_of(x, "dq_out or dk_out")
     rows, d = x.shape[0], x.shape[-1]
-    at = []
+    at, grads = [], []
     for n, dy, t, w, dx, dw in (("q", dq_out, q, q_weight, dq, dq_weight), ("k", dk_out, k, k_weight, dk, dk_weight)):
         if dy is None:
             at.append((0, 0, 0))
+            grads.append(None)
             continue
         ys, ts = _heads(dy, "the gradient of %s_out" % n, d, rows, index), 0
         if t is not None:
@@ -533,15 +542,18 @@ def msa_qk_norm_rope_backward(freqs, interleaved, mscale, dq_out, dk_out, q, q_w
                 raise ValueError("%s must be %s, got %s" % (n, tuple(dy.shape), tuple(t.shape)))
         elif w is not None:
             raise ValueError("%s is needed for the gradients of its norm" % n)
-        _like(dx, dy, "the gradient of %s" % n, d, rows, index)
+        dx = _output(dx, dy, "the gradient of " + n, d, rows, index)
         if dw is not None and (dw.dtype != torch.float32 or dw.shape != (d,) or not dw.is_contiguous() or dw.get_device() != index):
             raise ValueError("the gradient of %s_weight must be a contiguous fp32 vector of %d values on cuda:%d" % (n, d, index))
         at.append((ys, ts, dy.shape[1]))
+        grads.append(dx)
     w32 = _weights(d, index, q_weight, k_weight)
     rope = _rope(freqs, interleaved, mscale, index)
     _launch(index, "msa_qk_norm_rope_backward", _ref(rope), _at(dq_out), at[0][0], _at(dk_out), at[1][0], _at(q), at[0][1],
             at[0][2], _at(q_weight), _at(k), at[1][1], at[1][2], _at(k_weight), d, w32, eps, _positions(positions, rows, index),
-            rows, _at(dq), _at(dk), _at(dq_weight), _at(dk_weight), _at(workspace), _workspace(workspace, index))
+            rows, _at(grads[0]), _at(grads[1]), _at(dq_weight), _at(dk_weight), _at(workspace), _workspace(workspace, index),
+            stream=stream)
+    return grads[0], grads[1]
 
 
 def _paged(k_pool, v_pool, page_table, kv_lens, cu_q):
@@ -565,8 +577,9 @@ def _paged(k_pool, v_pool, page_table, kv_lens, cu_q):
 
 
 def msa_paged_append(k_pool, v_pool, page_table, kv_lens, cu_q, freqs, interleaved, mscale, q, q_weight, k, k_weight, v,
-                     eps, q_out):
-    """k, v (and q): bf16 [rows, heads, d], rows may be strided; q None: no queries; v None: a cache without values."""
+                     eps, q_out, stream=None):
+    """k, v (and q): bf16 [rows, heads, d], rows may be strided; q None: no queries; v None: a cache without values.
+    -> q_out, made if it is not given."""
     index, cache = _paged(k_pool, v_pool, page_table, kv_lens, cu_q)
     d, rows = cache.head_dim, k.shape[0]
     vs = qs = hq = 0
@@ -579,11 +592,12 @@ def msa_paged_append(k_pool, v_pool, page_table, kv_lens, cu_q, freqs, interleav
         raise ValueError("k and v must have the cache's %d heads" % cache.n_kv_heads)
     if q is not None:
         qs, hq = _heads(q, "q", d, rows, index), q.shape[1]
-        _like(q_out, q, "q_out", d, rows, index)
+        q_out = _output(q_out, q, "q_out", d, rows, index)
     w32 = _weights(d, index, q_weight, k_weight)
     rope = _rope(freqs, interleaved, mscale, index)
     _launch(index, "msa_paged_append", ctypes.byref(cache), _ref(rope), _at(q), qs, hq, _at(q_weight), _at(k), ks, _at(k_weight),
-            _at(v), vs, w32, eps, rows, _at(q_out))
+            _at(v), vs, w32, eps, rows, _at(q_out), stream=stream)
+    return q_out
 
 
 def msa_paged_attn_workspace_bytes(k_pool, n_q_heads: int) -> int:
@@ -596,19 +610,20 @@ def msa_paged_attn_workspace_bytes(k_pool, n_q_heads: int) -> int:
     return mn.value
 
 
-def msa_paged_attn(k_pool, v_pool, page_table, kv_lens, cu_q, q, softmax_scale, out, lse, workspace):
-    """q, out: bf16 [rows, heads, d] dense; lse fp32 [rows, heads] or None."""
+def msa_paged_attn(k_pool, v_pool, page_table, kv_lens, cu_q, q, softmax_scale, out, lse, workspace, stream=None):
+    """q, out: bf16 [rows, heads, d] dense; lse fp32 [rows, heads] or None.  -> out, made if it is not given."""
     index, cache = _paged(k_pool, v_pool, page_table, kv_lens, cu_q)
     d, rows = cache.head_dim, q.shape[0]
     if v_pool is None:
         raise ValueError("attention needs a value pool")
     _heads(q, "q", d, rows, index, dense=True)
-    _like(out, q, "out", d, rows, index)
+    out = _output(out, q, "out", d, rows, index)
     if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous() or
                             lse.get_device() != index):
         raise ValueError("lse must be contiguous fp32 %s on cuda:%d" % (tuple(q.shape[:2]), index))
     _launch(index, "msa_paged_attn", ctypes.byref(cache), q.data_ptr(), q.shape[1], rows, softmax_scale, out.data_ptr(), _at(lse),
-            _at(workspace), _workspace(workspace, index))
+            _at(workspace), _workspace(workspace, index), stream=stream)
+    return out
 
 
 # ------------------------------------------------------------------ allocation helpers

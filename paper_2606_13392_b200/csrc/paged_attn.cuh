@@ -262,7 +262,7 @@ __device__ __forceinline__ uint32_t pack2_f16(float a, float b) {
 }
 
 // Warps: 0-3 / 4-7 softmax of context 0 / 1 (thread = row), 8 loads K, 9 loads V, 10 issues the MMAs, 11 loads Q,
-// 12-15 (fp8 caches) widen the tiles to bf16.
+// 12-15 (fp8 caches) widen the tiles to fp16.
 template <bool F8>
 __global__ void __launch_bounds__(paged_threads(F8), 1)
 paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_q1,
@@ -311,208 +311,208 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     PagedItem it{};
 
     if (warp >= 8 && warp < 12) {
-    reg_release<kRegsIssue>();
-    if (warp == 8 || warp == 9) {
-        // ---------------- K / V producer: one box per page (or 128 keys of a larger one), a lane each
-        const bool is_v = warp == 9;
-        const int stages = is_v ? kPagedVStages : kPagedKStages;
-        const int boxes = kPagedKeys / box_keys;
-        const CUtensorMap* tm = is_v ? &tm_v : &tm_k;
-        const int nowhere = F8 ? a.c.n_pages * a.c.page_size : a.c.n_pages * a.c.page_size / 8;  // reads as zeros
-        bool ok = true;
-        int t = 0;
-        uint32_t tails = 0;
-        if (const long long late = g_debug_producer_delay; late > 0) spin_cycles(late);  // tests only
-        // coordinate of this lane's box of key tile b: its page's row, or outside the pool
-        auto place_of = [&](int b) {
-            const uint32_t key = (uint32_t)b * kPagedKeys + lane * box_keys, size = a.c.page_size;  // (below 2^31 + 128)
-            if (lane >= boxes || key >= (uint32_t)it.kv) return nowhere;
-            const uint32_t slot = key / size;
-            const int page = a.c.table[(int64_t)it.seq * a.c.max_pages + slot];
-            if (page < 0 || page >= a.c.n_pages) {
-                report_async(status, kAsyncBadIndex, 0x602);
-                return nowhere;
-            }
-            const int row = page * a.c.page_size + (int)(key - slot * size);
-            return F8 ? row : row / 8;
-        };
-        while (ok && walk.next(a, it)) {
-            int where = place_of(it.lo);
-            for (int b = it.lo; b < it.hi; ++b, ++t) {
-                const int where_next = b + 1 < it.hi ? place_of(b + 1) : 0;
-                const int st = t % stages;
-                const uint32_t use = t / stages;
-                uint64_t* empty = is_v ? &sm.v_empty[st] : &sm.k_empty[st];
-                uint64_t* full = is_v ? &sm.v_full[st] : &sm.k_full[st];
-                uint64_t* land = is_v ? &sm.v_land[st] : &sm.k_land[st];
-                uint8_t* dst = is_v ? sm.v[st] : sm.k[st];
-                if (use > 0 && !mbar_wait(empty, (use - 1) & 1, abort)) {
-                    if (lane == 0) report_async(status, kAsyncTimeout, 0x611);
-                    ok = false;
-                    break;
+        reg_release<kRegsIssue>();
+        if (warp == 8 || warp == 9) {
+            // ---------------- K / V producer: one box per page (or 128 keys of a larger one), a lane each
+            const bool is_v = warp == 9;
+            const int stages = is_v ? kPagedVStages : kPagedKStages;
+            const int boxes = kPagedKeys / box_keys;
+            const CUtensorMap* tm = is_v ? &tm_v : &tm_k;
+            const int nowhere = F8 ? a.c.n_pages * a.c.page_size : a.c.n_pages * a.c.page_size / 8;  // reads as zeros
+            bool ok = true;
+            int t = 0;
+            uint32_t tails = 0;
+            if (const long long late = g_debug_producer_delay; late > 0) spin_cycles(late);  // tests only
+            // coordinate of this lane's box of key tile b: its page's row, or outside the pool
+            auto place_of = [&](int b) {
+                const uint32_t key = (uint32_t)b * kPagedKeys + lane * box_keys, size = a.c.page_size;  // (below 2^31 + 128)
+                if (lane >= boxes || key >= (uint32_t)it.kv) return nowhere;
+                const uint32_t slot = key / size;
+                const int page = a.c.table[(int64_t)it.seq * a.c.max_pages + slot];
+                if (page < 0 || page >= a.c.n_pages) {
+                    report_async(status, kAsyncBadIndex, 0x602);
+                    return nowhere;
                 }
-                // The last tile's V rows behind the end may hold anything, and 0 * NaN is NaN: they are overwritten
-                // with zeros before the MMA sees the tile (fp8: by the widening warps).
-                const int rows = it.kv - b * kPagedKeys;  // rows inside the sequence
-                const bool tail = !F8 && is_v && rows < kPagedKeys;
-                uint64_t* bar = F8 ? land : (tail ? &sm.v_tail : full);
-                if (lane == 0) mbar_arrive_expect_tx(bar, TILE);
-                __syncwarp();
-                if (lane < boxes) {
-                    // (fp8: 32 keys into the upper half of the 8 KB of their fp16)
-                    if constexpr (F8) tma_load_3d(dst + (lane * box_keys >> 5) * 8192 + 4096 + (lane * box_keys & 31) * 128, tm, 0, it.head, where, bar);
-                    else tma_load_5d(dst + lane * box_keys * 256, tm, 0, 0, 0, it.head, where, bar);
-                }
-                if (tail) {
-                    if (!mbar_wait(&sm.v_tail, tails & 1, abort)) {
-                        if (lane == 0) report_async(status, kAsyncTimeout, 0x612);
+                const int row = page * a.c.page_size + (int)(key - slot * size);
+                return F8 ? row : row / 8;
+            };
+            while (ok && walk.next(a, it)) {
+                int where = place_of(it.lo);
+                for (int b = it.lo; b < it.hi; ++b, ++t) {
+                    const int where_next = b + 1 < it.hi ? place_of(b + 1) : 0;
+                    const int st = t % stages;
+                    const uint32_t use = t / stages;
+                    uint64_t* empty = is_v ? &sm.v_empty[st] : &sm.k_empty[st];
+                    uint64_t* full = is_v ? &sm.v_full[st] : &sm.k_full[st];
+                    uint64_t* land = is_v ? &sm.v_land[st] : &sm.k_land[st];
+                    uint8_t* dst = is_v ? sm.v[st] : sm.k[st];
+                    if (use > 0 && !mbar_wait(empty, (use - 1) & 1, abort)) {
+                        if (lane == 0) report_async(status, kAsyncTimeout, 0x611);
                         ok = false;
                         break;
                     }
-                    ++tails;
-                    for (int i = max(rows, 0) * 16 + lane; i < kPagedKeys * 16; i += 32) {
-                        const int key = i >> 4, c = i & 15;
-                        *reinterpret_cast<uint4*>(dst + (key >> 3) * 2048 + (c >> 3) * 1024 + (key & 7) * 128 + (c & 7) * 16) =
-                            make_uint4(0u, 0u, 0u, 0u);
-                    }
-                    fence_proxy_async_smem();
+                    // The last tile's V rows behind the end may hold anything, and 0 * NaN is NaN: they are overwritten
+                    // with zeros before the MMA sees the tile (fp8: by the widening warps).
+                    const int rows = it.kv - b * kPagedKeys;  // rows inside the sequence
+                    const bool tail = !F8 && is_v && rows < kPagedKeys;
+                    uint64_t* bar = F8 ? land : (tail ? &sm.v_tail : full);
+                    if (lane == 0) mbar_arrive_expect_tx(bar, TILE);
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(full);
+                    if (lane < boxes) {
+                        // (fp8: 32 keys into the upper half of the 8 KB of their fp16)
+                        if constexpr (F8) tma_load_3d(dst + (lane * box_keys >> 5) * 8192 + 4096 + (lane * box_keys & 31) * 128, tm, 0, it.head, where, bar);
+                        else tma_load_5d(dst + lane * box_keys * 256, tm, 0, 0, 0, it.head, where, bar);
+                    }
+                    if (tail) {
+                        if (!mbar_wait(&sm.v_tail, tails & 1, abort)) {
+                            if (lane == 0) report_async(status, kAsyncTimeout, 0x612);
+                            ok = false;
+                            break;
+                        }
+                        ++tails;
+                        for (int i = max(rows, 0) * 16 + lane; i < kPagedKeys * 16; i += 32) {
+                            const int key = i >> 4, c = i & 15;
+                            *reinterpret_cast<uint4*>(dst + (key >> 3) * 2048 + (c >> 3) * 1024 + (key & 7) * 128 + (c & 7) * 16) =
+                                make_uint4(0u, 0u, 0u, 0u);
+                        }
+                        fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(full);
+                    }
+                    where = where_next;
                 }
-                where = where_next;
             }
-        }
-        if (*abort != 0) spin_cycles(200000);
-    } else if (warp == 11) {
-        // ---------------- Q producer, and the note for the merge
-        PagedEnds e{};
-        bool ok = true;
-        uint32_t used[2] = {0, 0};
-        while (walk.next(a, it)) {
-            if (e.first == 0) e.first = it.lo == 0 ? 3 : (it.hi < it.nb ? 1 : 2);
-            e.open = it.lo == 0 && it.hi < it.nb;
-            e.q_row = it.q_row; e.tokens = it.n0 + it.n1; e.head = it.head;
-            for (int j = 0; j < 2 && ok; ++j) {
-                const int n = j == 0 ? it.n0 : it.n1;
-                if (n == 0) continue;
-                if (used[j] > 0 && !mbar_wait(&sm.q_empty[j], (used[j] - 1) & 1, abort)) {
-                    if (lane == 0) report_async(status, kAsyncTimeout, 0x621);
-                    ok = false;
-                    break;
+            if (*abort != 0) spin_cycles(200000);
+        } else if (warp == 11) {
+            // ---------------- Q producer, and the note for the merge
+            PagedEnds e{};
+            bool ok = true;
+            uint32_t used[2] = {0, 0};
+            while (walk.next(a, it)) {
+                if (e.first == 0) e.first = it.lo == 0 ? 3 : (it.hi < it.nb ? 1 : 2);
+                e.open = it.lo == 0 && it.hi < it.nb;
+                e.q_row = it.q_row; e.tokens = it.n0 + it.n1; e.head = it.head;
+                for (int j = 0; j < 2 && ok; ++j) {
+                    const int n = j == 0 ? it.n0 : it.n1;
+                    if (n == 0) continue;
+                    if (used[j] > 0 && !mbar_wait(&sm.q_empty[j], (used[j] - 1) & 1, abort)) {
+                        if (lane == 0) report_async(status, kAsyncTimeout, 0x621);
+                        ok = false;
+                        break;
+                    }
+                    ++used[j];
+                    const int row = it.q_row + j * a.TPT, head = it.head * a.G;
+                    // Few tokens: their own boxes (rows behind them keep what they held: no row reads another's).  All: one
+                    // box for each half of d; tokens of the next sequence come along, tokens that are not there read as zeros.
+                    const bool few = n * 2 <= 16 && n < a.TPT && a.G % 8 == 0;
+                    uint64_t* bar = F8 ? &sm.q_land[j] : &sm.q_full[j];
+                    if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)((few ? n : a.TPT) * a.G * 256));
+                    __syncwarp();
+                    if (few) {
+                        if (lane < 2 * n)
+                            tma_load_3d(sm.q[j] + (lane & 1) * 16384 + (lane >> 1) * a.G * 128, &tm_q1, (lane & 1) * 64, head, row + (lane >> 1),
+                                        bar);
+                    } else if (lane < 2) {
+                        tma_load_3d(sm.q[j] + lane * 16384, &tm_q, lane * 64, head, row, bar);
+                    }
                 }
-                ++used[j];
-                const int row = it.q_row + j * a.TPT, head = it.head * a.G;
-                // Few tokens: their own boxes (rows behind them keep what they held: no row reads another's).  All: one
-                // box for each half of d; tokens of the next sequence come along, tokens that are not there read as zeros.
-                const bool few = n * 2 <= 16 && n < a.TPT && a.G % 8 == 0;
-                uint64_t* bar = F8 ? &sm.q_land[j] : &sm.q_full[j];
-                if (lane == 0) mbar_arrive_expect_tx(bar, (uint32_t)((few ? n : a.TPT) * a.G * 256));
+            }
+            if (lane == 0) {
+                a.ends[blockIdx.x * 2] = make_int4(e.first, e.open, e.q_row, e.tokens);
+                a.ends[blockIdx.x * 2 + 1] = make_int4(e.head, 0, 0, 0);
+            }
+            if (*abort != 0) spin_cycles(200000);
+        } else if (warp == 10) {
+            // ---------------- MMA issuer: S_j(i) = Q_j K^T, then, once P_j(i) is written over it, O_j += P_j(i) V.
+            // S_j(i+1) is issued right behind O_j += P_j(i) V: MMAs run in issue order, so it may overwrite P_j(i), it runs
+            // while the other context's softmax is at work, and the barrier that says S_j(i) is there says as well that O_j
+            // holds all steps before.  P comes in halves, so that the product starts on the first.  (S in two 64-key
+            // buffers, one product ahead, was slower: 64-key products read Q twice as often, and shared memory is what the
+            // MMAs run short of; 128-row chunk 4.8 against 4.3 ms.)
+            // The whole warp walks and waits, one elected lane issues: descriptors then stay in uniform registers.
+            constexpr uint32_t idesc = F8 ? make_idesc_f16(128, 128, false, false) : make_idesc_bf16(128, 128, false, false);
+            constexpr uint32_t idesc_o = F8 ? make_idesc_f16(128, 128, false, true) : make_idesc_bf16(128, 128, false, true);
+            constexpr uint32_t kTile = kPagedKeys * 256 / 16;  // in descriptor units of 16 bytes
+            const uint64_t q_desc = make_smem_desc(smem_u32(sm.q[0]), 16, 1024), k_desc = make_smem_desc(smem_u32(sm.k[0]), 16, 2048);
+            // V as the MN-major B operand: 8-key groups 2 KB apart, the other 64 columns of d 1 KB away
+            const uint64_t v_desc = make_smem_desc(smem_u32(sm.v[0]), 1024, 2048);
+            uint32_t n_p[2] = {0, 0}, n_o[2] = {0, 0}, n_q[2] = {0, 0};  // P's, items and uses of Q so far
+            uint32_t ks = 0, k_phase = 0, vs = 0, v_phase = 0;            // stage of the next K / V tile and its use's parity
+            bool ok = true;
+            while (ok && walk.next(a, it)) {
+                const bool dual = it.dual();
+                const int st[2] = {it.steps(0), it.steps(1)};
+                for (int i = -1; ok && i < st[0]; ++i) {
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const uint32_t ts = tmem + j * 128, to = tmem + 256 + j * 128;
+                        const bool first_user = dual || j == 0, last_user = dual || j == 1;  // of a K or V tile
+                        // (K is waited for behind the product with V: where loads are the limit, V's stage is free sooner)
+                        if (i >= 0 && i < st[j]) {
+                            if ((first_user && !mbar_wait(&sm.v_full[vs], v_phase, abort)) ||
+                                (i == 0 && n_o[j] > 0 && !mbar_wait(&sm.o_empty[j], (n_o[j] - 1) & 1, abort)) ||
+                                !mbar_wait(&sm.p_full[j][0], n_p[j] & 1, abort)) {
+                                if (lane == 0) report_async(status, kAsyncTimeout, 0x631);
+                                ok = false;
+                                break;
+                            }
+                            tc_fence_after();
+                            const uint64_t vd = v_desc + vs * kTile;
+                            if (elect_one()) {
+#pragma unroll
+                                for (int kk = 0; kk < 4; ++kk) mma_bf16_ts(to, ts + kk * 8, vd + (uint64_t)(kk * 256), idesc_o, i > 0 || kk > 0);
+                            }
+                            __syncwarp();
+                            if (!mbar_wait(&sm.p_full[j][1], n_p[j]++ & 1, abort)) {
+                                if (lane == 0) report_async(status, kAsyncTimeout, 0x632);
+                                ok = false;
+                                break;
+                            }
+                            tc_fence_after();
+                            if (elect_one()) {
+#pragma unroll
+                                for (int kk = 4; kk < 8; ++kk) mma_bf16_ts(to, ts + kk * 8, vd + (uint64_t)(kk * 256), idesc_o, true);
+                                if (last_user) mma_commit(&sm.v_empty[vs]);
+                                if (i == st[j] - 1) mma_commit(&sm.o_full[j]);
+                            }
+                            __syncwarp();
+                            n_o[j] += i == st[j] - 1;
+                            if (last_user && ++vs == kPagedVStages) { vs = 0; v_phase ^= 1; }
+                        }
+                        if (i + 1 < st[j]) {
+                            const int qb = dual ? 0 : j;
+                            if ((first_user && !mbar_wait(&sm.k_full[ks], k_phase, abort)) ||
+                                (i == -1 && (!dual || j == 0) && !mbar_wait(&sm.q_full[qb], n_q[qb] & 1, abort))) {
+                                if (lane == 0) report_async(status, kAsyncTimeout, 0x633);
+                                ok = false;
+                                break;
+                            }
+                            tc_fence_after();
+                            const bool q_done = dual ? 2 * (i + 1) + j == it.hi - it.lo - 1 : i + 2 == st[j];
+                            if (elect_one()) {
+                                const uint64_t qd = q_desc + qb * (128 * 256 / 16), kd = k_desc + ks * kTile;
+#pragma unroll
+                                for (int kk = 0; kk < 8; ++kk)  // 16 of d each; second half of Q 16 KB on, of K 1 KB
+                                    mma_bf16_ss(ts, qd + (uint64_t)((kk >> 2) * 1024 + 2 * (kk & 3)),
+                                                kd + (uint64_t)((kk >> 2) * 64 + 2 * (kk & 3)), idesc, kk > 0);
+                                mma_commit(&sm.s_full[j]);
+                                if (last_user) mma_commit(&sm.k_empty[ks]);
+                                if (q_done) mma_commit(&sm.q_empty[qb]);
+                            }
+                            __syncwarp();
+                            if (last_user && ++ks == kPagedKStages) { ks = 0; k_phase ^= 1; }
+                        }
+                    }
+                }
+                ++n_q[0];
+                n_q[1] += !dual;
+            }
+            if (*abort != 0) {
+                if (elect_one()) mma_commit(&sm.drain);
                 __syncwarp();
-                if (few) {
-                    if (lane < 2 * n)
-                        tma_load_3d(sm.q[j] + (lane & 1) * 16384 + (lane >> 1) * a.G * 128, &tm_q1, (lane & 1) * 64, head, row + (lane >> 1),
-                                    bar);
-                } else if (lane < 2) {
-                    tma_load_3d(sm.q[j] + lane * 16384, &tm_q, lane * 64, head, row, bar);
-                }
+                mbar_wait_quiet(&sm.drain, 0, 20000000);
             }
         }
-        if (lane == 0) {
-            a.ends[blockIdx.x * 2] = make_int4(e.first, e.open, e.q_row, e.tokens);
-            a.ends[blockIdx.x * 2 + 1] = make_int4(e.head, 0, 0, 0);
-        }
-        if (*abort != 0) spin_cycles(200000);
-    } else if (warp == 10) {
-        // ---------------- MMA issuer: S_j(i) = Q_j K^T, then, once P_j(i) is written over it, O_j += P_j(i) V.
-        // S_j(i+1) is issued right behind O_j += P_j(i) V: MMAs run in issue order, so it may overwrite P_j(i), it runs
-        // while the other context's softmax is at work, and the barrier that says S_j(i) is there says as well that O_j
-        // holds all steps before.  P comes in halves, so that the product starts on the first.  (S in two 64-key
-        // buffers, one product ahead, was slower: 64-key products read Q twice as often, and shared memory is what the
-        // MMAs run short of; 128-row chunk 4.8 against 4.3 ms.)
-        // The whole warp walks and waits, one elected lane issues: descriptors then stay in uniform registers.
-        constexpr uint32_t idesc = F8 ? make_idesc_f16(128, 128, false, false) : make_idesc_bf16(128, 128, false, false);
-        constexpr uint32_t idesc_o = F8 ? make_idesc_f16(128, 128, false, true) : make_idesc_bf16(128, 128, false, true);
-        constexpr uint32_t kTile = kPagedKeys * 256 / 16;  // in descriptor units of 16 bytes
-        const uint64_t q_desc = make_smem_desc(smem_u32(sm.q[0]), 16, 1024), k_desc = make_smem_desc(smem_u32(sm.k[0]), 16, 2048);
-        // V as the MN-major B operand: 8-key groups 2 KB apart, the other 64 columns of d 1 KB away
-        const uint64_t v_desc = make_smem_desc(smem_u32(sm.v[0]), 1024, 2048);
-        uint32_t n_p[2] = {0, 0}, n_o[2] = {0, 0}, n_q[2] = {0, 0};  // P's, items and uses of Q so far
-        uint32_t ks = 0, k_phase = 0, vs = 0, v_phase = 0;            // stage of the next K / V tile and its use's parity
-        bool ok = true;
-        while (ok && walk.next(a, it)) {
-            const bool dual = it.dual();
-            const int st[2] = {it.steps(0), it.steps(1)};
-            for (int i = -1; ok && i < st[0]; ++i) {
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const uint32_t ts = tmem + j * 128, to = tmem + 256 + j * 128;
-                    const bool first_user = dual || j == 0, last_user = dual || j == 1;  // of a K or V tile
-                    // (K is waited for behind the product with V: where loads are the limit, V's stage is free sooner)
-                    if (i >= 0 && i < st[j]) {
-                        if ((first_user && !mbar_wait(&sm.v_full[vs], v_phase, abort)) ||
-                            (i == 0 && n_o[j] > 0 && !mbar_wait(&sm.o_empty[j], (n_o[j] - 1) & 1, abort)) ||
-                            !mbar_wait(&sm.p_full[j][0], n_p[j] & 1, abort)) {
-                            if (lane == 0) report_async(status, kAsyncTimeout, 0x631);
-                            ok = false;
-                            break;
-                        }
-                        tc_fence_after();
-                        const uint64_t vd = v_desc + vs * kTile;
-                        if (elect_one()) {
-#pragma unroll
-                            for (int kk = 0; kk < 4; ++kk) mma_bf16_ts(to, ts + kk * 8, vd + (uint64_t)(kk * 256), idesc_o, i > 0 || kk > 0);
-                        }
-                        __syncwarp();
-                        if (!mbar_wait(&sm.p_full[j][1], n_p[j]++ & 1, abort)) {
-                            if (lane == 0) report_async(status, kAsyncTimeout, 0x632);
-                            ok = false;
-                            break;
-                        }
-                        tc_fence_after();
-                        if (elect_one()) {
-#pragma unroll
-                            for (int kk = 4; kk < 8; ++kk) mma_bf16_ts(to, ts + kk * 8, vd + (uint64_t)(kk * 256), idesc_o, true);
-                            if (last_user) mma_commit(&sm.v_empty[vs]);
-                            if (i == st[j] - 1) mma_commit(&sm.o_full[j]);
-                        }
-                        __syncwarp();
-                        n_o[j] += i == st[j] - 1;
-                        if (last_user && ++vs == kPagedVStages) { vs = 0; v_phase ^= 1; }
-                    }
-                    if (i + 1 < st[j]) {
-                        const int qb = dual ? 0 : j;
-                        if ((first_user && !mbar_wait(&sm.k_full[ks], k_phase, abort)) ||
-                            (i == -1 && (!dual || j == 0) && !mbar_wait(&sm.q_full[qb], n_q[qb] & 1, abort))) {
-                            if (lane == 0) report_async(status, kAsyncTimeout, 0x633);
-                            ok = false;
-                            break;
-                        }
-                        tc_fence_after();
-                        const bool q_done = dual ? 2 * (i + 1) + j == it.hi - it.lo - 1 : i + 2 == st[j];
-                        if (elect_one()) {
-                            const uint64_t qd = q_desc + qb * (128 * 256 / 16), kd = k_desc + ks * kTile;
-#pragma unroll
-                            for (int kk = 0; kk < 8; ++kk)  // 16 of d each; second half of Q 16 KB on, of K 1 KB
-                                mma_bf16_ss(ts, qd + (uint64_t)((kk >> 2) * 1024 + 2 * (kk & 3)),
-                                            kd + (uint64_t)((kk >> 2) * 64 + 2 * (kk & 3)), idesc, kk > 0);
-                            mma_commit(&sm.s_full[j]);
-                            if (last_user) mma_commit(&sm.k_empty[ks]);
-                            if (q_done) mma_commit(&sm.q_empty[qb]);
-                        }
-                        __syncwarp();
-                        if (last_user && ++ks == kPagedKStages) { ks = 0; k_phase ^= 1; }
-                    }
-                }
-            }
-            ++n_q[0];
-            n_q[1] += !dual;
-        }
-        if (*abort != 0) {
-            if (elect_one()) mma_commit(&sm.drain);
-            __syncwarp();
-            mbar_wait_quiet(&sm.drain, 0, 20000000);
-        }
-    }
     } else if (warp >= 12) {
         // ---------------- widening (fp8): K and V become fp16, which holds every E4M3 value and takes one conversion
         // for two elements (bf16 takes four operations).  Warp w widens keys 32w .. 32w+31 of every tile: their 4 KB (row =

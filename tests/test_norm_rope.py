@@ -140,6 +140,21 @@ def test_far_positions_and_in_place():
 
 
 @pytest.mark.gpu
+def test_gradients_in_place_and_on_a_given_stream():
+    q, k, wq, wk, positions, freqs = make(777, 6, 2, 128, 64, True, True, True)
+    rope = api.Rope(freqs, False, 1.1)
+    dq, dk = torch.randn(777, 6, 128, device=DEV).bfloat16(), torch.randn(777, 2, 128, device=DEV).bfloat16()
+    want = api.qk_norm_rope_backward(dq, dk, q, k, positions, rope, wq, wk)
+    ws = B.alloc_workspace(B.msa_qk_norm_rope_backward_workspace_bytes(128, 777), DEV)
+    sums = torch.empty(2, 128, device=DEV)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    B.msa_qk_norm_rope_backward(freqs, False, 1.1, dq, dk, q, wq, k, wk, 1e-6, positions, dq, dk, sums[0], sums[1], ws, stream=side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip((dq, dk, sums[0], sums[1]), want))
+
+
+@pytest.mark.gpu
 def test_zeros_infinities_and_empty_calls():
     q = torch.zeros(3, 3, 128, device=DEV).bfloat16()
     q[1, 1, 5] = math.inf
