@@ -24,7 +24,7 @@ namespace msa {
 
 constexpr int kRopeThreads = 256;
 constexpr int kRopeWarps = kRopeThreads / 32;
-constexpr int kRopeMaxTile = 8;  // tokens a CTA prepares at a time
+constexpr int kRopeMaxTile = 32;  // tokens a CTA prepares at a time
 
 struct RopeArgs {
     const double* freqs;  // [rot/2] radians per position, or null (no rotation)

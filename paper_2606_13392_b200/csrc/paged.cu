@@ -71,14 +71,15 @@ template <int LPH, bool EXACT, bool APPEND, bool F8>
 static void launch_norm_rope(const RopeArgs& rp, const RopeHeads& q, const RopeHeads& k, const RopeHeads& v, int64_t n,
                              int d, float eps, bool w32, const int64_t* positions, const PagedView& cache, void* k_pool,
                              void* v_pool, cudaStream_t st) {
-    // Many tokens: eight a CTA at a time, so that 256 threads have an angle or two each and all warps have items.  Few: one
-    // a CTA, its items spread over CTAs until the machine has four CTAs per SM (each repeats the token's angles).  Twice
-    // the CTAs that are resident: the second half evens out the rounds.
+    // Many tokens: as many a CTA at a time as make about nine items a warp (eight of 64 + 8 heads of 128), so that the
+    // angles' latency is paid once for them.  Few: one a CTA, its items spread over CTAs until the machine has four CTAs
+    // per SM (each repeats the token's angles).  At most twice the CTAs that are resident: the second half evens out the
+    // rounds.
     const int run = 4 * (32 / LPH);
     const int items = (q.n_heads + run - 1) / run + (k.n_heads + run - 1) / run + (v.n_heads + run - 1) / run;
     const int64_t want = 4LL * sm_count();
     int tile = kRopeMaxTile;
-    while (tile > 1 && ceil_div64(n, tile) < want) tile /= 2;
+    while (tile > 1 && (tile * items > 9 * kRopeWarps || ceil_div64(n, tile) < want * 3 / 4)) tile /= 2;
     const int64_t tiles = ceil_div64(n, tile);
     const int parts = tiles >= want ? 1 : (int)std::min<int64_t>(items, ceil_div64(want, tiles));
     const int per = (items + parts - 1) / parts;
