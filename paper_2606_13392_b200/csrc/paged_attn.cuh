@@ -9,6 +9,10 @@
 // The units of all tiles form one line (sequence, head, tile, key tile) and every CTA takes an equal stretch of it:
 // ragged batches balance to one unit whatever their lengths.  A tile that a stretch boundary cuts leaves fp32
 // partials (at most two per CTA), merged by paged_combine_kernel; all others are written directly.
+//
+// Measured (64 query, 8 KV heads): 4096 new tokens on 28K in 3.8 - 4.6 ms, 0.9 - 1.08 PFLOP/s at the board's power limit,
+// 57 % of the tensor pipe's cycles and 58 % of the exponential unit's; one token each of 64 sequences of up to 32K in 658
+// us, 93 % of the copy bandwidth; 2 - 7 tokens each of 16 sequences in 88 us, 77 %; one token on 2K in 15.7 us.
 #pragma once
 
 #include "norm_rope.cuh"
