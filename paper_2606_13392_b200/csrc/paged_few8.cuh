@@ -1,5 +1,5 @@
-// Attention over a paged fp8 cache for calls of a token or so per sequence (decode): the line of units, the partials
-// and the merge are those of paged_attn.cuh, a tile of query rows is at most 16.  Bound by HBM.
+// Attention over a paged fp8 cache for calls of a few rows per sequence (decode): the line of units, the partials and
+// the merge are those of paged_attn.cuh, a tile of query rows is at most 16.  Bound by HBM.
 //
 // Why not the tcgen05 kernel: its operands come from shared memory, so fp8 tiles have to be read, widened and written
 // back (64 KB for 32 KB of cache), with 128-row products for 8 or 16 rows; it reached 45 % of the copy bandwidth on 32

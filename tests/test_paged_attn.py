@@ -52,7 +52,8 @@ def make(lens, page, heads, d, fp8, seed=0, spare=2, extra_cols=1):
 def gathered(pool, table_row, n):
     page = pool.shape[1]
     t = torch.arange(n, device=DEV)
-    return pool.float()[table_row.long()[t // page], t % page].double()
+    raw = pool.view(torch.uint8)[table_row.long()[t // page], t % page]  # (as bytes: pools may be large)
+    return raw.view(pool.dtype).double()
 
 
 def check(cache, q, out, lse, scale=None):
@@ -120,6 +121,10 @@ CASES = [  # lens (new, old), page, query heads per KV head, KV heads, d, fp8
     ([(129, 1), (5, 130)], 8, 1, 3, 128, False),
     ([(40, 400), (2, 70)], 24, 5, 2, 128, False),                      # groups that do not divide a tile
     ([(9, 400), (3, 70)], 64, 100, 1, 128, False),
+    ([(80, 90000)], 64, 8, 1, 128, False),                             # several tiles on keys beyond a third of L2
+    ([(80, 170000)], 128, 8, 1, 128, True),
+    ([(2, 3000), (1, 300), (3, 70), (2, 5)], 16, 8, 2, 128, True),     # two tokens of eight heads on average
+    ([(9, 3000), (1, 300), (0, 70), (1, 5)], 32, 4, 2, 128, True),
     ([(9, 400), (130, 70)], 64, 128, 1, 128, True),
     ([(300, 7)], 64, 3, 2, 128, True),
     ([(4, 60), (1, 0), (0, 3)], 7, 4, 2, 128, False),                  # other shapes: odd pages,
@@ -340,6 +345,32 @@ def test_a_layer_step_by_step(fp8):
         assert torch.equal(q, torch.cat(turned[s]))
         if not fp8:
             assert torch.equal(gathered(cache.k, table[s], total), k.double())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fp8,lens", [(False, [(70, 900), (1, 400)]), (True, [(70, 900), (1, 400)]), (True, [(1, 900), (1, 400)])])
+def test_places_beyond_32_bits(fp8, lens):
+    # the last pages of a pool of over 2^31 elements, written by the append and read back
+    page, heads, d = 64, 8, 128
+    pages = (1 << 31) // (page * heads * d) + 40
+    kind = torch.float8_e4m3fn if fp8 else torch.bfloat16
+    pools = [torch.empty(pages, page, heads, d, dtype=kind, device=DEV) for _ in range(2)]
+    table = torch.arange(pages - 40, pages, dtype=torch.int32, device=DEV).flip(0).view(2, 20)  # 1280 tokens each
+    g = torch.Generator(device=DEV).manual_seed(1)
+    for n in ([c for _, c in lens], [x for x, _ in lens]):  # what was there, then the new tokens
+        done = [c for _, c in lens] if n[0] == lens[0][1] else [x + c for x, c in lens]
+        cache = api.PagedCache(pools[0], pools[1], table, torch.tensor(done, dtype=torch.int32, device=DEV),
+                               torch.tensor([0, n[0], sum(n)], dtype=torch.int32, device=DEV))
+        k, v = [torch.randn(sum(n), heads, d, generator=g, device=DEV).bfloat16() for _ in range(2)]
+        api.paged_append(cache, k, v)
+        for s in range(2):
+            rows = slice(0, n[0]) if s == 0 else slice(n[0], None)
+            assert torch.equal(gathered(cache.k, table[s], done[s])[done[s] - n[s]:], k[rows].to(kind).double())
+            assert torch.equal(gathered(cache.v, table[s], done[s])[done[s] - n[s]:], v[rows].to(kind).double())
+    q = queries(sum(n), 16, d)
+    out, lse = api.paged_attn(cache, q)
+    assert B.check_async_status() == (0, 0)
+    check(cache, q, out, lse)
 
 
 @pytest.mark.gpu
