@@ -70,22 +70,29 @@ __host__ __device__ __forceinline__ int paged_blocks(const PagedSeq& q, int t) {
     return (int)((last + kPagedKeys - 1) / kPagedKeys);
 }
 
-// sum over i < n of floor((a i + b) / m), a, b >= 0: Euclid's steps on (a, m).
-__host__ __device__ inline int64_t floor_sum(int64_t n, int64_t m, int64_t a, int64_t b) {
+// sum over i < n of floor((a i + b) / m), a, b >= 0: Euclid's steps on (a, m).  T: 32 bits where a n + b fits (they
+// divide several times faster, and a CTA's prologue takes some twenty of these sums).
+template <class T>
+__host__ __device__ inline int64_t floor_sum_of(T n, T m, T a, T b) {
     int64_t sum = 0;
     while (n > 0) {
-        sum += n * (n - 1) / 2 * (a / m) + n * (b / m);
-        a %= m;
-        b %= m;
-        const int64_t y = a * n + b;
+        const T qa = a / m, qb = b / m;
+        sum += (int64_t)n * ((int64_t)n - 1) / 2 * (int64_t)qa + (int64_t)n * (int64_t)qb;
+        a -= qa * m;
+        b -= qb * m;
+        const T y = a * n + b;
         n = y / m;
-        b = y % m;
-        const int64_t t = m;
+        b = y - n * m;
+        const T t = m;
         m = a;
         a = t;
         if (m == 0) break;
     }
     return sum;
+}
+__host__ __device__ inline int64_t floor_sum(int64_t n, int64_t m, int64_t a, int64_t b) {
+    if (a * n + b < (1ll << 31)) return floor_sum_of<uint32_t>((uint32_t)n, (uint32_t)m, (uint32_t)a, (uint32_t)b);
+    return floor_sum_of<int64_t>(n, m, a, b);
 }
 
 // Units of the first t query tiles of one head.
@@ -263,6 +270,18 @@ constexpr int paged_threads(bool f8) { return f8 ? 512 : 384; }
 __device__ __forceinline__ uint32_t pack2_f16(float a, float b) {
     const __half2 v = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// 32 bytes to a 16-byte boundary of global memory: one store where it is a 32-byte boundary too.
+__device__ __forceinline__ void store32(void* to, const uint32_t* v) {
+    if ((reinterpret_cast<uintptr_t>(to) & 31) == 0) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
+                     "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                     : "memory");
+    } else {
+        reinterpret_cast<uint4*>(to)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<uint4*>(to)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+    }
 }
 
 // Warps: 0-3 / 4-7 softmax of context 0 / 1 (thread = row), 8 loads K, 9 loads V, 10 issues the MMAs, 11 loads Q,
@@ -757,21 +776,16 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
 #pragma unroll
                         for (int e = 0; e < 32; ++e) ov[e] = __float_as_uint(fmaf(__uint_as_float(o1[e]), w1, __uint_as_float(ov[e])));
                     }
+                    // (32 bytes a store: whole sectors, where the lanes' rows are 256 bytes and more apart)
                     if (row_on && partial) {
-                        float4* to = reinterpret_cast<float4*>(a.part_o + slot_row * 128 + c * 32);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            to[e] = make_float4(__uint_as_float(ov[4 * e]), __uint_as_float(ov[4 * e + 1]), __uint_as_float(ov[4 * e + 2]),
-                                                __uint_as_float(ov[4 * e + 3]));
+                        for (int e = 0; e < 4; ++e) store32(a.part_o + slot_row * 128 + c * 32 + e * 8, &ov[8 * e]);
                     } else if (row_on) {
-                        uint4* to = reinterpret_cast<uint4*>(a.out + out_row * 128 + c * 32);
+                        uint32_t pk[16];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            float f[8];
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(ov[8 * e + i]);
-                            to[e] = pack8(f);
-                        }
+                        for (int e = 0; e < 16; ++e) pk[e] = pack2(__uint_as_float(ov[2 * e]), __uint_as_float(ov[2 * e + 1]));
+                        store32(a.out + out_row * 128 + c * 32, pk);
+                        store32(a.out + out_row * 128 + c * 32 + 16, pk + 8);
                     }
                     __syncwarp();
                 }

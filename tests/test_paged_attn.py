@@ -291,6 +291,22 @@ def test_guard_bands():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("lens,fp8", [([(70, 200), (1, 400)], False), ([(70, 200), (1, 400)], True), ([(1, 200), (1, 400)], True)])
+def test_operands_on_16_byte_boundaries(lens, fp8):
+    cache = make(lens, 16, 2, 128, fp8)
+    n = sum(x for x, _ in lens)
+    q = queries(n, 16, 128)
+    want, lse = api.paged_attn(cache, q)
+    buffers = [torch.zeros(n * 16 * 128 + 8, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    moved, out = [b[8:].view(n, 16, 128) for b in buffers]
+    moved.copy_(q)
+    assert moved.data_ptr() % 32 == 16 and out.data_ptr() % 32 == 16
+    got, lse2 = api.paged_attn(cache, moved, out=out)
+    assert torch.equal(got, want) and torch.equal(lse, lse2)
+    check(cache, q, got, lse)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("lens,fp8", [([(40, 3000), (1, 900)], False), ([(40, 3000), (1, 900)], True), ([(1, 3000), (1, 900)], True)])
 def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_right(lens, fp8):
     cache = make(lens, 16, 2, 128, fp8)
