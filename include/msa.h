@@ -427,7 +427,7 @@ typedef struct {
  * n_q_heads * d: slices of a fused projection need no copy), likewise k; outputs are dense.
  * Weights are d bf16, or d fp32 with weight_fp32 = 1.  Sums and products are fp32, rounded once.
  * positions: int64 [n_tokens], any value (NULL allowed when nothing rotates).  Either tensor
- * may be absent (0 heads).  An output may be its own input when that one is dense.
+ * may be absent (0 heads; at most 1024).  An output may be its own input when that one is dense.
  */
 msa_status_t msa_qk_norm_rope(const msa_rope_t* rope, const void* q, int64_t q_stride, int32_t n_q_heads,
                               const void* q_weight, const void* k, int64_t k_stride, int32_t n_k_heads,
@@ -509,7 +509,7 @@ msa_status_t msa_paged_append(const msa_paged_cache_t* cache, const msa_rope_t* 
  * head_dim = 128 with pages of a multiple of 8 tokens and groups of at most 128 heads runs on the
  * tensor cores: P is rounded to bf16 before P V, as in Eq. 8's calls; on fp8 caches the products run
  * in fp16 (K and V exact, any Q, P to 2^-11 of itself or 2^-35 of its row's largest).  Other shapes
- * run on a generic kernel in fp32.
+ * (d a multiple of 8 up to 256, at most 1024 query heads) run on a generic kernel in fp32.
  * workspace (256-byte aligned) >= msa_paged_attn_workspace_bytes.  Of `cache`, that query reads the
  * sizes only.
  */

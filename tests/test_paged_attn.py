@@ -113,6 +113,8 @@ CASES = [  # lens (new, old), page, query heads per KV head, KV heads, d, fp8
     ([(5, 300)] + [(0, 4)] * 4, 64, 16, 1, 128, True),
     ([(3, 40), (0, 9), (7, 1000), (16, 0), (1, 64), (0, 0), (17, 512)], 16, 8, 2, 128, False),
     ([(3, 40), (0, 9), (7, 1000), (16, 0), (1, 64), (0, 0), (17, 512)], 48, 8, 2, 128, True),
+    ([(1 + i % 3 // 2, i % 150) for i in range(700)], 16, 8, 1, 128, False),   # more sequences than threads
+    ([(1, i % 150) for i in range(700)], 16, 8, 1, 128, True),
     ([(32, 0)], 64, 8, 1, 128, False),                                 # both contexts full
     ([(33, 0)], 64, 8, 1, 128, False),                                 # and one token more
     ([(1000, 0)], 64, 8, 2, 128, False),
