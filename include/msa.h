@@ -498,9 +498,9 @@ msa_status_t msa_paged_append(const msa_paged_cache_t* cache, const msa_rope_t* 
 /*
  * Dense causal attention of the new tokens over the cache, which already holds their own keys and
  * values (msa_paged_append): query head h of new token i of sequence s uses KV head h / G and sees
- * tokens 0 .. kv_lens[s] - (cu_q[s+1] - cu_q[s]) + i.  q, out [n_tokens, n_q_heads, d] bf16 dense,
- * lse [n_tokens, n_q_heads] fp32 or NULL (natural log).  softmax_scale 0 = 1/sqrt(d).  A token that
- * sees nothing gets zeros and -inf.  K and V of visible tokens must be finite (a value that is not
+ * tokens 0 .. kv_lens[s] - (cu_q[s+1] - cu_q[s]) + i.  n_tokens >= cu_q[batch]; q, out [n_tokens,
+ * n_q_heads, d] bf16 dense; lse [n_tokens, n_q_heads] fp32 or NULL (natural log).  softmax_scale 0 =
+ * 1/sqrt(d).  A token that sees nothing gets zeros and -inf.  K and V of visible tokens must be finite (a value that is not
  * would reach other tokens of its 128-key tile); what the pages hold behind kv_lens[s] is not read
  * into the result.  Sequences may be ragged and mixed, from one token on a long cache to long
  * chunks: work is split evenly over the device and split tiles are merged in a fixed order, so equal

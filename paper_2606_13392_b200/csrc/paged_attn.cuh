@@ -54,11 +54,11 @@ __host__ __device__ __forceinline__ int64_t paged_cap(const PagedView& c) { retu
 
 __host__ __device__ __forceinline__ PagedSeq paged_seq(const PagedAttnArgs& a, int s) {
     PagedSeq q;
-    const int lo = max(a.c.cu_q[s], 0), hi = min(a.c.cu_q[s + 1], a.n_tokens);
+    const int lo = max(a.c.cu_q[s], 0), end = a.c.cu_q[s + 1], hi = min(end, a.n_tokens);  // (rows that are not there: none)
     q.q_row = lo;
     q.q_len = max(hi - lo, 0);
     q.kv = (int)min((int64_t)max(a.c.kv_lens[s], 0), paged_cap(a.c));
-    q.base = q.kv - q.q_len;  // position of the first new token
+    q.base = q.kv - max(end - lo, 0);  // position of the first new token
     q.tile_tokens = q.q_len <= a.TPT ? a.TPT : a.tile_tokens;
     q.n_tiles = (q.q_len + q.tile_tokens - 1) / q.tile_tokens;
     return q;
@@ -887,7 +887,7 @@ paged_attn_generic_kernel(PagedAttnArgs a, const __nv_bfloat16* __restrict__ q, 
     const int len = a.c.kv_lens[s];
     if ((len < 0 || len > cap) && lane == 0) report_async(status, kAsyncBadIndex, 0x601);
     const int64_t kv = min((int64_t)max(len, 0), cap);
-    const int64_t pos = kv - (min(a.c.cu_q[s + 1], a.n_tokens) - i);
+    const int64_t pos = kv - (a.c.cu_q[s + 1] - i);
     for (int c = lane; c < d; c += 32) qs[warp][c] = __bfloat162float(q[unit * d + c]) * a.scale_log2e;
     __syncwarp();
     float m = -INFINITY, l = 0.f, o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
