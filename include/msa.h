@@ -436,6 +436,14 @@ msa_status_t msa_qk_norm_rope(const msa_rope_t* rope, const void* q, int64_t q_s
                               msa_stream_t stream);
 
 /*
+ * The launch shape of msa_qk_norm_rope (n_v_heads = 0) and msa_paged_append on the current device (a query for tests and
+ * tuning): a CTA prepares *tile_tokens tokens at a time, *ctas CTAs share the tokens and *parts a token's heads,
+ * *shared_bytes is a CTA's dynamic shared memory.  Any pointer may be NULL.  Launches nothing.
+ */
+msa_status_t msa_norm_rope_plan(int32_t head_dim, int32_t n_q_heads, int32_t n_k_heads, int32_t n_v_heads, int64_t n_tokens,
+                                int32_t* tile_tokens, int32_t* ctas, int32_t* parts, int32_t* shared_bytes);
+
+/*
  * Gradients of msa_qk_norm_rope: dq_out, dk_out (rows every dq_stride / dk_stride elements) are
  * the gradients of its outputs; dq, dk (bf16, dense) those of its inputs; dq_weight, dk_weight
  * (fp32 [d]; may be NULL, and untouched without a weight) those of its weights, summed over

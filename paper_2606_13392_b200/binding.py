@@ -33,7 +33,7 @@ EXPORTS = [
     "msa_prefill_forward_varlen_workspace_bytes", "msa_prefill_forward_host",
     "msa_prefill_forward_host_workspace_bytes", "msa_decode_forward", "msa_decode_forward_host",
     "msa_launch_count", "msa_profile_begin", "msa_profile_end", "msa_index_scores_plan", "msa_debug_set_wait",
-    "msa_qk_norm_rope", "msa_qk_norm_rope_backward", "msa_qk_norm_rope_backward_workspace_bytes", "msa_paged_append",
+    "msa_qk_norm_rope", "msa_norm_rope_plan", "msa_qk_norm_rope_backward", "msa_qk_norm_rope_backward_workspace_bytes", "msa_paged_append",
     "msa_paged_attn", "msa_paged_attn_workspace_bytes",
 ]
 
@@ -504,6 +504,15 @@ def msa_qk_norm_rope(freqs, interleaved, mscale, q, q_weight, k, k_weight, eps, 
     _launch(index, "msa_qk_norm_rope", _ref(rope), _at(q), qs, hq, _at(q_weight), _at(k), ks, hk, _at(k_weight), d, w32, eps,
             _positions(positions, rows, index), rows, _at(q_out), _at(k_out), stream=stream)
     return q_out, k_out
+
+
+def msa_norm_rope_plan(head_dim: int, n_q_heads: int, n_k_heads: int, n_v_heads: int, n_tokens: int) -> Tuple[int, int, int, int]:
+    """(tokens of a tile, CTAs along the tokens, CTAs along a token's heads, dynamic shared memory) of a rotation or an
+    append on the current device."""
+    out = [c_i32(0) for _ in range(4)]
+    _check(lib().msa_norm_rope_plan(c_i32(head_dim), c_i32(n_q_heads), c_i32(n_k_heads), c_i32(n_v_heads), c_i64(n_tokens),
+                                    *[ctypes.byref(o) for o in out]), "msa_norm_rope_plan")
+    return tuple(int(o.value) for o in out)
 
 
 def msa_qk_norm_rope_backward_workspace_bytes(head_dim: int, n_tokens: int) -> int:

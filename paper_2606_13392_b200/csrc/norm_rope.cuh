@@ -26,6 +26,15 @@ constexpr int kRopeThreads = 256;
 constexpr int kRopeWarps = kRopeThreads / 32;
 constexpr int kRopeMaxTile = 32;  // tokens a CTA prepares at a time
 
+// Shared memory of a token's coefficients: two sets of 16 floats a lane.  A launch gets 48 KB, the positions and places of
+// the tile's tokens included; more would have to be asked for and would cost the CTAs side by side that hide latencies.
+constexpr int rope_token_bytes(int lanes_per_head) { return 2 * lanes_per_head * 16 * (int)sizeof(float); }
+constexpr int rope_tile_limit(int lanes_per_head) { return kRopeMaxTile * 8 / lanes_per_head; }
+constexpr int kRopeStaticBytes = kRopeMaxTile * 2 * (int)sizeof(int64_t);
+static_assert(rope_tile_limit(8) * rope_token_bytes(8) + kRopeStaticBytes <= 48 * 1024 &&
+              rope_tile_limit(16) * rope_token_bytes(16) + kRopeStaticBytes <= 48 * 1024 &&
+              rope_tile_limit(32) * rope_token_bytes(32) + kRopeStaticBytes <= 48 * 1024, "shared memory of a launch");
+
 struct RopeArgs {
     const double* freqs;  // [rot/2] radians per position, or null (no rotation)
     int rot, interleaved;

@@ -67,27 +67,34 @@ constexpr int kMaxRopeHeads = 1024;
 // Lanes reserved for a head.
 static int lanes_per_head(int d) { return d <= 64 ? 8 : (d <= 128 ? 16 : 32); }
 
+// Launch shape.  Many tokens: as many a CTA at a time as make about nine items a warp (eight of 64 + 8 heads of 128), so
+// that the angles' latency is paid once for them, within the shared memory of a launch.  Few: one a CTA, its items spread
+// over CTAs until the machine has four CTAs per SM (each repeats the token's angles).  At most twice the CTAs that are
+// resident: the second half evens out the rounds.
+struct RopeGrid { int tile, per; dim3 grid; size_t smem; };
+static RopeGrid rope_grid(int d, int H_q, int H_k, int H_v, int64_t n) {
+    const int lanes = lanes_per_head(d), run = 4 * (32 / lanes);
+    const int items = (H_q + run - 1) / run + (H_k + run - 1) / run + (H_v + run - 1) / run;
+    const int64_t want = 4LL * sm_count();
+    RopeGrid g;
+    g.tile = rope_tile_limit(lanes);
+    while (g.tile > 1 && (g.tile * items > 9 * kRopeWarps || ceil_div64(n, g.tile) < want * 3 / 4)) g.tile /= 2;
+    const int64_t tiles = ceil_div64(n, g.tile);
+    const int parts = tiles >= want ? 1 : (int)std::min<int64_t>(items, ceil_div64(want, tiles));
+    g.per = (items + parts - 1) / parts;
+    g.grid = dim3((unsigned)std::min<int64_t>(tiles, 2 * want), (items + g.per - 1) / g.per);
+    g.smem = (size_t)g.tile * rope_token_bytes(lanes);
+    return g;
+}
+
 template <int LPH, bool EXACT, bool APPEND, bool F8>
 static void launch_norm_rope(const RopeArgs& rp, const RopeHeads& q, const RopeHeads& k, const RopeHeads& v, int64_t n,
                              int d, float eps, bool w32, const int64_t* positions, const PagedView& cache, void* k_pool,
                              void* v_pool, cudaStream_t st) {
-    // Many tokens: as many a CTA at a time as make about nine items a warp (eight of 64 + 8 heads of 128), so that the
-    // angles' latency is paid once for them.  Few: one a CTA, its items spread over CTAs until the machine has four CTAs
-    // per SM (each repeats the token's angles).  At most twice the CTAs that are resident: the second half evens out the
-    // rounds.
-    const int run = 4 * (32 / LPH);
-    const int items = (q.n_heads + run - 1) / run + (k.n_heads + run - 1) / run + (v.n_heads + run - 1) / run;
-    const int64_t want = 4LL * sm_count();
-    int tile = kRopeMaxTile;
-    while (tile > 1 && (tile * items > 9 * kRopeWarps || ceil_div64(n, tile) < want * 3 / 4)) tile /= 2;
-    const int64_t tiles = ceil_div64(n, tile);
-    const int parts = tiles >= want ? 1 : (int)std::min<int64_t>(items, ceil_div64(want, tiles));
-    const int per = (items + parts - 1) / parts;
-    const dim3 grid((unsigned)std::min<int64_t>(tiles, 2 * want), (items + per - 1) / per);
-    const size_t smem = (size_t)tile * 2 * LPH * 16 * sizeof(float);
+    const RopeGrid g = rope_grid(d, q.n_heads, k.n_heads, v.n_heads, n);
     StageScope sc(kStageNone, st);
-    norm_rope_kernel<LPH, EXACT, APPEND, F8><<<grid, kRopeThreads, smem, st>>>(rp, q, k, v, n, d, eps, w32, positions, tile, per, cache,
-                                                                             k_pool, v_pool, APPEND ? status_word() : nullptr);
+    norm_rope_kernel<LPH, EXACT, APPEND, F8><<<g.grid, kRopeThreads, g.smem, st>>>(rp, q, k, v, n, d, eps, w32, positions, g.tile, g.per,
+                                                                                 cache, k_pool, v_pool, APPEND ? status_word() : nullptr);
 }
 
 template <bool APPEND, bool F8>
@@ -284,6 +291,20 @@ msa_status_t msa_qk_norm_rope(const msa_rope_t* rope, const void* q, int64_t q_s
     const RopeHeads kh{(const __nv_bfloat16*)k, k_stride, n_k_heads, k_weight, (__nv_bfloat16*)k_out};
     return run_norm_rope<false, false>(rp, qh, kh, RopeHeads{}, n_tokens, head_dim, eps, w32, positions, PagedView{}, nullptr,
                                        nullptr, (cudaStream_t)stream);
+}
+
+msa_status_t msa_norm_rope_plan(int32_t head_dim, int32_t n_q_heads, int32_t n_k_heads, int32_t n_v_heads, int64_t n_tokens,
+                                int32_t* tile_tokens, int32_t* ctas, int32_t* parts, int32_t* shared_bytes) {
+    if (head_dim <= 0 || n_q_heads < 0 || n_k_heads < 0 || n_v_heads < 0 || n_tokens <= 0) return MSA_ERR_INVALID_ARG;
+    if ((int64_t)n_q_heads + n_k_heads + n_v_heads == 0) return MSA_ERR_INVALID_ARG;
+    if (head_dim % 8 != 0 || head_dim > 256 || n_q_heads > kMaxRopeHeads || n_k_heads > kMaxRopeHeads || n_v_heads > kMaxRopeHeads)
+        return MSA_ERR_UNSUPPORTED;
+    const RopeGrid g = rope_grid(head_dim, n_q_heads, n_k_heads, n_v_heads, n_tokens);
+    if (tile_tokens) *tile_tokens = g.tile;
+    if (ctas) *ctas = (int32_t)g.grid.x;
+    if (parts) *parts = (int32_t)g.grid.y;
+    if (shared_bytes) *shared_bytes = (int32_t)g.smem;
+    return MSA_OK;
 }
 
 msa_status_t msa_qk_norm_rope_backward_workspace_bytes(int32_t head_dim, int64_t n_tokens, size_t* min_bytes) {
