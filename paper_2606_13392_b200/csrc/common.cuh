@@ -85,6 +85,15 @@ __device__ __forceinline__ float warp_sum(float v) {
 
 inline int64_t ceil_div64(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// What a call returns when a CUDA call or launch of its own failed.  The runtime keeps an error until it is read: left there,
+// it would be taken for the failure of the next launch, whoever makes it.
+inline msa_status_t cuda_failed() {
+    cudaGetLastError();
+    return MSA_ERR_CUDA;
+}
+// Status of the launches just made.
+inline msa_status_t launch_status() { return cudaGetLastError() == cudaSuccess ? MSA_OK : MSA_ERR_CUDA; }
+
 int* async_status_ptr();  // device address of the status word of the current device
 bool paged_set_wait(long long limit, long long late);  // msa_debug_set_wait for the kernels of paged.cu
 

@@ -98,10 +98,6 @@ static msa_status_t check_range(int64_t q_begin, int64_t q_count, int64_t kv_len
 static int sm_count();
 static int current_device();
 
-static msa_status_t launch_status() {
-    return cudaPeekAtLastError() == cudaSuccess ? MSA_OK : MSA_ERR_CUDA;
-}
-
 // ---------------------------------------------------------------------- tensor maps
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
@@ -163,16 +159,16 @@ static msa_status_t launch_index_tc(const Resolved& r, const void* q_idx, const 
     const uint64_t ks[1] = {row_b};
     const uint32_t kb[2] = {64, kIdxTileK};
     if (!encode_tmap_bf16(&tm_q, q_idx, 3, qd, qs, qb) || !encode_tmap_bf16(&tm_k, k_idx, 2, kd, ks, kb))
-        return MSA_ERR_CUDA;
+        return cuda_failed();
     int* status = async_status_ptr();
-    if (status == nullptr) return MSA_ERR_CUDA;
+    if (status == nullptr) return cuda_failed();
     const size_t smem = sizeof(IdxSmem<NH, DI, ST, RUNL>) + 1024;
     static bool attr_set_dev[64] = {false};  // the attribute is per device
     const int dev_id = current_device();
     if (!attr_set_dev[dev_id]) {
         if (cudaFuncSetAttribute(index_scores_tc_kernel<BK, NH, DI, ST, FK, F8, RUNL>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                  (int)smem) != cudaSuccess)
-            return MSA_ERR_CUDA;
+            return cuda_failed();
         attr_set_dev[dev_id] = true;
     }
     // (a packed batch: q_count and kv_len are the batch's rows, for the tensor maps; the grid follows the tile list)
@@ -334,7 +330,7 @@ static msa_status_t run_topk(const Resolved& r, const float* scores, int64_t ld_
     if (grid > 2147483647LL) return MSA_ERR_UNSUPPORTED;
     const dim3 g((unsigned)grid), b(kTopkWarps * 32);
     int* status = async_status_ptr();
-    if (status == nullptr) return MSA_ERR_CUDA;
+    if (status == nullptr) return cuda_failed();
     StageScope sc(kStageTopk, st);
     if (r.k <= 32)
         topk_select_kernel<1><<<g, b, 0, st>>>(scores, ld_scores, rows, n_rows, r.H_kv, r.B_k, r.k, block_idx, status, lnb);
@@ -353,7 +349,7 @@ static msa_status_t run_attn_generic(const Resolved& r, const void* q, const voi
     const int64_t grid = n_q * r.H_kv;
     if (grid > 2147483647LL) return MSA_ERR_UNSUPPORTED;
     int* status = async_status_ptr();
-    if (status == nullptr) return MSA_ERR_CUDA;
+    if (status == nullptr) return cuda_failed();
     const size_t smem = sizeof(float) * (size_t)r.G * r.d;
     {
         StageScope sc(rows.seq_lens ? kStageAttnDecode : kStageAttn, st);
@@ -435,15 +431,17 @@ static int64_t attn_range_for(const Resolved& r, int64_t q_count, int64_t kv_len
 
 static int current_device() {
     int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) dev = 0;
-    return dev;
+    if (cudaGetDevice(&dev) != cudaSuccess) cuda_failed();
+    return dev < 0 || dev >= 64 ? 0 : dev;
 }
 
 static int sm_count() {
     static int n[64] = {0};  // per device
     const int dev = current_device();
-    if (n[dev] == 0 && cudaDeviceGetAttribute(&n[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    if (n[dev] == 0 && cudaDeviceGetAttribute(&n[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+        cuda_failed();
         n[dev] = 148;
+    }
     return n[dev];
 }
 
@@ -477,7 +475,7 @@ static msa_status_t wait_rows(const HostInHook& h, int64_t last_row, cudaStream_
     if (!h.on) return MSA_OK;
     int piece = (int)(last_row / h.piece_rows);
     if (piece >= h.n_pieces) piece = h.n_pieces - 1;
-    return cudaStreamWaitEvent(st, h.ev[piece], 0) == cudaSuccess ? MSA_OK : MSA_ERR_CUDA;
+    return cudaStreamWaitEvent(st, h.ev[piece], 0) == cudaSuccess ? MSA_OK : cuda_failed();
 }
 // Uploads `rows` rows of `row_bytes` each in pieces on the copy stream, an event after each piece.
 static msa_status_t upload_in_pieces(HostInHook& h, char* dst, const void* src, int64_t rows, size_t row_bytes,
@@ -489,7 +487,7 @@ static msa_status_t upload_in_pieces(HostInHook& h, char* dst, const void* src, 
     for (int i = 0; i < h.n_pieces; ++i) {
         const int64_t r0 = (int64_t)i * piece, n = (rows - r0) < piece ? (rows - r0) : piece;
         if (i >= h.created[dev]) {
-            if (cudaEventCreateWithFlags(&h.own[dev][i], cudaEventDisableTiming) != cudaSuccess) return MSA_ERR_CUDA;
+            if (cudaEventCreateWithFlags(&h.own[dev][i], cudaEventDisableTiming) != cudaSuccess) return cuda_failed();
             h.created[dev] = i + 1;
         }
         h.ev[i] = h.own[dev][i];
@@ -497,7 +495,7 @@ static msa_status_t upload_in_pieces(HostInHook& h, char* dst, const void* src, 
             cudaMemcpyAsync(dst + (size_t)r0 * row_bytes, (const char*)src + (size_t)r0 * row_bytes, (size_t)n * row_bytes,
                             cudaMemcpyHostToDevice, copy) != cudaSuccess ||
             cudaEventRecord(h.ev[i], copy) != cudaSuccess)
-            return MSA_ERR_CUDA;
+            return cuda_failed();
     }
     return MSA_OK;
 }
@@ -523,15 +521,15 @@ static msa_status_t hook_copy_rows(const Resolved& r, const void* out, const flo
     HostOutHook& h = g_out_hook;
     cudaEvent_t e = next_sync_event();
     if (e == nullptr || cudaEventRecord(e, st) != cudaSuccess || cudaStreamWaitEvent(h.copy, e, 0) != cudaSuccess)
-        return MSA_ERR_CUDA;
+        return cuda_failed();
     const size_t rb = (size_t)r.H_q * r.d * 2;
     if (cudaMemcpyAsync(h.out_host + (size_t)row0 * rb, (const char*)out + (size_t)row0 * rb, (size_t)rows * rb,
                         cudaMemcpyDeviceToHost, h.copy) != cudaSuccess)
-        return MSA_ERR_CUDA;
+        return cuda_failed();
     if (h.lse_host && lse &&
         cudaMemcpyAsync(h.lse_host + row0 * r.H_q, lse + row0 * r.H_q, (size_t)rows * r.H_q * 4,
                         cudaMemcpyDeviceToHost, h.copy) != cudaSuccess)
-        return MSA_ERR_CUDA;
+        return cuda_failed();
     h.rows_copied = row0 + rows;
     return MSA_OK;
 }
@@ -576,7 +574,7 @@ static msa_status_t run_attn_prefill_tc(const Resolved& r, const void* q, const 
         // (128-byte rows whose neighbours in memory are other heads' rows: no 256-byte L2 promotion)
         if (!encode_tmap_bf16(&tm_q, q, 3, qd, qs, qb) || !encode_tmap_bf16(&tm_k, k, 3, kd, ks, kb, true) ||
             !encode_tmap_bf16(&tm_v, v, 3, kd, ks, kb, true))
-            return MSA_ERR_CUDA;
+            return cuda_failed();
     } else {
         // Q as (64 d, 8 heads, 2 d halves, H_q/8 head groups, query): one box is a query's G heads.
         const uint64_t qd[5] = {64, 8, 2, (uint64_t)r.H_q / 8, (uint64_t)q_count};
@@ -587,17 +585,17 @@ static msa_status_t run_attn_prefill_tc(const Resolved& r, const void* q, const 
         const uint32_t kb[3] = {64, 1, (uint32_t)BK};
         if (!encode_tmap_bf16(&tm_q, q, 5, qd, qs, qb) || !encode_tmap_bf16(&tm_k, k, 3, kd, ks, kb) ||
             !encode_tmap_bf16(&tm_v, v, 3, kd, ks, kb))
-            return MSA_ERR_CUDA;
+            return cuda_failed();
     }
     int* status = async_status_ptr();
-    if (status == nullptr) return MSA_ERR_CUDA;
+    if (status == nullptr) return cuda_failed();
     const size_t smem = sizeof(AttnSmem<BK>) + 1024;
     static bool attr_set_dev[64] = {false};  // the attribute is per device
     const int dev_id = current_device();
     if (!attr_set_dev[dev_id]) {
         if (cudaFuncSetAttribute(attn_prefill_tc_kernel<BK, G, F8>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                  (int)smem) != cudaSuccess)
-            return MSA_ERR_CUDA;
+            return cuda_failed();
         attr_set_dev[dev_id] = true;
     }
     const float scale_log2e = r.softmax_scale * 1.4426950408889634f;
@@ -612,7 +610,7 @@ static msa_status_t run_attn_prefill_tc(const Resolved& r, const void* q, const 
         p.row_pos = pk.row_pos; p.row_blk0 = pk.row_blk0; p.blk_row0 = pk.blk_row0;
         const int n_tiles = p.n_blocks * r.H_kv;
         const unsigned eg = (unsigned)ceil_div64((int64_t)p.q_count * r.H_kv, 8);  // 8 warps (rows) per CTA
-        if (cudaMemsetAsync(cnt, 0, (size_t)(n_tiles + 1) * 4, st) != cudaSuccess) return MSA_ERR_CUDA;
+        if (cudaMemsetAsync(cnt, 0, (size_t)(n_tiles + 1) * 4, st) != cudaSuccess) return cuda_failed();
         {
             StageScope sc(kStageSchedule, st);
             revidx_kernel<BK><<<eg, 256, 0, st>>>(block_idx, p, 0, cnt, tile_off, rank, handles, status);
@@ -626,7 +624,7 @@ static msa_status_t run_attn_prefill_tc(const Resolved& r, const void* q, const 
             revidx_kernel<BK><<<eg, 256, 0, st>>>(block_idx, p, 1, cnt, tile_off, rank, handles, status);
         }
         if (q_begin == 0 && wait_rows(g_in_hook, q_first + p.q_count - 1, st) != MSA_OK)  // the range's Q rows
-            return MSA_ERR_CUDA;
+            return cuda_failed();
         {
             StageScope sc(kStageAttn, st);
             attn_prefill_tc_kernel<BK, G, F8><<<grid_attn, kAttnThreads, smem, st>>>(
@@ -637,7 +635,7 @@ static msa_status_t run_attn_prefill_tc(const Resolved& r, const void* q, const 
             combine_kernel<BK, G><<<(unsigned)(p.q_count * r.H_kv), G * 16, 0, st>>>(
                 block_idx, p, o_buf, lse_buf, (__nv_bfloat16*)out, lse);
         }
-        if (cudaPeekAtLastError() != cudaSuccess) return MSA_ERR_CUDA;
+        if (launch_status() != MSA_OK) return MSA_ERR_CUDA;
         if (g_out_hook.on && q_begin == 0 && g_out_hook.rows_copied == q_first) {
             const msa_status_t hs = hook_copy_rows(r, out, lse, q_first, p.q_count, st);
             if (hs != MSA_OK) return hs;
@@ -698,9 +696,9 @@ static msa_status_t run_attn_decode_tc(const Resolved& r, const void* q, const v
     const uint64_t ks[2] = {row_b, (uint64_t)r.H_kv * row_b};
     const uint32_t kb[3] = {64, 1, (uint32_t)BK};
     if (!encode_tmap_bf16(&tm_k, k_cache, 3, kd, ks, kb, KV8) || !encode_tmap_bf16(&tm_v, v_cache, 3, kd, ks, kb, KV8))
-        return MSA_ERR_CUDA;
+        return cuda_failed();
     int* status = async_status_ptr();
-    if (status == nullptr) return MSA_ERR_CUDA;
+    if (status == nullptr) return cuda_failed();
     const size_t smem = (KV8 ? sizeof(DecKv8Smem<BK>) : sizeof(DecSmem<BK>)) + 1024;
     static bool attr_set_dev[64] = {false};  // the attribute is per device
     const int dev_id = current_device();
@@ -708,7 +706,7 @@ static msa_status_t run_attn_decode_tc(const Resolved& r, const void* q, const v
         const cudaError_t e =
             KV8 ? cudaFuncSetAttribute(attn_decode_kv8_kernel<BK, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)
                 : cudaFuncSetAttribute(attn_decode_kernel<BK, G>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-        if (e != cudaSuccess) return MSA_ERR_CUDA;
+        if (e != cudaSuccess) return cuda_failed();
         attr_set_dev[dev_id] = true;
     }
     DecParams p;
@@ -780,14 +778,14 @@ static msa_status_t run_index_lse(const Resolved& r, const void* q_idx, const vo
     uint32_t* rank = (uint32_t*)(w + pl.off_rank);
     float* part = (float*)(w + pl.off_part);
     int* status = async_status_ptr();
-    if (status == nullptr) return MSA_ERR_CUDA;
+    if (status == nullptr) return cuda_failed();
     const size_t smem = (size_t)(BK + 2 * kLseItemQueries) * DIDX * 2 + 2 * kLseItemQueries * 4 + 1024;
     static bool attr_set_dev[64] = {false};  // the attribute is per device
     const int dev_id = current_device();
     if (!attr_set_dev[dev_id]) {
         if (cudaFuncSetAttribute(index_lse_kernel<BK, DIDX>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) !=
             cudaSuccess)
-            return MSA_ERR_CUDA;
+            return cuda_failed();
         attr_set_dev[dev_id] = true;
     }
     const float scale_log2e = r.index_scale * 1.4426950408889634f;
@@ -802,7 +800,7 @@ static msa_status_t run_index_lse(const Resolved& r, const void* q_idx, const vo
         p.H_kv = r.H_kv; p.top_k = r.k;
         const int n_tiles = p.n_blocks * r.H_kv;
         const unsigned eg = (unsigned)ceil_div64((int64_t)p.q_count * r.H_kv, 8);  // 8 warps (rows) per CTA
-        if (cudaMemsetAsync(cnt, 0, (size_t)(n_tiles + 1) * 4, st) != cudaSuccess) return MSA_ERR_CUDA;
+        if (cudaMemsetAsync(cnt, 0, (size_t)(n_tiles + 1) * 4, st) != cudaSuccess) return cuda_failed();
         {
             StageScope sc(kStageSchedule, st);
             revidx_kernel<BK><<<eg, 256, 0, st>>>(block_idx, p, 0, cnt, tile_off, rank, handles, status);
@@ -825,7 +823,7 @@ static msa_status_t run_index_lse(const Resolved& r, const void* q_idx, const vo
             StageScope sc(kStageIndexLse, st);
             index_lse_reduce_kernel<BK><<<eg, 256, 0, st>>>(block_idx, p, part, lse_idx);
         }
-        if (cudaPeekAtLastError() != cudaSuccess) return MSA_ERR_CUDA;
+        if (launch_status() != MSA_OK) return MSA_ERR_CUDA;
     }
     return MSA_OK;
 }
@@ -855,7 +853,7 @@ msa_status_t msa_profile_begin(void) {
     if (!g_prof_created) {
         for (int i = 0; i < kProfSlots; ++i)
             for (int j = 0; j < 2; ++j)
-                if (cudaEventCreate(&g_prof_ev[i][j]) != cudaSuccess) return MSA_ERR_CUDA;
+                if (cudaEventCreate(&g_prof_ev[i][j]) != cudaSuccess) return cuda_failed();
         g_prof_created = true;
     }
     g_prof_used = 0;
@@ -865,14 +863,14 @@ msa_status_t msa_profile_begin(void) {
 
 msa_status_t msa_profile_end(float* stage_ms_host, int64_t* stage_launches_host) {
     g_prof_on = false;
-    if (cudaDeviceSynchronize() != cudaSuccess) return MSA_ERR_CUDA;
+    if (cudaDeviceSynchronize() != cudaSuccess) return cuda_failed();
     for (int i = 0; i < kNumStages; ++i) {
         if (stage_ms_host) stage_ms_host[i] = 0.f;
         if (stage_launches_host) stage_launches_host[i] = 0;
     }
     for (int i = 0; i < g_prof_used; ++i) {
         float ms = 0.f;
-        if (cudaEventElapsedTime(&ms, g_prof_ev[i][0], g_prof_ev[i][1]) != cudaSuccess) return MSA_ERR_CUDA;
+        if (cudaEventElapsedTime(&ms, g_prof_ev[i][0], g_prof_ev[i][1]) != cudaSuccess) return cuda_failed();
         if (stage_ms_host) stage_ms_host[g_prof_stage[i]] += ms;
         if (stage_launches_host) stage_launches_host[g_prof_stage[i]] += 1;
     }
@@ -883,10 +881,10 @@ msa_status_t msa_profile_end(float* stage_ms_host, int64_t* stage_launches_host)
 
 msa_status_t msa_check_async_status(int32_t* detail_host) {
     int v = 0;
-    if (cudaMemcpyFromSymbol(&v, g_async_status, sizeof(int)) != cudaSuccess) return MSA_ERR_CUDA;
+    if (cudaMemcpyFromSymbol(&v, g_async_status, sizeof(int)) != cudaSuccess) return cuda_failed();
     if (v != 0) {
         const int zero = 0;
-        if (cudaMemcpyToSymbol(g_async_status, &zero, sizeof(int)) != cudaSuccess) return MSA_ERR_CUDA;
+        if (cudaMemcpyToSymbol(g_async_status, &zero, sizeof(int)) != cudaSuccess) return cuda_failed();
     }
     if (detail_host) *detail_host = v & 0xFFFFFF;
     const int code = v >> 24;
@@ -941,7 +939,7 @@ msa_status_t msa_debug_set_wait(int64_t wait_limit_cycles, int64_t producer_dela
     const long long late = (long long)producer_delay_cycles;
     if (cudaMemcpyToSymbol(g_wait_limit_cycles, &limit, sizeof(limit)) != cudaSuccess ||
         cudaMemcpyToSymbol(g_debug_producer_delay, &late, sizeof(late)) != cudaSuccess || !paged_set_wait(limit, late))
-        return MSA_ERR_CUDA;
+        return cuda_failed();
     return MSA_OK;
 }
 
@@ -1083,7 +1081,7 @@ static msa_status_t widen_kv(const Resolved& r, const void* k, const void* v, in
         StageScope sc(kStageAttn, st);
         e4m3_to_bf16_kernel<<<grid, 256, 0, st>>>((const uint4*)v, (uint4*)vb, n16);
     }
-    return cudaPeekAtLastError() == cudaSuccess ? MSA_OK : MSA_ERR_CUDA;
+    return launch_status();
 }
 
 msa_status_t msa_sparse_attn_prefill(const msa_shape_t* shape, const void* q, const void* k,
@@ -1192,11 +1190,11 @@ static msa_status_t static_scratch_ptr(void** out) {
     constexpr int kMaxDevices = 64;
     static void* cached[kMaxDevices] = {nullptr};
     int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return MSA_ERR_CUDA;
+    if (cudaGetDevice(&dev) != cudaSuccess) return cuda_failed();
     if (dev < 0 || dev >= kMaxDevices) return MSA_ERR_UNSUPPORTED;
     if (cached[dev] == nullptr) {
         void* p = nullptr;
-        if (cudaGetSymbolAddress(&p, g_static_scratch) != cudaSuccess || p == nullptr) return MSA_ERR_CUDA;
+        if (cudaGetSymbolAddress(&p, g_static_scratch) != cudaSuccess || p == nullptr) return cuda_failed();
         cached[dev] = p;
     }
     *out = cached[dev];
@@ -1346,7 +1344,7 @@ static msa_status_t prefill_stages_1_2(const msa_shape_t* shape, const Resolved&
                                        size_t workspace_bytes, msa_stream_t stream) {
     msa_status_t s = MSA_OK;
     if (index_topk_fused_ok(r, T, T)) {  // no score matrix, no chunks
-        if (wait_rows(g_in_idx_hook, T - 1, (cudaStream_t)stream) != MSA_OK) return MSA_ERR_CUDA;
+        if (wait_rows(g_in_idx_hook, T - 1, (cudaStream_t)stream) != MSA_OK) return cuda_failed();
         return run_index_topk_fused(r, q_idx, k_idx, 0, T, T, block_idx, (cudaStream_t)stream);
     }
     const int64_t ld = score_ld(T, r.B_k);
@@ -1359,7 +1357,7 @@ static msa_status_t prefill_stages_1_2(const msa_shape_t* shape, const Resolved&
         const char* qi = static_cast<const char*>(q_idx) + (size_t)q0 * r.H_kv * r.d_idx * r.idx_elt();
         // Only keys up to the chunk's last query are visible, so score that prefix.
         const int64_t kv_vis = q0 + qc;
-        if (wait_rows(g_in_idx_hook, q0 + qc - 1, (cudaStream_t)stream) != MSA_OK) return MSA_ERR_CUDA;
+        if (wait_rows(g_in_idx_hook, q0 + qc - 1, (cudaStream_t)stream) != MSA_OK) return cuda_failed();
         s = run_index_scores(r, qi, k_idx, prefill_rows(q0, kv_vis, r.B_k), qc, scores, ld, (cudaStream_t)stream, runs);
         if (s != MSA_OK) return s;
         s = run_topk(r, scores, ld, prefill_rows(q0, kv_vis, r.B_k), qc, block_idx + (size_t)q0 * r.H_kv * r.k,
@@ -1508,7 +1506,7 @@ msa_status_t msa_prefill_forward_varlen(const msa_shape_t* shape, const void* q,
         // (pageable host memory: the runtime has copied it out when the call returns)
         int32_t* blk_cum = (int32_t*)malloc((size_t)(n_seqs + 1) * 4);
         IdxPackedTile* tiles = (IdxPackedTile*)malloc((size_t)(vp.n_idx_tiles > 0 ? vp.n_idx_tiles : 1) * sizeof(IdxPackedTile));
-        if (!blk_cum || !tiles) { free(blk_cum); free(tiles); return MSA_ERR_CUDA; }
+        if (!blk_cum || !tiles) { free(blk_cum); free(tiles); return cuda_failed(); }
         blk_cum[0] = 0;
         int64_t max_qt = 0;
         for (int32_t i = 0; i < n_seqs; ++i) {
@@ -1536,7 +1534,7 @@ msa_status_t msa_prefill_forward_varlen(const msa_shape_t* shape, const void* q,
             list_tiles(0, n_seqs);
         } else {
             groups = (SeqGroup*)malloc((size_t)n_seqs * sizeof(SeqGroup));
-            if (!groups) { free(blk_cum); free(tiles); return MSA_ERR_CUDA; }
+            if (!groups) { free(blk_cum); free(tiles); return cuda_failed(); }
             group_ld = score_ld(max_qt * kIdxTileQ, r.B_k);
             const int64_t rows_cap = (int64_t)(stage_bytes / (sizeof(float) * (size_t)r.H_kv * (size_t)group_ld));
             int32_t a = 0;
@@ -1566,7 +1564,7 @@ msa_status_t msa_prefill_forward_varlen(const msa_shape_t* shape, const void* q,
                   (n == 0 || cudaMemcpyAsync(tiles_dev, tiles, (size_t)n * sizeof(IdxPackedTile), cudaMemcpyHostToDevice, st) == cudaSuccess);
         free(blk_cum);
         free(tiles);
-        if (!ok) { free(groups); return MSA_ERR_CUDA; }
+        if (!ok) { free(groups); return cuda_failed(); }
     }
     {
         const int64_t work = vp.rows + vp.n_blocks;
@@ -1574,7 +1572,7 @@ msa_status_t msa_prefill_forward_varlen(const msa_shape_t* shape, const void* q,
         StageScope sc(kStageSchedule, st);
         packed_map_kernel<<<grid, 256, 0, st>>>(cu_dev, blk_cum_dev, n_seqs, r.B_k, row_pos, row_blk0, blk_row0);
     }
-    if (cudaPeekAtLastError() != cudaSuccess) { free(groups); return MSA_ERR_CUDA; }
+    if (launch_status() != MSA_OK) { free(groups); return MSA_ERR_CUDA; }
     // tensors of the batch start at its first row
     const char* qb = (const char*)q + row0 * q_row;
     const char* kb = (const char*)k + row0 * kv_row;
@@ -1677,6 +1675,7 @@ msa_status_t msa_prefill_forward_host(const msa_shape_t* shape, const void* q_ho
         // caller's again only once both streams have drained.
         cudaStreamSynchronize((cudaStream_t)stream);
         cudaStreamSynchronize(copy);
+        cuda_failed();  // (whatever they said, s is what failed)
     }
     return s;
 }
@@ -1705,37 +1704,37 @@ static msa_status_t prefill_forward_host_body(const msa_shape_t* shape, const vo
     // while the next one is computed.
     static cudaStream_t copy_dev[64] = {};
     cudaStream_t& copy = copy_dev[current_device()];
-    if (copy == nullptr && cudaStreamCreateWithFlags(&copy, cudaStreamNonBlocking) != cudaSuccess) return MSA_ERR_CUDA;
+    if (copy == nullptr && cudaStreamCreateWithFlags(&copy, cudaStreamNonBlocking) != cudaSuccess) return cuda_failed();
     *copy_used = copy;
     cudaEvent_t e_in = next_sync_event(), e_idx = next_sync_event(), e_kv = next_sync_event();
-    if (!e_in || !e_idx || !e_kv) return MSA_ERR_CUDA;
-    if (cudaEventRecord(e_in, st) != cudaSuccess || cudaStreamWaitEvent(copy, e_in, 0) != cudaSuccess) return MSA_ERR_CUDA;
+    if (!e_in || !e_idx || !e_kv) return cuda_failed();
+    if (cudaEventRecord(e_in, st) != cudaSuccess || cudaStreamWaitEvent(copy, e_in, 0) != cudaSuccess) return cuda_failed();
     const void* src[5] = {q_host, k_host, v_host, q_idx_host, k_idx_host};
     const size_t nbytes[5] = {(size_t)T * r.H_q * r.d * r.q_elt(), (size_t)T * r.H_kv * r.d * r.kv_elt(),
                               (size_t)T * r.H_kv * r.d * r.kv_elt(), (size_t)T * r.H_kv * r.d_idx * r.idx_elt(),
                               (size_t)T * r.d_idx * r.idx_elt()};
     // Order on the copy stream: K_idx, Q_idx, K, V, Q; Q_idx and Q go in pieces with an event after each,
     // so that every scoring chunk and every attention range waits only for its own rows.
-    if (cudaMemcpyAsync(w + off[4], src[4], nbytes[4], cudaMemcpyHostToDevice, copy) != cudaSuccess) return MSA_ERR_CUDA;
-    if (cudaEventRecord(e_idx, copy) != cudaSuccess) return MSA_ERR_CUDA;
+    if (cudaMemcpyAsync(w + off[4], src[4], nbytes[4], cudaMemcpyHostToDevice, copy) != cudaSuccess) return cuda_failed();
+    if (cudaEventRecord(e_idx, copy) != cudaSuccess) return cuda_failed();
     const size_t qi_rb = (size_t)r.H_kv * r.d_idx * r.idx_elt(), q_rb = (size_t)r.H_q * r.d * r.q_elt();
-    if (upload_in_pieces(g_in_idx_hook, w + off[3], src[3], T, qi_rb, 65536, copy) != MSA_OK) return MSA_ERR_CUDA;
+    if (upload_in_pieces(g_in_idx_hook, w + off[3], src[3], T, qi_rb, 65536, copy) != MSA_OK) return cuda_failed();
     for (int i = 1; i <= 2; ++i)
-        if (cudaMemcpyAsync(w + off[i], src[i], nbytes[i], cudaMemcpyHostToDevice, copy) != cudaSuccess) return MSA_ERR_CUDA;
-    if (cudaEventRecord(e_kv, copy) != cudaSuccess) return MSA_ERR_CUDA;
-    if (upload_in_pieces(g_in_hook, w + off[0], src[0], T, q_rb, 16384, copy) != MSA_OK) return MSA_ERR_CUDA;
+        if (cudaMemcpyAsync(w + off[i], src[i], nbytes[i], cudaMemcpyHostToDevice, copy) != cudaSuccess) return cuda_failed();
+    if (cudaEventRecord(e_kv, copy) != cudaSuccess) return cuda_failed();
+    if (upload_in_pieces(g_in_hook, w + off[0], src[0], T, q_rb, 16384, copy) != MSA_OK) return cuda_failed();
     float* lse_dev = lse_host ? (float*)(w + off[6]) : nullptr;
     int32_t* bi_dev = (int32_t*)(w + off[7]);
-    if (cudaStreamWaitEvent(st, e_idx, 0) != cudaSuccess) return MSA_ERR_CUDA;
+    if (cudaStreamWaitEvent(st, e_idx, 0) != cudaSuccess) return cuda_failed();
     g_in_idx_hook.on = true;
     s = prefill_stages_1_2(shape, r, w + off[3], w + off[4], T, bi_dev, w + stage, workspace_bytes - stage, stream);
     g_in_idx_hook.on = false;
     if (s != MSA_OK) return s;
-    if (cudaStreamWaitEvent(st, e_kv, 0) != cudaSuccess) return MSA_ERR_CUDA;
+    if (cudaStreamWaitEvent(st, e_kv, 0) != cudaSuccess) return cuda_failed();
     // The tensor-core path waits for Q range by range; any other path waits for all of it here.
     g_in_hook.on = attn_tc_supported(r) && T < 2147483647LL;
     if (!g_in_hook.on && cudaStreamWaitEvent(st, g_in_hook.ev[g_in_hook.n_pieces - 1], 0) != cudaSuccess)
-        return MSA_ERR_CUDA;
+        return cuda_failed();
     g_out_hook.on = true; g_out_hook.copy = copy; g_out_hook.out_host = (char*)out_host;
     g_out_hook.lse_host = lse_host; g_out_hook.rows_copied = 0;
     s = msa_sparse_attn_prefill(shape, w + off[0], w + off[1], w + off[2], bi_dev, 0, T, T, w + off[5], lse_dev,
@@ -1750,8 +1749,8 @@ static msa_status_t prefill_forward_host_body(const msa_shape_t* shape, const vo
     }
     if (block_idx_host &&
         cudaMemcpyAsync(block_idx_host, bi_dev, (size_t)T * r.H_kv * r.k * 4, cudaMemcpyDeviceToHost, st) != cudaSuccess)
-        return MSA_ERR_CUDA;
-    if (cudaStreamSynchronize(st) != cudaSuccess || cudaStreamSynchronize(copy) != cudaSuccess) return MSA_ERR_CUDA;
+        return cuda_failed();
+    if (cudaStreamSynchronize(st) != cudaSuccess || cudaStreamSynchronize(copy) != cudaSuccess) return cuda_failed();
     return MSA_OK;
 }
 
@@ -1788,14 +1787,14 @@ msa_status_t msa_decode_forward_host(const msa_shape_t* shape, const void* q_hos
     if (!q_host || !q_idx_host || !q_dev || !q_idx_dev || !out_dev || !out_host) return MSA_ERR_INVALID_ARG;
     cudaStream_t st = (cudaStream_t)stream;
     const size_t qb = (size_t)batch * r.H_q * r.d * 2, qib = (size_t)batch * r.H_kv * r.d_idx * r.idx_elt();
-    if (cudaMemcpyAsync(q_dev, q_host, qb, cudaMemcpyHostToDevice, st) != cudaSuccess) return MSA_ERR_CUDA;
-    if (cudaMemcpyAsync(q_idx_dev, q_idx_host, qib, cudaMemcpyHostToDevice, st) != cudaSuccess) return MSA_ERR_CUDA;
+    if (cudaMemcpyAsync(q_dev, q_host, qb, cudaMemcpyHostToDevice, st) != cudaSuccess) return cuda_failed();
+    if (cudaMemcpyAsync(q_idx_dev, q_idx_host, qib, cudaMemcpyHostToDevice, st) != cudaSuccess) return cuda_failed();
     s = msa_decode_forward(shape, q_dev, q_idx_dev, k_cache, v_cache, k_idx_cache, cache_tokens,
                            seq_offsets, seq_lens, batch, max_seq_len, scores, ld_scores, block_idx,
                            out_dev, nullptr, workspace, workspace_bytes, stream);
     if (s != MSA_OK) return s;
-    if (cudaMemcpyAsync(out_host, out_dev, qb, cudaMemcpyDeviceToHost, st) != cudaSuccess) return MSA_ERR_CUDA;
-    return cudaStreamSynchronize(st) == cudaSuccess ? MSA_OK : MSA_ERR_CUDA;
+    if (cudaMemcpyAsync(out_host, out_dev, qb, cudaMemcpyDeviceToHost, st) != cudaSuccess) return cuda_failed();
+    return cudaStreamSynchronize(st) == cudaSuccess ? MSA_OK : cuda_failed();
 }
 
 }  // extern "C"

@@ -20,14 +20,17 @@ static bool aligned_to(const void* p, uintptr_t n) { return (reinterpret_cast<ui
 
 static int current_device() {
     int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) dev = 0;
-    return dev;
+    if (cudaGetDevice(&dev) != cudaSuccess) cuda_failed();
+    return dev < 0 || dev >= 64 ? 0 : dev;
 }
 
 static int sm_count() {
     static int n[64] = {0};  // per device
     const int dev = current_device();
-    if (n[dev] == 0 && cudaDeviceGetAttribute(&n[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) n[dev] = 148;
+    if (n[dev] == 0 && cudaDeviceGetAttribute(&n[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+        cuda_failed();
+        n[dev] = 148;
+    }
     return n[dev];
 }
 
@@ -38,8 +41,6 @@ static int* status_word() {
     if (word[dev] == nullptr) word[dev] = async_status_ptr();
     return word[dev];
 }
-
-static msa_status_t launch_status() { return cudaPeekAtLastError() == cudaSuccess ? MSA_OK : MSA_ERR_CUDA; }
 
 // ---------------------------------------------------------------------- norm and rotation
 static msa_status_t resolve_rope(const msa_rope_t* rope, int d, RopeArgs& rp) {
@@ -185,7 +186,7 @@ static msa_status_t launch_paged_combine(const PagedAttnArgs& a, int ctas, cudaS
     cfg.attrs = &early;
     cfg.numAttrs = 1;
     StageScope sc(kStageNone, st);
-    return cudaLaunchKernelEx(&cfg, paged_combine_kernel, a, ctas) == cudaSuccess ? MSA_OK : MSA_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, paged_combine_kernel, a, ctas) == cudaSuccess ? MSA_OK : cuda_failed();
 }
 
 // Calls whose sequences have on average no more rows (new tokens x group) than the small kernel's tiles, on fp8 caches:
@@ -207,21 +208,21 @@ static msa_status_t launch_paged_few8(PagedAttnArgs a, const msa_paged_cache_t& 
     const uint32_t kb[3] = {64, 1, (uint32_t)box};
     int* status = status_word();
     if (!encode_tmap_bf16(&tm_k, c.k, 3, kd, ks, kb, true) || !encode_tmap_bf16(&tm_v, c.v, 3, kd, ks, kb, true) || status == nullptr)
-        return MSA_ERR_CUDA;
+        return cuda_failed();
     const size_t smem = sizeof(FewSmem<HG>);
     static_assert(sizeof(FewSmem<HG>) <= 113 * 1024, "two CTAs per SM");
     static bool attr_set[64] = {false};  // per device
     const int dev = current_device(), grid = kFewCtas * sm_count();
     if (!attr_set[dev]) {
         if (cudaFuncSetAttribute(paged_few8_kernel<HG>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
-            return MSA_ERR_CUDA;
+            return cuda_failed();
         attr_set[dev] = true;
     }
     {
         StageScope sc(kStageNone, st);
         paged_few8_kernel<HG><<<grid, kFewThreads, smem, st>>>(tm_k, tm_v, a, (const __nv_bfloat16*)q, box, 1.0 / grid, status);
     }
-    if (cudaPeekAtLastError() != cudaSuccess) return MSA_ERR_CUDA;
+    if (launch_status() != MSA_OK) return MSA_ERR_CUDA;
     return launch_paged_combine(a, grid, st);
 }
 
@@ -243,13 +244,13 @@ static msa_status_t launch_paged_attn(const PagedAttnArgs& a, const msa_paged_ca
         ok = ok && encode_tmap_bf16(&tm_k, c.k, 5, kd, ks, kb) && encode_tmap_bf16(&tm_v, c.v, 5, kd, ks, kb);
     }
     int* status = status_word();
-    if (!ok || status == nullptr) return MSA_ERR_CUDA;
+    if (!ok || status == nullptr) return cuda_failed();
     const size_t smem = sizeof(PagedSmem);
     static bool attr_set[64] = {false};  // per device
     const int dev = current_device(), grid = sm_count();
     if (!attr_set[dev]) {
         if (cudaFuncSetAttribute(paged_attn_tc_kernel<F8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
-            return MSA_ERR_CUDA;
+            return cuda_failed();
         attr_set[dev] = true;
     }
     // K and V of one (sequence, head) beyond a third of L2: CTAs on different tiles of it should read in step
@@ -258,7 +259,7 @@ static msa_status_t launch_paged_attn(const PagedAttnArgs& a, const msa_paged_ca
         StageScope sc(kStageNone, st);
         paged_attn_tc_kernel<F8><<<grid, paged_threads(F8), smem, st>>>(tm_q, tm_q1, tm_k, tm_v, a, box, snap, 1.0 / grid, status);
     }
-    if (cudaPeekAtLastError() != cudaSuccess) return MSA_ERR_CUDA;
+    if (launch_status() != MSA_OK) return MSA_ERR_CUDA;
     return launch_paged_combine(a, grid, st);
 }
 
@@ -394,7 +395,7 @@ msa_status_t msa_paged_append(const msa_paged_cache_t* cache, const msa_rope_t* 
     if ((v == nullptr) != (cache->v == nullptr)) return MSA_ERR_INVALID_ARG;
     if (v != nullptr && !rows_ok(v, v_stride, H, d)) return MSA_ERR_INVALID_ARG;
     if (!weight_ok(q_weight, w32) || !weight_ok(k_weight, w32)) return MSA_ERR_INVALID_ARG;
-    if (status_word() == nullptr) return MSA_ERR_CUDA;
+    if (status_word() == nullptr) return cuda_failed();
     const RopeHeads qh{(const __nv_bfloat16*)q, q_stride, n_q_heads, q_weight, (__nv_bfloat16*)q_out};
     const RopeHeads kh{(const __nv_bfloat16*)k, k_stride, H, k_weight, nullptr};
     const RopeHeads vh{(const __nv_bfloat16*)v, v_stride, v != nullptr ? H : 0, nullptr, nullptr};
@@ -453,7 +454,7 @@ msa_status_t msa_paged_attn(const msa_paged_cache_t* cache, const void* q, int32
     const int64_t grid = ceil_div64(n_tokens * n_q_heads, 4);
     if (grid > 2147483647LL) return MSA_ERR_UNSUPPORTED;
     int* status = status_word();
-    if (status == nullptr) return MSA_ERR_CUDA;
+    if (status == nullptr) return cuda_failed();
     {
         StageScope sc(kStageNone, st);
         if (cache->fp8) paged_attn_generic_kernel<true><<<(unsigned)grid, 128, 0, st>>>(a, (const __nv_bfloat16*)q, cache->k, cache->v, d, status);
