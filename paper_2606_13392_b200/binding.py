@@ -431,10 +431,18 @@ def _heads(t: torch.Tensor, what: str, head_dim: int, rows: int, index: int, den
     return s[0]
 
 
-def _output(t: Optional[torch.Tensor], other: torch.Tensor, what: str, head_dim: int, rows: int, index: int) -> torch.Tensor:
+def _output(t: Optional[torch.Tensor], other: torch.Tensor, what: str, head_dim: int, rows: int, index: int, stream) -> torch.Tensor:
     """An output of another's shape: dense bf16, made here if there is none."""
     if t is None:
-        return torch.empty_like(other, memory_format=torch.contiguous_format)
+        if stream is None:
+            return torch.empty_like(other, memory_format=torch.contiguous_format)
+        # Memory of the stream that writes it: a block of the current stream may still be in use by work queued there, or
+        # be given to such work while the call runs.  The current stream is where the caller will read it.
+        current = torch.cuda.current_stream(index)
+        with torch.cuda.stream(stream):
+            t = torch.empty_like(other, memory_format=torch.contiguous_format)
+        t.record_stream(current)
+        return t
     if t.shape != other.shape:
         raise ValueError("%s must be %s, got %s" % (what, tuple(other.shape), tuple(t.shape)))
     _heads(t, what, head_dim, rows, index, dense=True)
@@ -495,10 +503,10 @@ def msa_qk_norm_rope(freqs, interleaved, mscale, q, q_weight, k, k_weight, eps, 
     qs = ks = hq = hk = 0
     if q is not None:
         qs, hq = _heads(q, "q", d, rows, index), q.shape[1]
-        q_out = _output(q_out, q, "q_out", d, rows, index)
+        q_out = _output(q_out, q, "q_out", d, rows, index, stream)
     if k is not None:
         ks, hk = _heads(k, "k", d, rows, index), k.shape[1]
-        k_out = _output(k_out, k, "k_out", d, rows, index)
+        k_out = _output(k_out, k, "k_out", d, rows, index, stream)
     w32 = _weights(d, index, q_weight, k_weight)
     rope = _rope(freqs, interleaved, mscale, index)
     _launch(index, "msa_qk_norm_rope", _ref(rope), _at(q), qs, hq, _at(q_weight), _at(k), ks, hk, _at(k_weight), d, w32, eps,
@@ -551,7 +559,7 @@ def msa_qk_norm_rope_backward(freqs, interleaved, mscale, dq_out, dk_out, q, q_w
                 raise ValueError("%s must be %s, got %s" % (n, tuple(dy.shape), tuple(t.shape)))
         elif w is not None:
             raise ValueError("%s is needed for the gradients of its norm" % n)
-        dx = _output(dx, dy, "the gradient of " + n, d, rows, index)
+        dx = _output(dx, dy, "the gradient of " + n, d, rows, index, stream)
         if dw is not None and (dw.dtype != torch.float32 or dw.shape != (d,) or not dw.is_contiguous() or dw.get_device() != index):
             raise ValueError("the gradient of %s_weight must be a contiguous fp32 vector of %d values on cuda:%d" % (n, d, index))
         at.append((ys, ts, dy.shape[1]))
@@ -601,7 +609,7 @@ def msa_paged_append(k_pool, v_pool, page_table, kv_lens, cu_q, freqs, interleav
         raise ValueError("k and v must have the cache's %d heads" % cache.n_kv_heads)
     if q is not None:
         qs, hq = _heads(q, "q", d, rows, index), q.shape[1]
-        q_out = _output(q_out, q, "q_out", d, rows, index)
+        q_out = _output(q_out, q, "q_out", d, rows, index, stream)
     w32 = _weights(d, index, q_weight, k_weight)
     rope = _rope(freqs, interleaved, mscale, index)
     _launch(index, "msa_paged_append", ctypes.byref(cache), _ref(rope), _at(q), qs, hq, _at(q_weight), _at(k), ks, _at(k_weight),
@@ -626,7 +634,7 @@ def msa_paged_attn(k_pool, v_pool, page_table, kv_lens, cu_q, q, softmax_scale, 
     if v_pool is None:
         raise ValueError("attention needs a value pool")
     _heads(q, "q", d, rows, index, dense=True)
-    out = _output(out, q, "out", d, rows, index)
+    out = _output(out, q, "out", d, rows, index, stream)
     if lse is not None and (lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous() or
                             lse.get_device() != index):
         raise ValueError("lse must be contiguous fp32 %s on cuda:%d" % (tuple(q.shape[:2]), index))
