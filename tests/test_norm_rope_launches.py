@@ -78,3 +78,61 @@ def test_append_without_queries(heads, d, values, fp8):
     close(pools[0].view(torch.uint8).flatten(0, 1)[at].view(kind), ref, *((2.0 ** -4, 2.0 ** -10) if fp8 else ()))
     if values:
         assert torch.equal(pools[1].view(torch.uint8).flatten(0, 1)[at], v.to(kind).contiguous().view(torch.uint8))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hk,d,rot,inter,norm,tokens", [(64, 8, 128, 64, False, True, 9600), (8, 1, 128, 128, True, True, 19200),
+                                                           (2, 1, 64, 64, False, False, 38400)])
+def test_more_tokens_than_ctas_hold_at_a_time(hq, hk, d, rot, inter, norm, tokens):
+    # a CTA's second round: the coefficients and positions of the first are overwritten behind the barrier that ends it
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    rows = tokens * sms // 148 + 3
+    tile, ctas, parts, _ = B.msa_norm_rope_plan(d, hq, hk, 0, rows)
+    assert tile > 1 and parts == 1 and ctas * tile < rows and rows % tile != 0
+    q, k, wq, wk, positions, freqs = make(rows, hq, hk, d, rot, norm, False, True)
+    outs = api.qk_norm_rope(q, k, positions, api.Rope(freqs, inter, 1.2), wq, wk, 1e-5)
+    for x, w, y in ((q, wq, outs[0]), (k, wk, outs[1])):
+        for lo in range(0, rows, 4096):  # (the definition's intermediates are large)
+            part = slice(lo, lo + 4096)
+            close(y[part], turn(x[part].double(), None if w is None else w.double(), positions[part], freqs, inter, 1.2, 1e-5))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fp8", [False, True])
+def test_an_append_of_more_tokens_than_ctas_hold_at_a_time(fp8):
+    hq, heads, d, page = 64, 8, 128, 128
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    n = 9600 * sms // 148 + 3
+    tile, ctas, parts, _ = B.msa_norm_rope_plan(d, hq, heads, heads, n)
+    assert tile > 1 and parts == 1 and ctas * tile < n and n % tile != 0
+    lens = [(n - 700, 100), (0, 9), (699, 0), (1, 77)]
+    kind = torch.float8_e4m3fn if fp8 else torch.bfloat16
+    used = [-(-(x + c) // page) for x, c in lens]
+    order = torch.randperm(sum(used) + 3, generator=torch.Generator().manual_seed(4)).to(torch.int32)
+    table = torch.full((4, max(used)), -7, dtype=torch.int32)
+    for s, part in enumerate(order[:sum(used)].split(used)):
+        table[s, :used[s]] = part
+    pools = [torch.zeros(len(order), page, heads, d, dtype=kind, device=DEV) for _ in range(2)]
+    cache = api.PagedCache(pools[0], pools[1], table.to(DEV), torch.tensor([x + c for x, c in lens], dtype=torch.int32, device=DEV),
+                           torch.tensor([0, n - 700, n - 700, n - 1, n], dtype=torch.int32, device=DEV))
+    extra = 5  # rows of a padded batch
+    q, k, v = [rows_of(n + extra, h, d, s) for s, h in ((1, hq), (2, heads), (3, heads))]
+    wq, wk = [(1 + 0.3 * torch.randn(d, device=DEV)).bfloat16() for _ in range(2)]
+    freqs = api.rope_frequencies(64, 1e6)
+    q_out = torch.full((n + extra, hq, d), 7.0, dtype=torch.bfloat16, device=DEV)
+    api.paged_append(cache, k, v, q, api.Rope(freqs, False, 1.1), wq, wk, 1e-5, q_out)
+    assert B.check_async_status() == (0, 0) and (q_out[n:] == 7).all()
+    positions = torch.cat([torch.arange(c, c + x) for x, c in lens])
+    seq = torch.repeat_interleave(torch.arange(4), torch.tensor([x for x, _ in lens]))
+    at = (table[seq, positions // page].long() * page + positions % page).to(DEV)
+    positions = positions.to(DEV)
+    stored = pools[0].view(torch.uint8).flatten(0, 1)[at].view(kind)
+    for lo in range(0, n, 4096):
+        part = slice(lo, min(lo + 4096, n))
+        close(q_out[part], turn(q[part].double(), wq.double(), positions[part], freqs, False, 1.1, 1e-5))
+        close(stored[part], turn(k[part].double(), wk.double(), positions[part], freqs, False, 1.1, 1e-5),
+              *((2.0 ** -4, 2.0 ** -10) if fp8 else ()))
+    assert torch.equal(pools[1].view(torch.uint8).flatten(0, 1)[at], v[:n].to(kind).contiguous().view(torch.uint8))
+    untouched = torch.ones(len(order) * page, dtype=torch.bool, device=DEV)
+    untouched[at] = False
+    assert not any(p.view(torch.uint8).flatten(0, 1)[untouched].any() for p in pools)
