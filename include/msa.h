@@ -519,7 +519,7 @@ msa_status_t msa_paged_append(const msa_paged_cache_t* cache, const msa_rope_t* 
  * in fp16 (K and V exact, any Q, P to 2^-11 of itself or 2^-35 of its row's largest).  Other shapes
  * (d a multiple of 8 up to 256, at most 1024 query heads) run on a generic kernel in fp32.
  * workspace (256-byte aligned) >= msa_paged_attn_workspace_bytes.  Of `cache`, that query reads the
- * sizes only.
+ * sizes and fp8 only.
  */
 msa_status_t msa_paged_attn(const msa_paged_cache_t* cache, const void* q, int32_t n_q_heads, int64_t n_tokens,
                             float softmax_scale, void* out, float* lse, void* workspace,

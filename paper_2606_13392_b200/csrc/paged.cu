@@ -149,17 +149,26 @@ static msa_status_t resolve_cache(const msa_paged_cache_t* c, int64_t n_tokens, 
 }
 
 // ---------------------------------------------------------------------- attention over the cache
-// Workspace: the CTAs' ends, then the partials.
-struct PagedWorkspace { size_t ends, ml, o, bytes; };
-static PagedWorkspace paged_workspace() {
-    const size_t n = sm_count(), rows = 2 * n * kPagedSlotRows;  // (more than the small tiles of kFewCtas * n CTAs take)
-    static_assert(kFewCtas * kFewRows <= kPagedSlotRows, "workspace");
+// Workspace: the CTAs' ends, then the partials; the same for the small kernel where a call may use it.
+struct PagedWorkspace { size_t ends, ml, o, few_ends, few_ml, few_o, bytes; };
+static PagedWorkspace paged_workspace(bool few) {
+    const size_t n = sm_count(), rows = 2 * n * kPagedSlotRows, few_ctas = few ? kFewCtas * n : 0, few_rows = 2 * few_ctas * kFewRows;
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t from = at; at += (bytes + 255) / 256 * 256; return from; };
     PagedWorkspace w;
-    w.ends = 0;
-    w.ml = (kFewCtas * n * sizeof(PagedEnds) + 255) / 256 * 256;
-    w.o = w.ml + rows * sizeof(float2);
-    w.bytes = w.o + rows * 128 * sizeof(float);
+    w.ends = take(n * sizeof(PagedEnds));
+    w.ml = take(rows * sizeof(float2));
+    w.o = take(rows * 128 * sizeof(float));
+    w.few_ends = take(few_ctas * sizeof(PagedEnds));
+    w.few_ml = take(few_rows * sizeof(float2));
+    w.few_o = take(few_rows * 128 * sizeof(float));
+    w.bytes = at;
     return w;
+}
+static void paged_place_workspace(PagedAttnArgs& a, void* workspace, size_t ends, size_t ml, size_t o) {
+    a.ends = (int4*)((char*)workspace + ends);
+    a.part_ml = (float2*)((char*)workspace + ml);
+    a.part_o = (float*)((char*)workspace + o);
 }
 
 static int common_divisor(int a, int b) { return b == 0 ? a : common_divisor(b, a % b); }
@@ -171,36 +180,54 @@ static bool paged_tc_ok(const msa_paged_cache_t& c, int G) {
            (int64_t)c.n_pages * c.page_size < 2147483647LL - 128;
 }
 
-// Merges the tiles that the boundaries between `ctas` CTAs cut.
-static msa_status_t launch_paged_combine(const PagedAttnArgs& a, int ctas, cudaStream_t st) {
-    // a cut tile has at most slot_rows rows: up to 16 CTAs of four rows at a time, as far as the call has rows
-    const int64_t most = std::min<int64_t>(a.slot_rows, (int64_t)a.n_tokens * a.G);
-    // (the launch overlaps the attention kernel's end; the kernel waits there before it reads)
+// A launch that may begin before the one in front of it has ended.
+template <class... Params, class... Args>
+static msa_status_t launch_early(void (*kernel)(Params...), dim3 grid, int threads, size_t smem, cudaStream_t st, const Args&... args) {
     cudaLaunchAttribute early;
     early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     early.val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(ctas, (unsigned)std::min<int64_t>(16, ceil_div64(most, 4)));
-    cfg.blockDim = dim3(128);
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cfg.attrs = &early;
     cfg.numAttrs = 1;
     StageScope sc(kStageNone, st);
-    return cudaLaunchKernelEx(&cfg, paged_combine_kernel, a, ctas) == cudaSuccess ? MSA_OK : cuda_failed();
+    return cudaLaunchKernelEx(&cfg, kernel, args...) == cudaSuccess ? MSA_OK : cuda_failed();
 }
 
-// Calls whose sequences have on average no more rows (new tokens x group) than the small kernel's tiles, on fp8 caches:
-// see paged_few8.cuh.  (The rule goes by what the host knows.  A longer sequence among the others takes several tiles and
-// reads its keys as often: right all the same, and worth it while that stays below 1.6 times on average, the ratio of the
-// two kernels on one tile: 171 against 105 us for 32 sequences.)
-static bool paged_few8_ok(const PagedAttnArgs& a, const msa_paged_cache_t& c) {
-    return c.fp8 == 1 && a.G <= kFewRows && a.n_tokens <= (int64_t)c.batch * (kFewRows / a.G);
+// Merges the tiles that the boundaries between the CTAs of a launch cut, or of two (b).  A cut tile has at most slot_rows rows:
+// up to 64 at a time, as far as the call has rows.  (The kernel waits for the attention kernels before it reads.)
+static msa_status_t launch_paged_combine(const PagedAttnArgs& a, int ctas, const PagedAttnArgs* b, int b_ctas, cudaStream_t st) {
+    const int64_t most = std::min<int64_t>(std::max(a.slot_rows, b != nullptr ? b->slot_rows : 0), (int64_t)a.n_tokens * a.G);
+    const PagedCuts c0{a.part_o, a.part_ml, a.ends, a.TPT, a.slot_rows, ctas};
+    const PagedCuts c1 = b != nullptr ? PagedCuts{b->part_o, b->part_ml, b->ends, b->TPT, b->slot_rows, b_ctas} : PagedCuts{};
+    const dim3 grid(c0.n_ctas + c1.n_ctas, (unsigned)std::min<int64_t>(64 / kMergeWarps, ceil_div64(most, kMergeWarps)));
+    return launch_early(paged_combine_kernel, grid, kMergeThreads, 0, st, a, c0, c1);
+}
+
+// Which kernels a call on an fp8 cache takes.  The small kernel (paged_few8.cuh) is the faster one for sequences whose rows
+// one of its tiles holds; of a longer one it would read the keys once for every tile (255 single tokens and a chunk of 257
+// on 28K, 8 heads per group: 1470 us on it alone, 510 us with the chunk on the tcgen05 kernel).  The lengths are on the device and
+// a captured call follows them; the host knows their sum and count.
+//   tokens: of the small kernel's tile: all new ones if it holds them, else the eight or sixteen rows that hold the
+//           average sequence; 0: not even sixteen do, the tcgen05 kernel takes all.
+//   alone:  no sequence is longer if none is empty: the small kernel takes all (right for any lengths, and slower where
+//           empty sequences leave room for a long one).  Else each kernel takes the sequences of its lengths; a second
+//           launch that finds none costs 3 to 7 us (32 sequences of two tokens on 4K - 32K 215 -> 222 us).
+struct PagedFew { int tokens; bool alone; };
+static PagedFew paged_few8(const PagedAttnArgs& a, const msa_paged_cache_t& c) {
+    if (c.fp8 != 1 || a.G > kFewRows) return PagedFew{0, false};
+    for (const int rows : {8, kFewRows})
+        if (a.n_tokens <= rows / a.G) return PagedFew{rows / a.G, true};
+    for (const int rows : {8, kFewRows})
+        if (a.n_tokens <= (int64_t)c.batch * (rows / a.G)) return PagedFew{rows / a.G, a.n_tokens - (c.batch - 1) <= rows / a.G};
+    return PagedFew{0, false};
 }
 
 template <int HG>
-static msa_status_t launch_paged_few8(PagedAttnArgs a, const msa_paged_cache_t& c, const void* q, cudaStream_t st) {
-    a.TPT = a.tile_tokens = HG * 8 / a.G;
-    a.slot_rows = kFewRows;
+static msa_status_t launch_paged_few8(const PagedAttnArgs& a, const msa_paged_cache_t& c, const void* q, int grid, cudaStream_t st) {
     CUtensorMap tm_k, tm_v;
     const uint64_t H = (uint64_t)a.c.H_kv, rows = (uint64_t)c.n_pages * c.page_size;
     const int box = common_divisor(c.page_size, kPagedKeys);
@@ -212,7 +239,7 @@ static msa_status_t launch_paged_few8(PagedAttnArgs a, const msa_paged_cache_t& 
     const size_t smem = sizeof(FewSmem<HG>);
     static_assert(sizeof(FewSmem<HG>) <= 113 * 1024, "two CTAs per SM");
     static bool attr_set[64] = {false};  // per device
-    const int dev = current_device(), grid = kFewCtas * sm_count();
+    const int dev = current_device();
     if (!attr_set[dev]) {
         if (cudaFuncSetAttribute(paged_few8_kernel<HG>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
             return cuda_failed();
@@ -222,12 +249,12 @@ static msa_status_t launch_paged_few8(PagedAttnArgs a, const msa_paged_cache_t& 
         StageScope sc(kStageNone, st);
         paged_few8_kernel<HG><<<grid, kFewThreads, smem, st>>>(tm_k, tm_v, a, (const __nv_bfloat16*)q, box, 1.0 / grid, status);
     }
-    if (launch_status() != MSA_OK) return MSA_ERR_CUDA;
-    return launch_paged_combine(a, grid, st);
+    return launch_status();
 }
 
 template <bool F8>
-static msa_status_t launch_paged_attn(const PagedAttnArgs& a, const msa_paged_cache_t& c, const void* q, cudaStream_t st) {
+static msa_status_t launch_paged_attn(const PagedAttnArgs& a, const msa_paged_cache_t& c, const void* q, int grid, bool early,
+                                      cudaStream_t st) {
     CUtensorMap tm_q, tm_q1, tm_k, tm_v;
     const uint64_t H_q = (uint64_t)a.c.H_kv * a.G, H = (uint64_t)a.c.H_kv, rows = (uint64_t)c.n_pages * c.page_size;
     const int box = std::min(common_divisor(c.page_size, kPagedKeys), F8 ? 32 : kPagedKeys);  // keys of a copy
@@ -247,7 +274,7 @@ static msa_status_t launch_paged_attn(const PagedAttnArgs& a, const msa_paged_ca
     if (!ok || status == nullptr) return cuda_failed();
     const size_t smem = sizeof(PagedSmem);
     static bool attr_set[64] = {false};  // per device
-    const int dev = current_device(), grid = sm_count();
+    const int dev = current_device();
     if (!attr_set[dev]) {
         if (cudaFuncSetAttribute(paged_attn_tc_kernel<F8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
             return cuda_failed();
@@ -255,12 +282,12 @@ static msa_status_t launch_paged_attn(const PagedAttnArgs& a, const msa_paged_ca
     }
     // K and V of one (sequence, head) beyond a third of L2: CTAs on different tiles of it should read in step
     const int64_t snap = (int64_t)40e6 / (F8 ? 256 : 512);
-    {
-        StageScope sc(kStageNone, st);
-        paged_attn_tc_kernel<F8><<<grid, paged_threads(F8), smem, st>>>(tm_q, tm_q1, tm_k, tm_v, a, box, snap, 1.0 / grid, status);
-    }
-    if (launch_status() != MSA_OK) return MSA_ERR_CUDA;
-    return launch_paged_combine(a, grid, st);
+    if (early)  // (behind the small kernel, which it shares nothing with)
+        return launch_early(paged_attn_tc_kernel<F8>, grid, paged_threads(F8), smem, st, tm_q, tm_q1, tm_k, tm_v, a, box, snap,
+                            1.0 / grid, status);
+    StageScope sc(kStageNone, st);
+    paged_attn_tc_kernel<F8><<<grid, paged_threads(F8), smem, st>>>(tm_q, tm_q1, tm_k, tm_v, a, box, snap, 1.0 / grid, status);
+    return launch_status();
 }
 
 }  // namespace msa
@@ -409,7 +436,8 @@ msa_status_t msa_paged_attn_workspace_bytes(const msa_paged_cache_t* cache, int3
     const msa_status_t s = resolve_cache(cache, 0, view);
     if (s != MSA_OK) return s;
     if (n_q_heads <= 0 || n_q_heads % cache->n_kv_heads != 0 || min_bytes == nullptr) return MSA_ERR_INVALID_ARG;
-    *min_bytes = paged_tc_ok(*cache, n_q_heads / cache->n_kv_heads) ? paged_workspace().bytes : 0;
+    const int G = n_q_heads / cache->n_kv_heads;
+    *min_bytes = paged_tc_ok(*cache, G) ? paged_workspace(cache->fp8 == 1 && G <= kFewRows).bytes : 0;
     return MSA_OK;
 }
 
@@ -436,20 +464,30 @@ msa_status_t msa_paged_attn(const msa_paged_cache_t* cache, const void* q, int32
     a.lse = lse;
     cudaStream_t st = (cudaStream_t)stream;
     if (paged_tc_ok(*cache, a.G)) {
-        const PagedWorkspace w = paged_workspace();
-        if (workspace == nullptr || !aligned_to(workspace, 256)) return MSA_ERR_INVALID_ARG;
-        if (workspace_bytes < w.bytes) return MSA_ERR_WORKSPACE;
         a.TPT = 128 / a.G;
         a.tile_tokens = 2 * a.TPT;
         a.slot_rows = kPagedSlotRows;
-        a.ends = (int4*)((char*)workspace + w.ends);
-        a.part_ml = (float2*)((char*)workspace + w.ml);
-        a.part_o = (float*)((char*)workspace + w.o);
-        if (paged_few8_ok(a, *cache)) {  // eight rows a tile if they hold the average sequence, else sixteen
-            if (a.G <= 8 && n_tokens <= (int64_t)cache->batch * (8 / a.G)) return launch_paged_few8<1>(a, *cache, q, st);
-            return launch_paged_few8<2>(a, *cache, q, st);
+        a.max_len = 2147483647;
+        const PagedFew few = paged_few8(a, *cache);
+        const PagedWorkspace w = paged_workspace(cache->fp8 == 1 && a.G <= kFewRows);
+        if (workspace == nullptr || !aligned_to(workspace, 256)) return MSA_ERR_INVALID_ARG;
+        if (workspace_bytes < w.bytes) return MSA_ERR_WORKSPACE;
+        paged_place_workspace(a, workspace, w.ends, w.ml, w.o);
+        const int ctas = sm_count(), few_ctas = kFewCtas * ctas;
+        PagedAttnArgs f = a;
+        msa_status_t s = MSA_OK;
+        if (few.tokens > 0) {
+            f.TPT = f.tile_tokens = few.tokens;
+            f.slot_rows = kFewRows;
+            if (!few.alone) { f.max_len = few.tokens; a.min_len = few.tokens + 1; }
+            paged_place_workspace(f, workspace, w.few_ends, w.few_ml, w.few_o);
+            s = few.tokens * a.G <= 8 ? launch_paged_few8<1>(f, *cache, q, few_ctas, st) : launch_paged_few8<2>(f, *cache, q, few_ctas, st);
+            if (s != MSA_OK) return s;
+            if (few.alone) return launch_paged_combine(f, few_ctas, nullptr, 0, st);
         }
-        return cache->fp8 ? launch_paged_attn<true>(a, *cache, q, st) : launch_paged_attn<false>(a, *cache, q, st);
+        s = cache->fp8 ? launch_paged_attn<true>(a, *cache, q, ctas, few.tokens > 0, st) : launch_paged_attn<false>(a, *cache, q, ctas, false, st);
+        if (s != MSA_OK) return s;
+        return few.tokens > 0 ? launch_paged_combine(f, few_ctas, &a, ctas, st) : launch_paged_combine(a, ctas, nullptr, 0, st);
     }
     const int64_t grid = ceil_div64(n_tokens * n_q_heads, 4);
     if (grid > 2147483647LL) return MSA_ERR_UNSUPPORTED;

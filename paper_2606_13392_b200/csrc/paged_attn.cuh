@@ -31,6 +31,7 @@ struct PagedAttnArgs {
     int tile_tokens;     // tokens of a query tile of a sequence with more than TPT: two contexts, or one
     int slot_rows;       // rows of a partial
     int n_tokens;
+    int min_len, max_len;  // new tokens of the sequences that this launch takes (another takes the rest)
     float scale_log2e;
     __nv_bfloat16* out;  // [n_tokens, H_kv*G, 128]
     float* lse;          // [n_tokens, H_kv*G] or null
@@ -57,6 +58,7 @@ __host__ __device__ __forceinline__ PagedSeq paged_seq(const PagedAttnArgs& a, i
     const int lo = max(a.c.cu_q[s], 0), end = a.c.cu_q[s + 1], hi = min(end, a.n_tokens);  // (rows that are not there: none)
     q.q_row = lo;
     q.q_len = max(hi - lo, 0);
+    if (q.q_len < a.min_len || q.q_len > a.max_len) q.q_len = 0;  // (another launch's: no rows here)
     q.kv = (int)min((int64_t)max(a.c.kv_lens[s], 0), paged_cap(a.c));
     q.base = q.kv - max(end - lo, 0);  // position of the first new token
     q.tile_tokens = q.q_len <= a.TPT ? a.TPT : a.tile_tokens;
@@ -301,8 +303,21 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     extern __shared__ __align__(1024) uint8_t paged_smem[];  // (no room to round the base up)
     PagedSmem& sm = *reinterpret_cast<PagedSmem*>(paged_smem);
     if ((smem_u32(paged_smem) & 1023) != 0) {  // swizzled tiles need it; the same for every thread
-        if (threadIdx.x == 0) report_async(status, kAsyncBadIndex, 0x6FF);
+        if (threadIdx.x == 0) {
+            report_async(status, kAsyncBadIndex, 0x6FF);
+            a.ends[blockIdx.x * 2] = make_int4(0, 0, 0, 0);  // (nothing to merge)
+        }
+        if constexpr (F8) asm volatile("griddepcontrol.wait;" ::: "memory");
         return;
+    }
+    if (F8 && a.min_len > 0) {  // paged_few8_kernel takes the shorter sequences, maybe all
+        bool any = false;
+        for (int s = threadIdx.x; s < a.c.batch; s += paged_threads(F8)) any |= a.c.cu_q[s + 1] - a.c.cu_q[s] >= a.min_len;
+        if (__syncthreads_or(any) == 0) {
+            if (threadIdx.x == 0) a.ends[blockIdx.x * 2] = make_int4(0, 0, 0, 0);
+            asm volatile("griddepcontrol.wait;" ::: "memory");
+            return;
+        }
     }
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int* abort = &sm.abort;
@@ -814,25 +829,42 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
+    // Launched early behind paged_few8_kernel, if that takes part: the merge waits for this kernel only, which therefore ends
+    // after that one.
+    if constexpr (F8) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 // Merges the partials of tiles that stretch boundaries cut: CTA (i, .) the tile that attention CTA i left open, a warp
 // per row.  With M the largest reference maximum, O = sum 2^(m - M) O_p, l likewise; out = O / l.  The order of the
-// parts is that of the line, so equal calls give equal bits.
-__global__ void __launch_bounds__(128)
-paged_combine_kernel(const PagedAttnArgs a, int n_ctas) {
-    const int c0 = blockIdx.x;
-    asm volatile("griddepcontrol.wait;" ::: "memory");  // launched early: what the attention kernel wrote is there after this
-    const int4 e = a.ends[c0 * 2];
+// parts is that of the line, so equal calls give equal bits.  One launch merges for both attention kernels of a call on an
+// fp8 cache: the first CTAs take the tiles cut in c0, the others those of c1.
+constexpr int kMergeThreads = 128, kMergeWarps = kMergeThreads / 32;
+struct PagedCuts {  // of one attention kernel; the members as in PagedAttnArgs
+    const float* part_o;
+    const float2* part_ml;
+    const int4* ends;
+    int TPT, slot_rows, n_ctas;
+};
+
+__global__ void __launch_bounds__(kMergeThreads)
+paged_combine_kernel(const PagedAttnArgs a, const PagedCuts c0, const PagedCuts c1) {
+    const bool other = (int)blockIdx.x >= c0.n_ctas;
+    const int cta = other ? blockIdx.x - c0.n_ctas : blockIdx.x, n_ctas = other ? c1.n_ctas : c0.n_ctas;
+    const int4* ends = other ? c1.ends : c0.ends;
+    asm volatile("griddepcontrol.wait;" ::: "memory");  // launched early: what the attention kernels wrote is there after this
+    const int4 e = ends[cta * 2];
     if (e.y == 0) return;
-    const int head = a.ends[c0 * 2 + 1].x, tokens = e.w, lane = threadIdx.x & 31;
+    const int TPT = other ? c1.TPT : c0.TPT, slot_rows = other ? c1.slot_rows : c0.slot_rows;
+    const float* part_o = other ? c1.part_o : c0.part_o;
+    const float2* part_ml = other ? c1.part_ml : c0.part_ml;
+    const int head = ends[cta * 2 + 1].x, tokens = e.w, lane = threadIdx.x & 31;
     __shared__ int s_slot[512];  // parts: at most one for each CTA
     __shared__ int s_n;
     if (threadIdx.x < 32) {
         int n = 1;
-        if (lane == 0) s_slot[0] = 2 * c0 + 1;
-        for (int c = c0 + 1; c < n_ctas; c += 32) {
-            const int first = c + lane < n_ctas ? a.ends[(c + lane) * 2].x : 3;
+        if (lane == 0) s_slot[0] = 2 * cta + 1;
+        for (int c = cta + 1; c < n_ctas; c += 32) {
+            const int first = c + lane < n_ctas ? ends[(c + lane) * 2].x : 3;
             const unsigned stop = __ballot_sync(0xffffffffu, first >= 2);  // 2: the last part, 3: none of this tile's
             const int upto = stop ? __ffs(stop) - 1 : 32;
             const bool part = (lane < upto && first == 1) || (lane == upto && first == 2);
@@ -845,18 +877,18 @@ paged_combine_kernel(const PagedAttnArgs a, int n_ctas) {
     }
     __syncthreads();
     const int n = s_n, rows = tokens * a.G, H_q = a.c.H_kv * a.G;
-    for (int r = blockIdx.y * 4 + (threadIdx.x >> 5); r < rows; r += gridDim.y * 4) {
+    for (int r = blockIdx.y * kMergeWarps + (threadIdx.x >> 5); r < rows; r += gridDim.y * kMergeWarps) {
         const int tok = r / a.G, g = r - tok * a.G;
-        const int in_slot = tok < a.TPT ? r : 128 + (tok - a.TPT) * a.G + g;
+        const int in_slot = tok < TPT ? r : 128 + (tok - TPT) * a.G + g;
         float M = -INFINITY;
-        for (int p = lane; p < n; p += 32) M = fmaxf(M, a.part_ml[(int64_t)s_slot[p] * a.slot_rows + in_slot].x);
+        for (int p = lane; p < n; p += 32) M = fmaxf(M, part_ml[(int64_t)s_slot[p] * slot_rows + in_slot].x);
         M = warp_max(M);
         float L = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
         for (int p = 0; p < n; ++p) {
-            const int64_t at = (int64_t)s_slot[p] * a.slot_rows + in_slot;
-            const float2 ml = a.part_ml[at];
-            const float4 x = *reinterpret_cast<const float4*>(a.part_o + at * 128 + lane * 4);
+            const int64_t at = (int64_t)s_slot[p] * slot_rows + in_slot;
+            const float2 ml = part_ml[at];
+            const float4 x = *reinterpret_cast<const float4*>(part_o + at * 128 + lane * 4);
             const float w = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - M);
             L = fmaf(w, ml.y, L);
             o[0] = fmaf(w, x.x, o[0]); o[1] = fmaf(w, x.y, o[1]); o[2] = fmaf(w, x.z, o[2]); o[3] = fmaf(w, x.w, o[3]);

@@ -54,9 +54,15 @@ paged_few8_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     extern __shared__ __align__(1024) uint8_t paged_smem[];
     FewSmem<HG>& sm = *reinterpret_cast<FewSmem<HG>*>(paged_smem);
     if ((smem_u32(paged_smem) & 1023) != 0) {  // swizzled tiles need it; the same for every thread
-        if (threadIdx.x == 0) report_async(status, kAsyncBadIndex, 0x7FF);
+        if (threadIdx.x == 0) {
+            report_async(status, kAsyncBadIndex, 0x7FF);
+            a.ends[blockIdx.x * 2] = make_int4(0, 0, 0, 0);  // (nothing to merge)
+        }
         return;
     }
+    // paged_attn_tc_kernel comes behind for the longer sequences: it shares nothing with this one, so its CTAs may take SMs
+    // that are done here.
+    if (a.max_len < a.n_tokens) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int* abort = &sm.abort;
     if (threadIdx.x == 0) {
