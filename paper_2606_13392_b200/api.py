@@ -148,6 +148,12 @@ class PagedCache(NamedTuple):
 _NO_ROPE = Rope(None)
 
 
+def _no_graph(call: str, instead: str, *tensors: Optional[torch.Tensor]) -> None:
+    """Refuses tensors whose gradients a call would lose: it records nothing for automatic differentiation."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        raise ValueError("%s records no graph and gradients would be lost: %s" % (call, instead))
+
+
 
 def _workspace(t: torch.Tensor, size, *args) -> torch.Tensor:
     """A workspace of size(*args) bytes on t's device (the size may depend on the device)."""
@@ -185,7 +191,9 @@ def qk_norm_rope(q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions
                  k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, q_out: Optional[torch.Tensor] = None,
                  k_out: Optional[torch.Tensor] = None):
     """Norm of each head (where there is a weight) and position rotation of q and k [rows, heads, d], which may be
-    slices of one projection; either may be None -> (q_out, k_out), dense."""
+    slices of one projection; either may be None -> (q_out, k_out), dense.  Records no graph: inputs that require
+    gradients are refused outside torch.no_grad (qk_norm_rope_backward has the gradients)."""
+    _no_graph("qk_norm_rope", "call it under torch.no_grad, and qk_norm_rope_backward in the backward pass", q, k, q_weight, k_weight)
     freqs, interleaved, mscale = rope or _NO_ROPE
     return B.msa_qk_norm_rope(freqs, interleaved, mscale, q, q_weight, k, k_weight, eps, positions, q_out, k_out)
 
@@ -214,7 +222,8 @@ def paged_append(cache: PagedCache, k: torch.Tensor, v: Optional[torch.Tensor], 
                  k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, q_out: Optional[torch.Tensor] = None):
     """Writes the new tokens' keys (normed, turned) and values into the cache and returns their queries, treated like
     the keys (None without queries).  Rows behind the last sequence are left as they are (uninitialised in a q_out
-    made here)."""
+    made here).  Inputs that require gradients are refused outside torch.no_grad."""
+    _no_graph("paged_append", "a cache takes none; call it under torch.no_grad", q, k, v, q_weight, k_weight)
     freqs, interleaved, mscale = rope or _NO_ROPE
     return B.msa_paged_append(cache.k, cache.v, cache.page_table, cache.kv_lens, cache.cu_q, freqs, interleaved, mscale, q,
                               q_weight, k, k_weight, v, eps, q_out)
@@ -223,7 +232,9 @@ def paged_append(cache: PagedCache, k: torch.Tensor, v: Optional[torch.Tensor], 
 def paged_attn(cache: PagedCache, q: torch.Tensor, softmax_scale: float = 0.0, out: Optional[torch.Tensor] = None,
                want_lse: bool = True, workspace: Optional[torch.Tensor] = None):
     """Dense causal attention of the new tokens q [rows, heads, d] over the cache, which already holds their keys and
-    values -> (out, lse).  Rows behind the last sequence are left as they are (uninitialised in outputs made here)."""
+    values -> (out, lse).  Rows behind the last sequence are left as they are (uninitialised in outputs made here).
+    A q that requires gradients is refused outside torch.no_grad."""
+    _no_graph("paged_attn", "it has no backward pass; call it under torch.no_grad", q)
     lse = q.new_empty(q.shape[:2], dtype=torch.float32) if want_lse else None
     if workspace is None:
         workspace = _workspace(q, B.msa_paged_attn_workspace_bytes, cache.k, q.shape[1])
