@@ -204,7 +204,7 @@ static msa_status_t launch_paged_combine(const PagedAttnArgs& a, int ctas, const
     const PagedCuts c0{a.part_o, a.part_ml, a.ends, a.TPT, a.slot_rows, ctas};
     const PagedCuts c1 = b != nullptr ? PagedCuts{b->part_o, b->part_ml, b->ends, b->TPT, b->slot_rows, b_ctas} : PagedCuts{};
     const dim3 grid(c0.n_ctas + c1.n_ctas, (unsigned)std::min<int64_t>(64 / kMergeWarps, ceil_div64(most, kMergeWarps)));
-    return launch_early(paged_combine_kernel, grid, kMergeThreads, 0, st, a, c0, c1);
+    return launch_early(b != nullptr ? paged_combine_kernel<true> : paged_combine_kernel<false>, grid, kMergeThreads, 0, st, a, c0, c1);
 }
 
 // Which kernels a call on an fp8 cache takes.  The small kernel (paged_few8.cuh) is the faster one for sequences whose rows

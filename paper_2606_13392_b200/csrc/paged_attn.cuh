@@ -836,8 +836,9 @@ paged_attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
 
 // Merges the partials of tiles that stretch boundaries cut: CTA (i, .) the tile that attention CTA i left open, a warp
 // per row.  With M the largest reference maximum, O = sum 2^(m - M) O_p, l likewise; out = O / l.  The order of the
-// parts is that of the line, so equal calls give equal bits.  One launch merges for both attention kernels of a call on an
-// fp8 cache: the first CTAs take the tiles cut in c0, the others those of c1.
+// parts is that of the line, so equal calls give equal bits.  BOTH: one launch merges for both attention kernels of a call on
+// an fp8 cache, the first CTAs the tiles cut in c0, the others those of c1 (choosing between them costs 0.5 us, so other calls
+// do without).
 constexpr int kMergeThreads = 128, kMergeWarps = kMergeThreads / 32;
 struct PagedCuts {  // of one attention kernel; the members as in PagedAttnArgs
     const float* part_o;
@@ -846,9 +847,10 @@ struct PagedCuts {  // of one attention kernel; the members as in PagedAttnArgs
     int TPT, slot_rows, n_ctas;
 };
 
+template <bool BOTH>
 __global__ void __launch_bounds__(kMergeThreads)
 paged_combine_kernel(const PagedAttnArgs a, const PagedCuts c0, const PagedCuts c1) {
-    const bool other = (int)blockIdx.x >= c0.n_ctas;
+    const bool other = BOTH && (int)blockIdx.x >= c0.n_ctas;
     const int cta = other ? blockIdx.x - c0.n_ctas : blockIdx.x, n_ctas = other ? c1.n_ctas : c0.n_ctas;
     const int4* ends = other ? c1.ends : c0.ends;
     asm volatile("griddepcontrol.wait;" ::: "memory");  // launched early: what the attention kernels wrote is there after this
