@@ -409,7 +409,8 @@ msa_status_t msa_decode_forward_host(const msa_shape_t* shape, const void* q_hos
  * Rotation.  Pair i < rot_dim/2 of a head (elements i and i + rot_dim/2, or 2i and 2i+1 with
  * interleaved = 1) turns by the angle position * freqs[i]; elements from rot_dim on stay.
  * freqs holds rot_dim/2 fp64 values in DEVICE memory, so any scaling rule for long contexts is
- * a matter of its values; mscale multiplies the rotated elements.  Angles are reduced in 64 bits.
+ * a matter of its values; mscale multiplies the rotated elements.  Angles are reduced in 64 bits:
+ * the angle is off by at most 2^-51 of itself (2^-31 at 2^20 radians) before its fp32 sine and cosine.
  * rot_dim is a multiple of 16 (8 when interleaved) and at most the head size; 0 = no rotation.
  */
 typedef struct {
@@ -470,8 +471,10 @@ msa_status_t msa_qk_norm_rope_backward_workspace_bytes(int32_t head_dim, int64_t
  * memory, so a captured graph follows their values.  Rows from cu_q[batch] on (a padded batch)
  * are left as they are in every output.  With pages in order a sequence is the contiguous cache
  * of msa_decode_forward (row offset = first page * page_size).
- * A page outside [0, n_pages), a length beyond max_pages * page_size or a new token in front of
- * position 0 is reported through the async status as a bad index and never followed.
+ * A page outside [0, n_pages) or a length beyond max_pages * page_size is reported through the async
+ * status as a bad index and never followed.  So is a new token in front of position 0 (more new
+ * tokens than the length says) by msa_paged_append, which has no place for it; in msa_paged_attn
+ * it is a token that sees nothing.
  */
 typedef struct {
     void* k;

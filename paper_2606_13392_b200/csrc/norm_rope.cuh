@@ -137,7 +137,8 @@ __device__ __forceinline__ int paged_seq_of(const PagedView& c, int i) {
     return lo;
 }
 
-// Measured: 32768 tokens of 64 + 8 heads of 128 in 214 us, 5.6 TB/s, 87 % of the copy bandwidth; 32 tokens in 4 us.
+// Measured: 32768 tokens of 64 + 8 heads of 128 in 204 - 227 us, 83 - 92 % of the copy bandwidth (boards and surroundings
+// differ); 8 + 1 heads of 128 in 53 us, 44 %, of 256 (16384 tokens) in 43 us, 54 %; 32 tokens of 64 + 8 heads in 4 us.
 // (Warps on their own with asynchronous copies, the gradient kernel's form, were slower here: 250 against 212 us for 32768
 // tokens of 64 + 8 heads.  One reduction and half the bytes per output leave the independent heads of an item enough.)
 // Forward (APPEND = false: q and k to q.out and k.out; true: k and v to the cache, q to q.out).
@@ -300,7 +301,7 @@ __device__ __forceinline__ void copy_async_wait() { asm volatile("cp.async.wait_
 // CTAs do the queries, the others the keys (one set of weights and sums in registers).  A lane accumulates its eight elements of dw over all its steps; lanes and warps of a CTA join in
 // a fixed order, CTAs leave a row each in the workspace and norm_rope_dw_kernel adds the rows in order, so equal calls
 // give equal bits.
-// Measured: 8192 tokens of 64 + 4 heads of 128 in 85 us, 5.0 TB/s, 78 % of the copy bandwidth, issue slots 65 % busy
+// Measured: 8192 tokens of 64 + 4 heads of 128 in 85 - 92 us, 72 - 78 % of the copy bandwidth, issue slots 65 % busy
 // (two heads per lane group in registers and CTA barriers: 117 us).
 // Table: [lane of the head][cos 0..7, signed sin 0..7].
 constexpr int kGradThreads = 128, kGradWarps = kGradThreads / 32;

@@ -12,8 +12,10 @@
 // partials (at most two per CTA), merged by paged_combine_kernel; all others are written directly.
 //
 // Measured (64 query, 8 KV heads): 4096 new tokens on 28K in 3.8 - 4.6 ms, 0.9 - 1.08 PFLOP/s at the board's power limit,
-// 57 % of the tensor pipe's cycles and 58 % of the exponential unit's; one token each of 64 sequences of up to 32K in 658
-// us, 93 % of the copy bandwidth; 2 - 7 tokens each of 16 sequences in 88 us, 77 %; one token on 2K in 15.7 us.
+// 57 % of the tensor pipe's cycles and 58 % of the exponential unit's; one token each of 64 sequences of up to 32K in 590 -
+// 680 us, 90 - 104 % of the copy bandwidth; 2 - 7 tokens each of 16 sequences in 86 - 92 us, 74 - 78 %; one token on 2K in 16
+// us.  On fp8 caches: 4096 on 28K in 3.7 - 3.8 ms, 512 on 7K in 153 us (0.8 PFLOP/s), 2 - 7 tokens each of 16 sequences in
+// 102 us (33 % of the copy bandwidth: tiles are read, widened and written back in shared memory).
 #pragma once
 
 #include "norm_rope.cuh"

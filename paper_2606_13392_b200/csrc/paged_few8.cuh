@@ -1,12 +1,12 @@
-// Attention over a paged fp8 cache for calls of a few rows per sequence (decode): the line of units, the partials and
-// the merge are those of paged_attn.cuh, a tile of query rows is at most 16.  Bound by HBM.
+// Attention over a paged fp8 cache for sequences of a few rows (decode): the line of units, the partials and the merge
+// are those of paged_attn.cuh, a tile of query rows is at most 16.  Bound by HBM.
 //
 // Why not the tcgen05 kernel: its operands come from shared memory, so fp8 tiles have to be read, widened and written
 // back (64 KB for 32 KB of cache), with 128-row products for 8 or 16 rows; it reached 45 % of the copy bandwidth on 32
-// sequences of 4K - 32K tokens (171 us; this kernel 105 us, 75 %).  Here the fragments of warp-level products are widened in registers: a
-// producer warp streams K and V tiles (16 KB each) through a ring of six, two CTAs per SM, four consumer warps own 32
-// keys of every tile: S = Q K^T, softmax, O^T += V^T P^T, all in registers; the four warps' results join at the end of
-// an item.  Fragment orders as in attn_decode_kv8_kernel: the contraction index of Q K^T and the row index of O^T are
+// sequences of 4K - 32K tokens (171 us; this kernel 101 - 112 us, 70 - 77 %).  Here the fragments of warp-level products are
+// widened in registers: a producer warp streams K and V tiles (16 KB each) through a ring of six, two CTAs per SM, four
+// consumer warps own 32 keys of every tile: S = Q K^T, softmax, O^T += V^T P^T, all in registers; the four warps' results
+// join at the end of an item.  Fragment orders as in attn_decode_kv8_kernel: the contraction index of Q K^T and the row index of O^T are
 // permuted to the order in which 16-bit shared-memory matrix loads hand out fp8 bytes.
 // K, V and P are fp16 in the products (E4M3 -> fp16 is exact), Q is fp16 with a power of two taken out of each row and
 // put back into the scale, P is held 2^10 up (see paged_attn.cuh for both).
