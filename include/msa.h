@@ -475,6 +475,11 @@ msa_status_t msa_qk_norm_rope_backward_workspace_bytes(int32_t head_dim, int64_t
  * status as a bad index and never followed.  So is a new token in front of position 0 (more new
  * tokens than the length says) by msa_paged_append, which has no place for it; in msa_paged_attn
  * it is a token that sees nothing.
+ * max_new: the most new tokens that a sequence of the call has, if the host knows (0: it does not).
+ * A hint to msa_paged_attn on fp8 caches, which reads a sequence once for each of the query tiles that
+ * it then chooses; results are right whatever it says.  Without it a batch whose rows leave no room for
+ * a sequence of more than a few, if each has one at least, is taken for such: say it where sequences may
+ * have none beside one of many.
  */
 typedef struct {
     void* k;
@@ -489,6 +494,7 @@ typedef struct {
     int32_t n_kv_heads;
     int32_t head_dim;
     int32_t fp8;
+    int32_t max_new;
 } msa_paged_cache_t;
 
 /*
@@ -522,7 +528,7 @@ msa_status_t msa_paged_append(const msa_paged_cache_t* cache, const msa_rope_t* 
  * in fp16 (K and V exact, any Q, P to 2^-11 of itself or 2^-35 of its row's largest).  Other shapes
  * (d a multiple of 8 up to 256, at most 1024 query heads) run on a generic kernel in fp32.
  * workspace (256-byte aligned) >= msa_paged_attn_workspace_bytes.  Of `cache`, that query reads the
- * sizes and fp8 only.
+ * sizes and fp8 only (not max_new).
  */
 msa_status_t msa_paged_attn(const msa_paged_cache_t* cache, const void* q, int32_t n_q_heads, int64_t n_tokens,
                             float softmax_scale, void* out, float* lse, void* workspace,

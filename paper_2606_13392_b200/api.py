@@ -230,13 +230,16 @@ def paged_append(cache: PagedCache, k: torch.Tensor, v: Optional[torch.Tensor], 
 
 
 def paged_attn(cache: PagedCache, q: torch.Tensor, softmax_scale: float = 0.0, out: Optional[torch.Tensor] = None,
-               want_lse: bool = True, workspace: Optional[torch.Tensor] = None):
+               want_lse: bool = True, workspace: Optional[torch.Tensor] = None, max_new: int = 0):
     """Dense causal attention of the new tokens q [rows, heads, d] over the cache, which already holds their keys and
     values -> (out, lse).  Rows behind the last sequence are left as they are (uninitialised in outputs made here).
-    A q that requires gradients is refused outside torch.no_grad."""
+    max_new: the most new tokens that a sequence has, if known (a hint, results do not depend on it; worth giving on fp8
+    caches where sequences may have no new tokens beside one of many).  A q that requires gradients is refused outside
+    torch.no_grad."""
     _no_graph("paged_attn", "it has no backward pass; call it under torch.no_grad", q)
     lse = q.new_empty(q.shape[:2], dtype=torch.float32) if want_lse else None
     if workspace is None:
         workspace = _workspace(q, B.msa_paged_attn_workspace_bytes, cache.k, q.shape[1])
-    out = B.msa_paged_attn(cache.k, cache.v, cache.page_table, cache.kv_lens, cache.cu_q, q, softmax_scale, out, lse, workspace)
+    out = B.msa_paged_attn(cache.k, cache.v, cache.page_table, cache.kv_lens, cache.cu_q, q, softmax_scale, out, lse, workspace,
+                           max_new=max_new)
     return out, lse

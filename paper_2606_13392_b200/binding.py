@@ -52,7 +52,7 @@ class MsaRope(ctypes.Structure):
 class MsaPagedCache(ctypes.Structure):
     _fields_ = [("k", c_vp), ("v", c_vp), ("page_table", c_vp), ("kv_lens", c_vp), ("cu_q", c_vp), ("batch", c_i32),
                 ("max_pages", c_i32), ("n_pages", c_i32), ("page_size", c_i32), ("n_kv_heads", c_i32),
-                ("head_dim", c_i32), ("fp8", c_i32)]
+                ("head_dim", c_i32), ("fp8", c_i32), ("max_new", c_i32)]
 
 
 class MsaError(RuntimeError):
@@ -627,9 +627,11 @@ def msa_paged_attn_workspace_bytes(k_pool, n_q_heads: int) -> int:
     return mn.value
 
 
-def msa_paged_attn(k_pool, v_pool, page_table, kv_lens, cu_q, q, softmax_scale, out, lse, workspace, stream=None):
-    """q, out: bf16 [rows, heads, d] dense; lse fp32 [rows, heads] or None.  -> out, made if it is not given."""
+def msa_paged_attn(k_pool, v_pool, page_table, kv_lens, cu_q, q, softmax_scale, out, lse, workspace, stream=None, max_new=0):
+    """q, out: bf16 [rows, heads, d] dense; lse fp32 [rows, heads] or None; max_new: the most new tokens of a sequence, 0 if
+    not known.  -> out, made if it is not given."""
     index, cache = _paged(k_pool, v_pool, page_table, kv_lens, cu_q)
+    cache.max_new = max_new
     d, rows = cache.head_dim, q.shape[0]
     if v_pool is None:
         raise ValueError("attention needs a value pool")

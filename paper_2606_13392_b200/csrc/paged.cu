@@ -138,7 +138,7 @@ static msa_status_t resolve_cache(const msa_paged_cache_t* c, int64_t n_tokens, 
     if (c == nullptr || n_tokens < 0 || n_tokens > 2147483647LL) return MSA_ERR_INVALID_ARG;
     if (c->batch < 0 || c->max_pages < 0 || c->n_pages < 0 || c->page_size <= 0 || c->n_kv_heads <= 0 || c->head_dim <= 0)
         return MSA_ERR_INVALID_ARG;
-    if (c->fp8 != 0 && c->fp8 != 1) return MSA_ERR_INVALID_ARG;
+    if ((c->fp8 != 0 && c->fp8 != 1) || c->max_new < 0) return MSA_ERR_INVALID_ARG;
     if (c->head_dim % 8 != 0 || c->head_dim > 256 || c->n_kv_heads > kMaxRopeHeads) return MSA_ERR_UNSUPPORTED;
     v = PagedView{c->cu_q, c->kv_lens, c->page_table, c->batch, c->max_pages, c->n_pages, c->page_size, c->n_kv_heads};
     if (c->batch == 0 || n_tokens == 0) return MSA_OK;
@@ -210,19 +210,22 @@ static msa_status_t launch_paged_combine(const PagedAttnArgs& a, int ctas, const
 // Which kernels a call on an fp8 cache takes.  The small kernel (paged_few8.cuh) is the faster one for sequences whose rows
 // one of its tiles holds; of a longer one it would read the keys once for every tile (255 single tokens and a chunk of 257
 // on 28K, 8 heads per group: 1470 us on it alone, 510 us with the chunk on the tcgen05 kernel).  The lengths are on the device and
-// a captured call follows them; the host knows their sum and count.
-//   tokens: of the small kernel's tile: all new ones if it holds them, else the eight or sixteen rows that hold the
-//           average sequence; 0: not even sixteen do, the tcgen05 kernel takes all.
-//   alone:  no sequence is longer if none is empty: the small kernel takes all (right for any lengths, and slower where
-//           empty sequences leave room for a long one).  Else each kernel takes the sequences of its lengths; a second
-//           launch that finds none costs 3 to 7 us (32 sequences of two tokens on 4K - 32K 215 -> 222 us).
+// a captured call follows them; the host knows their sum and count, and the caller may say the longest.
+//   tokens: of the small kernel's tile: the eight or sixteen rows that hold the longest sequence, or the average one; 0:
+//           not even sixteen do, the tcgen05 kernel takes all.
+//   alone:  no sequence is longer than the tile, if what the caller says holds or none is empty: the small kernel takes all
+//           (right for any lengths, and slow where that is not so: 256 tokens on 28K beside 255 empty sequences 1904 us
+//           against 240).  Else each kernel takes the sequences of its lengths; a second launch that finds none costs 2 to
+//           8 us (32 sequences of two tokens on 4K - 32K 215 -> 222 us).
 struct PagedFew { int tokens; bool alone; };
 static PagedFew paged_few8(const PagedAttnArgs& a, const msa_paged_cache_t& c) {
     if (c.fp8 != 1 || a.G > kFewRows) return PagedFew{0, false};
+    const int longest = c.max_new > 0 ? std::min(c.max_new, a.n_tokens) : a.n_tokens;
     for (const int rows : {8, kFewRows})
-        if (a.n_tokens <= rows / a.G) return PagedFew{rows / a.G, true};
+        if (longest <= rows / a.G) return PagedFew{rows / a.G, true};
     for (const int rows : {8, kFewRows})
-        if (a.n_tokens <= (int64_t)c.batch * (rows / a.G)) return PagedFew{rows / a.G, a.n_tokens - (c.batch - 1) <= rows / a.G};
+        if (a.n_tokens <= (int64_t)c.batch * (rows / a.G))
+            return PagedFew{rows / a.G, c.max_new == 0 && a.n_tokens - (c.batch - 1) <= rows / a.G};
     return PagedFew{0, false};
 }
 

@@ -45,6 +45,11 @@ def test_mixed_batches(lens, page, group, hkv, extra):
     check(cache, q, out, lse)
     again, lse2 = api.paged_attn(cache, q)
     assert torch.equal(again[:n], out[:n]) and torch.equal(lse[:n], lse2[:n])
+    for said in (1, max(x for x, _ in lens), 5000, (1 << 31) - 1):  # a hint, which may be wrong
+        out.fill_(5.0)
+        _, lse = api.paged_attn(cache, q, out=out, max_new=said)
+        assert B.check_async_status() == (0, 0) and (out[n:] == 5).all()
+        check(cache, q, out, lse)
 
 
 @pytest.mark.gpu
@@ -64,11 +69,11 @@ def test_random_mixed_batches(seed):
 
 @pytest.mark.gpu
 def test_which_kernels_a_call_launches():
-    def launches(lens, group, fp8=True):
+    def launches(lens, group, fp8=True, said=0):
         cache = make(lens, 16, 2, 128, fp8)
         q = queries(sum(n for n, _ in lens), 2 * group, 128)
         before = B.lib().msa_launch_count()
-        api.paged_attn(cache, q)
+        api.paged_attn(cache, q, max_new=said)
         return B.lib().msa_launch_count() - before
 
     chunk = [(1, 50)] * 63 + [(65, 500)]
@@ -77,6 +82,9 @@ def test_which_kernels_a_call_launches():
     assert launches([(1, 90)], 8) == 2 and launches([(1, 90)] * 2, 8) == 2   # no room for a longer one
     assert launches([(1, 90)] * 40, 8) == 2 and launches([(1, 90)] * 40, 16) == 2   # nor here
     assert launches([(2, 90)] * 40, 8) == 3 and launches([(5, 90)] * 40, 8) == 2     # some may be longer; all are
+    idle = [(0, 90)] * 63 + [(64, 500)]              # sequences without new tokens leave room that the sum does not show
+    assert launches(idle, 8) == 2 and launches(idle, 8, said=64) == 3
+    assert launches([(2, 90)] * 40, 8, said=2) == 2 and launches([(3, 90), (1, 5)] * 20, 8, said=3) == 3
     assert launches([(65, 90)], 32) == 2         # groups beyond the small tiles
 
 
@@ -140,3 +148,13 @@ def test_a_wait_that_runs_out_in_both_kernels():
     out, lse = api.paged_attn(cache, q)
     assert B.check_async_status() == (0, 0)
     check(cache, q, out, lse)
+
+
+def test_a_hint_below_zero_is_refused():
+    import ctypes
+    one = ctypes.c_void_p(256)  # non-null and aligned, never followed on this path
+    cache = B.MsaPagedCache(k=256, v=256, page_table=256, kv_lens=256, cu_q=256, batch=2, max_pages=3, n_pages=9, page_size=16, n_kv_heads=2,
+                            head_dim=128, fp8=1, max_new=-1)
+    assert B.lib().msa_paged_attn(ctypes.byref(cache), one, B.c_i32(8), B.c_i64(5), ctypes.c_float(0), one, None, one, B.c_sz(16), None) == 1
+    cache.max_new = 3
+    assert B.lib().msa_paged_attn(ctypes.byref(cache), one, B.c_i32(8), B.c_i64(5), ctypes.c_float(0), one, None, one, B.c_sz(16), None) == 3
