@@ -535,6 +535,85 @@ msa_status_t msa_paged_attn(const msa_paged_cache_t* cache, const void* q, int32
                             size_t workspace_bytes, msa_stream_t stream);
 msa_status_t msa_paged_attn_workspace_bytes(const msa_paged_cache_t* cache, int32_t n_q_heads, size_t* min_bytes);
 
+/* ------------------------------------------------------------------------------------
+ * Keeping a paged cache within a budget (the paper has no counterpart): the attention weight that cached tokens have
+ * received, the tokens that stay, their move to the front of the sequence's pages.  A step of a bounded cache is
+ * msa_paged_append, msa_paged_attn, msa_paged_weights and, once the sequences are over their budget, msa_paged_keep and
+ * msa_paged_compact; from then on kv_lens starts from the new lengths.  Dropped tokens leave no gap, so a token's place is
+ * no longer its position: keys that are rotated take msa_qk_norm_rope with the true positions, then msa_paged_append
+ * without rotation.
+ *
+ * weights is a pool like the keys' and values', fp32 [n_pages, n_kv_heads, page_size]: the weight of token t of sequence s and
+ * KV head h is element t mod page_size of row h of the token's page.
+ *
+ * After msa_paged_attn, with its q and lse: for every place j < kv_lens[s] of a sequence with new tokens and every KV head,
+ *   w[j] = (j before the first new token ? decay * w[j] : 0)
+ *        + sum over new tokens i that see j and query heads h of the group of exp(softmax_scale <q[i, h], k_j> - lse[i, h]).
+ * With decay = 0 old weights are not read (they need not be set).  A row whose lse is -infinity gives nothing; sequences without new
+ * tokens are left as they are.  q [n_tokens, n_q_heads, d] bf16 dense, lse [n_tokens, n_q_heads]; n_tokens >= cu_q[batch], cu_q, kv_lens,
+ * softmax_scale and max_new as in msa_paged_attn.  The rows may be some of the queries only (cu_q counts those given): the
+ * last tokens of a prompt as observers of all of it, say - they are the last tokens of kv_lens[s], and what comes before them
+ * counts as old.  Sums are fp32 in a fixed order: equal calls give equal bits.  Sequences must not share pages (their weights
+ * would).  Places on bad pages are reported and left out.  head_dim = 128 runs on the tensor cores, other sizes on a generic kernel.
+ * workspace (256-byte aligned; may be NULL where it has 0 bytes) >= msa_paged_weights_workspace_bytes.
+ */
+msa_status_t msa_paged_weights(const msa_paged_cache_t* cache, const void* q, int32_t n_q_heads, const float* lse,
+                               int64_t n_tokens, float softmax_scale, float decay, float* weights, void* workspace,
+                               size_t workspace_bytes, msa_stream_t stream);
+msa_status_t msa_paged_weights_workspace_bytes(const msa_paged_cache_t* cache, int32_t n_q_heads, size_t* min_bytes);
+
+/*
+ * The tokens that stay: of a sequence of L = kv_lens[s] tokens n = min(L, budget), for each KV head by itself - the last
+ * r = min(recent, n), the first min(sinks, n - r), and of those between the ones with the largest weights (equal weights: the
+ * lower place; NaN counts as lowest).  keep [batch, n_kv_heads, budget] int32 gets their places in ascending order, -1
+ * behind; new_lens [batch] int32 (may be NULL, may not be kv_lens) gets n.  Of `cache` it uses page_table, kv_lens and the sizes only.
+ */
+msa_status_t msa_paged_keep(const msa_paged_cache_t* cache, const float* weights, int32_t budget, int32_t sinks, int32_t recent,
+                            int32_t* keep, int32_t* new_lens, msa_stream_t stream);
+
+/*
+ * Moves token keep[s, h, i] of KV head h to place i of its sequence, for every i < width: its key, its value (cache->v may be
+ * NULL) and its weight (weights may be NULL).  keep [batch, n_kv_heads, width] int32 as msa_paged_keep writes it: ascending
+ * places below kv_lens[s] (still the old lengths), -1 = none.  In place: what stood at places that nothing moves to
+ * stays.  Sequences must not share pages.  A place that is not below the length, on a bad page or below its own i is
+ * reported as a bad index and not moved; of a list that is not ascending the result is otherwise unspecified.
+ */
+msa_status_t msa_paged_compact(const msa_paged_cache_t* cache, const int32_t* keep, int32_t width, float* weights,
+                               msa_stream_t stream);
+
+/* ------------------------------------------------------------------------------------
+ * The next token from its logits (the end of a decode step; the paper has no counterpart).
+ * Settings, each a number for all rows or, where the pointer is not NULL, a value for every row in DEVICE memory:
+ *   temperature  T; 0 or less: the largest logit (lowest index of equal ones), whatever the rest says
+ *   top_k        the top_k largest logits stay (equal ones: lower index first); 0 or less, or vocab or more: all
+ *   top_p        of these, largest first, the shortest run whose probabilities reach top_p of their sum stays (at least
+ *                one token); 1 or more: all
+ *   min_p        of these stay the ones whose probability is at least min_p times the largest; 0 or less: all
+ */
+typedef struct {
+    float temperature;
+    int32_t top_k;
+    float top_p;
+    float min_p;
+    const float* temperatures;
+    const int32_t* top_ks;
+    const float* top_ps;
+    const float* min_ps;
+} msa_sampling_t;
+
+enum { MSA_BF16 = 0, MSA_FP16 = 1, MSA_FP32 = 2 };
+
+/*
+ * For every row: p = softmax(logits / T), what the settings keep of it, and with uniform[row] = u in [0, 1) the first token
+ * index at which the running sum of the kept probabilities exceeds u times their sum -> token[row]; logprob[row] (logprob may
+ * be NULL) is the natural log of its probability among the kept.  Sums are exact to 2^-42 of the largest probability for each
+ * token, in any order: equal calls choose equal tokens.  A logit of -infinity is never chosen; if there are logits of
+ * +infinity, one of them is.  A row with nothing to choose from (all -infinity) or with a NaN (logits, u or T) gives
+ * -1 and NaN.  Rows of `vocab` (at most 2^21) values of logits_type start every `stride` elements.
+ */
+msa_status_t msa_sample(const msa_sampling_t* settings, const void* logits, int32_t logits_type, int64_t stride, int64_t n_rows,
+                        int32_t vocab, const float* uniform, int64_t* token, float* logprob, msa_stream_t stream);
+
 /*
  * Test hook for the device-side bounded waits (the paper has no counterpart).  Every wait of a
  * kernel on an mbarrier gives up after a limit of SM cycles (about two seconds by default),

@@ -243,3 +243,37 @@ def paged_attn(cache: PagedCache, q: torch.Tensor, softmax_scale: float = 0.0, o
     out = B.msa_paged_attn(cache.k, cache.v, cache.page_table, cache.kv_lens, cache.cu_q, q, softmax_scale, out, lse, workspace,
                            max_new=max_new)
     return out, lse
+
+
+def paged_weights(cache: PagedCache, q: torch.Tensor, lse: torch.Tensor, weights: torch.Tensor, decay: float = 1.0,
+                  softmax_scale: float = 0.0, workspace: Optional[torch.Tensor] = None, max_new: int = 0) -> torch.Tensor:
+    """Adds the attention weight that cached tokens receive from the new tokens to `weights` (fp32 [pages, KV heads, page
+    size], in place, returned), after fading what is there by `decay` (0: it is not read).  q and lse as given to and
+    returned by paged_attn - or some of its rows, with a cu_q that counts those (the last tokens of prompts as observers)."""
+    _no_graph("paged_weights", "it has no backward pass; call it under torch.no_grad", q, lse, weights)
+    if workspace is None:
+        workspace = _workspace(q, B.msa_paged_weights_workspace_bytes, cache.k, q.shape[1])
+    B.msa_paged_weights(cache.k, cache.page_table, cache.kv_lens, cache.cu_q, q, lse, softmax_scale, decay, weights, workspace,
+                        max_new=max_new)
+    return weights
+
+
+def paged_keep(cache: PagedCache, weights: torch.Tensor, budget: int, sinks: int = 0, recent: int = 0):
+    """The tokens of each sequence and KV head that stay within a budget: the first `sinks`, the last `recent`, and the
+    largest weights between -> (their places int32 [batch, KV heads, budget], ascending, -1 behind; the new lengths int32
+    [batch])."""
+    return B.msa_paged_keep(cache.k, cache.page_table, cache.kv_lens, cache.cu_q, weights, budget, sinks, recent)
+
+
+def paged_compact(cache: PagedCache, keep: torch.Tensor, weights: Optional[torch.Tensor] = None) -> None:
+    """Moves the tokens at the places `keep` (as paged_keep gives them) to the front of their sequences: keys, values and
+    weights, in place.  cache.kv_lens still holds the old lengths; later calls take the new ones."""
+    B.msa_paged_compact(cache.k, cache.v, cache.page_table, cache.kv_lens, cache.cu_q, keep, weights)
+
+
+def sample(logits: torch.Tensor, uniform: torch.Tensor, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """The next token of each row of logits [rows, vocabulary] (bf16, fp16 or fp32) for given random numbers in [0, 1) (fp32
+    [rows]) -> (token int64 [rows], its log-probability fp32 [rows]).  Settings are numbers or vectors with one for each
+    row; temperature 0 takes the largest logit.  Logits that require gradients are refused outside torch.no_grad."""
+    _no_graph("sample", "a choice has none; call it under torch.no_grad", logits)
+    return B.msa_sample(logits, uniform, temperature, top_k, top_p, min_p)

@@ -34,7 +34,8 @@ EXPORTS = [
     "msa_prefill_forward_host_workspace_bytes", "msa_decode_forward", "msa_decode_forward_host",
     "msa_launch_count", "msa_profile_begin", "msa_profile_end", "msa_index_scores_plan", "msa_debug_set_wait",
     "msa_qk_norm_rope", "msa_norm_rope_plan", "msa_qk_norm_rope_backward", "msa_qk_norm_rope_backward_workspace_bytes", "msa_paged_append",
-    "msa_paged_attn", "msa_paged_attn_workspace_bytes",
+    "msa_paged_attn", "msa_paged_attn_workspace_bytes", "msa_paged_weights", "msa_paged_weights_workspace_bytes",
+    "msa_paged_keep", "msa_paged_compact", "msa_sample",
 ]
 
 
@@ -53,6 +54,11 @@ class MsaPagedCache(ctypes.Structure):
     _fields_ = [("k", c_vp), ("v", c_vp), ("page_table", c_vp), ("kv_lens", c_vp), ("cu_q", c_vp), ("batch", c_i32),
                 ("max_pages", c_i32), ("n_pages", c_i32), ("page_size", c_i32), ("n_kv_heads", c_i32),
                 ("head_dim", c_i32), ("fp8", c_i32), ("max_new", c_i32)]
+
+
+class MsaSampling(ctypes.Structure):
+    _fields_ = [("temperature", ctypes.c_float), ("top_k", c_i32), ("top_p", ctypes.c_float), ("min_p", ctypes.c_float),
+                ("temperatures", c_vp), ("top_ks", c_vp), ("top_ps", c_vp), ("min_ps", c_vp)]
 
 
 class MsaError(RuntimeError):
@@ -386,6 +392,11 @@ _ARGTYPES = {
     "msa_paged_attn_workspace_bytes": [c_vp, c_i32, c_vp],
     "msa_paged_attn": [c_vp, c_vp, c_i32, c_i64, _F32, c_vp, c_vp, c_vp, c_sz, c_vp],
     "msa_paged_append": [c_vp, c_vp, c_vp, c_i64, c_i32, c_vp, c_vp, c_i64, c_vp, c_vp, c_i64, c_i32, _F32, c_i64, c_vp, c_vp],
+    "msa_paged_weights_workspace_bytes": [c_vp, c_i32, c_vp],
+    "msa_paged_weights": [c_vp, c_vp, c_i32, c_vp, c_i64, _F32, _F32, c_vp, c_vp, c_sz, c_vp],
+    "msa_paged_keep": [c_vp, c_vp, c_i32, c_i32, c_i32, c_vp, c_vp, c_vp],
+    "msa_paged_compact": [c_vp, c_vp, c_i32, c_vp, c_vp],
+    "msa_sample": [c_vp, c_vp, c_i32, c_i64, c_i64, c_i32, c_vp, c_vp, c_vp, c_vp],
 }
 _fns = {}
 _POOL_TYPES = {torch.bfloat16: 0, torch.float8_e4m3fn: 1}  # msa_paged_cache_t.fp8
@@ -643,6 +654,105 @@ def msa_paged_attn(k_pool, v_pool, page_table, kv_lens, cu_q, q, softmax_scale, 
     _launch(index, "msa_paged_attn", ctypes.byref(cache), q.data_ptr(), q.shape[1], rows, softmax_scale, out.data_ptr(), _at(lse),
             _at(workspace), _workspace(workspace, index), stream=stream)
     return out
+
+
+def _made(t: Optional[torch.Tensor], shape, dtype, what: str, index: int, stream) -> torch.Tensor:
+    """A dense output of a given shape and type, made here (on the stream that writes it) if there is none."""
+    if t is None:
+        if stream is None:
+            return torch.empty(shape, dtype=dtype, device="cuda:%d" % index)
+        current = torch.cuda.current_stream(index)
+        with torch.cuda.stream(stream):
+            t = torch.empty(shape, dtype=dtype, device="cuda:%d" % index)
+        t.record_stream(current)
+        return t
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.get_device() != index:
+        raise ValueError("%s must be contiguous %s %s on cuda:%d, got %s %s" % (what, dtype, tuple(shape), index, t.dtype, tuple(t.shape)))
+    return t
+
+
+def _weight_pool(t: torch.Tensor, cache: MsaPagedCache, index: int) -> int:
+    want = (cache.n_pages, cache.n_kv_heads, cache.page_size)
+    if t.dtype != torch.float32 or tuple(t.shape) != want or not t.is_contiguous() or t.get_device() != index:
+        raise ValueError("the weights must be contiguous fp32 [pages, KV heads, page size] = %s on cuda:%d, got %s %s"
+                         % (want, index, t.dtype, tuple(t.shape)))
+    return t.data_ptr()
+
+
+def msa_paged_weights_workspace_bytes(k_pool, n_q_heads: int) -> int:
+    pages, size, heads, d = k_pool.shape
+    cache = MsaPagedCache(n_pages=pages, page_size=size, n_kv_heads=heads, head_dim=d, fp8=0 if k_pool.dtype == torch.bfloat16 else 1)
+    mn = c_sz(0)
+    _check(_fn("msa_paged_weights_workspace_bytes")(ctypes.byref(cache), n_q_heads, ctypes.byref(mn)), "msa_paged_weights_workspace_bytes")
+    return mn.value
+
+
+def msa_paged_weights(k_pool, page_table, kv_lens, cu_q, q, lse, softmax_scale, decay, weights, workspace, stream=None, max_new=0):
+    """q: bf16 [rows, heads, d] dense; lse: fp32 [rows, heads]; weights: fp32 [pages, KV heads, page size], updated in place."""
+    index, cache = _paged(k_pool, None, page_table, kv_lens, cu_q)
+    cache.max_new = max_new
+    d, rows = cache.head_dim, q.shape[0]
+    _heads(q, "q", d, rows, index, dense=True)
+    if lse.dtype != torch.float32 or lse.shape != q.shape[:2] or not lse.is_contiguous() or lse.get_device() != index:
+        raise ValueError("lse must be contiguous fp32 %s on cuda:%d" % (tuple(q.shape[:2]), index))
+    _launch(index, "msa_paged_weights", ctypes.byref(cache), q.data_ptr(), q.shape[1], lse.data_ptr(), rows, softmax_scale, decay,
+            _weight_pool(weights, cache, index), _at(workspace), _workspace(workspace, index), stream=stream)
+
+
+def msa_paged_keep(k_pool, page_table, kv_lens, cu_q, weights, budget, sinks, recent, keep=None, new_lens=None, stream=None):
+    """-> (keep int32 [batch, KV heads, budget], new_lens int32 [batch]); those that are not given are made."""
+    index, cache = _paged(k_pool, None, page_table, kv_lens, cu_q)
+    at = _weight_pool(weights, cache, index)
+    keep = _made(keep, (cache.batch, cache.n_kv_heads, max(budget, 0)), torch.int32, "keep", index, stream)
+    new_lens = _made(new_lens, (cache.batch,), torch.int32, "new_lens", index, stream)
+    _launch(index, "msa_paged_keep", ctypes.byref(cache), at, budget, sinks, recent, keep.data_ptr(), new_lens.data_ptr(), stream=stream)
+    return keep, new_lens
+
+
+def msa_paged_compact(k_pool, v_pool, page_table, kv_lens, cu_q, keep, weights, stream=None):
+    """keep: int32 [batch, KV heads, width]; weights: fp32 [pages, KV heads, page size] or None.  Pools and weights change in place."""
+    index, cache = _paged(k_pool, v_pool, page_table, kv_lens, cu_q)
+    if (keep.dtype != torch.int32 or keep.dim() != 3 or tuple(keep.shape[:2]) != (cache.batch, cache.n_kv_heads) or
+            not keep.is_contiguous() or keep.get_device() != index):
+        raise ValueError("keep must be contiguous int32 [%d, %d, width] on cuda:%d, got %s %s"
+                         % (cache.batch, cache.n_kv_heads, index, keep.dtype, tuple(keep.shape)))
+    at = None if weights is None else _weight_pool(weights, cache, index)
+    _launch(index, "msa_paged_compact", ctypes.byref(cache), keep.data_ptr(), keep.shape[2], at, stream=stream)
+
+
+_LOGIT_TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+
+
+def _setting(v, dtype, rows: int, index: int, what: str):
+    """(number, device pointer) of a setting: a number for all rows or a tensor of one for every row."""
+    if not torch.is_tensor(v):
+        return v, None
+    if v.dtype != dtype or v.shape != (rows,) or not v.is_contiguous() or v.get_device() != index:
+        raise ValueError("%s must be a number or a contiguous %s vector, one for each of %d rows, on cuda:%d" % (what, dtype, rows, index))
+    return 0, v.data_ptr()
+
+
+def msa_sample(logits, uniform, temperature, top_k, top_p, min_p, token=None, logprob=None, stream=None):
+    """logits: [rows, vocabulary] of bf16, fp16 or fp32, rows may be strided; uniform: fp32 [rows]; settings: numbers, or fp32
+    (top_k: int32) vectors.  -> (token int64 [rows], logprob fp32 [rows]); those that are not given are made."""
+    index = _device_of(logits, "the logits")
+    if logits.dtype not in _LOGIT_TYPES or logits.dim() != 2 or logits.shape[1] < 1 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("the logits must be bf16, fp16 or fp32 [rows, vocabulary] with dense rows, got %s %s, strides %s"
+                         % (logits.dtype, tuple(logits.shape), logits.stride()))
+    rows, vocab = logits.shape
+    stride = logits.stride(0) if rows > 1 else vocab
+    if stride < vocab:
+        raise ValueError("rows of the logits must not overlap: %d values every %d" % (vocab, stride))
+    if uniform.dtype != torch.float32 or uniform.shape != (rows,) or not uniform.is_contiguous() or uniform.get_device() != index:
+        raise ValueError("the random numbers must be a contiguous fp32 vector, one for each of %d rows, on cuda:%d" % (rows, index))
+    f32 = torch.float32
+    (t, ts), (k, ks) = _setting(temperature, f32, rows, index, "temperature"), _setting(top_k, torch.int32, rows, index, "top_k")
+    (p, ps), (m, ms) = _setting(top_p, f32, rows, index, "top_p"), _setting(min_p, f32, rows, index, "min_p")
+    token = _made(token, (rows,), torch.int64, "token", index, stream)
+    logprob = _made(logprob, (rows,), f32, "logprob", index, stream)
+    _launch(index, "msa_sample", ctypes.byref(MsaSampling(t, k, p, m, ts, ks, ps, ms)), logits.data_ptr(), _LOGIT_TYPES[logits.dtype],
+            stride, rows, vocab, uniform.data_ptr(), token.data_ptr(), logprob.data_ptr(), stream=stream)
+    return token, logprob
 
 
 # ------------------------------------------------------------------ allocation helpers

@@ -1,13 +1,15 @@
 // C ABI of what stands around the sparse path (see include/msa.h): norms of queries and keys with the position
-// rotation and their gradients, the paged K/V cache, attention of new tokens over it.  Argument validation,
-// launch shapes and dispatch; the arithmetic is in the kernels included below.
+// rotation and their gradients, the paged K/V cache, attention of new tokens over it, and keeping it within a budget.
+// Argument validation, launch shapes and dispatch; the arithmetic is in the kernels included below.
 #include <algorithm>
 #include <cmath>
 
+#include "evict.cuh"
 #include "norm_rope.cuh"
 #include "paged_attn.cuh"
 #include "paged_few8.cuh"
 #include "tc_common.cuh"
+#include "weigh.cuh"
 
 namespace msa {
 
@@ -293,6 +295,43 @@ static msa_status_t launch_paged_attn(const PagedAttnArgs& a, const msa_paged_ca
     return launch_status();
 }
 
+// ---------------------------------------------------------------------- keeping the cache within a budget
+template <bool F8>
+static msa_status_t launch_weigh(const WeighArgs& a, int d, int64_t cap, cudaStream_t st) {
+    int* status = status_word();
+    if (status == nullptr) return cuda_failed();
+    if (d != 128) {
+        const dim3 grid((unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div64(cap, 128), 1024)),
+                        (unsigned)std::min<int64_t>((int64_t)a.c.batch * a.c.H_kv, 65535));
+        StageScope sc(kStageNone, st);
+        weigh_generic_kernel<F8><<<grid, 128, 0, st>>>(a, d, status);
+        return launch_status();
+    }
+    // rows of a sequence if all have as many: eight, sixteen or more of them stay in registers
+    const int64_t rows = ceil_div64(a.n_tokens, a.c.batch) * a.G;
+    const int grid = (rows <= 16 ? 2 : 1) * sm_count();
+    StageScope sc(kStageNone, st);
+    if (rows <= 8) weigh_few_kernel<1, F8><<<grid, kWeighWarps * 32, 0, st>>>(a, 1.0 / grid, status);
+    else if (rows <= 16) weigh_few_kernel<2, F8><<<grid, kWeighWarps * 32, 0, st>>>(a, 1.0 / grid, status);
+    else weigh_few_kernel<4, F8><<<grid, kWeighWarps * 32, 0, st>>>(a, 1.0 / grid, status);
+    return launch_status();
+}
+
+// What a call on the cache's places needs of it (no new tokens, maybe no keys).
+static msa_status_t resolve_places(const msa_paged_cache_t* c, PagedView& v) {
+    if (c == nullptr) return MSA_ERR_INVALID_ARG;
+    if (c->batch < 0 || c->max_pages < 0 || c->n_pages < 0 || c->page_size <= 0 || c->n_kv_heads <= 0 || c->head_dim <= 0)
+        return MSA_ERR_INVALID_ARG;
+    if (c->fp8 != 0 && c->fp8 != 1) return MSA_ERR_INVALID_ARG;
+    if (c->head_dim % 8 != 0 || c->head_dim > 256 || c->n_kv_heads > kMaxRopeHeads) return MSA_ERR_UNSUPPORTED;
+    if ((int64_t)c->batch * c->n_kv_heads > 2147483647LL) return MSA_ERR_UNSUPPORTED;
+    v = PagedView{nullptr, c->kv_lens, c->page_table, c->batch, c->max_pages, c->n_pages, c->page_size, c->n_kv_heads};
+    if (c->batch == 0) return MSA_OK;
+    if (!c->kv_lens || !aligned_to(c->kv_lens, 4)) return MSA_ERR_INVALID_ARG;
+    if (c->max_pages > 0 && (!c->page_table || !aligned_to(c->page_table, 4))) return MSA_ERR_INVALID_ARG;
+    return MSA_OK;
+}
+
 }  // namespace msa
 
 using namespace msa;
@@ -501,6 +540,89 @@ msa_status_t msa_paged_attn(const msa_paged_cache_t* cache, const void* q, int32
         if (cache->fp8) paged_attn_generic_kernel<true><<<(unsigned)grid, 128, 0, st>>>(a, (const __nv_bfloat16*)q, cache->k, cache->v, d, status);
         else paged_attn_generic_kernel<false><<<(unsigned)grid, 128, 0, st>>>(a, (const __nv_bfloat16*)q, cache->k, cache->v, d, status);
     }
+    return launch_status();
+}
+
+msa_status_t msa_paged_weights_workspace_bytes(const msa_paged_cache_t* cache, int32_t n_q_heads, size_t* min_bytes) {
+    PagedView view;
+    const msa_status_t s = resolve_cache(cache, 0, view);
+    if (s != MSA_OK) return s;
+    if (n_q_heads <= 0 || n_q_heads % cache->n_kv_heads != 0 || min_bytes == nullptr) return MSA_ERR_INVALID_ARG;
+    *min_bytes = 0;
+    return MSA_OK;
+}
+
+msa_status_t msa_paged_weights(const msa_paged_cache_t* cache, const void* q, int32_t n_q_heads, const float* lse,
+                               int64_t n_tokens, float softmax_scale, float decay, float* weights, void* workspace,
+                               size_t workspace_bytes, msa_stream_t stream) {
+    PagedView view;
+    const msa_status_t s = resolve_cache(cache, n_tokens, view);
+    if (s != MSA_OK) return s;
+    const int d = cache->head_dim;
+    if (n_q_heads <= 0 || n_q_heads % cache->n_kv_heads != 0) return MSA_ERR_INVALID_ARG;
+    if (!(softmax_scale >= 0.f) || !std::isfinite(softmax_scale) || !(decay >= 0.f) || !std::isfinite(decay)) return MSA_ERR_INVALID_ARG;
+    if (n_q_heads > kMaxRopeHeads) return MSA_ERR_UNSUPPORTED;
+    if (n_tokens == 0 || cache->batch == 0) return MSA_OK;
+    if (!rows_ok(q, (int64_t)n_q_heads * d, n_q_heads, d) || lse == nullptr || !aligned_to(lse, 4)) return MSA_ERR_INVALID_ARG;
+    if (cache->n_pages > 0 && (weights == nullptr || !aligned_to(weights, 4))) return MSA_ERR_INVALID_ARG;
+    const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)d);
+    WeighArgs a{};
+    a.c = view;
+    a.k = cache->k;
+    a.q = (const __nv_bfloat16*)q;
+    a.lse = lse;
+    a.w = weights;
+    a.G = n_q_heads / cache->n_kv_heads;
+    a.n_tokens = (int)n_tokens;
+    a.max_len = 2147483647;
+    a.scale_log2e = scale * 1.4426950408889634f;
+    a.decay = decay;
+    const int64_t cap = (int64_t)cache->max_pages * cache->page_size;
+    return cache->fp8 ? launch_weigh<true>(a, d, cap, (cudaStream_t)stream) : launch_weigh<false>(a, d, cap, (cudaStream_t)stream);
+}
+
+msa_status_t msa_paged_keep(const msa_paged_cache_t* cache, const float* weights, int32_t budget, int32_t sinks, int32_t recent,
+                            int32_t* keep, int32_t* new_lens, msa_stream_t stream) {
+    PagedView view;
+    const msa_status_t s = resolve_places(cache, view);
+    if (s != MSA_OK) return s;
+    if (budget <= 0 || sinks < 0 || recent < 0) return MSA_ERR_INVALID_ARG;
+    if (cache->batch == 0) return MSA_OK;
+    if (keep == nullptr || !aligned_to(keep, 4) || !aligned_to(new_lens, 4)) return MSA_ERR_INVALID_ARG;
+    if (cache->n_pages > 0 && (weights == nullptr || !aligned_to(weights, 4))) return MSA_ERR_INVALID_ARG;
+    const KeepArgs a{view, weights, keep, new_lens, budget, sinks, recent};
+    int* status = status_word();
+    if (status == nullptr) return cuda_failed();
+    const unsigned grid = (unsigned)(cache->batch * cache->n_kv_heads);
+    cudaStream_t st = (cudaStream_t)stream;
+    StageScope sc(kStageNone, st);
+    if (cache->page_size % 4 == 0 && aligned_to(weights, 16)) paged_keep_kernel<4><<<grid, kKeepThreads, 0, st>>>(a, status);
+    else paged_keep_kernel<1><<<grid, kKeepThreads, 0, st>>>(a, status);
+    return launch_status();
+}
+
+msa_status_t msa_paged_compact(const msa_paged_cache_t* cache, const int32_t* keep, int32_t width, float* weights,
+                               msa_stream_t stream) {
+    PagedView view;
+    const msa_status_t s = resolve_places(cache, view);
+    if (s != MSA_OK) return s;
+    if (width < 0) return MSA_ERR_INVALID_ARG;
+    if (cache->batch == 0 || width == 0) return MSA_OK;
+    if (keep == nullptr || !aligned_to(keep, 4) || !aligned_to(weights, 4)) return MSA_ERR_INVALID_ARG;
+    if (cache->n_pages > 0 && (!cache->k || !aligned_to(cache->k, 16) || !aligned_to(cache->v, 16))) return MSA_ERR_INVALID_ARG;
+    const int row = cache->head_dim * (cache->fp8 ? 1 : 2);
+    CompactArgs a{view, {(uint8_t*)cache->k, (uint8_t*)cache->v}, weights, keep, width, row, row};
+    // Slices of a row (whole sectors) until the machine has four CTAs per SM.
+    const int64_t heads = (int64_t)cache->batch * cache->n_kv_heads;
+    while (a.slice_bytes % 64 == 0 && heads * 2 * (row / a.slice_bytes) < 4LL * sm_count()) a.slice_bytes /= 2;
+    const int slices = row / a.slice_bytes;
+    int* status = status_word();
+    if (status == nullptr) return cuda_failed();
+    const dim3 grid((unsigned)heads, 2 * slices + (weights != nullptr ? 1 : 0));
+    cudaStream_t st = (cudaStream_t)stream;
+    StageScope sc(kStageNone, st);
+    if (a.slice_bytes % 16 == 0) paged_compact_kernel<uint4><<<grid, kCompactThreads, 0, st>>>(a, slices, status);
+    else paged_compact_kernel<uint2><<<grid, kCompactThreads, 0, st>>>(a, slices, status);
     return launch_status();
 }
 
