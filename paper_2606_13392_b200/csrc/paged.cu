@@ -10,6 +10,7 @@
 #include "paged_few8.cuh"
 #include "tc_common.cuh"
 #include "weigh.cuh"
+#include "weigh_tc.cuh"
 
 namespace msa {
 
@@ -296,25 +297,76 @@ static msa_status_t launch_paged_attn(const PagedAttnArgs& a, const msa_paged_ca
 }
 
 // ---------------------------------------------------------------------- keeping the cache within a budget
+// Workspace of the tcgen05 kernel: the CTAs' ends, then two blocks of partial sums each.
+struct WeighWorkspace { size_t ends, part, bytes; };
+static WeighWorkspace weigh_workspace() {
+    const size_t n = sm_count(), ends = (n * sizeof(WeighEnds) + 255) / 256 * 256;
+    return WeighWorkspace{0, ends, ends + 2 * n * kWtKeys * sizeof(float)};
+}
+
+// Which kernels a call takes.  weigh_few_kernel reads the keys of a sequence once as long as its rows stay in registers (32);
+// beyond, it would read queries again for every key.  The lengths are on the device; the host knows their sum and count, and
+// the caller may say the longest (as in paged_few8).
+//   tokens: of the longest sequence that the small kernel takes, 0: none.  alone: it takes all.
+static PagedFew weigh_few(const WeighArgs& a, const msa_paged_cache_t& c) {
+    const int most = kWeighFewRows / a.G;
+    if (!paged_tc_ok(c, a.G)) return PagedFew{1, true};
+    const int longest = c.max_new > 0 ? std::min(c.max_new, a.n_tokens) : a.n_tokens;
+    if (longest <= most) return PagedFew{longest, true};
+    if (most > 0 && a.n_tokens <= (int64_t)c.batch * most)
+        return PagedFew{most, c.max_new == 0 && a.n_tokens - (c.batch - 1) <= most};
+    return PagedFew{0, false};
+}
+
 template <bool F8>
-static msa_status_t launch_weigh(const WeighArgs& a, int d, int64_t cap, cudaStream_t st) {
+static msa_status_t launch_weigh(WeighArgs a, const msa_paged_cache_t& c, void* workspace, cudaStream_t st) {
     int* status = status_word();
     if (status == nullptr) return cuda_failed();
-    if (d != 128) {
-        const dim3 grid((unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div64(cap, 128), 1024)),
+    if (c.head_dim != 128) {
+        const dim3 grid((unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div64((int64_t)c.max_pages * c.page_size, 128), 1024)),
                         (unsigned)std::min<int64_t>((int64_t)a.c.batch * a.c.H_kv, 65535));
         StageScope sc(kStageNone, st);
-        weigh_generic_kernel<F8><<<grid, 128, 0, st>>>(a, d, status);
+        weigh_generic_kernel<F8><<<grid, 128, 0, st>>>(a, c.head_dim, status);
         return launch_status();
     }
-    // rows of a sequence if all have as many: eight, sixteen or more of them stay in registers
-    const int64_t rows = ceil_div64(a.n_tokens, a.c.batch) * a.G;
-    const int grid = (rows <= 16 ? 2 : 1) * sm_count();
-    StageScope sc(kStageNone, st);
-    if (rows <= 8) weigh_few_kernel<1, F8><<<grid, kWeighWarps * 32, 0, st>>>(a, 1.0 / grid, status);
-    else if (rows <= 16) weigh_few_kernel<2, F8><<<grid, kWeighWarps * 32, 0, st>>>(a, 1.0 / grid, status);
-    else weigh_few_kernel<4, F8><<<grid, kWeighWarps * 32, 0, st>>>(a, 1.0 / grid, status);
-    return launch_status();
+    const PagedFew few = weigh_few(a, c);
+    if (few.tokens > 0) {
+        WeighArgs f = a;
+        if (!few.alone) { f.max_len = few.tokens; a.min_len = few.tokens + 1; }
+        // rows of a sequence if all have as many: eight, sixteen or more of them stay in registers
+        const int64_t rows = std::min<int64_t>(ceil_div64(a.n_tokens, c.batch), few.tokens) * a.G;
+        const int grid = (rows <= 16 ? 2 : 1) * sm_count();
+        {
+            StageScope sc(kStageNone, st);
+            if (rows <= 8) weigh_few_kernel<1, F8><<<grid, kWeighWarps * 32, 0, st>>>(f, 1.0 / grid, status);
+            else if (rows <= 16) weigh_few_kernel<2, F8><<<grid, kWeighWarps * 32, 0, st>>>(f, 1.0 / grid, status);
+            else weigh_few_kernel<4, F8><<<grid, kWeighWarps * 32, 0, st>>>(f, 1.0 / grid, status);
+        }
+        const msa_status_t s = launch_status();
+        if (few.alone || s != MSA_OK) return s;
+    }
+    const int TPT = 128 / a.G, grid = sm_count();
+    CUtensorMap tm_q;
+    const uint64_t H_q = (uint64_t)a.c.H_kv * a.G, qd[3] = {128, H_q, (uint64_t)a.n_tokens}, qs[2] = {256, H_q * 256};
+    const uint32_t qb[3] = {64, (uint32_t)a.G, (uint32_t)TPT};
+    if (!encode_tmap_bf16(&tm_q, a.q, 3, qd, qs, qb)) return cuda_failed();
+    static bool attr_set[64] = {false};  // per device
+    const int dev = current_device();
+    if (!attr_set[dev]) {
+        if (cudaFuncSetAttribute(weigh_tc_kernel<F8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(WeighTcSmem)) != cudaSuccess)
+            return cuda_failed();
+        attr_set[dev] = true;
+    }
+    const WeighWorkspace w = weigh_workspace();
+    float* part = (float*)((char*)workspace + w.part);
+    WeighEnds* ends = (WeighEnds*)((char*)workspace + w.ends);
+    {
+        StageScope sc(kStageNone, st);
+        weigh_tc_kernel<F8><<<grid, kWtThreads, sizeof(WeighTcSmem), st>>>(tm_q, a, TPT, part, ends, 1.0 / grid, status);
+    }
+    const msa_status_t s = launch_status();
+    if (s != MSA_OK) return s;
+    return launch_early(weigh_merge_kernel, dim3(grid), kWtKeys, 0, st, a, TPT, (const float*)part, (const WeighEnds*)ends, grid, status);
 }
 
 // What a call on the cache's places needs of it (no new tokens, maybe no keys).
@@ -548,7 +600,7 @@ msa_status_t msa_paged_weights_workspace_bytes(const msa_paged_cache_t* cache, i
     const msa_status_t s = resolve_cache(cache, 0, view);
     if (s != MSA_OK) return s;
     if (n_q_heads <= 0 || n_q_heads % cache->n_kv_heads != 0 || min_bytes == nullptr) return MSA_ERR_INVALID_ARG;
-    *min_bytes = 0;
+    *min_bytes = paged_tc_ok(*cache, n_q_heads / cache->n_kv_heads) ? weigh_workspace().bytes : 0;
     return MSA_OK;
 }
 
@@ -577,8 +629,11 @@ msa_status_t msa_paged_weights(const msa_paged_cache_t* cache, const void* q, in
     a.max_len = 2147483647;
     a.scale_log2e = scale * 1.4426950408889634f;
     a.decay = decay;
-    const int64_t cap = (int64_t)cache->max_pages * cache->page_size;
-    return cache->fp8 ? launch_weigh<true>(a, d, cap, (cudaStream_t)stream) : launch_weigh<false>(a, d, cap, (cudaStream_t)stream);
+    if (paged_tc_ok(*cache, a.G)) {
+        if (workspace == nullptr || !aligned_to(workspace, 256)) return MSA_ERR_INVALID_ARG;
+        if (workspace_bytes < weigh_workspace().bytes) return MSA_ERR_WORKSPACE;
+    }
+    return cache->fp8 ? launch_weigh<true>(a, *cache, workspace, (cudaStream_t)stream) : launch_weigh<false>(a, *cache, workspace, (cudaStream_t)stream);
 }
 
 msa_status_t msa_paged_keep(const msa_paged_cache_t* cache, const float* weights, int32_t budget, int32_t sinks, int32_t recent,

@@ -1,0 +1,463 @@
+// The attention weight that cached tokens receive (see weigh.cuh), for sequences of more than a few query rows: tcgen05.
+//
+// Keys are the rows of the products, D = K Q^T, so that the sum over queries runs along a row of the accumulator: a thread
+// owns a key, adds exp2(scale D - lse) over the columns, and nothing is exchanged until a part ends.  256 keys (two
+// operand tiles) stay in shared memory while the queries' tiles of 128 rows - (token, head of the group) pairs, TPT = 128 / G
+// tokens - stream past them; each tile is read once for two products.
+// One exponential for 2 * 128 flops: the exponential unit (16 a cycle and SM) and the tensor pipe are both near their limits.
+//
+// Unit of work: one tile of rows against 256 keys of a (sequence, KV head).  All units form one line (sequence, head, key
+// block, tile), tiles that see none of the keys left out; every CTA takes an equal stretch, so that neither ragged batches nor the
+// causal triangle leave CTAs idle.  A key block that a boundary cuts leaves partial sums (at most two per CTA), which
+// weigh_merge_kernel adds up in order.
+#pragma once
+
+#include "paged_attn.cuh"
+#include "weigh.cuh"
+
+namespace msa {
+
+constexpr int kWtKeys = 256, kWtStages = 3;
+constexpr int kWtEpiWarps = 16, kWtLoadWarps = 4, kWtThreads = (kWtEpiWarps + 2 + kWtLoadWarps) * 32;
+constexpr int kWtBlockCost = 2;  // tiles' worth of a key block's beginning and end
+
+// kb0: first key block behind `base`; [kb_lim, n_kb): blocks that no row of the call sees (it may lack rows)
+struct WeighTcSeq { int q_row, q_len, kv, base, n_tiles, kb0, kb_lim, n_kb; };
+
+__host__ __device__ __forceinline__ WeighTcSeq weigh_tc_seq(const WeighArgs& a, int TPT, int s) {
+    WeighTcSeq q;
+    const int lo = max(a.c.cu_q[s], 0), end = a.c.cu_q[s + 1], hi = min(end, a.n_tokens);
+    q.q_row = lo;
+    q.q_len = max(hi - lo, 0);
+    if (q.q_len < a.min_len || q.q_len > a.max_len) q.q_len = 0;
+    q.kv = (int)min((int64_t)max(a.c.kv_lens[s], 0), (int64_t)a.c.max_pages * a.c.page_size);
+    q.base = q.kv - max(end - lo, 0);
+    q.n_tiles = (q.q_len + TPT - 1) / TPT;
+    q.n_kb = q.q_len == 0 ? 0 : (int)(((int64_t)q.kv + kWtKeys - 1) / kWtKeys);
+    q.kb0 = q.base <= 0 ? 0 : (int)min(((int64_t)q.base + kWtKeys - 1) / kWtKeys, (int64_t)q.n_kb);
+    q.kb_lim = (int)min((max((int64_t)q.base + (int64_t)q.n_tiles * TPT, (int64_t)0) + kWtKeys - 1) / kWtKeys, (int64_t)q.n_kb);
+    return q;
+}
+
+// First tile with a token that sees a key of block kb (n_tiles where the call lacks those rows).
+__host__ __device__ __forceinline__ int weigh_tc_first(const WeighTcSeq& q, int TPT, int kb) {
+    const int64_t tok = (int64_t)kb * kWtKeys - q.base;
+    return tok <= 0 ? 0 : (int)min(tok / TPT, (int64_t)q.n_tiles);
+}
+
+// Units of the first kb key blocks of one head, their cost included.
+__host__ __device__ inline int64_t weigh_tc_before(const WeighTcSeq& q, int TPT, int kb) {
+    const int seen = min(kb, q.kb_lim), extra = max(seen - q.kb0, 0);
+    int64_t u = (int64_t)seen * q.n_tiles + (int64_t)kb * kWtBlockCost;
+    if (extra > 0) u -= floor_sum(extra, TPT, kWtKeys, (int64_t)q.kb0 * kWtKeys - q.base);
+    return u;
+}
+
+struct WeighTcSpot { int seq, head, kb, tile; };
+
+struct WeighPart {
+    int seq, head, kb, q_row, q_len, kv, base;
+    int t0, lo, hi, n;  // tiles [lo, hi) of the block's [t0, n)
+    __device__ bool whole() const { return lo == t0 && hi == n; }
+};
+
+struct WeighTcWalk {
+    WeighTcSpot at, end;
+    WeighTcSeq q;
+    int loaded;
+    __device__ WeighTcWalk(const WeighTcSpot& from, const WeighTcSpot& to) : at(from), end(to), loaded(-1) {}
+    __device__ bool next(const WeighArgs& a, int TPT, WeighPart& p) {
+        while (at.seq < a.c.batch) {
+            if (loaded != at.seq) { q = weigh_tc_seq(a, TPT, at.seq); loaded = at.seq; }
+            if (at.kb >= q.n_kb) {
+                at.kb = 0;
+                if (++at.head >= a.c.H_kv || q.n_kb == 0) {
+                    if (at.seq >= end.seq) { at.seq = a.c.batch; return false; }
+                    at.head = 0;
+                    ++at.seq;
+                }
+                at.tile = 0;
+                continue;
+            }
+            const bool last = at.seq == end.seq && at.head == end.head && at.kb == end.kb;
+            const int t0 = weigh_tc_first(q, TPT, at.kb), lo = max(at.tile, t0), hi = last ? min(end.tile, q.n_tiles) : q.n_tiles;
+            p = WeighPart{at.seq, at.head, at.kb, q.q_row, q.q_len, q.kv, q.base, t0, lo, hi, q.n_tiles};
+            at.tile = 0;
+            ++at.kb;
+            if (last) at.seq = a.c.batch;
+            // (a block that no row of the call sees is still visited once: its old weights fade)
+            if (lo < hi || (t0 == q.n_tiles && !last)) return true;
+        }
+        return false;
+    }
+};
+
+struct WeighTcPlan {
+    int64_t scan[kWtThreads / 32], targets[2];
+    WeighTcSpot spot[2];
+};
+
+__device__ inline void weigh_tc_stretch(const WeighArgs& a, int TPT, WeighTcPlan& p, double inv_grid, int* status) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    constexpr int WARPS = kWtThreads / 32;
+    if (threadIdx.x < 2) { p.targets[threadIdx.x] = -1; p.spot[threadIdx.x] = WeighTcSpot{a.c.batch, 0, 0, 0}; }
+    const int per = (a.c.batch + kWtThreads - 1) / kWtThreads;
+    const int lo = min((int)threadIdx.x * per, a.c.batch), hi = min(lo + per, a.c.batch);
+    auto units = [&](int s) {
+        const WeighTcSeq q = weigh_tc_seq(a, TPT, s);
+        return (int64_t)a.c.H_kv * weigh_tc_before(q, TPT, q.n_kb);
+    };
+    int64_t mine = 0;
+    for (int s = lo; s < hi; ++s) {
+        mine += units(s);
+        if (blockIdx.x == 0 && (a.c.kv_lens[s] < 0 || a.c.kv_lens[s] > (int64_t)a.c.max_pages * a.c.page_size))
+            report_async(status, kAsyncBadIndex, 0x801);
+    }
+    int64_t upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t below = __shfl_up_sync(0xffffffffu, upto, o);
+        if (lane >= o) upto += below;
+    }
+    if (lane == 31) p.scan[warp] = upto;
+    __syncthreads();
+    int64_t total = 0;
+    for (int w = 0; w < WARPS; ++w) {
+        if (w < warp) upto += p.scan[w];
+        total += p.scan[w];
+    }
+    for (int e = 0; e < 2; ++e) {
+        int64_t u = (int64_t)((double)total * (double)(blockIdx.x + e) * inv_grid);
+        if (blockIdx.x + e >= gridDim.x || u < upto - mine || u >= upto) continue;  // (one thread)
+        u -= upto - mine;
+        for (int s = lo; s < hi; ++s) {
+            const int64_t all = units(s);
+            if (u < all) {
+                p.targets[e] = u;
+                p.spot[e].seq = s;
+                break;
+            }
+            u -= all;
+        }
+    }
+    __syncthreads();
+    if (lane == 0 && warp < 2 && p.targets[warp] >= 0) {
+        WeighTcSpot& spot = p.spot[warp];
+        const WeighTcSeq q = weigh_tc_seq(a, TPT, spot.seq);
+        const int64_t per_head = weigh_tc_before(q, TPT, q.n_kb);
+        int64_t u = p.targets[warp];
+        spot.head = (int)(u / per_head);
+        u -= spot.head * per_head;
+        int b = 0, e = q.n_kb;  // before(b) <= u < before(e)
+        while (e - b > 1) {
+            const int mid = (b + e) >> 1;
+            if (weigh_tc_before(q, TPT, mid) <= u) b = mid; else e = mid;
+        }
+        spot.kb = b;
+        // (a boundary in the block's cost is its end)
+        spot.tile = (int)min((int64_t)weigh_tc_first(q, TPT, b) + u - weigh_tc_before(q, TPT, b), (int64_t)q.n_tiles);
+    }
+}
+
+// What weigh_merge_kernel has to know about a CTA: first 0 no part; 1 its first block came from an earlier CTA and goes on in a
+// later one; 2 came from an earlier one and ends here; 3 begins here.  open: its last block begins here and ends later.
+struct WeighEnds { int first, open, seq, head, kb, pad[3]; };
+static_assert(sizeof(WeighEnds) == 32, "two int4");
+
+struct WeighTcSmem {
+    alignas(1024) uint8_t k[2][2][128 * 256];  // [buffer][128 keys]: [d half][key][64 bf16], 128-byte swizzle
+    alignas(1024) uint8_t q[kWtStages][128 * 256];
+    float nl[kWtStages][128];                  // -lse of the tile's rows, base two
+    union {
+        float join[kWtKeys];                   // the second half of the columns' sums on their way to the first's threads
+        WeighTcPlan plan;
+    };
+    alignas(8) uint64_t q_full[kWtStages], q_empty[kWtStages], l_full[kWtStages], l_empty[kWtStages];
+    uint64_t d_full[2][2], d_empty[2][2], k_full[2], k_empty[2], j_full[2], j_empty[2], drain;
+    uint32_t tmem_base;
+    int abort;
+};
+static_assert(sizeof(WeighTcSmem) <= 227 * 1024, "a CTA's shared memory");
+
+__device__ __forceinline__ uint32_t weigh_tc_off(int row, int chunk) {  // 16-byte chunk of an operand row
+    return (uint32_t)((chunk >> 3) * 16384 + row * 128 + (((chunk & 7) ^ (row & 7)) << 4));
+}
+
+// Warps: 0-15 sums (quadrant of lanes w mod 4, key tile (w / 4) mod 2, half of the columns w / 8), 16 issues the products, 17
+// loads queries, 18-21 load keys.
+template <bool F8>
+__global__ void __launch_bounds__(kWtThreads, 1)
+weigh_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const WeighArgs a, int TPT, float* part, WeighEnds* ends, double inv_grid, int* status) {
+    extern __shared__ __align__(1024) uint8_t weigh_smem[];  // (no room to round the base up)
+    WeighTcSmem& sm = *reinterpret_cast<WeighTcSmem*>(weigh_smem);
+    if ((smem_u32(weigh_smem) & 1023) != 0) {  // swizzled tiles need it; the same for every thread
+        if (threadIdx.x == 0) {
+            report_async(status, kAsyncBadIndex, 0x8FF);
+            ends[blockIdx.x] = WeighEnds{};
+        }
+        return;
+    }
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    volatile int* abort = &sm.abort;
+    weigh_tc_stretch(a, TPT, sm.plan, inv_grid, status);
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kWtStages; ++i) {
+            mbar_init(&sm.q_full[i], 1); mbar_init(&sm.q_empty[i], 1); mbar_init(&sm.l_full[i], 32); mbar_init(&sm.l_empty[i], kWtEpiWarps);
+        }
+        for (int i = 0; i < 2; ++i) {
+            for (int j = 0; j < 2; ++j) { mbar_init(&sm.d_full[i][j], 1); mbar_init(&sm.d_empty[i][j], kWtEpiWarps / 2); }
+            mbar_init(&sm.k_full[i], kWtLoadWarps * 32); mbar_init(&sm.k_empty[i], 1);
+            mbar_init(&sm.j_full[i], kWtEpiWarps / 4); mbar_init(&sm.j_empty[i], kWtEpiWarps / 4);
+        }
+        mbar_init(&sm.drain, 1);
+        sm.abort = 0;
+        fence_mbar_init();
+        tma_prefetch_desc(&tm_q);
+    }
+    if (warp == 16) tmem_alloc(&sm.tmem_base, 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sm.tmem_base;
+    WeighTcWalk walk(sm.plan.spot[0], sm.plan.spot[1]);
+    __syncthreads();  // (the plan's memory is the sums' from here on)
+    WeighPart p{};
+    const int H_q = a.c.H_kv * a.G;
+    bool ok = true;
+    int T = 0;  // tiles so far
+
+    if (warp < kWtEpiWarps) {
+        // ---------------- sums
+        const int quad = warp & 3, dd = (warp >> 2) & 1, half = warp >> 3;
+        const int in_block = dd * 128 + quad * 32 + lane;
+        WeighEnds e{};
+        for (int n = 0; ok && walk.next(a, TPT, p); ++n) {
+            const int key = p.kb * kWtKeys + in_block;
+            const int first_tok = key - p.base;  // first token that sees the key
+            float total = 0.f;
+            for (int t = p.lo; t < p.hi; ++t, ++T) {
+                const int st = T % kWtStages, buf = T & 1;
+                if (!mbar_wait(&sm.l_full[st], (T / kWtStages) & 1, abort) || !mbar_wait(&sm.d_full[buf][dd], (T >> 1) & 1, abort)) {
+                    if (lane == 0) report_async(status, kAsyncTimeout, 0x821);
+                    ok = false;
+                    break;
+                }
+                tc_fence_after();
+                // visible columns [c_lo, c_hi) of this thread's key; all of them for all keys of the warp: no masks
+                const int tok0 = t * TPT;
+                const int c_hi = min(TPT, p.q_len - tok0) * a.G - half * 64;
+                const int c_lo = (int)min(max((int64_t)(first_tok - tok0) * a.G, (int64_t)0), (int64_t)256) - half * 64;
+                const bool all = c_hi >= 64 && __all_sync(0xffffffffu, c_lo <= 0);
+                const float* nl = sm.nl[st] + half * 64;
+                float s4[4] = {0.f, 0.f, 0.f, 0.f};
+                const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)((buf * 2 + dd) * 128 + half * 64);
+#pragma unroll
+                for (int c0 = 0; c0 < 64; c0 += 32) {
+                    uint32_t v[32];
+                    tmem_ld_32x32(from + c0, v);
+                    tmem_wait_ld();
+                    if (c0 == 32) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&sm.d_empty[buf][dd]);
+                    }
+#pragma unroll
+                    for (int c = 0; c < 32; c += 4) {
+                        const float4 l = *reinterpret_cast<const float4*>(nl + c0 + c);
+                        const float li[4] = {l.x, l.y, l.z, l.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float x = ex2_approx(fmaf(__uint_as_float(v[c + i]), a.scale_log2e, li[i]));
+                            s4[i] += all || (c0 + c + i >= c_lo && c0 + c + i < c_hi) ? x : 0.f;
+                        }
+                    }
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sm.l_empty[st]);
+                total += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+            }
+            // the two halves of the columns, then the key's place (or this CTA's partial sums)
+            if (half == 1) {
+                ok = ok && (n == 0 || mbar_wait(&sm.j_empty[dd], (n - 1) & 1, abort));
+                sm.join[in_block] = total;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sm.j_full[dd]);
+            } else {
+                ok = ok && mbar_wait(&sm.j_full[dd], n & 1, abort);
+                total += sm.join[in_block];
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&sm.j_empty[dd]);
+                const int which = p.lo > p.t0 ? 0 : 1;
+                if (p.whole()) {
+                    if (key < p.kv) {
+                        const WeighPlace w = weigh_place(a, p.seq, p.head, key, status);
+                        if (w.row >= 0) a.w[w.w] = weigh_old(a, w.w, key, p.base) + total;
+                    }
+                } else {
+                    part[((int64_t)blockIdx.x * 2 + which) * kWtKeys + in_block] = total;
+                }
+            }
+            if (e.first == 0) e.first = p.lo == p.t0 ? 3 : (p.hi < p.n ? 1 : 2);
+            e.open = p.lo == p.t0 && p.hi < p.n;
+            e.seq = p.seq; e.head = p.head; e.kb = p.kb;
+        }
+        if (threadIdx.x == 0) ends[blockIdx.x] = e;
+    } else if (warp == 16) {
+        // ---------------- products
+        constexpr uint32_t idesc = make_idesc_bf16(128, 128, false, false);
+        for (int i = 0; ok && walk.next(a, TPT, p); ++i) {
+            const int kb = i & 1;
+            if (!mbar_wait(&sm.k_full[kb], (i >> 1) & 1, abort)) {
+                if (lane == 0) report_async(status, kAsyncTimeout, 0x822);
+                break;
+            }
+            for (int t = p.lo; t < p.hi; ++t, ++T) {
+                const int st = T % kWtStages, buf = T & 1;
+                ok = mbar_wait(&sm.q_full[st], (T / kWtStages) & 1, abort);
+                for (int dd = 0; ok && dd < 2; ++dd) {
+                    if (T > 1) ok = mbar_wait(&sm.d_empty[buf][dd], ((T >> 1) - 1) & 1, abort);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint64_t kd = make_smem_desc(smem_u32(sm.k[kb][dd]), 16, 1024), qd = make_smem_desc(smem_u32(sm.q[st]), 16, 1024);
+#pragma unroll
+                        for (int kk = 0; kk < 8; ++kk) {  // 16 of d: 32 bytes of a row; the second 64 are 16 KB on
+                            const uint64_t step = (uint64_t)((kk >> 2) * 1024 + 2 * (kk & 3));
+                            mma_bf16_ss(tmem + (buf * 2 + dd) * 128, kd + step, qd + step, idesc, kk > 0);
+                        }
+                        mma_commit(&sm.d_full[buf][dd]);
+                        if (dd == 1) mma_commit(&sm.q_empty[st]);
+                        if (dd == 1 && t == p.hi - 1) mma_commit(&sm.k_empty[kb]);
+                    }
+                    __syncwarp();
+                }
+                if (!ok) {
+                    if (lane == 0) report_async(status, kAsyncTimeout, 0x823);
+                    break;
+                }
+            }
+            if (p.lo >= p.hi && lane == 0) mbar_arrive(&sm.k_empty[kb]);  // (nothing to multiply)
+        }
+    } else if (warp == 17) {
+        // ---------------- queries: two boxes (halves of d) of TPT tokens' heads of the group, and their lse
+        if (const long long late = g_debug_producer_delay; late > 0) spin_cycles(late);  // tests only
+        const uint32_t bytes = (uint32_t)(TPT * a.G) * 256;
+        while (ok && walk.next(a, TPT, p)) {
+            for (int t = p.lo; t < p.hi; ++t, ++T) {
+                const int st = T % kWtStages;
+                float l[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = lane * 4 + i, tok = t * TPT + r / a.G;
+                    const bool here = r < TPT * a.G && tok < p.q_len;
+                    l[i] = here ? __ldg(a.lse + (int64_t)(p.q_row + tok) * H_q + p.head * a.G + r % a.G) : 0.f;
+                }
+                if (T >= kWtStages && (!mbar_wait(&sm.q_empty[st], (T / kWtStages - 1) & 1, abort) ||
+                                       !mbar_wait(&sm.l_empty[st], (T / kWtStages - 1) & 1, abort))) {
+                    if (lane == 0) report_async(status, kAsyncTimeout, 0x824);
+                    ok = false;
+                    break;
+                }
+                if (lane == 0) {
+                    mbar_arrive_expect_tx(&sm.q_full[st], bytes);
+                    for (int h = 0; h < 2; ++h) tma_load_3d(sm.q[st] + h * 16384, &tm_q, h * 64, p.head * a.G, p.q_row + t * TPT, &sm.q_full[st]);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) l[i] = l[i] == -INFINITY ? -INFINITY : -l[i] * 1.4426950408889634f;
+                *reinterpret_cast<float4*>(sm.nl[st] + lane * 4) = make_float4(l[0], l[1], l[2], l[3]);
+                mbar_arrive(&sm.l_full[st]);
+            }
+        }
+    } else {
+        // ---------------- keys: a warp 64 of a block, 16 bytes a lane
+        const int lw = warp - 18;
+        for (int i = 0; ok && walk.next(a, TPT, p); ++i) {
+            const int kb = i & 1;
+            int64_t row[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int64_t key = (int64_t)p.kb * kWtKeys + lw * 64 + j * 32 + lane;
+                row[j] = key < p.kv ? weigh_place(a, p.seq, p.head, (int)key, status).row : -1;
+            }
+            if (i >= 2 && !mbar_wait(&sm.k_empty[kb], ((i >> 1) - 1) & 1, abort)) {
+                if (lane == 0) report_async(status, kAsyncTimeout, 0x825);
+                break;
+            }
+            uint8_t* tile = sm.k[kb][lw >> 1];
+            const int key0 = (lw & 1) * 64;
+            if constexpr (!F8) {
+#pragma unroll 8
+                for (int s = 0; s < 32; ++s) {
+                    const int k = s * 2 + (lane >> 4), chunk = lane & 15;
+                    const int64_t r = __shfl_sync(0xffffffffu, s < 16 ? row[0] : row[1], k & 31);
+                    const uint8_t* from = static_cast<const uint8_t*>(a.k) + (max(r, (int64_t)0) * a.c.H_kv + p.head) * 256 + chunk * 16;
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(tile + weigh_tc_off(key0 + k, chunk))), "l"(from),
+                                 "r"(r >= 0 ? 16 : 0)
+                                 : "memory");
+                }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+                asm volatile("cp.async.wait_group 0;" ::: "memory");
+            } else {
+#pragma unroll
+                for (int s0 = 0; s0 < 16; s0 += 8) {
+                    uint4 x[8];
+#pragma unroll
+                    for (int s = 0; s < 8; ++s) {
+                        const int k = (s0 + s) * 4 + (lane >> 3), chunk = lane & 7;
+                        const int64_t r = __shfl_sync(0xffffffffu, row[s0 >> 3], k & 31);
+                        const uint8_t* from = static_cast<const uint8_t*>(a.k) + (max(r, (int64_t)0) * a.c.H_kv + p.head) * 128 + chunk * 16;
+                        x[s] = r >= 0 ? __ldg(reinterpret_cast<const uint4*>(from)) : make_uint4(0u, 0u, 0u, 0u);
+                    }
+#pragma unroll
+                    for (int s = 0; s < 8; ++s) {
+                        const int k = (s0 + s) * 4 + (lane >> 3), chunk = lane & 7;
+                        const uint32_t w[4] = {x[s].x, x[s].y, x[s].z, x[s].w};
+                        uint32_t o[8];
+                        e4m3x16_to_bf16x16(w, o);
+                        *reinterpret_cast<uint4*>(tile + weigh_tc_off(key0 + k, 2 * chunk)) = make_uint4(o[0], o[1], o[2], o[3]);
+                        *reinterpret_cast<uint4*>(tile + weigh_tc_off(key0 + k, 2 * chunk + 1)) = make_uint4(o[4], o[5], o[6], o[7]);
+                    }
+                }
+            }
+            fence_proxy_async_smem();  // written through the generic proxy, read by the products
+            mbar_arrive(&sm.k_full[kb]);
+        }
+    }
+    if (*abort != 0) spin_cycles(200000);  // copies in flight land
+    __syncwarp();
+    if (warp == 16) {  // products in flight end before their memory goes
+        if (elect_one()) mma_commit(&sm.drain);
+        __syncwarp();
+        mbar_wait_quiet(&sm.drain, 0, 20000000);
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 16) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// Adds up the key blocks that the boundaries between CTAs cut: CTA c the one that c begins and a later one ends.
+__global__ void __launch_bounds__(kWtKeys)
+weigh_merge_kernel(const WeighArgs a, int TPT, const float* part, const WeighEnds* ends, int n_ctas, int* status) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int c = blockIdx.x;
+    const WeighEnds e = ends[c];
+    if (e.open == 0) return;
+    float sum = part[((int64_t)c * 2 + 1) * kWtKeys + threadIdx.x];
+    for (int i = c + 1; i < n_ctas; ++i) {
+        const int first = ends[i].first;
+        if (first == 3) break;
+        if (first == 0) continue;
+        sum += part[(int64_t)i * 2 * kWtKeys + threadIdx.x];
+        if (first == 2) break;
+    }
+    const WeighTcSeq q = weigh_tc_seq(a, TPT, e.seq);
+    const int64_t key = (int64_t)e.kb * kWtKeys + threadIdx.x;
+    if (key >= q.kv) return;
+    const WeighPlace w = weigh_place(a, e.seq, e.head, (int)key, status);
+    if (w.row >= 0) a.w[w.w] = weigh_old(a, w.w, (int)key, q.base) + sum;
+}
+
+}  // namespace msa
