@@ -258,24 +258,31 @@ static msa_status_t launch_paged_few8(const PagedAttnArgs& a, const msa_paged_ca
     return launch_status();
 }
 
+// Map of a pool whose copies of `box` keys of a head land as operand atoms.
+template <bool F8>
+static bool encode_paged_map(CUtensorMap* map, const void* pool, const msa_paged_cache_t& c, int box) {
+    const uint64_t H = (uint64_t)c.n_kv_heads, rows = (uint64_t)c.n_pages * c.page_size;
+    if constexpr (F8) {  // (128 bytes of a key as 64 two-byte elements: only bytes move)
+        const uint64_t kd[3] = {64, H, rows}, ks[2] = {128, H * 128};
+        const uint32_t kb[3] = {64, 1, (uint32_t)box};
+        return encode_tmap_bf16(map, pool, 3, kd, ks, kb, true);
+    } else {  // 64 of d, 8 keys, the two halves of d, head, groups of 8 keys: a box is a run of operand atoms
+        const uint64_t kd[5] = {64, 8, 2, H, rows / 8}, ks[4] = {H * 256, 128, 256, H * 2048};
+        const uint32_t kb[5] = {64, 8, 2, 1, (uint32_t)box / 8};
+        return encode_tmap_bf16(map, pool, 5, kd, ks, kb);
+    }
+}
+
 template <bool F8>
 static msa_status_t launch_paged_attn(const PagedAttnArgs& a, const msa_paged_cache_t& c, const void* q, int grid, bool early,
                                       cudaStream_t st) {
     CUtensorMap tm_q, tm_q1, tm_k, tm_v;
-    const uint64_t H_q = (uint64_t)a.c.H_kv * a.G, H = (uint64_t)a.c.H_kv, rows = (uint64_t)c.n_pages * c.page_size;
+    const uint64_t H_q = (uint64_t)a.c.H_kv * a.G;
     const int box = std::min(common_divisor(c.page_size, kPagedKeys), F8 ? 32 : kPagedKeys);  // keys of a copy
     const uint64_t qd[3] = {128, H_q, (uint64_t)a.n_tokens}, qs[2] = {256, H_q * 256};
     const uint32_t qb[3] = {64, (uint32_t)a.G, (uint32_t)a.TPT}, qb1[3] = {64, (uint32_t)a.G, 1};
     bool ok = encode_tmap_bf16(&tm_q, q, 3, qd, qs, qb) && encode_tmap_bf16(&tm_q1, q, 3, qd, qs, qb1);
-    if constexpr (F8) {  // (128 bytes of a key as 64 two-byte elements: only bytes move)
-        const uint64_t kd[3] = {64, H, rows}, ks[2] = {128, H * 128};
-        const uint32_t kb[3] = {64, 1, (uint32_t)box};
-        ok = ok && encode_tmap_bf16(&tm_k, c.k, 3, kd, ks, kb, true) && encode_tmap_bf16(&tm_v, c.v, 3, kd, ks, kb, true);
-    } else {  // 64 of d, 8 keys, the two halves of d, head, groups of 8 keys: a box is a run of operand atoms
-        const uint64_t kd[5] = {64, 8, 2, H, rows / 8}, ks[4] = {H * 256, 128, 256, H * 2048};
-        const uint32_t kb[5] = {64, 8, 2, 1, (uint32_t)box / 8};
-        ok = ok && encode_tmap_bf16(&tm_k, c.k, 5, kd, ks, kb) && encode_tmap_bf16(&tm_v, c.v, 5, kd, ks, kb);
-    }
+    ok = ok && encode_paged_map<F8>(&tm_k, c.k, c, box) && encode_paged_map<F8>(&tm_v, c.v, c, box);
     int* status = status_word();
     if (!ok || status == nullptr) return cuda_failed();
     const size_t smem = sizeof(PagedSmem);
@@ -322,7 +329,7 @@ template <bool F8>
 static msa_status_t launch_weigh(WeighArgs a, const msa_paged_cache_t& c, void* workspace, cudaStream_t st) {
     int* status = status_word();
     if (status == nullptr) return cuda_failed();
-    if (c.head_dim != 128) {
+    if (c.head_dim != 128 || (int64_t)c.n_pages * c.page_size >= 2147483647LL) {  // (rows of the pool are 32-bit numbers in the others)
         const dim3 grid((unsigned)std::max<int64_t>(1, std::min<int64_t>(ceil_div64((int64_t)c.max_pages * c.page_size, 128), 1024)),
                         (unsigned)std::min<int64_t>((int64_t)a.c.batch * a.c.H_kv, 65535));
         StageScope sc(kStageNone, st);
@@ -346,10 +353,11 @@ static msa_status_t launch_weigh(WeighArgs a, const msa_paged_cache_t& c, void* 
         if (few.alone || s != MSA_OK) return s;
     }
     const int TPT = 128 / a.G, grid = sm_count();
-    CUtensorMap tm_q;
+    CUtensorMap tm_q, tm_k;
     const uint64_t H_q = (uint64_t)a.c.H_kv * a.G, qd[3] = {128, H_q, (uint64_t)a.n_tokens}, qs[2] = {256, H_q * 256};
     const uint32_t qb[3] = {64, (uint32_t)a.G, (uint32_t)TPT};
-    if (!encode_tmap_bf16(&tm_q, a.q, 3, qd, qs, qb)) return cuda_failed();
+    const int box = std::min(common_divisor(c.page_size, kPagedKeys), F8 ? 32 : kPagedKeys);  // keys of a copy
+    if (!encode_tmap_bf16(&tm_q, a.q, 3, qd, qs, qb) || !encode_paged_map<F8>(&tm_k, c.k, c, box)) return cuda_failed();
     static bool attr_set[64] = {false};  // per device
     const int dev = current_device();
     if (!attr_set[dev]) {
@@ -362,7 +370,7 @@ static msa_status_t launch_weigh(WeighArgs a, const msa_paged_cache_t& c, void* 
     WeighEnds* ends = (WeighEnds*)((char*)workspace + w.ends);
     {
         StageScope sc(kStageNone, st);
-        weigh_tc_kernel<F8><<<grid, kWtThreads, sizeof(WeighTcSmem), st>>>(tm_q, a, TPT, part, ends, 1.0 / grid, status);
+        weigh_tc_kernel<F8><<<grid, weigh_tc_threads(F8), sizeof(WeighTcSmem), st>>>(tm_q, tm_k, a, TPT, box, part, ends, 1.0 / grid, status);
     }
     const msa_status_t s = launch_status();
     if (s != MSA_OK) return s;

@@ -148,24 +148,32 @@ weigh_few_kernel(const WeighArgs a, double inv_grid, int* status) {
         if (t >= hi) continue;
 
         // ---- a tile's places (of key lane mod 16), its keys
+        struct Place { int row, off; };  // row of the pool (the host has seen that they are below 2^31), place in its page
         auto places_of = [&](int tile) {
-            const int key = tile * kWeighKeys + (lane & 15);
-            return tile < hi && key < sq.kv ? weigh_place(a, seq, head, key, status) : WeighPlace{-1, 0};
+            const uint32_t key = tile * kWeighKeys + (lane & 15), size = a.c.page_size, slot = key / size;
+            Place p{-1, (int)(key - slot * size)};
+            if (tile < hi && key < (uint32_t)sq.kv) {
+                const int page = a.c.table[(int64_t)seq * a.c.max_pages + slot];
+                if (page >= 0 && page < a.c.n_pages) p.row = page * (int)size + p.off;
+                else report_async(status, kAsyncBadIndex, 0x802);
+            }
+            return p;
         };
         struct Tile { uint4 k[2][LD]; int64_t w; float old; };
-        auto fetch = [&](const WeighPlace& p, int tile, Tile& x) {
-            const int64_t r0 = __shfl_sync(0xffffffffu, p.row, g), r1 = __shfl_sync(0xffffffffu, p.row, 8 + g);
-            const int64_t w = __shfl_sync(0xffffffffu, p.w, (t4 & 1) * 8 + g);
+        auto fetch = [&](const Place& p, int tile, Tile& x) {
+            const int r0 = __shfl_sync(0xffffffffu, p.row, g), r1 = __shfl_sync(0xffffffffu, p.row, 8 + g);
+            const int off = __shfl_sync(0xffffffffu, p.off, (t4 & 1) * 8 + g);
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int64_t row = i == 0 ? r0 : r1;
-                const uint4* from = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(a.k) + (row * a.c.H_kv + head) * (F8 ? 128 : 256)) + t4;
+                const int row = i == 0 ? r0 : r1;
+                const uint4* from = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(a.k) + ((int64_t)row * a.c.H_kv + head) * (F8 ? 128 : 256)) + t4;
 #pragma unroll
                 for (int j = 0; j < LD; ++j) x.k[i][j] = row >= 0 ? __ldg(from + 4 * j) : make_uint4(0u, 0u, 0u, 0u);
             }
             // lanes 0 and 1 of four look after the weights of keys g and g + 8
             const int key = tile * kWeighKeys + (t4 & 1) * 8 + g;
-            x.w = t4 < 2 && (t4 == 0 ? r0 : r1) >= 0 ? w : -1;
+            const int mine = t4 == 0 ? r0 : r1;
+            x.w = t4 < 2 && mine >= 0 ? (int64_t)(mine - off) * a.c.H_kv + (int64_t)head * a.c.page_size + off : -1;
             x.old = x.w >= 0 ? weigh_old(a, x.w, key, sq.base) : 0.f;
         };
 
@@ -231,35 +239,46 @@ weigh_few_kernel(const WeighArgs a, double inv_grid, int* status) {
         auto finish = [&](int tile, const Tile& x) {
             const int key0 = tile * kWeighKeys + g, key1 = key0 + 8;
             float s0 = 0.f, s1 = 0.f;
+            // first operand: [16 of d][row g, row g + 8, and the same two elements on]
+            uint32_t k[8][4];
+#pragma unroll
+            for (int j = 0; j < LD; ++j) {
+                const uint32_t u[4] = {x.k[0][j].x, x.k[0][j].y, x.k[0][j].z, x.k[0][j].w};
+                const uint32_t v[4] = {x.k[1][j].x, x.k[1][j].y, x.k[1][j].z, x.k[1][j].w};
+                if constexpr (F8) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        e4m3x4_to_f16x2x2(u[i], k[4 * j + i][0], k[4 * j + i][2]);
+                        e4m3x4_to_f16x2x2(v[i], k[4 * j + i][1], k[4 * j + i][3]);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        k[2 * j + i][0] = u[2 * i]; k[2 * j + i][1] = v[2 * i];
+                        k[2 * j + i][2] = u[2 * i + 1]; k[2 * j + i][3] = v[2 * i + 1];
+                    }
+                }
+            }
             for (int first = 0; first < rows; first += 8 * NT) {
                 if (rows > 8 * NT) load_q(first);
+                float part0 = 0.f, part1 = 0.f;
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     float c[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int j = 0; j < LD; ++j) {
-                        const uint32_t u[4] = {x.k[0][j].x, x.k[0][j].y, x.k[0][j].z, x.k[0][j].w};
-                        const uint32_t v[4] = {x.k[1][j].x, x.k[1][j].y, x.k[1][j].z, x.k[1][j].w};
-                        if constexpr (F8) {
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                uint32_t u0, u1, v0, v1;
-                                e4m3x4_to_f16x2x2(u[i], u0, u1);
-                                e4m3x4_to_f16x2x2(v[i], v0, v1);
-                                mma_m16n8k16_f16(c, u0, v0, u1, v1, qf[n][4 * j + i][0], qf[n][4 * j + i][1]);
-                            }
-                        } else {
-                            mma_m16n8k16_bf16(c, u[0], v[0], u[1], v[1], qf[n][2 * j][0], qf[n][2 * j][1]);
-                            mma_m16n8k16_bf16(c, u[2], v[2], u[3], v[3], qf[n][2 * j + 1][0], qf[n][2 * j + 1][1]);
-                        }
+                    for (int ks = 0; ks < 8; ++ks) {
+                        if constexpr (F8) mma_m16n8k16_f16(c, k[ks][0], k[ks][1], k[ks][2], k[ks][3], qf[n][ks][0], qf[n][ks][1]);
+                        else mma_m16n8k16_bf16(c, k[ks][0], k[ks][1], k[ks][2], k[ks][3], qf[n][ks][0], qf[n][ks][1]);
                     }
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         const float p0 = ex2_approx(fmaf(c[i], sc[n][i], nl[n][i])), p1 = ex2_approx(fmaf(c[2 + i], sc[n][i], nl[n][i]));
-                        if (key0 <= lim[n][i]) s0 += p0;
-                        if (key1 <= lim[n][i]) s1 += p1;
+                        if (key0 <= lim[n][i]) part0 += p0;
+                        if (key1 <= lim[n][i]) part1 += p1;
                     }
                 }
+                s0 += part0;
+                s1 += part1;
             }
             s0 += __shfl_xor_sync(0xffffffffu, s0, 1);
             s1 += __shfl_xor_sync(0xffffffffu, s1, 1);
@@ -268,7 +287,7 @@ weigh_few_kernel(const WeighArgs a, double inv_grid, int* status) {
             if (x.w >= 0) a.w[x.w] = x.old + (t4 == 0 ? s0 : s1);
         };
 
-        WeighPlace p = places_of(t);
+        Place p = places_of(t);
         Tile x, y;
         fetch(p, t, x);
         p = places_of(t + kWeighWarps);

@@ -18,7 +18,8 @@
 namespace msa {
 
 constexpr int kWtKeys = 256, kWtStages = 3;
-constexpr int kWtEpiWarps = 16, kWtLoadWarps = 4, kWtThreads = (kWtEpiWarps + 2 + kWtLoadWarps) * 32;
+constexpr int kWtEpiWarps = 16, kWtWidenWarps = 4;
+constexpr int weigh_tc_threads(bool f8) { return (kWtEpiWarps + 4 + (f8 ? kWtWidenWarps : 0)) * 32; }
 constexpr int kWtBlockCost = 2;  // tiles' worth of a key block's beginning and end
 
 // kb0: first key block behind `base`; [kb_lim, n_kb): blocks that no row of the call sees (it may lack rows)
@@ -42,7 +43,7 @@ __host__ __device__ __forceinline__ WeighTcSeq weigh_tc_seq(const WeighArgs& a, 
 // First tile with a token that sees a key of block kb (n_tiles where the call lacks those rows).
 __host__ __device__ __forceinline__ int weigh_tc_first(const WeighTcSeq& q, int TPT, int kb) {
     const int64_t tok = (int64_t)kb * kWtKeys - q.base;
-    return tok <= 0 ? 0 : (int)min(tok / TPT, (int64_t)q.n_tiles);
+    return tok <= 0 ? 0 : (int)min((uint32_t)tok / (uint32_t)TPT, (uint32_t)q.n_tiles);  // (lengths are below 2^31)
 }
 
 // Units of the first kb key blocks of one head, their cost included.
@@ -93,15 +94,15 @@ struct WeighTcWalk {
 };
 
 struct WeighTcPlan {
-    int64_t scan[kWtThreads / 32], targets[2];
+    int64_t scan[32], targets[2];
     WeighTcSpot spot[2];
 };
 
 __device__ inline void weigh_tc_stretch(const WeighArgs& a, int TPT, WeighTcPlan& p, double inv_grid, int* status) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    constexpr int WARPS = kWtThreads / 32;
+    const int WARPS = blockDim.x >> 5;
     if (threadIdx.x < 2) { p.targets[threadIdx.x] = -1; p.spot[threadIdx.x] = WeighTcSpot{a.c.batch, 0, 0, 0}; }
-    const int per = (a.c.batch + kWtThreads - 1) / kWtThreads;
+    const int per = (a.c.batch + (int)blockDim.x - 1) / (int)blockDim.x;
     const int lo = min((int)threadIdx.x * per, a.c.batch), hi = min(lo + per, a.c.batch);
     auto units = [&](int s) {
         const WeighTcSeq q = weigh_tc_seq(a, TPT, s);
@@ -165,29 +166,59 @@ struct WeighEnds { int first, open, seq, head, kb, pad[3]; };
 static_assert(sizeof(WeighEnds) == 32, "two int4");
 
 struct WeighTcSmem {
-    alignas(1024) uint8_t k[2][2][128 * 256];  // [buffer][128 keys]: [d half][key][64 bf16], 128-byte swizzle
-    alignas(1024) uint8_t q[kWtStages][128 * 256];
+    alignas(1024) uint8_t k[2][2][128 * 256];  // [buffer][128 keys]: [8 keys][d half][key][64 bf16], 128-byte swizzle
+    alignas(1024) uint8_t q[kWtStages][128 * 256];  // [d half][row][64 bf16]
     float nl[kWtStages][128];                  // -lse of the tile's rows, base two
     union {
         float join[kWtKeys];                   // the second half of the columns' sums on their way to the first's threads
         WeighTcPlan plan;
     };
     alignas(8) uint64_t q_full[kWtStages], q_empty[kWtStages], l_full[kWtStages], l_empty[kWtStages];
-    uint64_t d_full[2][2], d_empty[2][2], k_full[2], k_empty[2], j_full[2], j_empty[2], drain;
+    uint64_t d_full[2][2], d_empty[2][2], k_full[2], k_empty[2], k_land[2], j_full[2], j_empty[2], drain;
     uint32_t tmem_base;
     int abort;
 };
 static_assert(sizeof(WeighTcSmem) <= 227 * 1024, "a CTA's shared memory");
 
-__device__ __forceinline__ uint32_t weigh_tc_off(int row, int chunk) {  // 16-byte chunk of an operand row
-    return (uint32_t)((chunk >> 3) * 16384 + row * 128 + (((chunk & 7) ^ (row & 7)) << 4));
+// 2^x by arithmetic, two at a time: x = n + f with n the nearest whole number, |f| <= 1/2; 2^f = 1 + f r(f) with r of degree 4
+// fitted to the least relative error (1.6e-7 with fp32 roundings); n goes to the exponent's place.  Below 2^-126 the result is a
+// part of the smallest numbers, at -127 zero; from 128 on infinity.
+__device__ __forceinline__ float2 exp2_by_arithmetic(float2 x) {
+    constexpr float M = 12582912.f;  // 1.5 * 2^23: a sum with it has the whole number in its last bits
+    x.x = fminf(fmaxf(x.x, -127.f), 128.f);
+    x.y = fminf(fmaxf(x.y, -127.f), 128.f);
+    const float2 t = __fadd2_rn(x, make_float2(M, M));
+    const float2 n = __fadd2_rn(t, make_float2(-M, -M));
+    const float2 f = __ffma2_rn(n, make_float2(-1.f, -1.f), x);
+    float2 r = __ffma2_rn(make_float2(1.326466561295092e-3f, 1.326466561295092e-3f), f, make_float2(9.671512991189957e-3f, 9.671512991189957e-3f));
+    r = __ffma2_rn(r, f, make_float2(5.550733953714371e-2f, 5.550733953714371e-2f));
+    r = __ffma2_rn(r, f, make_float2(0.24022242426872253f, 0.24022242426872253f));
+    r = __ffma2_rn(r, f, make_float2(0.6931470036506653f, 0.6931470036506653f));
+    r = __ffma2_rn(r, f, make_float2(1.f, 1.f));
+    return make_float2(__int_as_float(__float_as_int(r.x) + (__float_as_int(t.x) << 23)),
+                       __int_as_float(__float_as_int(r.y) + (__float_as_int(t.y) << 23)));
 }
 
+// Waits for this thread's loads from tensor memory; the registers are named so that nothing reads them earlier.
+__device__ __forceinline__ void tmem_landed(uint32_t (&r)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]),
+                   "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+                 :
+                 : "memory");
+}
+
+// One of eight pairs of columns takes its exponentials by arithmetic (4096 tokens on 28K: none 2.47 ms, one 2.36, two 2.42, three
+// 2.56: the exponential unit is relieved, but arithmetic costs issue slots and power).
+__host__ __device__ constexpr bool weigh_by_arithmetic(int pair) { return pair % 8 == 0; }
+template <bool V> struct Flag { static constexpr bool value = V; };
+
 // Warps: 0-15 sums (quadrant of lanes w mod 4, key tile (w / 4) mod 2, half of the columns w / 8), 16 issues the products, 17
-// loads queries, 18-21 load keys.
+// loads queries, 18 their lse, 19 loads keys, 20-23 (fp8 caches) widen them to bf16.
 template <bool F8>
-__global__ void __launch_bounds__(kWtThreads, 1)
-weigh_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const WeighArgs a, int TPT, float* part, WeighEnds* ends, double inv_grid, int* status) {
+__global__ void __launch_bounds__(weigh_tc_threads(F8), 1)
+weigh_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const WeighArgs a, int TPT, int box_keys,
+                float* part, WeighEnds* ends, double inv_grid, int* status) {
     extern __shared__ __align__(1024) uint8_t weigh_smem[];  // (no room to round the base up)
     WeighTcSmem& sm = *reinterpret_cast<WeighTcSmem*>(weigh_smem);
     if ((smem_u32(weigh_smem) & 1023) != 0) {  // swizzled tiles need it; the same for every thread
@@ -206,13 +237,14 @@ weigh_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const WeighArgs a, int
         }
         for (int i = 0; i < 2; ++i) {
             for (int j = 0; j < 2; ++j) { mbar_init(&sm.d_full[i][j], 1); mbar_init(&sm.d_empty[i][j], kWtEpiWarps / 2); }
-            mbar_init(&sm.k_full[i], kWtLoadWarps * 32); mbar_init(&sm.k_empty[i], 1);
+            mbar_init(&sm.k_full[i], F8 ? kWtWidenWarps : 1); mbar_init(&sm.k_empty[i], 1); mbar_init(&sm.k_land[i], 1);
             mbar_init(&sm.j_full[i], kWtEpiWarps / 4); mbar_init(&sm.j_empty[i], kWtEpiWarps / 4);
         }
         mbar_init(&sm.drain, 1);
         sm.abort = 0;
         fence_mbar_init();
         tma_prefetch_desc(&tm_q);
+        tma_prefetch_desc(&tm_k);
     }
     if (warp == 16) tmem_alloc(&sm.tmem_base, 512);
     tc_fence_before();
@@ -234,48 +266,80 @@ weigh_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const WeighArgs a, int
         for (int n = 0; ok && walk.next(a, TPT, p); ++n) {
             const int key = p.kb * kWtKeys + in_block;
             const int first_tok = key - p.base;  // first token that sees the key
-            float total = 0.f;
-            for (int t = p.lo; t < p.hi; ++t, ++T) {
-                const int st = T % kWtStages, buf = T & 1;
-                if (!mbar_wait(&sm.l_full[st], (T / kWtStages) & 1, abort) || !mbar_wait(&sm.d_full[buf][dd], (T >> 1) & 1, abort)) {
-                    if (lane == 0) report_async(status, kAsyncTimeout, 0x821);
-                    ok = false;
-                    break;
+            // where the sum goes, and what stands there: looked up while the first products are made
+            int64_t w = -1;
+            float old = 0.f;
+            if (half == 0 && p.whole() && key < p.kv) {
+                const WeighPlace place = weigh_place(a, p.seq, p.head, key, status);
+                if (place.row >= 0) {
+                    w = place.w;
+                    old = weigh_old(a, w, key, p.base);
                 }
+            }
+            float total = 0.f;
+            // Sixteen columns at a time: the next ones (the next tile's, in the end) are on their way while these are added.
+            uint32_t v[2][16];
+            const uint32_t lane0 = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)(dd * 128 + half * 64);
+            auto tile_there = [&](int tile) {
+                ok = mbar_wait(&sm.d_full[tile & 1][dd], (tile >> 1) & 1, abort);
                 tc_fence_after();
+                return ok;
+            };
+            if (p.lo < p.hi && tile_there(T)) {
+                tmem_ld_32x16(lane0 + (T & 1) * 256, v[0]);
+                tmem_landed(v[0]);
+            }
+            for (int t = p.lo; ok && t < p.hi; ++t, ++T) {
+                const int st = T % kWtStages, buf = T & 1;
+                if (!mbar_wait(&sm.l_full[st], (T / kWtStages) & 1, abort)) { ok = false; break; }
                 // visible columns [c_lo, c_hi) of this thread's key; all of them for all keys of the warp: no masks
                 const int tok0 = t * TPT;
                 const int c_hi = min(TPT, p.q_len - tok0) * a.G - half * 64;
-                const int c_lo = (int)min(max((int64_t)(first_tok - tok0) * a.G, (int64_t)0), (int64_t)256) - half * 64;
+                const int c_lo = min(max(first_tok - tok0, 0), 256) * a.G - half * 64;
                 const bool all = c_hi >= 64 && __all_sync(0xffffffffu, c_lo <= 0);
                 const float* nl = sm.nl[st] + half * 64;
-                float s4[4] = {0.f, 0.f, 0.f, 0.f};
-                const uint32_t from = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)((buf * 2 + dd) * 128 + half * 64);
+                float2 s2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                auto add = [&](auto masked) {  // (two loops: with the masks in one the selects bound it)
 #pragma unroll
-                for (int c0 = 0; c0 < 64; c0 += 32) {
-                    uint32_t v[32];
-                    tmem_ld_32x32(from + c0, v);
-                    tmem_wait_ld();
-                    if (c0 == 32) {
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&sm.d_empty[buf][dd]);
-                    }
+                    for (int ch = 0; ch < 4; ++ch) {
+                        const bool more = ch < 3 || t + 1 < p.hi;
+                        if (ch < 3) tmem_ld_32x16(lane0 + buf * 256 + (ch + 1) * 16, v[(ch + 1) & 1]);
+                        else if (more && tile_there(T + 1)) tmem_ld_32x16(lane0 + (buf ^ 1) * 256, v[0]);
+                        if (!decltype(masked)::value || ch * 16 < c_hi)
 #pragma unroll
-                    for (int c = 0; c < 32; c += 4) {
-                        const float4 l = *reinterpret_cast<const float4*>(nl + c0 + c);
-                        const float li[4] = {l.x, l.y, l.z, l.w};
+                        for (int c = 0; c < 16; c += 4) {
+                            const float4 l = *reinterpret_cast<const float4*>(nl + ch * 16 + c);
+                            const float2 sc = make_float2(a.scale_log2e, a.scale_log2e);
+                            const uint32_t* w = v[ch & 1] + c;
+                            float2 x[2] = {__ffma2_rn(make_float2(__uint_as_float(w[0]), __uint_as_float(w[1])), sc, make_float2(l.x, l.y)),
+                                           __ffma2_rn(make_float2(__uint_as_float(w[2]), __uint_as_float(w[3])), sc, make_float2(l.z, l.w))};
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float x = ex2_approx(fmaf(__uint_as_float(v[c + i]), a.scale_log2e, li[i]));
-                            s4[i] += all || (c0 + c + i >= c_lo && c0 + c + i < c_hi) ? x : 0.f;
+                            for (int i = 0; i < 2; ++i) {
+                                                                if (weigh_by_arithmetic((c >> 1) + i)) x[i] = exp2_by_arithmetic(x[i]);
+                                else { x[i].x = ex2_approx(x[i].x); x[i].y = ex2_approx(x[i].y); }
+                                if constexpr (decltype(masked)::value) {
+                                    const int col = ch * 16 + c + 2 * i;
+                                    x[i].x = col >= c_lo && col < c_hi ? x[i].x : 0.f;
+                                    x[i].y = col + 1 >= c_lo && col + 1 < c_hi ? x[i].y : 0.f;
+                                }
+                                s2[i] = __fadd2_rn(s2[i], x[i]);
+                            }
+                        }
+                        if (more) tmem_landed(v[(ch + 1) & 1]);
+                        if (ch == 2) {  // the tile is in registers
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&sm.d_empty[buf][dd]);
                         }
                     }
-                }
+                };
+                if (all) add(Flag<false>{});
+                else add(Flag<true>{});
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sm.l_empty[st]);
-                total += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+                total += (s2[0].x + s2[0].y) + (s2[1].x + s2[1].y);
             }
+            if (!ok && lane == 0) report_async(status, kAsyncTimeout, 0x821);
             // the two halves of the columns, then the key's place (or this CTA's partial sums)
             if (half == 1) {
                 ok = ok && (n == 0 || mbar_wait(&sm.j_empty[dd], (n - 1) & 1, abort));
@@ -289,10 +353,7 @@ weigh_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const WeighArgs a, int
                 if (lane == 0) mbar_arrive(&sm.j_empty[dd]);
                 const int which = p.lo > p.t0 ? 0 : 1;
                 if (p.whole()) {
-                    if (key < p.kv) {
-                        const WeighPlace w = weigh_place(a, p.seq, p.head, key, status);
-                        if (w.row >= 0) a.w[w.w] = weigh_old(a, w.w, key, p.base) + total;
-                    }
+                    if (w >= 0) a.w[w] = old + total;
                 } else {
                     part[((int64_t)blockIdx.x * 2 + which) * kWtKeys + in_block] = total;
                 }
@@ -319,12 +380,11 @@ weigh_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const WeighArgs a, int
                     if (!ok) break;
                     tc_fence_after();
                     if (elect_one()) {
-                        const uint64_t kd = make_smem_desc(smem_u32(sm.k[kb][dd]), 16, 1024), qd = make_smem_desc(smem_u32(sm.q[st]), 16, 1024);
+                        const uint64_t kd = make_smem_desc(smem_u32(sm.k[kb][dd]), 16, 2048), qd = make_smem_desc(smem_u32(sm.q[st]), 16, 1024);
 #pragma unroll
-                        for (int kk = 0; kk < 8; ++kk) {  // 16 of d: 32 bytes of a row; the second 64 are 16 KB on
-                            const uint64_t step = (uint64_t)((kk >> 2) * 1024 + 2 * (kk & 3));
-                            mma_bf16_ss(tmem + (buf * 2 + dd) * 128, kd + step, qd + step, idesc, kk > 0);
-                        }
+                        for (int kk = 0; kk < 8; ++kk)  // 16 of d: 32 bytes of a row; the second 64 are 1 KB on, of the queries 16 KB
+                            mma_bf16_ss(tmem + (buf * 2 + dd) * 128, kd + (uint64_t)((kk >> 2) * 64 + 2 * (kk & 3)),
+                                        qd + (uint64_t)((kk >> 2) * 1024 + 2 * (kk & 3)), idesc, kk > 0);
                         mma_commit(&sm.d_full[buf][dd]);
                         if (dd == 1) mma_commit(&sm.q_empty[st]);
                         if (dd == 1 && t == p.hi - 1) mma_commit(&sm.k_empty[kb]);
@@ -339,21 +399,13 @@ weigh_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const WeighArgs a, int
             if (p.lo >= p.hi && lane == 0) mbar_arrive(&sm.k_empty[kb]);  // (nothing to multiply)
         }
     } else if (warp == 17) {
-        // ---------------- queries: two boxes (halves of d) of TPT tokens' heads of the group, and their lse
+        // ---------------- queries: two boxes (halves of d) of TPT tokens' heads of the group
         if (const long long late = g_debug_producer_delay; late > 0) spin_cycles(late);  // tests only
         const uint32_t bytes = (uint32_t)(TPT * a.G) * 256;
         while (ok && walk.next(a, TPT, p)) {
             for (int t = p.lo; t < p.hi; ++t, ++T) {
                 const int st = T % kWtStages;
-                float l[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int r = lane * 4 + i, tok = t * TPT + r / a.G;
-                    const bool here = r < TPT * a.G && tok < p.q_len;
-                    l[i] = here ? __ldg(a.lse + (int64_t)(p.q_row + tok) * H_q + p.head * a.G + r % a.G) : 0.f;
-                }
-                if (T >= kWtStages && (!mbar_wait(&sm.q_empty[st], (T / kWtStages - 1) & 1, abort) ||
-                                       !mbar_wait(&sm.l_empty[st], (T / kWtStages - 1) & 1, abort))) {
+                if (T >= kWtStages && !mbar_wait(&sm.q_empty[st], (T / kWtStages - 1) & 1, abort)) {
                     if (lane == 0) report_async(status, kAsyncTimeout, 0x824);
                     ok = false;
                     break;
@@ -362,65 +414,109 @@ weigh_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const WeighArgs a, int
                     mbar_arrive_expect_tx(&sm.q_full[st], bytes);
                     for (int h = 0; h < 2; ++h) tma_load_3d(sm.q[st] + h * 16384, &tm_q, h * 64, p.head * a.G, p.q_row + t * TPT, &sm.q_full[st]);
                 }
+                __syncwarp();
+            }
+        }
+    } else if (warp == 18) {
+        // ---------------- lse of the rows, four a lane, a tile ahead
+        int tok[4], at[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = lane * 4 + i;
+            tok[i] = r < TPT * a.G ? r / a.G : 1 << 30;
+            at[i] = r / a.G * H_q + r % a.G;
+        }
+        while (ok && walk.next(a, TPT, p)) {
+            const float* lse = a.lse + (int64_t)p.q_row * H_q + p.head * a.G;
+            float l[4], ahead[4];
+            auto fetch = [&](int t, float (&x)[4]) {
+                const float* from = lse + (int64_t)t * TPT * H_q;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = t < p.hi && tok[i] < p.q_len - t * TPT ? __ldg(from + at[i]) : 0.f;
+            };
+            fetch(p.lo, ahead);
+            for (int t = p.lo; t < p.hi; ++t, ++T) {
+                const int st = T % kWtStages;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) l[i] = ahead[i];
+                fetch(t + 1, ahead);
+                if (T >= kWtStages && !mbar_wait(&sm.l_empty[st], (T / kWtStages - 1) & 1, abort)) {
+                    if (lane == 0) report_async(status, kAsyncTimeout, 0x826);
+                    ok = false;
+                    break;
+                }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) l[i] = l[i] == -INFINITY ? -INFINITY : -l[i] * 1.4426950408889634f;
                 *reinterpret_cast<float4*>(sm.nl[st] + lane * 4) = make_float4(l[0], l[1], l[2], l[3]);
                 mbar_arrive(&sm.l_full[st]);
             }
         }
-    } else {
-        // ---------------- keys: a warp 64 of a block, 16 bytes a lane
-        const int lw = warp - 18;
-        for (int i = 0; ok && walk.next(a, TPT, p); ++i) {
-            const int kb = i & 1;
-            int64_t row[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int64_t key = (int64_t)p.kb * kWtKeys + lw * 64 + j * 32 + lane;
-                row[j] = key < p.kv ? weigh_place(a, p.seq, p.head, (int)key, status).row : -1;
+    } else if (warp == 19) {
+        // ---------------- keys: one box per page (or 128 keys of a larger one), a lane each, two blocks on their way
+        const int boxes = kWtKeys / box_keys;
+        const int nowhere = F8 ? a.c.n_pages * a.c.page_size : a.c.n_pages * a.c.page_size / 8;  // reads as zeros
+        auto place_of = [&]() {
+            const uint32_t key = (uint32_t)p.kb * kWtKeys + lane * box_keys, size = a.c.page_size;  // (below 2^31 + 256)
+            if (lane >= boxes || key >= (uint32_t)p.kv) return nowhere;
+            const uint32_t slot = key / size;
+            const int page = a.c.table[(int64_t)p.seq * a.c.max_pages + slot];
+            if (page < 0 || page >= a.c.n_pages) {
+                report_async(status, kAsyncBadIndex, 0x802);
+                return nowhere;
             }
-            if (i >= 2 && !mbar_wait(&sm.k_empty[kb], ((i >> 1) - 1) & 1, abort)) {
+            const int row = page * a.c.page_size + (int)(key - slot * size);
+            return F8 ? row : row / 8;
+        };
+        for (int i = 0; walk.next(a, TPT, p); ++i) {
+            const int where = place_of(), buf = i & 1;
+            if (i >= 2 && !mbar_wait(&sm.k_empty[buf], ((i >> 1) - 1) & 1, abort)) {
                 if (lane == 0) report_async(status, kAsyncTimeout, 0x825);
                 break;
             }
-            uint8_t* tile = sm.k[kb][lw >> 1];
-            const int key0 = (lw & 1) * 64;
-            if constexpr (!F8) {
-#pragma unroll 8
-                for (int s = 0; s < 32; ++s) {
-                    const int k = s * 2 + (lane >> 4), chunk = lane & 15;
-                    const int64_t r = __shfl_sync(0xffffffffu, s < 16 ? row[0] : row[1], k & 31);
-                    const uint8_t* from = static_cast<const uint8_t*>(a.k) + (max(r, (int64_t)0) * a.c.H_kv + p.head) * 256 + chunk * 16;
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(tile + weigh_tc_off(key0 + k, chunk))), "l"(from),
-                                 "r"(r >= 0 ? 16 : 0)
-                                 : "memory");
+            uint64_t* bar = F8 ? &sm.k_land[buf] : &sm.k_full[buf];
+            if (lane == 0) mbar_arrive_expect_tx(bar, kWtKeys * (F8 ? 128 : 256));
+            __syncwarp();
+            uint8_t* dst = sm.k[buf][0];
+            if (lane < boxes) {
+                // (fp8: 32 keys into the upper half of the 8 KB of their bf16)
+                if constexpr (F8) tma_load_3d(dst + (lane * box_keys >> 5) * 8192 + 4096 + (lane * box_keys & 31) * 128, &tm_k, 0, p.head, where, bar);
+                else tma_load_5d(dst + lane * box_keys * 256, &tm_k, 0, 0, 0, p.head, where, bar);
+            }
+            __syncwarp();
+        }
+    } else if constexpr (F8) {
+        // ---------------- widening: 64 keys of a block a warp, 32 at a time
+        const int w = warp - 20;
+        for (int i = 0; walk.next(a, TPT, p); ++i) {
+            const int buf = i & 1;
+            if (!mbar_wait(&sm.k_land[buf], (i >> 1) & 1, abort)) {
+                if (lane == 0) report_async(status, kAsyncTimeout, 0x827);
+                break;
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint8_t* keys = sm.k[buf][0] + (w * 2 + h) * 8192;
+                uint4 x[8];
+#pragma unroll
+                for (int s = 0; s < 8; ++s) {
+                    const int k = s * 4 + (lane >> 3), chunk = lane & 7;
+                    x[s] = *reinterpret_cast<const uint4*>(keys + 4096 + k * 128 + ((chunk ^ (k & 7)) << 4));
                 }
-                asm volatile("cp.async.commit_group;" ::: "memory");
-                asm volatile("cp.async.wait_group 0;" ::: "memory");
-            } else {
+                __syncwarp();
 #pragma unroll
-                for (int s0 = 0; s0 < 16; s0 += 8) {
-                    uint4 x[8];
-#pragma unroll
-                    for (int s = 0; s < 8; ++s) {
-                        const int k = (s0 + s) * 4 + (lane >> 3), chunk = lane & 7;
-                        const int64_t r = __shfl_sync(0xffffffffu, row[s0 >> 3], k & 31);
-                        const uint8_t* from = static_cast<const uint8_t*>(a.k) + (max(r, (int64_t)0) * a.c.H_kv + p.head) * 128 + chunk * 16;
-                        x[s] = r >= 0 ? __ldg(reinterpret_cast<const uint4*>(from)) : make_uint4(0u, 0u, 0u, 0u);
-                    }
-#pragma unroll
-                    for (int s = 0; s < 8; ++s) {
-                        const int k = (s0 + s) * 4 + (lane >> 3), chunk = lane & 7;
-                        const uint32_t w[4] = {x[s].x, x[s].y, x[s].z, x[s].w};
-                        uint32_t o[8];
-                        e4m3x16_to_bf16x16(w, o);
-                        *reinterpret_cast<uint4*>(tile + weigh_tc_off(key0 + k, 2 * chunk)) = make_uint4(o[0], o[1], o[2], o[3]);
-                        *reinterpret_cast<uint4*>(tile + weigh_tc_off(key0 + k, 2 * chunk + 1)) = make_uint4(o[4], o[5], o[6], o[7]);
-                    }
+                for (int s = 0; s < 8; ++s) {
+                    const int k = s * 4 + (lane >> 3), chunk = lane & 7;
+                    const uint32_t v[4] = {x[s].x, x[s].y, x[s].z, x[s].w};
+                    uint32_t o[8];
+                    e4m3x16_to_bf16x16(v, o);
+                    uint8_t* to = keys + (k >> 3) * 2048 + (chunk >> 2) * 1024 + (k & 7) * 128;
+                    *reinterpret_cast<uint4*>(to + (((2 * chunk & 7) ^ (k & 7)) << 4)) = make_uint4(o[0], o[1], o[2], o[3]);
+                    *reinterpret_cast<uint4*>(to + ((((2 * chunk + 1) & 7) ^ (k & 7)) << 4)) = make_uint4(o[4], o[5], o[6], o[7]);
                 }
             }
             fence_proxy_async_smem();  // written through the generic proxy, read by the products
-            mbar_arrive(&sm.k_full[kb]);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm.k_full[buf]);
         }
     }
     if (*abort != 0) spin_cycles(200000);  // copies in flight land
