@@ -5,11 +5,37 @@
 
 using namespace msa;
 
+// CTAs of a row: as many as are resident at once (two per SM) and have some 8 KB of it each.
+static int sample_ctas(int64_t rows, int64_t row_bytes) {
+    static int sms[64] = {0};  // per device
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) cuda_failed();
+    dev = dev < 0 || dev >= 64 ? 0 : dev;
+    if (sms[dev] == 0 && cudaDeviceGetAttribute(&sms[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+        cuda_failed();
+        sms[dev] = 148;
+    }
+    int ctas = 1;
+    while (ctas < 8 && rows * ctas <= sms[dev] && row_bytes >= 2 * ctas * 8192) ctas *= 2;
+    return ctas;
+}
+
 template <class T>
 static msa_status_t launch_sample(const SampleArgs& a, int64_t rows, cudaStream_t st) {
+    const int ctas = sample_ctas(rows, (int64_t)a.vocab * (int64_t)sizeof(T));
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = ctas;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(rows * ctas));
+    cfg.blockDim = dim3(kSampleThreads);
+    cfg.dynamicSmemBytes = sizeof(SampleSmem);
+    cfg.stream = st;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
     StageScope sc(kStageNone, st);
-    sample_kernel<T><<<(unsigned)rows, kSampleThreads, 0, st>>>(a);
-    return launch_status();
+    return cudaLaunchKernelEx(&cfg, sample_kernel<T>, a) == cudaSuccess ? MSA_OK : cuda_failed();
 }
 
 extern "C" {
