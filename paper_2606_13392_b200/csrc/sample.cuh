@@ -29,22 +29,33 @@ struct SampleArgs {
 
 constexpr int kSampleThreads = 512, kSampleWarps = kSampleThreads / 32, kSampleTable = 256;
 constexpr int kSampleBins = 2048, kSampleList = 4096;
+constexpr int kSampleSort = 1024;               // nuclei up to this are sorted, of larger ones only the bin they end in
 constexpr int kSampleBits = 42;
 constexpr double kSampleOne = 4398046511104.0;  // 2^42
 constexpr float kSampleReach = 43.f;            // 2^-43 of the largest is no whole number any more
+
+// Larger of two, NaN if either is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
+}
 
 // Two or four bytes of a row: 16 bytes at a time.
 template <class T> struct Logits;
 template <> struct Logits<float> {
     static constexpr int E = 4;
-    static __device__ __forceinline__ float one(const float* x) { return __ldg(x); }
+    static constexpr bool HALF = false;
     static __device__ __forceinline__ void widen(const uint4& r, float (&v)[4]) {
         v[0] = __uint_as_float(r.x); v[1] = __uint_as_float(r.y); v[2] = __uint_as_float(r.z); v[3] = __uint_as_float(r.w);
+    }
+    static __device__ __forceinline__ float largest(const uint4& r) {
+        return max_nan(max_nan(__uint_as_float(r.x), __uint_as_float(r.y)), max_nan(__uint_as_float(r.z), __uint_as_float(r.w)));
     }
 };
 template <> struct Logits<__half> {
     static constexpr int E = 8;
-    static __device__ __forceinline__ float one(const __half* x) { return __half2float(__ldg(x)); }
+    static constexpr bool HALF = true;
     static __device__ __forceinline__ void widen(const uint4& r, float (&v)[8]) {
         const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
@@ -53,10 +64,15 @@ template <> struct Logits<__half> {
             v[2 * i] = f.x; v[2 * i + 1] = f.y;
         }
     }
+    static __device__ __forceinline__ float largest(const uint4& r) {
+        const __half2* h = reinterpret_cast<const __half2*>(&r);
+        const __half2 m = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
+        return max_nan(__low2float(m), __high2float(m));
+    }
 };
 template <> struct Logits<__nv_bfloat16> {
     static constexpr int E = 8;
-    static __device__ __forceinline__ float one(const __nv_bfloat16* x) { return __bfloat162float(__ldg(x)); }
+    static constexpr bool HALF = false;
     static __device__ __forceinline__ void widen(const uint4& r, float (&v)[8]) {
         const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
@@ -64,6 +80,11 @@ template <> struct Logits<__nv_bfloat16> {
             const float2 f = bf16x2_to_float2(w[i]);
             v[2 * i] = f.x; v[2 * i + 1] = f.y;
         }
+    }
+    static __device__ __forceinline__ float largest(const uint4& r) {
+        const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(&r);
+        const __nv_bfloat162 m = __hmax2_nan(__hmax2_nan(h[0], h[1]), __hmax2_nan(h[2], h[3]));
+        return max_nan(__low2float(m), __high2float(m));
     }
 };
 
@@ -79,38 +100,46 @@ struct SampleRow {
         pieces = (skip + v + E - 1) / E;
     }
     __device__ __forceinline__ int index(int piece) const { return piece * E - skip; }  // of the piece's first value
-    __device__ __forceinline__ void load(int piece, float (&v)[E]) const {
+    __device__ __forceinline__ uint4 load(int piece) const {
         const int at = index(piece);
-        if (at >= 0 && at + E <= vocab) {
-            Logits<T>::widen(__ldg(reinterpret_cast<const uint4*>(x + at)), v);
-        } else {
+        if (at >= 0 && at + E <= vocab) return __ldg(reinterpret_cast<const uint4*>(x + at));
+        T v[E];
 #pragma unroll
-            for (int e = 0; e < E; ++e) v[e] = at + e >= 0 && at + e < vocab ? Logits<T>::one(x + at + e) : -INFINITY;
-        }
+        for (int e = 0; e < E; ++e) v[e] = at + e >= 0 && at + e < vocab ? __ldg(x + at + e) : T(-INFINITY);
+        return *reinterpret_cast<const uint4*>(v);
+    }
+    static __device__ __forceinline__ uint4 nothing() {
+        const uint32_t w = sizeof(T) == 4 ? 0xFF800000u : (E == 8 && Logits<T>::HALF ? 0xFC00FC00u : 0xFF80FF80u);
+        return make_uint4(w, w, w, w);
     }
 };
 
-// Pieces [lo, hi) of a warp: a run of the row, lanes side by side.  f(values, index of the first) is called by all lanes of the warp
-// (beyond the run: with -infinities).
+// Pieces [lo, hi) of a warp: a run of the row, lanes side by side, four in flight.  f(piece, index of its first value) is called by
+// all lanes of the warp (beyond the run: with -infinities).
 template <class T, class F>
-__device__ __forceinline__ void sample_run(const SampleRow<T>& row, int lo, int hi, F f) {
-    constexpr int E = SampleRow<T>::E, U = 4;
+__device__ __forceinline__ void sample_pieces(const SampleRow<T>& row, int lo, int hi, F f) {
+    constexpr int U = 4;
     const int lane = threadIdx.x & 31;
     for (int p0 = lo; p0 < hi; p0 += 32 * U) {
-        float v[U][E];
+        uint4 raw[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int p = p0 + u * 32 + lane;
-            if (p < hi) row.load(p, v[u]);
-            else {
-#pragma unroll
-                for (int e = 0; e < E; ++e) v[u][e] = -INFINITY;
-            }
+            raw[u] = p < hi ? row.load(p) : SampleRow<T>::nothing();
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (p0 + u * 32 < hi) f(v[u], row.index(p0 + u * 32 + lane));
+            if (p0 + u * 32 < hi) f(raw[u], row.index(p0 + u * 32 + lane));
     }
+}
+// The same with the values as floats.
+template <class T, class F>
+__device__ __forceinline__ void sample_run(const SampleRow<T>& row, int lo, int hi, F f) {
+    sample_pieces(row, lo, hi, [&](const uint4& raw, int at) {
+        float v[SampleRow<T>::E];
+        Logits<T>::widen(raw, v);
+        f(v, at);
+    });
 }
 
 // What a token's weight and place in the order are computed from.
@@ -120,14 +149,14 @@ struct SampleScale {
     double least;      // largest distance to the top that min_p allows
     const double* table;
 
-    // (In 32 bits the difference would be rounded.)
-    __device__ __forceinline__ double below(float v) const { return v == top ? 0.0 : (double)top - (double)v; }
+    // Distance to the top (in 32 bits it would be rounded); a top of infinity comes with sample_slow only.
+    __device__ __forceinline__ double below(float v) const { return (double)top - (double)v; }
     // 2^42 2^-z, z = d c, rounded to a whole number: z = k/256 + r with k whole, |r| <= 2^-9; 2^(-k/256) from a table and an exponent,
     // 2^-r by its Taylor series to the fourth power (off by less than 2^-51).  Both roundings to whole numbers by adding 1.5 2^52 or
     // 2^52, which leaves the whole number in the last bits.  From z = 43 on (infinity, too): 0.
     __device__ __forceinline__ uint64_t weight(double d) const {
         const double z = d * c;
-        if (!(z < (double)kSampleReach)) return 0;
+        const bool some = z < (double)kSampleReach;  // (false for NaN: an infinite distance at an infinite T)
         const double t = fma(z, (double)kSampleTable, 6755399441055744.0);
         const int k = __double2loint(t);
         const double r = fma(t - 6755399441055744.0, -1.0 / kSampleTable, z);
@@ -135,12 +164,13 @@ struct SampleScale {
         const double p = fma(r, fma(r, fma(r, fma(r, L * L * L * L / 24, L * L * L / 6), L * L / 2), L), 1.0);
         const double w = table[k & (kSampleTable - 1)] * p;
         const double scaled = __hiloint2double(__double2hiint(w) + ((kSampleBits - (k >> 8)) << 20), __double2loint(w));
-        return (uint64_t)__double_as_longlong(scaled + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
+        const uint64_t whole = (uint64_t)__double_as_longlong(scaled + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
+        return some ? whole : 0;  // (no branch: what is computed beyond the reach is not used)
     }
     __device__ __forceinline__ uint64_t weight_of(float v) const { return weight(below(v)); }
     // Bin of a logit, larger logits in lower bins; kSampleBins: its weight is 0.
     __device__ __forceinline__ int bin(float v) const {
-        const float z = v == top ? 0.f : (top - v) * c32;  // (c32 may be infinite)
+        const float z = (top - v) * c32;
         return z < kSampleReach ? min((int)(z * (kSampleBins / kSampleReach)), kSampleBins - 1) : kSampleBins;
     }
 };
@@ -207,7 +237,7 @@ __device__ inline void sample_sort(uint64_t* list, int n) {
     for (int k = 2; k <= size; k *= 2) {
         for (int j = k / 2; j > 0; j /= 2) {
             for (int t = threadIdx.x; t < size / 2; t += kSampleThreads) {
-                const int a = (t / j) * 2 * j + t % j, b = a + j;
+                const int a = 2 * t - (t & (j - 1)), b = a + j;
                 const uint64_t x = list[a], y = list[b];
                 if ((x < y) == ((a & k) == 0)) { list[a] = y; list[b] = x; }
             }
@@ -222,7 +252,7 @@ __device__ __forceinline__ float key_value(uint32_t key) { return __uint_as_floa
 // Whatever is kept, however many are equal: thresholds by the bits of the logits, 11, 11 and 10 at a time, each a pass over
 // the row that adds up counts or weights of the digits; then the index among equal ones.  For rows that the lists below do not hold.
 template <class T>
-__device__ inline void sample_slow(const SampleArgs& a, int64_t row_number, const SampleRow<T>& row, const SampleScale& sc, SampleSmem& sm,
+__device__ __noinline__ void sample_slow(const SampleArgs& a, int64_t row_number, const SampleRow<T>& row, const SampleScale& sc, SampleSmem& sm,
                                    bool greedy, int top_k, float top_p, double temperature, double u) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int per = (row.pieces + 32 * kSampleWarps - 1) / (32 * kSampleWarps) * 32;
@@ -235,6 +265,8 @@ __device__ inline void sample_slow(const SampleArgs& a, int64_t row_number, cons
         const uint32_t k = order_key(v);
         return v > -INFINITY && (k > key || (k == key && i <= last));
     };
+    auto below = [&](float v) { return v == sc.top ? 0.0 : sc.below(v); };  // (the top may be infinite)
+    auto weight_of = [&](float v) { return sc.weight(below(v)); };
     auto narrow = [&](bool by_mass, uint64_t target) {
         uint32_t prefix = 0;
         uint64_t want = target;
@@ -250,7 +282,7 @@ __device__ inline void sample_slow(const SampleArgs& a, int64_t row_number, cons
                     const uint32_t bin = (k >> shift) & ((1u << bits) - 1);
                     atomicAdd(&sm.count[bin], 1u);
                     if (by_mass) {
-                        const uint64_t w = sc.weight_of(v[e]);
+                        const uint64_t w = weight_of(v[e]);
                         const uint32_t old = atomicAdd(&sm.mass.lo[bin], (uint32_t)w);
                         const uint32_t high = (uint32_t)(w >> 32) + (old + (uint32_t)w < old ? 1u : 0u);
                         if (high != 0) atomicAdd(&sm.mass.hi[bin], high);
@@ -281,7 +313,7 @@ __device__ inline void sample_slow(const SampleArgs& a, int64_t row_number, cons
 #pragma unroll
             for (int e = 0; e < E; ++e) ties += order_key(v[e]) == prefix && kept(v[e], at + e);
         });
-        const uint64_t one = by_mass ? sc.weight_of(key_value(prefix)) : 1;
+        const uint64_t one = by_mass ? weight_of(key_value(prefix)) : 1;
         const uint32_t mine = __reduce_add_sync(0xffffffffu, ties);
         uint32_t all, before = block_scan(lane == 0 ? mine : 0u, sm.scan, &all);
         before = __shfl_sync(0xffffffffu, before, 0);
@@ -310,19 +342,16 @@ __device__ inline void sample_slow(const SampleArgs& a, int64_t row_number, cons
         key = prefix;
         last = (int)sm.found32[1];
     };
-    auto in = [&](float v, int i) { return kept(v, i) && sc.below(v) <= sc.least; };
+    auto in = [&](float v, int i) { return kept(v, i) && below(v) <= sc.least; };
     auto add_up = [&]() {
         uint64_t mine = 0;
         sample_run(row, run_lo, run_hi, [&](const float (&v)[E], int at) {
 #pragma unroll
             for (int e = 0; e < E; ++e)
-                if (in(v[e], at + e)) mine += sc.weight_of(v[e]);
+                if (in(v[e], at + e)) mine += weight_of(v[e]);
         });
         return warp_add64(mine);
     };
-    // (min_p asks for less than the others let through: it comes in at the end)
-    SampleScale all_of = sc;
-    all_of.least = INFINITY;
     if (greedy) narrow(false, 1);
     else {
         if (top_k > 0 && top_k < row.vocab) narrow(false, top_k);
@@ -331,7 +360,7 @@ __device__ inline void sample_slow(const SampleArgs& a, int64_t row_number, cons
             sample_run(row, run_lo, run_hi, [&](const float (&v)[E], int at) {
 #pragma unroll
                 for (int e = 0; e < E; ++e)
-                    if (kept(v[e], at + e)) mine += all_of.weight_of(v[e]);
+                    if (kept(v[e], at + e)) mine += weight_of(v[e]);
             });
             block_upto64(mine, sm.sums);
             const double target = (double)sm.sums[kSampleWarps] * (double)fmaxf(top_p, 0.f);
@@ -349,7 +378,7 @@ __device__ inline void sample_slow(const SampleArgs& a, int64_t row_number, cons
             if (done) return;
             uint64_t w[E], here = 0;
 #pragma unroll
-            for (int e = 0; e < E; ++e) { w[e] = in(v[e], at + e) ? sc.weight_of(v[e]) : 0; here += w[e]; }
+            for (int e = 0; e < E; ++e) { w[e] = in(v[e], at + e) ? weight_of(v[e]) : 0; here += w[e]; }
             const uint64_t upto = warp_upto64(here);
             uint64_t n = sum + upto - here;
             const bool mine_is = here > 0 && ((double)(n + here) > target || n + here == total);
@@ -365,7 +394,7 @@ __device__ inline void sample_slow(const SampleArgs& a, int64_t row_number, cons
                             chosen = true;
                             a.token[row_number] = at + e;
                             if (a.logprob)
-                                a.logprob[row_number] = greedy ? 0.f : (float)(-sc.below(v[e]) / temperature - log((double)total / kSampleOne));
+                                a.logprob[row_number] = greedy ? 0.f : (float)(-below(v[e]) / temperature - log((double)total / kSampleOne));
                         }
                     }
                 }
@@ -378,8 +407,9 @@ __device__ inline void sample_slow(const SampleArgs& a, int64_t row_number, cons
 // ---------------------------------------------------------------- the rows
 // A cluster of CTAs per row (one CTA where there are many rows), each with a run of it: a pass for the maximum; where something
 // is filtered, a pass that counts the row in 2048 bins of equal width in log w, which the CTAs add up.
-//   top_k: the bins that hold the k largest are known; their tokens go to a list in the first CTA, which sorts it, cuts it and
-//          chooses from it.
+//   top_k: what is counted are the threads' own maxima, which the pass for the maximum has left: k of them are a bound that the k largest
+//          reach, and hardly more.  (Every logit, where the threads are not many more than k.)  The tokens that reach it go to a
+//          list in the first CTA, which sorts it, cuts it and chooses from it.
 //   top_p alone: the counts bound the weight of each bin, and so the bins where the nucleus may end; a pass adds up the weights exactly,
 //          of the row, and bin by bin between the bounds.  If the nucleus fits the list it is chosen from there; else only
 //          the bin in which it ends is listed, to find its last token, and the choice is made as without filters:
@@ -408,21 +438,15 @@ sample_kernel(const SampleArgs a) {
     for (int i = threadIdx.x; i < kSampleBins; i += kSampleThreads) sm.count[i] = sm.mass.lo[i] = sm.mass.hi[i] = 0;
     if (threadIdx.x == 0) sm.listed = 0;
 
-    // ---- the largest logit
+    // ---- the largest logit; this thread's own
     SampleScale sc;
+    float own_top = -INFINITY;
     {
-        float top = -INFINITY;
-        bool nan = false;
-        sample_run(row, run_lo, run_hi, [&](const float (&v)[E], int) {
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                nan |= v[e] != v[e];
-                top = fmaxf(top, v[e]);
-            }
-        });
-        top = warp_max(top);
+        sample_pieces(row, run_lo, run_hi, [&](const uint4& raw, int) { own_top = max_nan(own_top, Logits<T>::largest(raw)); });
+        bool nan = __syncthreads_or(own_top != own_top) != 0;
+        float top = warp_max(own_top);
         if (lane == 0) sm.tops[warp] = top;
-        nan = __syncthreads_or(nan) != 0;
+        __syncthreads();
         top = warp_max(sm.tops[lane % kSampleWarps]);
         if (ctas > 1) {
             if (threadIdx.x == 0) { sm.said.top = top; sm.said.nan = nan; }
@@ -445,7 +469,7 @@ sample_kernel(const SampleArgs a) {
     const bool greedy = !(temperature > 0.f);
     const double T_ = greedy ? 1.0 : (double)temperature;
     sc.c = 1.4426950408889634074 / T_;
-    sc.c32 = (float)sc.c;
+    sc.c32 = fminf((float)sc.c, 3e38f);
     sc.least = INFINITY;
     sc.table = sm.table;
     const double least = !greedy && min_p > 0.f ? fmax(0.0, -log((double)min_p) * T_) : INFINITY;
@@ -476,7 +500,41 @@ sample_kernel(const SampleArgs a) {
     enum { kAll, kList, kBin, kSlow };
     int mode = kAll, bin_lo = 0, bin_hi = kSampleBins;  // bins that are listed
     uint64_t whole = 0, above = 0;                      // weight of the row, of the bins before the listed ones
-    if (by_k || by_p) {
+    constexpr int PER = kSampleBins / kSampleThreads;
+    const int b0 = (int)threadIdx.x * PER;
+    // the bin in which a count from the top reaches k: to found32[0], the count up to its end to found32[1]
+    auto bin_of_count = [&](uint32_t* all) {
+        uint32_t n[PER], mine = 0;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) { n[j] = sm.count[b0 + j]; mine += n[j]; }
+        uint32_t upto = block_scan(mine, sm.scan, all);
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            if (upto < (uint32_t)k && upto + n[j] >= (uint32_t)k) { sm.found32[0] = b0 + j; sm.found32[1] = upto + n[j]; }  // (one thread)
+            upto += n[j];
+        }
+        __syncthreads();
+    };
+    // Twice as many threads as k, at least, or most of what they would list is not wanted.
+    bool by_maxima = by_k && (int64_t)k * 2 <= (int64_t)ctas * kSampleThreads && sc.top < INFINITY;
+    if (by_maxima) {
+        const int b = sc.bin(own_top);
+        if (b < kSampleBins) atomicAdd(&sm.count[b], 1u);
+        merge(sm.count, nullptr);
+        uint32_t all;
+        bin_of_count(&all);
+        by_maxima = all >= (uint32_t)k;
+        if (by_maxima) {
+            // (in units of the bins: what reaches the bin, not just the maxima)
+            bin_hi = (int)sm.found32[0] + 1;
+            mode = kList;
+        } else {  // the threads' maxima are too few: count all
+            for (int i = threadIdx.x; i < kSampleBins; i += kSampleThreads) sm.count[i] = 0;
+            __syncthreads();
+        }
+    }
+    if (sc.top == INFINITY) mode = kSlow;
+    else if (!by_maxima && (by_k || by_p)) {
         sample_run(row, run_lo, run_hi, [&](const float (&v)[E], int) {
 #pragma unroll
             for (int e = 0; e < E; ++e) {
@@ -485,27 +543,19 @@ sample_kernel(const SampleArgs a) {
             }
         });
         merge(sm.count, nullptr);
-        // four bins a thread, from the top
-        constexpr int PER = kSampleBins / kSampleThreads;
-        const int b0 = (int)threadIdx.x * PER;
-        uint32_t n[PER], mine = 0, all;
-#pragma unroll
-        for (int j = 0; j < PER; ++j) { n[j] = sm.count[b0 + j]; mine += n[j]; }
-        const uint32_t before = block_scan(mine, sm.scan, &all);
+        uint32_t all;
+        bin_of_count(&all);
         by_k = by_k && (uint32_t)k < all;  // (the rest weighs nothing)
         if (by_k) {
-            uint32_t upto = before;
-#pragma unroll
-            for (int j = 0; j < PER; ++j) {
-                if (upto < (uint32_t)k && upto + n[j] >= (uint32_t)k) { sm.found32[0] = b0 + j; sm.found32[1] = upto + n[j]; }  // (one thread)
-                upto += n[j];
-            }
-            __syncthreads();
             bin_hi = (int)sm.found32[0] + 1;
             mode = sm.found32[1] <= kSampleList ? kList : kSlow;
         } else if (by_p) {
             // Bounds of the weight up to each bin: a logit of bin b weighs 2^-(b+1)h to 2^-bh, h the width (and 10^-5 for the
             // 32-bit arithmetic of the bins).  The nucleus ends where the weight reaches top_p of the whole.
+            uint32_t n[PER], counts = 0;
+#pragma unroll
+            for (int j = 0; j < PER; ++j) { n[j] = sm.count[b0 + j]; counts += n[j]; }
+            const uint32_t before = block_scan(counts, sm.scan, &all);
             const double h = (double)kSampleReach / kSampleBins, p = (double)fmaxf(top_p, 0.f);
             double low = 0.0, low_of[PER], high_of[PER];
 #pragma unroll
@@ -576,7 +626,7 @@ sample_kernel(const SampleArgs a) {
             __syncthreads();
             bin_hi = (int)sm.found32[0] + 1;
             if (sm.found32[1] == 0xFFFFFFFFu) mode = kSlow;
-            else if (sm.found32[1] <= kSampleList) { mode = kList; above = 0; }
+            else if (sm.found32[1] <= kSampleSort) { mode = kList; above = 0; }
             else if (sm.found32[2] <= kSampleList) { mode = kBin; bin_lo = bin_hi - 1; above = sm.found64[0]; }
             else mode = kSlow;
         }
@@ -593,11 +643,19 @@ sample_kernel(const SampleArgs a) {
         // ---- the tokens of bins [bin_lo, bin_hi) into the first CTA's list: each CTA its own, then side by side
         __syncthreads();  // (the lists take the place of the masses, which the others have read)
         uint64_t* list = sm.list;
-        sample_run(row, run_lo, run_hi, [&](const float (&v)[E], int at) {
+        // (logits that reach the bins' lower end, or a little below: most pieces have none)
+        const float least_listed = sc.top - (float)bin_hi * (kSampleReach / kSampleBins) / sc.c32 * 1.0001f - 1e-6f * fabsf(sc.top);
+        sample_pieces(row, run_lo, run_hi, [&](const uint4& raw, int at) {
+            if (!(Logits<T>::largest(raw) >= least_listed)) return;
+            float v[E];
+            Logits<T>::widen(raw, v);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 const int b = sc.bin(v[e]);
-                if (b >= bin_lo && b < bin_hi) list[atomicAdd(&sm.listed, 1u)] = (uint64_t)order_key(v[e]) << 32 | (uint32_t)~(at + e);
+                if (b >= bin_lo && b < bin_hi) {
+                    const uint32_t to = atomicAdd(&sm.listed, 1u);
+                    if (to < kSampleList) list[to] = (uint64_t)order_key(v[e]) << 32 | (uint32_t)~(at + e);
+                }
             }
         });
         uint32_t size = 0;
@@ -610,12 +668,16 @@ sample_kernel(const SampleArgs a) {
                 size += n;
             }
             uint64_t* to = cluster.map_shared_rank(list, 0);
-            if (rank > 0)
+            if (rank > 0 && size <= kSampleList)
                 for (uint32_t i = threadIdx.x; i < sm.listed; i += kSampleThreads) to[first + i] = list[i];
             cluster.sync();
         } else {
             __syncthreads();
             size = sm.listed;
+        }
+        if (size > kSampleList) {  // (more reach the bound than the list holds)
+            if (rank == 0) sample_slow<T>(a, r, row, cut, sm, greedy, top_k, top_p, T_, u);
+            return;
         }
         if (mode == kList && rank > 0) return;
         if (rank == 0) {
@@ -698,10 +760,22 @@ sample_kernel(const SampleArgs a) {
         return d <= least ? sc.weight(d) : 0;
     };
     uint64_t mine = 0;
-    sample_run(row, run_lo, run_hi, [&](const float (&v)[E], int at) {
+    if (mode == kAll && least == INFINITY) {
+        sample_run(row, run_lo, run_hi, [&](const float (&v)[E], int) {
 #pragma unroll
-        for (int e = 0; e < E; ++e) mine += weight_in(v[e], at + e);
-    });
+            for (int e = 0; e < E; ++e) mine += sc.weight_of(v[e]);
+        });
+    } else {
+        // (most pieces hold nothing that is kept; a little below what min_p asks for)
+        const float from = fmaxf(mode == kBin ? key_value(last_key) : -INFINITY, sc.top - (float)least * 1.0001f - 1e-6f * fabsf(sc.top));
+        sample_pieces(row, run_lo, run_hi, [&](const uint4& raw, int at) {
+            if (!(Logits<T>::largest(raw) >= from)) return;
+            float v[E];
+            Logits<T>::widen(raw, v);
+#pragma unroll
+            for (int e = 0; e < E; ++e) mine += weight_in(v[e], at + e);
+        });
+    }
     mine = warp_add64(mine);
     uint64_t start = block_upto64(lane == 0 ? mine : 0, sm.sums) - mine;
     start = __shfl_sync(0xffffffffu, start, 0);
