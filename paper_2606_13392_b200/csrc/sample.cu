@@ -6,11 +6,8 @@
 using namespace msa;
 
 // CTAs of a row: as many as are resident at once (two per SM) and have some 8 KB of it each.
-static int sample_ctas(int64_t rows, int64_t row_bytes) {
+static int sample_ctas(int dev, int64_t rows, int64_t row_bytes) {
     static int sms[64] = {0};  // per device
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) cuda_failed();
-    dev = dev < 0 || dev >= 64 ? 0 : dev;
     if (sms[dev] == 0 && cudaDeviceGetAttribute(&sms[dev], cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
         cuda_failed();
         sms[dev] = 148;
@@ -22,7 +19,16 @@ static int sample_ctas(int64_t rows, int64_t row_bytes) {
 
 template <class T>
 static msa_status_t launch_sample(const SampleArgs& a, int64_t rows, cudaStream_t st) {
-    const int ctas = sample_ctas(rows, (int64_t)a.vocab * (int64_t)sizeof(T));
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) cuda_failed();
+    dev = dev < 0 || dev >= 64 ? 0 : dev;
+    static bool attr_set[64] = {false};  // per device
+    if (!attr_set[dev]) {
+        if (cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SampleSmem)) != cudaSuccess)
+            return cuda_failed();
+        attr_set[dev] = true;
+    }
+    const int ctas = sample_ctas(dev, rows, (int64_t)a.vocab * (int64_t)sizeof(T));
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = ctas;

@@ -27,7 +27,7 @@ struct SampleArgs {
     float* logprob;
 };
 
-constexpr int kSampleThreads = 512, kSampleWarps = kSampleThreads / 32, kSampleTable = 256;
+constexpr int kSampleThreads = 512, kSampleWarps = kSampleThreads / 32, kSampleTable = 1024;
 constexpr int kSampleBins = 2048, kSampleList = 4096;
 constexpr int kSampleSort = 1024;               // nuclei up to this are sorted, of larger ones only the bin they end in
 constexpr int kSampleBits = 42;
@@ -144,30 +144,43 @@ __device__ __forceinline__ void sample_run(const SampleRow<T>& row, int lo, int 
 
 // What a token's weight and place in the order are computed from.
 struct SampleScale {
-    float top, c32;    // largest logit; c in 32 bits, for bins
-    double c;          // log2(e) / T
-    double least;      // largest distance to the top that min_p allows
+    float top, c32;         // largest logit; c in 32 bits, for bins
+    double c, tc, ct, tct;  // log2(e) / T; top c; c and top c times the table's size, the latter with 1.5 2^52 in front
     const double* table;
+    static constexpr double kFront = 6755399441055744.0;  // 1.5 2^52: a sum with it has the nearest whole number in its last bits
 
+    __device__ __forceinline__ SampleScale(float top_, double T, const double* table_) : top(top_), table(table_) {
+        c = 1.4426950408889634074 / T;
+        c32 = fminf((float)c, 3e38f);
+        tc = (double)top * c;
+        ct = c * kSampleTable;
+        tct = (double)top * ct + kFront;
+    }
     // Distance to the top (in 32 bits it would be rounded); a top of infinity comes with sample_slow only.
     __device__ __forceinline__ double below(float v) const { return (double)top - (double)v; }
-    // 2^42 2^-z, z = d c, rounded to a whole number: z = k/256 + r with k whole, |r| <= 2^-9; 2^(-k/256) from a table and an exponent,
-    // 2^-r by its Taylor series to the fourth power (off by less than 2^-51).  Both roundings to whole numbers by adding 1.5 2^52 or
-    // 2^52, which leaves the whole number in the last bits.  From z = 43 on (infinity, too): 0.
-    __device__ __forceinline__ uint64_t weight(double d) const {
-        const double z = d * c;
-        const bool some = z < (double)kSampleReach;  // (false for NaN: an infinite distance at an infinite T)
-        const double t = fma(z, (double)kSampleTable, 6755399441055744.0);
-        const int k = __double2loint(t);
-        const double r = fma(t - 6755399441055744.0, -1.0 / kSampleTable, z);
+    // 2^42 2^(-k/1024) 2^-r to the nearest whole number, `some` is false: 0.  2^(-k/1024) from a table and an exponent, 2^-r, |r| <=
+    // 2^-10, by its Taylor series to the third power (off by less than 2^-46); the rounding by adding 2^52.
+    __device__ __forceinline__ uint64_t power(int k, double r, bool some) const {
         constexpr double L = -0.69314718055994530942;
-        const double p = fma(r, fma(r, fma(r, fma(r, L * L * L * L / 24, L * L * L / 6), L * L / 2), L), 1.0);
+        const double p = fma(r, fma(r, fma(r, L * L * L / 6, L * L / 2), L), 1.0);
         const double w = table[k & (kSampleTable - 1)] * p;
-        const double scaled = __hiloint2double(__double2hiint(w) + ((kSampleBits - (k >> 8)) << 20), __double2loint(w));
+        const double scaled = __hiloint2double(__double2hiint(w) + ((kSampleBits - (k >> 10)) << 20), __double2loint(w));
         const uint64_t whole = (uint64_t)__double_as_longlong(scaled + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
         return some ? whole : 0;  // (no branch: what is computed beyond the reach is not used)
     }
-    __device__ __forceinline__ uint64_t weight_of(float v) const { return weight(below(v)); }
+    // Weight at a distance d >= 0 of the top: z = d c = k / 1024 + r.  From z = 43 on (infinity, too; NaN): 0.
+    __device__ __forceinline__ uint64_t weight(double d) const {
+        const double z = d * c, t = fma(z, (double)kSampleTable, kFront);
+        return power(__double2loint(t), fma(t - kFront, -1.0 / kSampleTable, z), z < (double)kSampleReach);
+    }
+    // The same of a logit, for |top c| < 2^20: z = top c - v c with one rounding.  (That of top c is the same for all, and so a common
+    // factor of all weights, of less than 1 + 2^-33.)
+    __device__ __forceinline__ uint64_t weight_of(float v) const {
+        const double x = (double)v, t = fma(x, -ct, tct);
+        const int k = __double2loint(t);  // whole and small where the upper half is that of 1.5 2^52
+        const bool some = __double2hiint(t) == 0x43380000 && (uint32_t)k < (uint32_t)(kSampleReach * kSampleTable);
+        return power(k, fma(x, -c, fma(t - kFront, -1.0 / kSampleTable, tc)), some);
+    }
     // Bin of a logit, larger logits in lower bins; kSampleBins: its weight is 0.
     __device__ __forceinline__ int bin(float v) const {
         const float z = (top - v) * c32;
@@ -207,7 +220,7 @@ __device__ __forceinline__ uint64_t block_upto64(uint64_t v, uint64_t* s) {
 }
 
 struct SampleSmem {
-    double table[kSampleTable];
+    double table[kSampleTable], root[64];
     uint32_t count[kSampleBins];
     union {
         struct { uint32_t lo[kSampleBins], hi[kSampleBins]; } mass;
@@ -246,13 +259,39 @@ __device__ inline void sample_sort(uint64_t* list, int n) {
     }
 }
 
+// The same for n <= kSampleThreads, a value a thread: thread i gets the i-th largest (0 from n on).  Partners of one warp trade
+// places in registers.  `list` holds the values before; it is written on.
+__device__ inline uint64_t sample_sort_short(uint64_t* list, int n) {
+    const int i = threadIdx.x;
+    int size = 32;
+    while (size < n) size *= 2;
+    uint64_t x = i < n ? list[i] : 0;
+    if (size > 32) __syncthreads();
+    for (int k = 2; k <= size; k *= 2) {
+        for (int j = k / 2; j > 0; j /= 2) {
+            uint64_t y = 0;
+            if (j >= 32) {
+                if (i < size) list[i] = x;
+                __syncthreads();
+                if (i < size) y = list[i ^ j];
+                __syncthreads();
+            } else {
+                y = __shfl_xor_sync(0xffffffffu, x, j);
+            }
+            const bool larger = ((i & k) == 0) == ((i & j) == 0);  // this thread keeps the larger of the two
+            x = (x > y) == larger ? x : y;
+        }
+    }
+    return x;
+}
+
 __device__ __forceinline__ float key_value(uint32_t key) { return __uint_as_float((key & 0x80000000u) ? key & 0x7FFFFFFFu : ~key); }
 
 // ---------------------------------------------------------------- any row, by one CTA
 // Whatever is kept, however many are equal: thresholds by the bits of the logits, 11, 11 and 10 at a time, each a pass over
 // the row that adds up counts or weights of the digits; then the index among equal ones.  For rows that the lists below do not hold.
 template <class T>
-__device__ __noinline__ void sample_slow(const SampleArgs& a, int64_t row_number, const SampleRow<T>& row, const SampleScale& sc, SampleSmem& sm,
+__device__ __noinline__ void sample_slow(const SampleArgs& a, int64_t row_number, const SampleRow<T>& row, const SampleScale& sc, double least, SampleSmem& sm,
                                    bool greedy, int top_k, float top_p, double temperature, double u) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int per = (row.pieces + 32 * kSampleWarps - 1) / (32 * kSampleWarps) * 32;
@@ -342,7 +381,7 @@ __device__ __noinline__ void sample_slow(const SampleArgs& a, int64_t row_number
         key = prefix;
         last = (int)sm.found32[1];
     };
-    auto in = [&](float v, int i) { return kept(v, i) && below(v) <= sc.least; };
+    auto in = [&](float v, int i) { return kept(v, i) && below(v) <= least; };
     auto add_up = [&]() {
         uint64_t mine = 0;
         sample_run(row, run_lo, run_hi, [&](const float (&v)[E], int at) {
@@ -434,17 +473,19 @@ sample_kernel(const SampleArgs a) {
     const int warps = ctas * kSampleWarps, per = (row.pieces + 32 * warps - 1) / (32 * warps) * 32;
     const int run_lo = min(row.pieces, (rank * kSampleWarps + warp) * per), run_hi = min(row.pieces, run_lo + per);
 
-    for (int i = threadIdx.x; i < kSampleTable; i += kSampleThreads) sm.table[i] = exp2((double)-i / kSampleTable);
+    // 2^(-i/1024) from 2^(-i/32) and 2^(-i/1024) of the first 32
+    if (threadIdx.x < 64) sm.root[threadIdx.x] = exp2((threadIdx.x < 32 ? (double)threadIdx.x / -32 : (double)(threadIdx.x - 32) / -1024));
     for (int i = threadIdx.x; i < kSampleBins; i += kSampleThreads) sm.count[i] = sm.mass.lo[i] = sm.mass.hi[i] = 0;
     if (threadIdx.x == 0) sm.listed = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < kSampleTable; i += kSampleThreads) sm.table[i] = sm.root[i >> 5] * sm.root[32 + (i & 31)];
 
     // ---- the largest logit; this thread's own
-    SampleScale sc;
-    float own_top = -INFINITY;
+    float own_top = -INFINITY, top;
     {
         sample_pieces(row, run_lo, run_hi, [&](const uint4& raw, int) { own_top = max_nan(own_top, Logits<T>::largest(raw)); });
         bool nan = __syncthreads_or(own_top != own_top) != 0;
-        float top = warp_max(own_top);
+        top = warp_max(own_top);
         if (lane == 0) sm.tops[warp] = top;
         __syncthreads();
         top = warp_max(sm.tops[lane % kSampleWarps]);
@@ -464,14 +505,10 @@ sample_kernel(const SampleArgs a) {
             if (ctas > 1) cluster.sync();  // (the others may still read what this CTA said)
             return;
         }
-        sc.top = top;
     }
     const bool greedy = !(temperature > 0.f);
     const double T_ = greedy ? 1.0 : (double)temperature;
-    sc.c = 1.4426950408889634074 / T_;
-    sc.c32 = fminf((float)sc.c, 3e38f);
-    sc.least = INFINITY;
-    sc.table = sm.table;
+    const SampleScale sc(top, T_, sm.table);
     const double least = !greedy && min_p > 0.f ? fmax(0.0, -log((double)min_p) * T_) : INFINITY;
     const int k = greedy ? 1 : top_k;
     bool by_k = k > 0 && k < a.vocab;
@@ -515,8 +552,9 @@ sample_kernel(const SampleArgs a) {
         }
         __syncthreads();
     };
+    const bool tame = fabs(sc.tc) < 1048576.0;  // (weight_of; a top of infinity is not)
     // Twice as many threads as k, at least, or most of what they would list is not wanted.
-    bool by_maxima = by_k && (int64_t)k * 2 <= (int64_t)ctas * kSampleThreads && sc.top < INFINITY;
+    bool by_maxima = by_k && (int64_t)k * 2 <= (int64_t)ctas * kSampleThreads && tame;
     if (by_maxima) {
         const int b = sc.bin(own_top);
         if (b < kSampleBins) atomicAdd(&sm.count[b], 1u);
@@ -533,7 +571,7 @@ sample_kernel(const SampleArgs a) {
             __syncthreads();
         }
     }
-    if (sc.top == INFINITY) mode = kSlow;
+    if (!tame) mode = kSlow;
     else if (!by_maxima && (by_k || by_p)) {
         sample_run(row, run_lo, run_hi, [&](const float (&v)[E], int) {
 #pragma unroll
@@ -565,7 +603,7 @@ sample_kernel(const SampleArgs a) {
                 low_of[j] = w * 0.98555 * 0.99997;  // 2^-h
                 low += low_of[j];
             }
-            static_assert(kSampleBins == 2048, "the factor is 2^(-43/2048)");
+            static_assert(kSampleTable == 1024 && kSampleBins == 2048, "the factor is 2^(-43/2048)");
             // (in whole numbers, for the scan: 2^-20 of the largest; rounded to the safe side below)
             const uint64_t lows = (uint64_t)(low * 1048576.0), low_upto = block_upto64(lows, sm.sums), low_all = sm.sums[kSampleWarps];
             double high = 0.0;
@@ -631,18 +669,18 @@ sample_kernel(const SampleArgs a) {
             else mode = kSlow;
         }
     }
-    SampleScale cut = sc;  // with min_p
-    cut.least = least;
     if (mode == kSlow) {
         if (ctas > 1) cluster.sync();  // (nobody reads the first CTA's memory any more)
-        if (rank == 0) sample_slow<T>(a, r, row, cut, sm, greedy, top_k, top_p, T_, u);
+        if (rank == 0) sample_slow<T>(a, r, row, sc, least, sm, greedy, top_k, top_p, T_, u);
         return;
     }
 
     if (mode != kAll) {
-        // ---- the tokens of bins [bin_lo, bin_hi) into the first CTA's list: each CTA its own, then side by side
-        __syncthreads();  // (the lists take the place of the masses, which the others have read)
-        uint64_t* list = sm.list;
+        // ---- the tokens of bins [bin_lo, bin_hi) into the first CTA's list, in any order
+        if (ctas > 1) cluster.sync();  // (the list takes the place of the masses, which have been read)
+        else __syncthreads();
+        uint64_t *list = sm.list, *to = cluster.map_shared_rank(list, 0);
+        uint32_t* listed = cluster.map_shared_rank(&sm.listed, 0);
         // (logits that reach the bins' lower end, or a little below: most pieces have none)
         const float least_listed = sc.top - (float)bin_hi * (kSampleReach / kSampleBins) / sc.c32 * 1.0001f - 1e-6f * fabsf(sc.top);
         sample_pieces(row, run_lo, run_hi, [&](const uint4& raw, int at) {
@@ -653,33 +691,47 @@ sample_kernel(const SampleArgs a) {
             for (int e = 0; e < E; ++e) {
                 const int b = sc.bin(v[e]);
                 if (b >= bin_lo && b < bin_hi) {
-                    const uint32_t to = atomicAdd(&sm.listed, 1u);
-                    if (to < kSampleList) list[to] = (uint64_t)order_key(v[e]) << 32 | (uint32_t)~(at + e);
+                    const uint32_t n = atomicAdd(listed, 1u);
+                    if (n < kSampleList) to[n] = (uint64_t)order_key(v[e]) << 32 | (uint32_t)~(at + e);
                 }
             }
         });
-        uint32_t size = 0;
-        if (ctas > 1) {
-            cluster.sync();
-            uint32_t first = 0;
-            for (int c = 0; c < ctas; ++c) {
-                const uint32_t n = *cluster.map_shared_rank(&sm.listed, c);
-                if (c < rank) first += n;
-                size += n;
-            }
-            uint64_t* to = cluster.map_shared_rank(list, 0);
-            if (rank > 0 && size <= kSampleList)
-                for (uint32_t i = threadIdx.x; i < sm.listed; i += kSampleThreads) to[first + i] = list[i];
-            cluster.sync();
-        } else {
-            __syncthreads();
-            size = sm.listed;
-        }
-        if (size > kSampleList) {  // (more reach the bound than the list holds)
-            if (rank == 0) sample_slow<T>(a, r, row, cut, sm, greedy, top_k, top_p, T_, u);
+        if (ctas > 1) cluster.sync();
+        else __syncthreads();
+        const uint32_t size = *listed;
+        if (ctas > 1 && mode == kBin) cluster.sync();  // (read by all before the first one goes on)
+        if (mode == kList && rank > 0) return;  // (a bin's list is never too long: it was counted)
+        if (size > kSampleList) {               // (more reach the bound than the list holds)
+            sample_slow<T>(a, r, row, sc, least, sm, greedy, top_k, top_p, T_, u);
             return;
         }
-        if (mode == kList && rank > 0) return;
+        if (mode == kList && size <= kSampleThreads) {
+            // ---- the choice from a short list: a token a thread
+            const uint32_t i = threadIdx.x, limit = by_k ? min((uint32_t)k, size) : size;
+            uint64_t x = sample_sort_short(list, (int)size);
+            float v = key_value((uint32_t)(x >> 32));
+            uint64_t w = i < limit ? sc.weight_of(v) : 0;
+            uint64_t upto = block_upto64(w, sm.sums);
+            if (by_k) whole = sm.sums[kSampleWarps];
+            // kept: what comes before the goal is reached
+            const uint64_t goal = by_p ? max((uint64_t)1, (uint64_t)ceil((double)fmaxf(top_p, 0.f) * (double)whole)) : ~0ull;
+            const bool kept = i < limit && upto - w < goal && sc.below(v) <= least;
+            const int n = __syncthreads_count(kept);  // (a beginning of the order)
+            if (kept) list[i] = x << 32 | x >> 32;    // by ~index, descending: by index, ascending
+            __syncthreads();
+            x = sample_sort_short(list, n);
+            v = key_value((uint32_t)x);
+            w = i < (uint32_t)n ? sc.weight_of(v) : 0;
+            upto = block_upto64(w, sm.sums);
+            const uint64_t total = sm.sums[kSampleWarps];
+            const double target = u * (double)total;
+            // the first whose sum is beyond the target (where there is none: the last)
+            if (w > 0 && ((double)upto > target || upto == total) && (double)(upto - w) <= target && upto - w < total) {
+                a.token[r] = (int)~(uint32_t)(x >> 32);
+                if (a.logprob) a.logprob[r] = greedy ? 0.f : (float)(-sc.below(v) / T_ - log((double)total / kSampleOne));
+            }
+            return;
+        }
         if (rank == 0) {
             sample_sort(list, (int)size);
             constexpr int PER = kSampleList / kSampleThreads;
@@ -777,49 +829,62 @@ sample_kernel(const SampleArgs a) {
         });
     }
     mine = warp_add64(mine);
-    uint64_t start = block_upto64(lane == 0 ? mine : 0, sm.sums) - mine;
-    start = __shfl_sync(0xffffffffu, start, 0);
-    uint64_t total = sm.sums[kSampleWarps];
+    uint64_t start = __shfl_sync(0xffffffffu, block_upto64(lane == 0 ? mine : 0, sm.sums) - mine, 0);
+    uint64_t total = sm.sums[kSampleWarps], cta_start = 0;
     if (ctas > 1) {
         if (threadIdx.x == 0) sm.part_total = total;
         cluster.sync();
         total = 0;
         for (int c = 0; c < ctas; ++c) {
             const uint64_t x = *cluster.map_shared_rank(&sm.part_total, c);
-            if (c < rank) start += x;
+            if (c < rank) cta_start += x;
             total += x;
         }
+        start += cta_start;
     }
     const double target = u * (double)total;
-    // (the last kept one, where rounding or a u of 1 or more leaves none)
-    if (mine > 0 && ((double)(start + mine) > target || start + mine == total) && ((double)start <= target || start == 0)) {
-        uint64_t sum = start;
-        bool done = false;
-        sample_run(row, run_lo, run_hi, [&](const float (&v)[E], int at) {
-            if (done) return;
-            uint64_t w[E], here = 0;
+    // Does the choice fall to weights [from, from + n)?  (The last kept token, where rounding or a u of 1 or more leaves none.)
+    auto falls_to = [&](uint64_t from, uint64_t n) {
+        return n > 0 && ((double)(from + n) > target || from + n == total) && ((double)from <= target || from == 0);
+    };
+    if (threadIdx.x == 0) sm.found32[0] = kSampleWarps;
+    __syncthreads();
+    if (lane == 0 && falls_to(start, mine)) { sm.found32[0] = warp; sm.found64[0] = start; }  // (one warp of the row)
+    __syncthreads();
+    if (sm.found32[0] < kSampleWarps) {
+        // its run again, a part for each warp of the CTA
+        const int whose = (int)sm.found32[0], lo = min(row.pieces, (rank * kSampleWarps + whose) * per), hi = min(row.pieces, lo + per);
+        const int each = (per / 32 + kSampleWarps - 1) / kSampleWarps * 32, part_lo = min(hi, lo + warp * each), part_hi = min(hi, part_lo + each);
+        mine = 0;
+        sample_run(row, part_lo, part_hi, [&](const float (&v)[E], int at) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) { w[e] = weight_in(v[e], at + e); here += w[e]; }
-            const uint64_t upto = warp_upto64(here);
-            uint64_t n = sum + upto - here;
-            const unsigned hit = __ballot_sync(0xffffffffu, here > 0 && ((double)(n + here) > target || n + here == total));
-            if (hit != 0) {
-                done = true;
-                if (lane == __ffs(hit) - 1) {
+            for (int e = 0; e < E; ++e) mine += weight_in(v[e], at + e);
+        });
+        mine = warp_add64(mine);
+        start = sm.found64[0] + __shfl_sync(0xffffffffu, block_upto64(lane == 0 ? mine : 0, sm.sums) - mine, 0);
+        if (falls_to(start, mine)) {
+            uint64_t sum = start;
+            sample_run(row, part_lo, part_hi, [&](const float (&v)[E], int at) {
+                uint64_t w[E], here = 0;
+#pragma unroll
+                for (int e = 0; e < E; ++e) { w[e] = weight_in(v[e], at + e); here += w[e]; }
+                const uint64_t upto = warp_upto64(here);
+                uint64_t n = sum + upto - here;
+                if (falls_to(n, here)) {  // (one lane, once)
                     bool chosen = false;
 #pragma unroll
                     for (int e = 0; e < E; ++e) {
-                        n += w[e];
-                        if (!chosen && w[e] > 0 && ((double)n > target || n == total)) {
+                        if (!chosen && falls_to(n, w[e])) {
                             chosen = true;
                             a.token[r] = at + e;
                             if (a.logprob) a.logprob[r] = (float)(-sc.below(v[e]) / T_ - log((double)total / kSampleOne));
                         }
+                        n += w[e];
                     }
                 }
-            }
-            sum += __shfl_sync(0xffffffffu, upto, 31);
-        });
+                sum += __shfl_sync(0xffffffffu, upto, 31);
+            });
+        }
     }
     if (ctas > 1) cluster.sync();  // (the others may still read this CTA's sum)
 }
