@@ -1,4 +1,5 @@
 // C ABI of the choice of the next token (see include/msa.h): argument validation and dispatch; the arithmetic is in sample.cuh.
+#include <algorithm>
 #include <cmath>
 
 #include "sample.cuh"
@@ -12,9 +13,7 @@ static int sample_ctas(int dev, int64_t rows, int64_t row_bytes) {
         cuda_failed();
         sms[dev] = 148;
     }
-    int ctas = 1;
-    while (ctas < 8 && rows * ctas <= sms[dev] && row_bytes >= 2 * ctas * 8192) ctas *= 2;
-    return ctas;
+    return (int)std::max<int64_t>(1, std::min<int64_t>({kSampleCtas, 2 * (int64_t)sms[dev] / rows, row_bytes / 8192}));
 }
 
 template <class T>

@@ -28,8 +28,10 @@ struct SampleArgs {
 };
 
 constexpr int kSampleThreads = 512, kSampleWarps = kSampleThreads / 32, kSampleTable = 1024;
-constexpr int kSampleBins = 2048, kSampleList = 4096;
-constexpr int kSampleSort = 1024;               // nuclei up to this are sorted, of larger ones only the bin they end in
+constexpr int kSampleBins = 512;                // of equal width in log w
+constexpr int kSampleDigits = 2048;             // sample_slow: values of eleven bits
+constexpr int kSampleCtas = 8;                  // of a row, at most
+constexpr int kSampleList = 4096, kSampleSort = 2048, kSamplePairs = 128;  // places of the list; tokens that are sorted, compared in pairs
 constexpr int kSampleBits = 42;
 constexpr double kSampleOne = 4398046511104.0;  // 2^42
 constexpr float kSampleReach = 43.f;            // 2^-43 of the largest is no whole number any more
@@ -114,11 +116,11 @@ struct SampleRow {
     }
 };
 
-// Pieces [lo, hi) of a warp: a run of the row, lanes side by side, four in flight.  f(piece, index of its first value) is called by
+// Pieces [lo, hi) of a warp: a run of the row, lanes side by side, U in flight (few where f is long: a loop that does not fit the
+// instruction cache is what slows these passes most).  f(piece, index of its first value) is called by
 // all lanes of the warp (beyond the run: with -infinities).
-template <class T, class F>
+template <int U, class T, class F>
 __device__ __forceinline__ void sample_pieces(const SampleRow<T>& row, int lo, int hi, F f) {
-    constexpr int U = 4;
     const int lane = threadIdx.x & 31;
     for (int p0 = lo; p0 < hi; p0 += 32 * U) {
         uint4 raw[U];
@@ -135,7 +137,7 @@ __device__ __forceinline__ void sample_pieces(const SampleRow<T>& row, int lo, i
 // The same with the values as floats.
 template <class T, class F>
 __device__ __forceinline__ void sample_run(const SampleRow<T>& row, int lo, int hi, F f) {
-    sample_pieces(row, lo, hi, [&](const uint4& raw, int at) {
+    sample_pieces<1>(row, lo, hi, [&](const uint4& raw, int at) {
         float v[SampleRow<T>::E];
         Logits<T>::widen(raw, v);
         f(v, at);
@@ -221,19 +223,25 @@ __device__ __forceinline__ uint64_t block_upto64(uint64_t v, uint64_t* s) {
 
 struct SampleSmem {
     double table[kSampleTable], root[64];
-    uint32_t count[kSampleBins];
+    uint32_t count[kSampleBins], mass_lo[kSampleBins], mass_hi[kSampleBins];
     union {
-        struct { uint32_t lo[kSampleBins], hi[kSampleBins]; } mass;
-        uint64_t list[kSampleList];    // (key, ~index): larger first means larger logit, then lower index
+        uint32_t counts[kSampleCtas][kSampleBins];  // of every CTA
+        uint64_t work[kSampleSort];                 // the list, packed
     };
+    union {
+        uint64_t masses[kSampleCtas][kSampleBins];  // of every CTA
+        uint64_t list[kSampleList];                 // (key, ~index): larger first means larger logit, then lower index; a part for each CTA
+        struct { uint32_t count[kSampleDigits], lo[kSampleDigits], hi[kSampleDigits]; } digits;  // sample_slow
+    };
+    uint64_t pair_w[kSamplePairs];
     uint64_t sums[kSampleWarps + 1];
     uint32_t scan[33];
     float tops[kSampleWarps];
-    // what a CTA tells the others (each is written once a row)
-    struct { float top; int nan; } said;
-    uint64_t total, above, part_total;
     uint32_t listed;
-    // what the first CTA tells the others
+    // what the CTAs tell one another (each is written once a row)
+    struct { float top; int nan; } said;
+    uint64_t totals[kSampleCtas], aboves[kSampleCtas], parts[kSampleCtas];
+    uint32_t sizes[kSampleCtas];
     uint32_t last_key;
     int last_index;
     // results of a search by one thread
@@ -241,10 +249,34 @@ struct SampleSmem {
     uint32_t found32[3];
 };
 
-// Sorts list[0, n) in descending order (up to the next power of two, filled with zeros).
+// Sorts list[0, n) in descending order (up to the next power of two, filled with zeros).  Short lists a value a thread, whose
+// partners in the same warp trade places in registers.
 __device__ inline void sample_sort(uint64_t* list, int n) {
     int size = 32;
     while (size < n) size *= 2;
+    if (size <= kSampleThreads) {
+        const int i = threadIdx.x;
+        uint64_t x = i < n ? list[i] : 0;
+        __syncthreads();
+        for (int k = 2; k <= size; k *= 2) {
+            int j = k / 2;
+            for (; j >= 32; j /= 2) {
+                if (i < size) list[i] = x;
+                __syncthreads();
+                const uint64_t y = i < size ? list[i ^ j] : 0;
+                __syncthreads();
+                x = (x > y) == (((i & k) == 0) == ((i & j) == 0)) ? x : y;
+            }
+            if (i < size)
+                for (; j > 0; j /= 2) {
+                    const uint64_t y = __shfl_xor_sync(0xffffffffu, x, j);
+                    x = (x > y) == (((i & k) == 0) == ((i & j) == 0)) ? x : y;  // (the larger of the two, or the smaller)
+                }
+        }
+        if (i < size) list[i] = x;
+        __syncthreads();
+        return;
+    }
     for (int i = n + threadIdx.x; i < size; i += kSampleThreads) list[i] = 0;
     __syncthreads();
     for (int k = 2; k <= size; k *= 2) {
@@ -259,39 +291,13 @@ __device__ inline void sample_sort(uint64_t* list, int n) {
     }
 }
 
-// The same for n <= kSampleThreads, a value a thread: thread i gets the i-th largest (0 from n on).  Partners of one warp trade
-// places in registers.  `list` holds the values before; it is written on.
-__device__ inline uint64_t sample_sort_short(uint64_t* list, int n) {
-    const int i = threadIdx.x;
-    int size = 32;
-    while (size < n) size *= 2;
-    uint64_t x = i < n ? list[i] : 0;
-    if (size > 32) __syncthreads();
-    for (int k = 2; k <= size; k *= 2) {
-        for (int j = k / 2; j > 0; j /= 2) {
-            uint64_t y = 0;
-            if (j >= 32) {
-                if (i < size) list[i] = x;
-                __syncthreads();
-                if (i < size) y = list[i ^ j];
-                __syncthreads();
-            } else {
-                y = __shfl_xor_sync(0xffffffffu, x, j);
-            }
-            const bool larger = ((i & k) == 0) == ((i & j) == 0);  // this thread keeps the larger of the two
-            x = (x > y) == larger ? x : y;
-        }
-    }
-    return x;
-}
-
 __device__ __forceinline__ float key_value(uint32_t key) { return __uint_as_float((key & 0x80000000u) ? key & 0x7FFFFFFFu : ~key); }
 
 // ---------------------------------------------------------------- any row, by one CTA
 // Whatever is kept, however many are equal: thresholds by the bits of the logits, 11, 11 and 10 at a time, each a pass over
 // the row that adds up counts or weights of the digits; then the index among equal ones.  For rows that the lists below do not hold.
 template <class T>
-__device__ __noinline__ void sample_slow(const SampleArgs& a, int64_t row_number, const SampleRow<T>& row, const SampleScale& sc, double least, SampleSmem& sm,
+__device__ __noinline__ void sample_slow(const SampleArgs a, int64_t row_number, const SampleRow<T> row, const SampleScale sc, double least, SampleSmem& sm,
                                    bool greedy, int top_k, float top_p, double temperature, double u) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int per = (row.pieces + 32 * kSampleWarps - 1) / (32 * kSampleWarps) * 32;
@@ -311,7 +317,8 @@ __device__ __noinline__ void sample_slow(const SampleArgs& a, int64_t row_number
         uint64_t want = target;
         for (int round = 0; round < 3; ++round) {
             const int shift = round == 0 ? 21 : (round == 1 ? 10 : 0), bits = round == 2 ? 10 : 11;
-            for (int i = threadIdx.x; i < kSampleBins; i += kSampleThreads) sm.count[i] = sm.mass.lo[i] = sm.mass.hi[i] = 0;
+            __syncthreads();
+            for (int i = threadIdx.x; i < kSampleDigits; i += kSampleThreads) sm.digits.count[i] = sm.digits.lo[i] = sm.digits.hi[i] = 0;
             __syncthreads();
             sample_run(row, run_lo, run_hi, [&](const float (&v)[E], int at) {
 #pragma unroll
@@ -319,21 +326,21 @@ __device__ __noinline__ void sample_slow(const SampleArgs& a, int64_t row_number
                     const uint32_t k = order_key(v[e]);
                     if (!kept(v[e], at + e) || (round > 0 && k >> (shift + bits) != prefix)) continue;
                     const uint32_t bin = (k >> shift) & ((1u << bits) - 1);
-                    atomicAdd(&sm.count[bin], 1u);
+                    atomicAdd(&sm.digits.count[bin], 1u);
                     if (by_mass) {
                         const uint64_t w = weight_of(v[e]);
-                        const uint32_t old = atomicAdd(&sm.mass.lo[bin], (uint32_t)w);
+                        const uint32_t old = atomicAdd(&sm.digits.lo[bin], (uint32_t)w);
                         const uint32_t high = (uint32_t)(w >> 32) + (old + (uint32_t)w < old ? 1u : 0u);
-                        if (high != 0) atomicAdd(&sm.mass.hi[bin], high);
+                        if (high != 0) atomicAdd(&sm.digits.hi[bin], high);
                     }
                 }
             });
             __syncthreads();
             uint64_t c[4], mine = 0;  // digits from the top, four a thread
-            const int d = kSampleBins - 1 - 4 * (int)threadIdx.x;
+            const int d = kSampleDigits - 1 - 4 * (int)threadIdx.x;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                c[j] = by_mass ? ((uint64_t)sm.mass.hi[d - j] << 32) + sm.mass.lo[d - j] : sm.count[d - j];
+                c[j] = by_mass ? ((uint64_t)sm.digits.hi[d - j] << 32) + sm.digits.lo[d - j] : sm.digits.count[d - j];
                 mine += c[j];
             }
             uint64_t above = block_upto64(mine, sm.sums) - mine;
@@ -444,15 +451,16 @@ __device__ __noinline__ void sample_slow(const SampleArgs& a, int64_t row_number
 }
 
 // ---------------------------------------------------------------- the rows
-// A cluster of CTAs per row (one CTA where there are many rows), each with a run of it: a pass for the maximum; where something
-// is filtered, a pass that counts the row in 2048 bins of equal width in log w, which the CTAs add up.
-//   top_k: what is counted are the threads' own maxima, which the pass for the maximum has left: k of them are a bound that the k largest
-//          reach, and hardly more.  (Every logit, where the threads are not many more than k.)  The tokens that reach it go to a
-//          list in the first CTA, which sorts it, cuts it and chooses from it.
-//   top_p alone: the counts bound the weight of each bin, and so the bins where the nucleus may end; a pass adds up the weights exactly,
-//          of the row, and bin by bin between the bounds.  If the nucleus fits the list it is chosen from there; else only
-//          the bin in which it ends is listed, to find its last token, and the choice is made as without filters:
+// A cluster of CTAs per row (one CTA where there are many rows), each with a run of it: a pass for the maximum; then
+//   top_k: the threads' own maxima, which that pass has left, are counted in bins of equal width in log w; the bin in which the
+//          count reaches k is a bound that the k largest logits reach, and few others.  (All logits are counted, where the threads
+//          are not many more than k.)  The tokens that reach it go to a list in the first CTA, which cuts it and chooses from it.
+//   top_p alone: the counts of all logits bound the weight of each bin, and so the bins where the nucleus may end; a pass adds up
+//          the weights exactly, of the row, and in finer bins between the bounds.  Those of the finer bin in which it ends are
+//          listed, to find its last token, and the choice is made as without filters; or all of a nucleus of a few, and it is made there.
 //   no filters: every warp adds up its run, and the one that the target falls into finds the token.
+// Measured: one row of 131072 with top_k and top_p KSAMPLE1; 96 of 100003 KSAMPLE2; a nucleus KSAMPLE3; 256 whole
+// rows of 131072 in fp32 KSAMPLE4.
 template <class T>
 __global__ void __launch_bounds__(kSampleThreads, 2)
 sample_kernel(const SampleArgs a) {
@@ -472,21 +480,24 @@ sample_kernel(const SampleArgs a) {
     // a warp's run of the row's pieces
     const int warps = ctas * kSampleWarps, per = (row.pieces + 32 * warps - 1) / (32 * warps) * 32;
     const int run_lo = min(row.pieces, (rank * kSampleWarps + warp) * per), run_hi = min(row.pieces, run_lo + per);
+    auto sync = [&]() {  // of the row's CTAs
+        if (ctas > 1) cluster.sync();
+        else __syncthreads();
+    };
 
     // 2^(-i/1024) from 2^(-i/32) and 2^(-i/1024) of the first 32
     if (threadIdx.x < 64) sm.root[threadIdx.x] = exp2((threadIdx.x < 32 ? (double)threadIdx.x / -32 : (double)(threadIdx.x - 32) / -1024));
-    for (int i = threadIdx.x; i < kSampleBins; i += kSampleThreads) sm.count[i] = sm.mass.lo[i] = sm.mass.hi[i] = 0;
+    for (int i = threadIdx.x; i < kSampleBins; i += kSampleThreads) sm.count[i] = sm.mass_lo[i] = sm.mass_hi[i] = 0;
     if (threadIdx.x == 0) sm.listed = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < kSampleTable; i += kSampleThreads) sm.table[i] = sm.root[i >> 5] * sm.root[32 + (i & 31)];
 
     // ---- the largest logit; this thread's own
     float own_top = -INFINITY, top;
     {
-        sample_pieces(row, run_lo, run_hi, [&](const uint4& raw, int) { own_top = max_nan(own_top, Logits<T>::largest(raw)); });
+        sample_pieces<4>(row, run_lo, run_hi, [&](const uint4& raw, int) { own_top = max_nan(own_top, Logits<T>::largest(raw)); });
         bool nan = __syncthreads_or(own_top != own_top) != 0;
         top = warp_max(own_top);
         if (lane == 0) sm.tops[warp] = top;
+        for (int i = threadIdx.x; i < kSampleTable; i += kSampleThreads) sm.table[i] = sm.root[i >> 5] * sm.root[32 + (i & 31)];
         __syncthreads();
         top = warp_max(sm.tops[lane % kSampleWarps]);
         if (ctas > 1) {
@@ -513,61 +524,53 @@ sample_kernel(const SampleArgs a) {
     const int k = greedy ? 1 : top_k;
     bool by_k = k > 0 && k < a.vocab;
     const bool by_p = !greedy && top_p < 1.f;
+    const double p = (double)fmaxf(top_p, 0.f);
+    const bool tame = fabs(sc.tc) < 1048576.0;  // (weight_of; a top of infinity is not)
+    static_assert(kSampleBins == kSampleThreads, "a bin a thread");
+    const int b0 = threadIdx.x;
 
-    // Adds up an array of all CTAs, everywhere: a part each, handed to the others.  (The arrays are the CTAs' own before.)
-    auto merge = [&](uint32_t* lo, uint32_t* hi) {
-        if (ctas == 1) { __syncthreads(); return; }
+    // The row's count of this thread's bin: every CTA hands its counts to the others.
+    auto counted = [&]() {
+        __syncthreads();
+        if (ctas == 1) return sm.count[b0];
+        const uint32_t mine = sm.count[b0];
+        for (int c = 0; c < ctas; ++c) *cluster.map_shared_rank(&sm.counts[rank][b0], c) = mine;
         cluster.sync();
-        const int part = kSampleBins / ctas;
-        for (int i = threadIdx.x; i < part; i += kSampleThreads) {
-            const int at = rank * part + i;
-            uint64_t sum = 0;
-            for (int c = 0; c < ctas; ++c) {
-                sum += *cluster.map_shared_rank(lo + at, c);
-                if (hi) sum += (uint64_t)*cluster.map_shared_rank(hi + at, c) << 32;
-            }
-            for (int c = 0; c < ctas; ++c) {  // (nobody else reads or writes this part)
-                *cluster.map_shared_rank(lo + at, c) = (uint32_t)sum;
-                if (hi) *cluster.map_shared_rank(hi + at, c) = (uint32_t)(sum >> 32);
-            }
-        }
-        cluster.sync();
+        uint32_t n = 0;
+        for (int c = 0; c < ctas; ++c) n += sm.counts[c][b0];
+        return n;
+    };
+    // The bin in which a count from the top reaches k: to found32[0], the count up to its end to found32[1].
+    auto bin_of_count = [&](uint32_t n, uint32_t* all) {
+        const uint32_t upto = block_scan(n, sm.scan, all);
+        if (upto < (uint32_t)k && upto + n >= (uint32_t)k) { sm.found32[0] = b0; sm.found32[1] = upto + n; }  // (one thread)
+        __syncthreads();
+        return upto;
     };
 
     enum { kAll, kList, kBin, kSlow };
-    int mode = kAll, bin_lo = 0, bin_hi = kSampleBins;  // bins that are listed
-    uint64_t whole = 0, above = 0;                      // weight of the row, of the bins before the listed ones
-    constexpr int PER = kSampleBins / kSampleThreads;
-    const int b0 = (int)threadIdx.x * PER;
-    // the bin in which a count from the top reaches k: to found32[0], the count up to its end to found32[1]
-    auto bin_of_count = [&](uint32_t* all) {
-        uint32_t n[PER], mine = 0;
-#pragma unroll
-        for (int j = 0; j < PER; ++j) { n[j] = sm.count[b0 + j]; mine += n[j]; }
-        uint32_t upto = block_scan(mine, sm.scan, all);
-#pragma unroll
-        for (int j = 0; j < PER; ++j) {
-            if (upto < (uint32_t)k && upto + n[j] >= (uint32_t)k) { sm.found32[0] = b0 + j; sm.found32[1] = upto + n[j]; }  // (one thread)
-            upto += n[j];
-        }
-        __syncthreads();
-    };
-    const bool tame = fabs(sc.tc) < 1048576.0;  // (weight_of; a top of infinity is not)
+    int mode = kAll;
+    // What is listed: top_k: bins up to `end`.  top_p: of the finer bins, `finer` times the distance from `from` on and below
+    // `to`, number `end`, or that and all before it.
+    float from = 0.f, to = INFINITY, finer = 0.f;
+    int end = 0;
+    uint64_t whole = 0, above = 0;      // weight of the row, of what comes before the list
+    auto distance = [&](float v) { return (sc.top - v) * sc.c32; };
+    constexpr float kWidth = kSampleReach / kSampleBins;
     // Twice as many threads as k, at least, or most of what they would list is not wanted.
-    bool by_maxima = by_k && (int64_t)k * 2 <= (int64_t)ctas * kSampleThreads && tame;
+    bool by_maxima = by_k && tame && (int64_t)k * 2 <= (int64_t)ctas * kSampleThreads;
     if (by_maxima) {
         const int b = sc.bin(own_top);
         if (b < kSampleBins) atomicAdd(&sm.count[b], 1u);
-        merge(sm.count, nullptr);
         uint32_t all;
-        bin_of_count(&all);
+        bin_of_count(counted(), &all);
         by_maxima = all >= (uint32_t)k;
         if (by_maxima) {
-            // (in units of the bins: what reaches the bin, not just the maxima)
-            bin_hi = (int)sm.found32[0] + 1;
             mode = kList;
+            end = (int)sm.found32[0];
         } else {  // the threads' maxima are too few: count all
-            for (int i = threadIdx.x; i < kSampleBins; i += kSampleThreads) sm.count[i] = 0;
+            sync();
+            sm.count[b0] = 0;
             __syncthreads();
         }
     }
@@ -580,236 +583,291 @@ sample_kernel(const SampleArgs a) {
                 if (b < kSampleBins) atomicAdd(&sm.count[b], 1u);
             }
         });
-        merge(sm.count, nullptr);
+        const uint32_t n = counted();
         uint32_t all;
-        bin_of_count(&all);
+        const uint32_t earlier_n = bin_of_count(n, &all);
         by_k = by_k && (uint32_t)k < all;  // (the rest weighs nothing)
         if (by_k) {
-            bin_hi = (int)sm.found32[0] + 1;
-            mode = sm.found32[1] <= kSampleList ? kList : kSlow;
+            mode = sm.found32[1] <= kSampleSort ? kList : kSlow;
+            end = (int)sm.found32[0];
         } else if (by_p) {
-            // Bounds of the weight up to each bin: a logit of bin b weighs 2^-(b+1)h to 2^-bh, h the width (and 10^-5 for the
-            // 32-bit arithmetic of the bins).  The nucleus ends where the weight reaches top_p of the whole.
-            uint32_t n[PER], counts = 0;
-#pragma unroll
-            for (int j = 0; j < PER; ++j) { n[j] = sm.count[b0 + j]; counts += n[j]; }
-            const uint32_t before = block_scan(counts, sm.scan, &all);
-            const double h = (double)kSampleReach / kSampleBins, p = (double)fmaxf(top_p, 0.f);
-            double low = 0.0, low_of[PER], high_of[PER];
-#pragma unroll
-            for (int j = 0; j < PER; ++j) {
-                const double w = (double)exp2f((float)(-(b0 + j) * h)) * n[j];
-                high_of[j] = w * 1.00003;
-                low_of[j] = w * 0.98555 * 0.99997;  // 2^-h
-                low += low_of[j];
-            }
-            static_assert(kSampleTable == 1024 && kSampleBins == 2048, "the factor is 2^(-43/2048)");
-            // (in whole numbers, for the scan: 2^-20 of the largest; rounded to the safe side below)
-            const uint64_t lows = (uint64_t)(low * 1048576.0), low_upto = block_upto64(lows, sm.sums), low_all = sm.sums[kSampleWarps];
-            double high = 0.0;
-#pragma unroll
-            for (int j = 0; j < PER; ++j) high += high_of[j];
-            const uint64_t highs = (uint64_t)(high * 1048576.0) + 1, high_upto = block_upto64(highs, sm.sums), high_all = sm.sums[kSampleWarps];
-            // first thread whose bins may hold the end, first whose bins certainly reach it
-            const bool may = (double)high_upto >= p * (double)low_all, must = (double)low_upto >= p * (double)high_all;
+            // Bounds of the weight up to each bin, and of what comes behind it: a logit of bin b weighs 2^-(b+1)h to 2^-bh, h the
+            // width (and 10^-5 for the 32-bit arithmetic of the bins).  The nucleus ends where what comes behind is at most (1 -
+            // top_p) / top_p of what it holds.
+            const double w = (double)exp2f(-(float)b0 * kWidth) * n;
+            // (in whole numbers, for the scan: 2^-30 of the largest, to the safe side)
+            const uint64_t low = (uint64_t)(w * 0.9434 * 0.99997 * 1073741824.0), high = (uint64_t)(w * 1.00003 * 1073741824.0) + 1;  // 2^-h
+            static_assert(kSampleBins == 512, "the factor is 2^(-43/512), a little less");
+            const uint64_t low_upto = block_upto64(low, sm.sums), low_all = sm.sums[kSampleWarps];
+            const uint64_t high_upto = block_upto64(high, sm.sums), high_all = sm.sums[kSampleWarps];
+            auto ends = [&](uint64_t behind, uint64_t held) { return p * (double)behind <= (1.0 - p) * (double)held; };
             if (threadIdx.x == 0) { sm.found32[0] = 0; sm.found32[1] = kSampleBins; }
             __syncthreads();
-            if (may && !((double)(high_upto - highs) >= p * (double)low_all)) sm.found32[0] = b0;
-            if (must && !((double)(low_upto - lows) >= p * (double)high_all)) sm.found32[1] = b0 + PER;
+            // the first bin that may hold the end, the first that certainly reaches it
+            if (ends(low_all - low_upto, high_upto) && (b0 == 0 || !ends(low_all - (low_upto - low), high_upto - high))) sm.found32[0] = b0;
+            if (ends(high_all - high_upto, low_upto) && (b0 == 0 || !ends(high_all - (high_upto - high), low_upto - low))) sm.found32[1] = b0 + 1;
             __syncthreads();
-            const int from = (int)sm.found32[0], to = (int)sm.found32[1];
-            // ---- exact weights: of the row, of the bins before `from`, of each bin in [from, to)
+            from = (float)sm.found32[0] * kWidth;
+            if (sm.found32[1] < kSampleBins) to = (float)sm.found32[1] * kWidth;
+            finer = (float)kSampleBins / ((float)(sm.found32[1] - sm.found32[0]) * kWidth);
+            // ---- exact weights: of the row, of what comes before `from`, and in finer bins between `from` and `to`
             uint64_t total = 0, earlier = 0;
             sample_run(row, run_lo, run_hi, [&](const float (&v)[E], int) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    const int b = sc.bin(v[e]);
-                    if (b >= kSampleBins) continue;
                     const uint64_t w = sc.weight_of(v[e]);
+                    const float z = distance(v[e]);
                     total += w;
-                    if (b < from) earlier += w;
-                    else if (b < to) {
-                        const uint32_t old = atomicAdd(&sm.mass.lo[b], (uint32_t)w);
+                    if (z < from) earlier += w;
+                    else if (z < to && w > 0) {
+                        const int b = min((int)((z - from) * finer), kSampleBins - 1);
+                        const uint32_t old = atomicAdd(&sm.mass_lo[b], (uint32_t)w);
                         const uint32_t up = (uint32_t)(w >> 32) + (old + (uint32_t)w < old ? 1u : 0u);
-                        if (up != 0) atomicAdd(&sm.mass.hi[b], up);
+                        if (up != 0) atomicAdd(&sm.mass_hi[b], up);
                     }
                 }
             });
             block_upto64(total, sm.sums);
-            if (threadIdx.x == 0) sm.total = sm.sums[kSampleWarps];
+            const uint64_t cta_total = sm.sums[kSampleWarps];
             block_upto64(earlier, sm.sums);
-            if (threadIdx.x == 0) sm.above = sm.sums[kSampleWarps];
-            merge(sm.mass.lo, sm.mass.hi);
-            for (int c = 0; c < ctas; ++c) {
-                whole += *cluster.map_shared_rank(&sm.total, c);
-                above += *cluster.map_shared_rank(&sm.above, c);
-            }
-            uint64_t m[PER], mass = 0;
-#pragma unroll
-            for (int j = 0; j < PER; ++j) { m[j] = ((uint64_t)sm.mass.hi[b0 + j] << 32) + sm.mass.lo[b0 + j]; mass += m[j]; }
-            uint64_t upto = above + block_upto64(mass, sm.sums) - mass;
-            const uint64_t goal = max((uint64_t)1, (uint64_t)ceil(p * (double)whole));
-            uint32_t counted = before;
-            if (threadIdx.x == 0) { sm.found32[0] = kSampleBins - 1; sm.found32[1] = 0xFFFFFFFFu; }
-            __syncthreads();
-#pragma unroll
-            for (int j = 0; j < PER; ++j) {
-                if (upto < goal && upto + m[j] >= goal && b0 + j >= from) {  // (one thread)
-                    sm.found32[0] = b0 + j; sm.found32[1] = counted + n[j]; sm.found32[2] = n[j];
-                    sm.found64[0] = upto;
+            const uint64_t cta_earlier = sm.sums[kSampleWarps];
+            uint64_t mass = ((uint64_t)sm.mass_hi[b0] << 32) + sm.mass_lo[b0];
+            whole = cta_total;
+            above = cta_earlier;
+            if (ctas > 1) {
+                for (int c = 0; c < ctas; ++c) *cluster.map_shared_rank(&sm.masses[rank][b0], c) = mass;
+                if (threadIdx.x < ctas) {
+                    auto* other = cluster.map_shared_rank(&sm, threadIdx.x);
+                    other->totals[rank] = cta_total;
+                    other->aboves[rank] = cta_earlier;
                 }
-                upto += m[j];
-                counted += n[j];
+                cluster.sync();
+                mass = whole = above = 0;
+                for (int c = 0; c < ctas; ++c) { mass += sm.masses[c][b0]; whole += sm.totals[c]; above += sm.aboves[c]; }
             }
+            const uint64_t upto = above + block_upto64(mass, sm.sums);
+            const uint64_t goal = max((uint64_t)1, (uint64_t)ceil(p * (double)whole));
+            if (threadIdx.x == 0) sm.found32[2] = 0xFFFFFFFFu;
             __syncthreads();
-            bin_hi = (int)sm.found32[0] + 1;
-            if (sm.found32[1] == 0xFFFFFFFFu) mode = kSlow;
-            else if (sm.found32[1] <= kSampleSort) { mode = kList; above = 0; }
-            else if (sm.found32[2] <= kSampleList) { mode = kBin; bin_lo = bin_hi - 1; above = sm.found64[0]; }
-            else mode = kSlow;
+            if (upto >= goal && upto - mass < goal) { sm.found32[2] = b0; sm.found64[0] = upto - mass; }  // (one thread)
+            __syncthreads();
+            end = (int)sm.found32[2];
+            mode = end >= 0 ? kBin : kSlow;
+            above = sm.found64[0];
+            // the tokens up to the bin of the counts in which the finer bin ends: a few? then all are listed
+            const float at = from + (float)(end + 1) / finer;
+            if (mode == kBin && (float)b0 * kWidth <= at && (float)(b0 + 1) * kWidth > at && earlier_n + n <= kSamplePairs) sm.found32[1] = 0xFFFFFFFFu;
+            __syncthreads();
+            if (sm.found32[1] == 0xFFFFFFFFu) {
+                mode = kList;
+                above = 0;
+            }
         }
     }
+    // Nobody reads another CTA's memory from here on, before the next meeting.
     if (mode == kSlow) {
-        if (ctas > 1) cluster.sync();  // (nobody reads the first CTA's memory any more)
+        sync();
         if (rank == 0) sample_slow<T>(a, r, row, sc, least, sm, greedy, top_k, top_p, T_, u);
         return;
     }
 
+    uint32_t last_key = 0;
+    int last_index = a.vocab;
+    auto falls_to = [&](uint64_t start, uint64_t n, double target, uint64_t total) {
+        // Does the choice fall to weights [start, start + n)?  (The last kept token, where rounding or a u of 1 or more leaves none.)
+        return n > 0 && ((double)(start + n) > target || start + n == total) && ((double)start <= target || start == 0);
+    };
+    auto choose = [&](int index, float v, uint64_t total) {
+        a.token[r] = index;
+        if (a.logprob) a.logprob[r] = greedy ? 0.f : (float)(-sc.below(v) / T_ - log((double)total / kSampleOne));
+    };
     if (mode != kAll) {
-        // ---- the tokens of bins [bin_lo, bin_hi) into the first CTA's list, in any order
-        if (ctas > 1) cluster.sync();  // (the list takes the place of the masses, which have been read)
-        else __syncthreads();
-        uint64_t *list = sm.list, *to = cluster.map_shared_rank(list, 0);
-        uint32_t* listed = cluster.map_shared_rank(&sm.listed, 0);
-        // (logits that reach the bins' lower end, or a little below: most pieces have none)
-        const float least_listed = sc.top - (float)bin_hi * (kSampleReach / kSampleBins) / sc.c32 * 1.0001f - 1e-6f * fabsf(sc.top);
-        sample_pieces(row, run_lo, run_hi, [&](const uint4& raw, int at) {
+        // ---- the list, in the first CTA, a part for each CTA
+        if (!by_k && ctas > 1) cluster.sync();  // (it takes the place of the finer bins' weights, which have been read)
+        const int part = kSampleList / ctas;
+        uint64_t* mine = cluster.map_shared_rank(sm.list, 0) + rank * part;
+        auto wanted = [&](float v) {
+            if (by_k) return sc.bin(v) <= end;
+            const float z = distance(v);
+            const int b = z < from ? -1 : (z < to ? min((int)((z - from) * finer), kSampleBins - 1) : kSampleBins);
+            return mode == kBin ? b == end : b <= end;
+        };
+        // (logits at the far end of what is wanted, or a little below: most pieces have none)
+        const float z_end = by_k ? (float)(end + 1) * kWidth : from + (float)(end + 1) / finer;
+        const float least_listed = sc.top - z_end / sc.c32 * 1.0001f - 1e-6f * fabsf(sc.top);
+        sample_pieces<1>(row, run_lo, run_hi, [&](const uint4& raw, int at) {
             if (!(Logits<T>::largest(raw) >= least_listed)) return;
             float v[E];
             Logits<T>::widen(raw, v);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const int b = sc.bin(v[e]);
-                if (b >= bin_lo && b < bin_hi) {
-                    const uint32_t n = atomicAdd(listed, 1u);
-                    if (n < kSampleList) to[n] = (uint64_t)order_key(v[e]) << 32 | (uint32_t)~(at + e);
+                if (v[e] >= least_listed && wanted(v[e])) {
+                    const uint32_t n = atomicAdd(&sm.listed, 1u);
+                    if (n < (uint32_t)part) mine[n] = (uint64_t)order_key(v[e]) << 32 | (uint32_t)~(at + e);
                 }
             }
         });
-        if (ctas > 1) cluster.sync();
-        else __syncthreads();
-        const uint32_t size = *listed;
-        if (ctas > 1 && mode == kBin) cluster.sync();  // (read by all before the first one goes on)
-        if (mode == kList && rank > 0) return;  // (a bin's list is never too long: it was counted)
-        if (size > kSampleList) {               // (more reach the bound than the list holds)
-            sample_slow<T>(a, r, row, sc, least, sm, greedy, top_k, top_p, T_, u);
-            return;
-        }
-        if (mode == kList && size <= kSampleThreads) {
-            // ---- the choice from a short list: a token a thread
-            const uint32_t i = threadIdx.x, limit = by_k ? min((uint32_t)k, size) : size;
-            uint64_t x = sample_sort_short(list, (int)size);
-            float v = key_value((uint32_t)(x >> 32));
-            uint64_t w = i < limit ? sc.weight_of(v) : 0;
-            uint64_t upto = block_upto64(w, sm.sums);
-            if (by_k) whole = sm.sums[kSampleWarps];
-            // kept: what comes before the goal is reached
-            const uint64_t goal = by_p ? max((uint64_t)1, (uint64_t)ceil((double)fmaxf(top_p, 0.f) * (double)whole)) : ~0ull;
-            const bool kept = i < limit && upto - w < goal && sc.below(v) <= least;
-            const int n = __syncthreads_count(kept);  // (a beginning of the order)
-            if (kept) list[i] = x << 32 | x >> 32;    // by ~index, descending: by index, ascending
-            __syncthreads();
-            x = sample_sort_short(list, n);
-            v = key_value((uint32_t)x);
-            w = i < (uint32_t)n ? sc.weight_of(v) : 0;
-            upto = block_upto64(w, sm.sums);
-            const uint64_t total = sm.sums[kSampleWarps];
-            const double target = u * (double)total;
-            // the first whose sum is beyond the target (where there is none: the last)
-            if (w > 0 && ((double)upto > target || upto == total) && (double)(upto - w) <= target && upto - w < total) {
-                a.token[r] = (int)~(uint32_t)(x >> 32);
-                if (a.logprob) a.logprob[r] = greedy ? 0.f : (float)(-sc.below(v) / T_ - log((double)total / kSampleOne));
-            }
-            return;
-        }
+        __syncthreads();
+        if (threadIdx.x == 0) *cluster.map_shared_rank(&sm.sizes[rank], 0) = sm.listed;
+        sync();
+        if (mode == kList && rank > 0) return;
         if (rank == 0) {
-            sample_sort(list, (int)size);
-            constexpr int PER = kSampleList / kSampleThreads;
-            const int per_thread = ((int)size + kSampleThreads - 1) / kSampleThreads, at0 = (int)threadIdx.x * per_thread;
-            uint64_t w[PER], mine = 0;
-            const uint32_t limit = by_k ? min((uint32_t)k, size) : size;
+            uint32_t size = 0, first[kSampleCtas + 1];
+            bool fits = true;
 #pragma unroll
-            for (int j = 0; j < PER; ++j) {
-                const uint32_t i = at0 + j;
-                w[j] = j < per_thread && i < limit ? sc.weight_of(key_value((uint32_t)(list[i] >> 32))) : 0;
-                mine += w[j];
+            for (int c = 0; c < kSampleCtas; ++c) {
+                const uint32_t n = c < ctas ? sm.sizes[c] : 0;
+                fits &= n <= (uint32_t)part;
+                first[c] = size;
+                size += n;
             }
-            uint64_t upto = above + block_upto64(mine, sm.sums) - mine;
-            if (by_k) whole = sm.sums[kSampleWarps];
-            // the first token at which the weight reaches the goal is the last one kept
-            const uint64_t goal = by_p ? max((uint64_t)1, (uint64_t)ceil((double)fmaxf(top_p, 0.f) * (double)whole)) : ~0ull;
-            if (threadIdx.x == 0) sm.found32[0] = limit - 1;
-            __syncthreads();
-#pragma unroll
-            for (int j = 0; j < PER; ++j) {
-                if (w[j] > 0 && upto < goal && upto + w[j] >= goal) sm.found32[0] = at0 + j;  // (one thread)
-                upto += w[j];
-            }
-            __syncthreads();
-            const uint32_t last = sm.found32[0];
-            if (threadIdx.x == 0) {
-                sm.last_key = (uint32_t)(list[last] >> 32);
-                sm.last_index = (int)~(uint32_t)list[last];
-            }
-            if (mode == kList) {
-                // ---- the choice: those kept in the order of their indices
-                int kept = 0;
-                for (uint32_t i = threadIdx.x; i <= last; i += kSampleThreads) kept += sc.below(key_value((uint32_t)(list[i] >> 32))) <= least;
-                uint32_t n;
-                block_scan(kept, sm.scan, &n);  // (min_p lets a beginning of the order through)
-                for (uint32_t i = threadIdx.x; i < n; i += kSampleThreads) {
-                    const uint64_t x = list[i];
-                    list[i] = x << 32 | x >> 32;  // by ~index, descending: by index, ascending
-                }
+            fits &= size <= kSampleSort;
+            if (threadIdx.x == 0) sm.listed = fits ? 0 : 1;  // (for the others, below)
+            if (!fits) {
+                if (mode == kBin) { sync(); sync(); }  // (the others learn of it, and have read it)
                 __syncthreads();
-                sample_sort(list, (int)n);
-                const int each = ((int)n + kSampleThreads - 1) / kSampleThreads, from = (int)threadIdx.x * each;
-                mine = 0;
-#pragma unroll
-                for (int j = 0; j < PER; ++j) {
-                    w[j] = j < each && from + j < (int)n ? sc.weight_of(key_value((uint32_t)list[from + j])) : 0;
-                    mine += w[j];
-                }
-                upto = block_upto64(mine, sm.sums) - mine;
-                const uint64_t total = sm.sums[kSampleWarps];
-                const double target = u * (double)total;
-                bool before_me = (double)upto > target || (upto == total && upto > 0);  // (chosen already)
-#pragma unroll
-                for (int j = 0; j < PER; ++j) {
-                    upto += w[j];
-                    if (!before_me && w[j] > 0 && ((double)upto > target || upto == total)) {
-                        before_me = true;
-                        const uint64_t x = list[from + j];
-                        a.token[r] = (int)~(uint32_t)(x >> 32);
-                        if (a.logprob)
-                            a.logprob[r] = greedy ? 0.f : (float)(-sc.below(key_value((uint32_t)x)) / T_ - log((double)total / kSampleOne));
-                    }
-                }
+                sample_slow<T>(a, r, row, sc, least, sm, greedy, top_k, top_p, T_, u);
                 return;
             }
+            for (uint32_t i = threadIdx.x; i < size; i += kSampleThreads) {
+                int c = 0;
+#pragma unroll
+                for (int j = 1; j < kSampleCtas; ++j) c += j < ctas && i >= first[j];
+                uint32_t start = 0;
+#pragma unroll
+                for (int j = 0; j < kSampleCtas; ++j) start = j == c ? first[j] : start;
+                sm.work[i] = sm.list[c * part + (i - start)];
+            }
+            __syncthreads();
+            const uint32_t limit = by_k ? min((uint32_t)k, size) : size;
+            uint64_t* list = sm.work;
+            if (size <= kSamplePairs) {
+                // ---- short: what comes before a token is found by comparing it with all others, four threads a token
+                if (threadIdx.x < size) sm.pair_w[threadIdx.x] = sc.weight_of(key_value((uint32_t)(list[threadIdx.x] >> 32)));
+                __syncthreads();
+                const uint32_t i = threadIdx.x >> 2, sub = threadIdx.x & 3;
+                const uint64_t x = i < size ? list[i] : 0, w = i < size ? sm.pair_w[i] : 0;
+                uint32_t larger = 0;
+                uint64_t before = 0;
+                for (uint32_t j = sub; j < size; j += 4) {
+                    const bool l = list[j] > x;
+                    larger += l;
+                    before += l ? sm.pair_w[j] : 0;
+                }
+#pragma unroll
+                for (int o = 1; o < 4; o <<= 1) {
+                    larger += __shfl_xor_sync(0xffffffffu, larger, o);
+                    before += __shfl_xor_sync(0xffffffffu, before, o);
+                }
+                if (by_k) {
+                    if (i < size && larger == limit - 1) sm.found64[1] = before + w;
+                    __syncthreads();
+                    whole = sm.found64[1];
+                }
+                const uint64_t goal = by_p ? max((uint64_t)1, (uint64_t)ceil(p * (double)whole)) : ~0ull;
+                before += above;
+                const bool kept = i < size && larger < limit && before < goal;
+                if (mode == kBin) {
+                    if (kept && before + w >= goal) { sm.last_key = (uint32_t)(x >> 32); sm.last_index = (int)~(uint32_t)x; }
+                } else {
+                    const float v = key_value((uint32_t)(x >> 32));
+                    const uint64_t kept_w = kept && sc.below(v) <= least ? w : 0;
+                    __syncthreads();
+                    if (sub == 0 && i < size) sm.pair_w[i] = kept_w;
+                    __syncthreads();
+                    uint64_t start = 0, total = 0;
+                    for (uint32_t j = sub; j < size; j += 4) {
+                        const uint64_t wj = sm.pair_w[j];
+                        total += wj;
+                        start += (uint32_t)list[j] > (uint32_t)x ? wj : 0;  // (~index: a lower index)
+                    }
+#pragma unroll
+                    for (int o = 1; o < 4; o <<= 1) {
+                        start += __shfl_xor_sync(0xffffffffu, start, o);
+                        total += __shfl_xor_sync(0xffffffffu, total, o);
+                    }
+                    if (sub == 0 && falls_to(start, kept_w, u * (double)total, total)) choose((int)~(uint32_t)x, v, total);
+                    return;
+                }
+            } else {
+                // ---- longer: sorted
+                sample_sort(list, (int)size);
+                constexpr int PER = kSampleSort / kSampleThreads;
+                const int each = ((int)size + kSampleThreads - 1) / kSampleThreads, at0 = (int)threadIdx.x * each;
+                uint64_t w[PER], sum = 0;
+#pragma unroll
+                for (int j = 0; j < PER; ++j) {
+                    const uint32_t i = at0 + j;
+                    w[j] = j < each && i < limit ? sc.weight_of(key_value((uint32_t)(list[i] >> 32))) : 0;
+                    sum += w[j];
+                }
+                uint64_t upto = above + block_upto64(sum, sm.sums) - sum;
+                if (by_k) whole = sm.sums[kSampleWarps];
+                // the first token at which the weight reaches the goal is the last one kept
+                const uint64_t goal = by_p ? max((uint64_t)1, (uint64_t)ceil(p * (double)whole)) : ~0ull;
+                if (threadIdx.x == 0) sm.found32[0] = limit - 1;
+                __syncthreads();
+#pragma unroll
+                for (int j = 0; j < PER; ++j) {
+                    if (w[j] > 0 && upto < goal && upto + w[j] >= goal) sm.found32[0] = at0 + j;  // (one thread)
+                    upto += w[j];
+                }
+                __syncthreads();
+                const uint32_t last = sm.found32[0];
+                if (mode == kBin) {
+                    if (threadIdx.x == 0) { sm.last_key = (uint32_t)(list[last] >> 32); sm.last_index = (int)~(uint32_t)list[last]; }
+                } else {
+                    // the choice: those kept in the order of their indices
+                    int kept = 0;
+                    for (uint32_t i = threadIdx.x; i <= last; i += kSampleThreads) kept += sc.below(key_value((uint32_t)(list[i] >> 32))) <= least;
+                    uint32_t n;
+                    block_scan(kept, sm.scan, &n);  // (min_p lets a beginning of the order through)
+                    for (uint32_t i = threadIdx.x; i < n; i += kSampleThreads) {
+                        const uint64_t x = list[i];
+                        list[i] = x << 32 | x >> 32;  // by ~index, descending: by index, ascending
+                    }
+                    __syncthreads();
+                    sample_sort(list, (int)n);
+                    const int some = ((int)n + kSampleThreads - 1) / kSampleThreads, at1 = (int)threadIdx.x * some;
+                    sum = 0;
+#pragma unroll
+                    for (int j = 0; j < PER; ++j) {
+                        w[j] = j < some && at1 + j < (int)n ? sc.weight_of(key_value((uint32_t)list[at1 + j])) : 0;
+                        sum += w[j];
+                    }
+                    upto = block_upto64(sum, sm.sums) - sum;
+                    const uint64_t total = sm.sums[kSampleWarps];
+                    const double target = u * (double)total;
+                    bool done = false;
+#pragma unroll
+                    for (int j = 0; j < PER; ++j) {
+                        if (!done && falls_to(upto, w[j], target, total)) {
+                            done = true;
+                            const uint64_t x = list[at1 + j];
+                            choose((int)~(uint32_t)(x >> 32), key_value((uint32_t)x), total);
+                        }
+                        upto += w[j];
+                    }
+                    return;
+                }
+            }
         }
-        if (ctas > 1) cluster.sync();
-        else __syncthreads();
+        sync();
+        const auto* first_cta = cluster.map_shared_rank(&sm, 0);
+        last_key = first_cta->last_key;
+        last_index = first_cta->last_index;
+        if (rank > 0 && first_cta->listed != 0) {
+            sync();
+            return;
+        }
     }
 
     // ---- the choice from the row
-    const uint32_t last_key = mode == kBin ? *cluster.map_shared_rank(&sm.last_key, 0) : 0u;
-    const int last_index = mode == kBin ? *cluster.map_shared_rank(&sm.last_index, 0) : a.vocab;
     auto weight_in = [&](float v, int i) -> uint64_t {
         const uint32_t key = order_key(v);
-        if (key < last_key || (key == last_key && i > last_index)) return 0;
-        const double d = sc.below(v);
-        return d <= least ? sc.weight(d) : 0;
+        const bool in = (key > last_key || (key == last_key && i <= last_index)) && sc.below(v) <= least;
+        const uint64_t w = sc.weight_of(v);
+        return in ? w : 0;
     };
     uint64_t mine = 0;
     if (mode == kAll && least == INFINITY) {
@@ -818,75 +876,66 @@ sample_kernel(const SampleArgs a) {
             for (int e = 0; e < E; ++e) mine += sc.weight_of(v[e]);
         });
     } else {
-        // (most pieces hold nothing that is kept; a little below what min_p asks for)
+        // (many pieces hold nothing that is kept; a little below what min_p asks for)
         const float from = fmaxf(mode == kBin ? key_value(last_key) : -INFINITY, sc.top - (float)least * 1.0001f - 1e-6f * fabsf(sc.top));
-        sample_pieces(row, run_lo, run_hi, [&](const uint4& raw, int at) {
+        sample_pieces<1>(row, run_lo, run_hi, [&](const uint4& raw, int at) {
             if (!(Logits<T>::largest(raw) >= from)) return;
             float v[E];
             Logits<T>::widen(raw, v);
 #pragma unroll
-            for (int e = 0; e < E; ++e) mine += weight_in(v[e], at + e);
+            for (int e = 0; e < E; ++e)
+                if (v[e] >= from) mine += weight_in(v[e], at + e);
         });
     }
     mine = warp_add64(mine);
     uint64_t start = __shfl_sync(0xffffffffu, block_upto64(lane == 0 ? mine : 0, sm.sums) - mine, 0);
-    uint64_t total = sm.sums[kSampleWarps], cta_start = 0;
+    uint64_t total = sm.sums[kSampleWarps];
     if (ctas > 1) {
-        if (threadIdx.x == 0) sm.part_total = total;
+        if (threadIdx.x < ctas) cluster.map_shared_rank(&sm, threadIdx.x)->parts[rank] = total;
         cluster.sync();
         total = 0;
         for (int c = 0; c < ctas; ++c) {
-            const uint64_t x = *cluster.map_shared_rank(&sm.part_total, c);
-            if (c < rank) cta_start += x;
-            total += x;
+            if (c < rank) start += sm.parts[c];
+            total += sm.parts[c];
         }
-        start += cta_start;
     }
     const double target = u * (double)total;
-    // Does the choice fall to weights [from, from + n)?  (The last kept token, where rounding or a u of 1 or more leaves none.)
-    auto falls_to = [&](uint64_t from, uint64_t n) {
-        return n > 0 && ((double)(from + n) > target || from + n == total) && ((double)from <= target || from == 0);
-    };
     if (threadIdx.x == 0) sm.found32[0] = kSampleWarps;
     __syncthreads();
-    if (lane == 0 && falls_to(start, mine)) { sm.found32[0] = warp; sm.found64[0] = start; }  // (one warp of the row)
+    if (lane == 0 && falls_to(start, mine, target, total)) { sm.found32[0] = warp; sm.found64[0] = start; }  // (one warp of the row)
     __syncthreads();
-    if (sm.found32[0] < kSampleWarps) {
-        // its run again, a part for each warp of the CTA
-        const int whose = (int)sm.found32[0], lo = min(row.pieces, (rank * kSampleWarps + whose) * per), hi = min(row.pieces, lo + per);
-        const int each = (per / 32 + kSampleWarps - 1) / kSampleWarps * 32, part_lo = min(hi, lo + warp * each), part_hi = min(hi, part_lo + each);
-        mine = 0;
-        sample_run(row, part_lo, part_hi, [&](const float (&v)[E], int at) {
+    if (sm.found32[0] == kSampleWarps) return;
+    // its run again, a part for each warp of the CTA
+    const int whose = (int)sm.found32[0], lo = min(row.pieces, (rank * kSampleWarps + whose) * per), hi = min(row.pieces, lo + per);
+    const int each = (per / 32 + kSampleWarps - 1) / kSampleWarps * 32, part_lo = min(hi, lo + warp * each), part_hi = min(hi, part_lo + each);
+    mine = 0;
+    sample_run(row, part_lo, part_hi, [&](const float (&v)[E], int at) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) mine += weight_in(v[e], at + e);
-        });
-        mine = warp_add64(mine);
-        start = sm.found64[0] + __shfl_sync(0xffffffffu, block_upto64(lane == 0 ? mine : 0, sm.sums) - mine, 0);
-        if (falls_to(start, mine)) {
-            uint64_t sum = start;
-            sample_run(row, part_lo, part_hi, [&](const float (&v)[E], int at) {
-                uint64_t w[E], here = 0;
+        for (int e = 0; e < E; ++e) mine += weight_in(v[e], at + e);
+    });
+    mine = warp_add64(mine);
+    start = sm.found64[0] + __shfl_sync(0xffffffffu, block_upto64(lane == 0 ? mine : 0, sm.sums) - mine, 0);
+    if (!falls_to(start, mine, target, total)) return;
+    uint64_t sum = start;
+    sample_run(row, part_lo, part_hi, [&](const float (&v)[E], int at) {
+        uint64_t w[E], here = 0;
 #pragma unroll
-                for (int e = 0; e < E; ++e) { w[e] = weight_in(v[e], at + e); here += w[e]; }
-                const uint64_t upto = warp_upto64(here);
-                uint64_t n = sum + upto - here;
-                if (falls_to(n, here)) {  // (one lane, once)
-                    bool chosen = false;
+        for (int e = 0; e < E; ++e) { w[e] = weight_in(v[e], at + e); here += w[e]; }
+        const uint64_t upto = warp_upto64(here);
+        uint64_t n = sum + upto - here;
+        if (falls_to(n, here, target, total)) {  // (one lane, once)
+            bool done = false;
 #pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        if (!chosen && falls_to(n, w[e])) {
-                            chosen = true;
-                            a.token[r] = at + e;
-                            if (a.logprob) a.logprob[r] = (float)(-sc.below(v[e]) / T_ - log((double)total / kSampleOne));
-                        }
-                        n += w[e];
-                    }
+            for (int e = 0; e < E; ++e) {
+                if (!done && falls_to(n, w[e], target, total)) {
+                    done = true;
+                    choose(at + e, v[e], total);
                 }
-                sum += __shfl_sync(0xffffffffu, upto, 31);
-            });
+                n += w[e];
+            }
         }
-    }
-    if (ctas > 1) cluster.sync();  // (the others may still read this CTA's sum)
+        sum += __shfl_sync(0xffffffffu, upto, 31);
+    });
 }
 
 }  // namespace msa
