@@ -377,6 +377,33 @@ static msa_status_t launch_weigh(WeighArgs a, const msa_paged_cache_t& c, void* 
     return launch_early(weigh_merge_kernel, dim3(grid), kWtKeys, 0, st, a, TPT, (const float*)part, (const WeighEnds*)ends, grid, status);
 }
 
+template <int VEC>
+static msa_status_t launch_keep(const KeepArgs& a, int64_t heads, int ctas, cudaStream_t st) {
+    int* status = status_word();
+    if (status == nullptr) return cuda_failed();
+    constexpr size_t kMost = sizeof(KeepSmem) + 49152 * sizeof(uint32_t);
+    static_assert(kMost <= 227 * 1024, "a CTA's shared memory");
+    static bool attr_set[64] = {false};  // per device
+    const int dev = current_device();
+    if (!attr_set[dev]) {
+        if (cudaFuncSetAttribute(paged_keep_kernel<VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMost) != cudaSuccess) return cuda_failed();
+        attr_set[dev] = true;
+    }
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = ctas;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(heads * ctas));
+    cfg.blockDim = dim3(kKeepThreads);
+    cfg.dynamicSmemBytes = sizeof(KeepSmem) + a.cached * sizeof(uint32_t);
+    cfg.stream = st;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    StageScope sc(kStageNone, st);
+    return cudaLaunchKernelEx(&cfg, paged_keep_kernel<VEC>, a, status) == cudaSuccess ? MSA_OK : cuda_failed();
+}
+
 // What a call on the cache's places needs of it (no new tokens, maybe no keys).
 static msa_status_t resolve_places(const msa_paged_cache_t* c, PagedView& v) {
     if (c == nullptr) return MSA_ERR_INVALID_ARG;
@@ -653,15 +680,15 @@ msa_status_t msa_paged_keep(const msa_paged_cache_t* cache, const float* weights
     if (cache->batch == 0) return MSA_OK;
     if (keep == nullptr || !aligned_to(keep, 4) || !aligned_to(new_lens, 4)) return MSA_ERR_INVALID_ARG;
     if (cache->n_pages > 0 && (weights == nullptr || !aligned_to(weights, 4))) return MSA_ERR_INVALID_ARG;
-    const KeepArgs a{view, weights, keep, new_lens, budget, sinks, recent};
-    int* status = status_word();
-    if (status == nullptr) return cuda_failed();
-    const unsigned grid = (unsigned)(cache->batch * cache->n_kv_heads);
+    // CTAs of a (sequence, head): as many as are resident at once (one per SM), each with some 8K places or more of the longest.
+    const int64_t heads = (int64_t)cache->batch * cache->n_kv_heads, cap = (int64_t)cache->max_pages * cache->page_size;
+    const int ctas = (int)std::max<int64_t>(1, std::min<int64_t>({kKeepCtas, sm_count() / heads, cap / 8192}));
+    if (heads * ctas > 2147483647LL) return MSA_ERR_UNSUPPORTED;
+    KeepArgs a{view, weights, keep, new_lens, budget, sinks, recent, 0};
+    a.cached = (int)std::min<int64_t>((ceil_div64(cap, ctas) + 8191) / 4096 * 4096, 49152);
+    const bool wide = cache->page_size % 4 == 0 && aligned_to(weights, 16);
     cudaStream_t st = (cudaStream_t)stream;
-    StageScope sc(kStageNone, st);
-    if (cache->page_size % 4 == 0 && aligned_to(weights, 16)) paged_keep_kernel<4><<<grid, kKeepThreads, 0, st>>>(a, status);
-    else paged_keep_kernel<1><<<grid, kKeepThreads, 0, st>>>(a, status);
-    return launch_status();
+    return wide ? launch_keep<4>(a, heads, ctas, st) : launch_keep<1>(a, heads, ctas, st);
 }
 
 msa_status_t msa_paged_compact(const msa_paged_cache_t* cache, const int32_t* keep, int32_t width, float* weights,
