@@ -23,18 +23,18 @@ struct KeepArgs {
     int cached;         // keys of a CTA that fit its shared memory (beyond, weights are read again)
 };
 
-constexpr int kKeepThreads = 1024, kKeepWarps = 32, kKeepBins = 2048, kKeepCtas = 8;
+constexpr int kKeepBins = 2048, kKeepCtas = 8;
 
 struct KeepSmem {
-    uint32_t hist[3][kKeepBins];
+    alignas(16) uint32_t hist[3][kKeepBins];
     uint32_t scan[33], found[2];
     uint2 totals[kKeepCtas];  // above, equal: of every CTA
-    alignas(16) uint32_t key[1];
+    alignas(16) uint32_t key[4];
 };
 
 // VEC: weights that a lane reads at a time, 4 where pages are whole runs of 16 bytes.
-template <int VEC>
-__global__ void __launch_bounds__(kKeepThreads)
+template <int VEC, int kKeepThreads>
+__global__ void __launch_bounds__(kKeepThreads, 1024 / kKeepThreads)
 paged_keep_kernel(const KeepArgs a, int* status) {
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
@@ -43,6 +43,7 @@ paged_keep_kernel(const KeepArgs a, int* status) {
     const int ctas = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
     const int unit = blockIdx.x / ctas, s = unit / a.c.H_kv, head = unit - s * a.c.H_kv;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    constexpr int kKeepWarps = kKeepThreads / 32;
     const int64_t cap = (int64_t)a.c.max_pages * a.c.page_size;
     const int len = a.c.kv_lens[s];
     if ((len < 0 || len > cap) && threadIdx.x == 0 && head == 0 && rank == 0) report_async(status, kAsyncBadIndex, 0x901);
@@ -65,7 +66,7 @@ paged_keep_kernel(const KeepArgs a, int* status) {
     const int from = lo / VEC * VEC, steps = (hi - from + 32 * VEC - 1) / (32 * VEC), per = (steps + ctas * kKeepWarps - 1) / (ctas * kKeepWarps);
     const int w0 = rank * kKeepWarps + warp;
     const int run_lo = from + min(steps, w0 * per) * 32 * VEC, run_hi = from + min(steps, (w0 + 1) * per) * 32 * VEC;
-    // keys of places at .. at + VEC - 1
+    // keys of places at .. at + VEC - 1: 0 outside the middle, where nothing else has it (a NaN has 1, -infinity more)
     auto keys_of = [&](int at, uint32_t (&key)[VEC]) {
         float v[VEC];
 #pragma unroll
@@ -86,7 +87,7 @@ paged_keep_kernel(const KeepArgs a, int* status) {
             }
         }
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) key[e] = order_key(v[e]);
+        for (int e = 0; e < VEC; ++e) key[e] = at + e >= lo && at + e < hi ? max(order_key(v[e]), 1u) : 0u;
     };
     // ... from this warp's part of shared memory as far as that goes
     const int mine_cached = min(run_hi - run_lo, a.cached / kKeepWarps / (32 * VEC) * (32 * VEC));
@@ -110,11 +111,10 @@ paged_keep_kernel(const KeepArgs a, int* status) {
     for (int round = 0; round < 3; ++round) {
         const int shift = round == 0 ? 21 : (round == 1 ? 10 : 0), bits = round == 2 ? 10 : 11;
         uint32_t* hist = sm.hist[round];
-        auto count = [&](int at, const uint32_t (&key)[VEC]) {
+        auto count = [&](const uint32_t (&key)[VEC]) {  // (what is outside is counted below everything: it changes nothing)
 #pragma unroll
             for (int e = 0; e < VEC; ++e)
-                if (at + e >= lo && at + e < hi && (round == 0 || key[e] >> (shift + bits) == prefix))
-                    atomicAdd(&hist[(key[e] >> shift) & ((1u << bits) - 1)], 1u);
+                if (round == 0 || key[e] >> (shift + bits) == prefix) atomicAdd(&hist[(key[e] >> shift) & ((1u << bits) - 1)], 1u);
         };
         if (round == 0) {
             constexpr int U = 4;  // pieces in flight
@@ -131,32 +131,39 @@ paged_keep_kernel(const KeepArgs a, int* status) {
                         if constexpr (VEC == 4) *reinterpret_cast<uint4*>(cache + (at - run_lo)) = make_uint4(key[u][0], key[u][1], key[u][2], key[u][3]);
                         else cache[at - run_lo] = key[u][0];
                     }
-                    count(at, key[u]);
+                    count(key[u]);
                 }
             }
         } else {
             for (int at = run_lo + lane * VEC; at < run_hi; at += 32 * VEC) {
                 uint32_t key[VEC];
                 keys_at(at, key);
-                count(at, key);
+                count(key);
             }
         }
         if (ctas > 1) cluster.sync();
         else __syncthreads();
-        // digits from the top: two a thread
-        const int d = kKeepBins - 1 - 2 * (int)threadIdx.x;
-        uint32_t c0 = 0, c1 = 0;
-        for (int c = 0; c < ctas; ++c) {
-            const uint2 x = *reinterpret_cast<const uint2*>(cluster.map_shared_rank(hist + d - 1, c));
-            c0 += x.y;
-            c1 += x.x;
+        // digits from the top, a few a thread
+        constexpr int PER = kKeepBins / kKeepThreads;
+        static_assert(PER == 2 || PER == 4, "read as one");
+        const int d = kKeepBins - PER * (1 + (int)threadIdx.x);
+        uint32_t c[PER] = {}, mine = 0, all;
+        for (int r = 0; r < ctas; ++r) {
+            if constexpr (PER == 2) {
+                const uint2 x = *reinterpret_cast<const uint2*>(cluster.map_shared_rank(hist + d, r));
+                c[0] += x.x; c[1] += x.y;
+            } else {
+                const uint4 x = *reinterpret_cast<const uint4*>(cluster.map_shared_rank(hist + d, r));
+                c[0] += x.x; c[1] += x.y; c[2] += x.z; c[3] += x.w;
+            }
         }
-        uint32_t all;
-        const uint32_t above = block_scan(c0 + c1, sm.scan, &all);
-        if (above < want && above + c0 + c1 >= want) {  // (one thread)
-            const bool first = above + c0 >= want;
-            sm.found[0] = first ? d : d - 1;
-            sm.found[1] = want - above - (first ? 0u : c0);
+#pragma unroll
+        for (int j = 0; j < PER; ++j) mine += c[j];
+        uint32_t above = block_scan(mine, sm.scan, &all);
+#pragma unroll
+        for (int j = PER - 1; j >= 0; --j) {
+            if (above < want && above + c[j] >= want) { sm.found[0] = d + j; sm.found[1] = want - above; }  // (one thread)
+            above += c[j];
         }
         __syncthreads();
         prefix = round == 0 ? sm.found[0] : (prefix << bits) | sm.found[0];
@@ -169,9 +176,8 @@ paged_keep_kernel(const KeepArgs a, int* status) {
         keys_at(at, key);
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-            const bool in = at + e >= lo && at + e < hi;
-            mine_above += in && key[e] > prefix;
-            mine_equal += in && key[e] == prefix;
+            mine_above += key[e] > prefix;
+            mine_equal += key[e] == prefix;
         }
     }
     mine_above = __reduce_add_sync(0xffffffffu, mine_above);
@@ -196,11 +202,24 @@ paged_keep_kernel(const KeepArgs a, int* status) {
         uint32_t eq = 0, ab = 0;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-            const bool in = at + e >= lo && at + e < hi;
-            eq += in && key[e] == prefix;
-            ab += in && key[e] > prefix;
+            eq += key[e] == prefix;
+            ab += key[e] > prefix;
         }
-        if (!__any_sync(0xffffffffu, (eq | ab) != 0)) continue;
+        if (!__any_sync(0xffffffffu, eq != 0)) {  // (nearly always: who is kept is seen by all)
+            uint32_t before = 0, own = 0, sum = 0;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const uint32_t who = __ballot_sync(0xffffffffu, key[e] > prefix);
+                before += __popc(who & ((1u << lane) - 1));
+                sum += __popc(who);
+            }
+            const uint32_t to = sinks + rank_above + min(equal, want) + before;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e)
+                if (key[e] > prefix) out[to + own++] = at + e;
+            rank_above += sum;
+            continue;
+        }
         uint32_t both = eq << 16 | ab, upto = both;  // (at most 128 each)
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -210,7 +229,7 @@ paged_keep_kernel(const KeepArgs a, int* status) {
         uint32_t order = equal + (upto - both >> 16), above = rank_above + (upto - both & 0xFFFFu);
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-            const bool in = at + e >= lo && at + e < hi, same = in && key[e] == prefix, more = in && key[e] > prefix;
+            const bool same = key[e] == prefix, more = key[e] > prefix;
             if (more || (same && order < want)) out[sinks + above + min(order, want)] = at + e;  // (places before it that stay)
             order += same;
             above += more;
@@ -234,111 +253,92 @@ struct CompactArgs {
     int width, row_bytes, slice_bytes;
 };
 
-constexpr int kCompactThreads = 256, kCompactLoads = 4;
+constexpr int kCompactLoads = 4;
 
-// Row of a pool that a place stands at, -1: nowhere.
-__device__ __forceinline__ int64_t compact_row(const PagedView& c, const int32_t* table, int place, int64_t len, int* status) {
-    if (place < 0) return -1;
-    if (place >= len) {
-        report_async(status, kAsyncBadIndex, 0xA01);
-        return -1;
-    }
-    const int page = table[(uint32_t)place / (uint32_t)c.page_size];
-    if (page < 0 || page >= c.n_pages) {
-        report_async(status, kAsyncBadIndex, 0xA02);
-        return -1;
-    }
-    return (int64_t)page * c.page_size + (uint32_t)place % (uint32_t)c.page_size;
-}
-
-// V: what a lane moves at a time.  blockIdx.y: slice of the keys, of the values, then the weights.
-// A run of rows is looked up (a thread a row, to shared memory) while the one before it is read, and read while the one before
-// that is written: its sources lie behind everything that is written then.
-template <class V>
-__global__ void __launch_bounds__(kCompactThreads)
+// V: what a lane moves at a time.  blockIdx.y: slice of the keys, of the values; the first slice of the keys moves the weights, too.
+// A run of rows (a thread looks up one) is read while the run before it is written: its sources lie behind everything that is
+// written then.  The look-ups are spread over the runs before, one load of the chain place -> pages -> rows in each.
+// kCompactThreads: 256, four CTAs per SM; 1024 where there are few.
+template <class V, int kCompactThreads>
+__global__ void __launch_bounds__(kCompactThreads, 1024 / kCompactThreads)
 paged_compact_kernel(const CompactArgs a, int slices, int* status) {
-    __shared__ int64_t s_from[3][kCompactThreads], s_to[3][kCompactThreads];
-    const int s = blockIdx.x / a.c.H_kv, head = blockIdx.x - s * a.c.H_kv;
+    __shared__ int64_t s_from[3][kCompactThreads], s_to[3][kCompactThreads];  // rows of the pools; to = -1: it does not move
+    const int s = blockIdx.x / a.c.H_kv, head = blockIdx.x - s * a.c.H_kv, tid = threadIdx.x;
     const int32_t* keep = a.keep + (int64_t)blockIdx.x * a.width;
     const int32_t* table = a.c.table + (int64_t)s * a.c.max_pages;
     const int64_t len = min((int64_t)max(a.c.kv_lens[s], 0), (int64_t)a.c.max_pages * a.c.page_size);
-    const int part = blockIdx.y;
-    // source and destination of the i-th token, -1: it does not move
-    auto look_up = [&](int i, int64_t& from, int64_t& to) {
-        const int place = i < a.width ? keep[i] : -1;
-        if (place >= 0 && place < i) report_async(status, kAsyncBadIndex, 0xA03);  // (not ascending from 0)
-        to = -1;
-        if (place <= i) return;
-        from = compact_row(a.c, table, place, len, status);
-        to = from >= 0 ? compact_row(a.c, table, i, len, status) : -1;
-    };
-    if (part == 2 * slices) {
-        for (int first = 0; first < a.width; first += kCompactThreads * kCompactLoads) {
-            float v[kCompactLoads];
-            int64_t to[kCompactLoads];
-#pragma unroll
-            for (int j = 0; j < kCompactLoads; ++j) {
-                int64_t row;
-                look_up(first + j * kCompactThreads + (int)threadIdx.x, row, to[j]);
-                if (to[j] >= 0) {
-                    const int64_t off = row % a.c.page_size, off2 = to[j] % a.c.page_size;
-                    v[j] = a.w[(row - off) * a.c.H_kv + (int64_t)head * a.c.page_size + off];
-                    to[j] = (to[j] - off2) * a.c.H_kv + (int64_t)head * a.c.page_size + off2;
-                }
-            }
-            __syncthreads();
-#pragma unroll
-            for (int j = 0; j < kCompactLoads; ++j)
-                if (to[j] >= 0) a.w[to[j]] = v[j];
-            __syncthreads();
-        }
-        return;
-    }
-    uint8_t* pool = a.pool[part >= slices];
-    if (pool == nullptr) return;
-    const int slice = part >= slices ? part - slices : part;
+    const bool values = (int)blockIdx.y >= slices, weights = blockIdx.y == 0 && a.w != nullptr;
+    uint8_t* pool = a.pool[values];
+    const int slice = values ? blockIdx.y - slices : blockIdx.y;
     const int lanes = a.slice_bytes / (int)sizeof(V), rows = kCompactThreads / lanes;  // rows of a load of the CTA
-    const int in_row = threadIdx.x % lanes, row0 = threadIdx.x / lanes;
+    const int in_row = tid % lanes, row0 = tid / lanes;
     const int64_t column = (int64_t)head * a.row_bytes + slice * a.slice_bytes + in_row * (int)sizeof(V);
     const int64_t pitch = (int64_t)a.c.H_kv * a.row_bytes;
     const int run = min(rows * kCompactLoads, kCompactThreads), runs = (a.width + run - 1) / run;
-    auto prepare = [&](int r) {  // run r's rows
-        if ((int)threadIdx.x >= run) return;
-        int64_t from = 0, to = -1;
-        if (r < runs) look_up(r * run + (int)threadIdx.x, from, to);
-        s_from[r % 3][threadIdx.x] = from;
-        s_to[r % 3][threadIdx.x] = to;
+    const uint32_t size = a.c.page_size;
+
+    // the chain of a thread's row of a run: its place; the pages of where it is and where it goes; the rows
+    int place_next = -1, place = -1, page_from = -1, page_to = -1;
+    auto load_place = [&](int r) {
+        const int i = r * run + tid;
+        place_next = tid < run && i < a.width ? keep[i] : -1;
     };
-    auto read = [&](int r, V (&v)[kCompactLoads]) {
+    auto load_pages = [&](int r) {
+        const int i = r * run + tid;
+        place = place_next;
+        page_from = page_to = -2;
+        if (place >= 0 && place < i) report_async(status, kAsyncBadIndex, 0xA03);  // (not ascending from 0)
+        if (place >= len) report_async(status, kAsyncBadIndex, 0xA01);
+        if (place > i && place < len) {
+            page_from = table[(uint32_t)place / size];
+            page_to = table[(uint32_t)i / size];
+        }
+    };
+    auto set_rows = [&](int r) {
+        const int i = r * run + tid;
+        const bool moves = page_from != -2, good = page_from >= 0 && page_from < a.c.n_pages && page_to >= 0 && page_to < a.c.n_pages;
+        if (moves && !good) report_async(status, kAsyncBadIndex, 0xA02);
+        s_from[r % 3][tid] = moves && good ? (int64_t)page_from * size + (uint32_t)place % size : 0;
+        s_to[r % 3][tid] = moves && good ? (int64_t)page_to * size + (uint32_t)i % size : -1;
+    };
+    auto weight_at = [&](int64_t row) { return (row / size * a.c.H_kv + head) * size + row % size; };
+    auto read = [&](int r, V (&v)[kCompactLoads], float& w) {
+        const int64_t* from = s_from[r % 3];
+        const int64_t* to = s_to[r % 3];
 #pragma unroll
         for (int j = 0; j < kCompactLoads; ++j) {
             const int i = j * rows + row0;
-            if (row0 < rows && i < run && s_to[r % 3][i] >= 0) v[j] = *reinterpret_cast<const V*>(pool + s_from[r % 3][i] * pitch + column);
+            if (row0 < rows && i < run && to[i] >= 0 && pool != nullptr) v[j] = *reinterpret_cast<const V*>(pool + from[i] * pitch + column);
         }
+        if (weights && tid < run && to[tid] >= 0) w = a.w[weight_at(from[tid])];
     };
-    auto write = [&](int r, const V (&v)[kCompactLoads]) {
+    auto write = [&](int r, const V (&v)[kCompactLoads], float w) {
+        const int64_t* to = s_to[r % 3];
 #pragma unroll
         for (int j = 0; j < kCompactLoads; ++j) {
             const int i = j * rows + row0;
-            if (row0 < rows && i < run && s_to[r % 3][i] >= 0) *reinterpret_cast<V*>(pool + s_to[r % 3][i] * pitch + column) = v[j];
+            if (row0 < rows && i < run && to[i] >= 0 && pool != nullptr) *reinterpret_cast<V*>(pool + to[i] * pitch + column) = v[j];
         }
+        if (weights && tid < run && to[tid] >= 0) a.w[weight_at(to[tid])] = w;
     };
     V v[2][kCompactLoads];
-    prepare(0);
-    prepare(1);
+    float w[2];
+    load_place(0); load_pages(0); load_place(1); set_rows(0);
+    load_pages(1); load_place(2); set_rows(1);
+    load_pages(2); load_place(3);
     __syncthreads();
-    read(0, v[0]);
-    for (int r = 0; r < runs; r += 2) {  // (two runs' registers, taken in turn)
-        read(r + 1, v[1]);       // (nothing beyond the last run: its rows say so)
-        prepare(r + 2);
-        __syncthreads();         // all of run r has been read
-        write(r, v[0]);
+    read(0, v[0], w[0]);
+    for (int r = 0; r < runs; r += 2) {  // (two runs' registers, taken in turn; rows beyond the last run do not move)
+        read(r + 1, v[1], w[1]);
+        set_rows(r + 2); load_pages(r + 3); load_place(r + 4);
+        __syncthreads();  // all of run r has been read
+        write(r, v[0], w[0]);
         if (r + 1 >= runs) break;
-        __syncthreads();         // the rows of run r + 2 are there; those of run r are not needed any more
-        read(r + 2, v[0]);
-        prepare(r + 3);
+        __syncthreads();  // its rows are not needed any more
+        read(r + 2, v[0], w[0]);
+        set_rows(r + 3); load_pages(r + 4); load_place(r + 5);
         __syncthreads();
-        write(r + 1, v[1]);
+        write(r + 1, v[1], w[1]);
         __syncthreads();
     }
 }

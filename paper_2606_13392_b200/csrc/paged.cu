@@ -377,16 +377,21 @@ static msa_status_t launch_weigh(WeighArgs a, const msa_paged_cache_t& c, void* 
     return launch_early(weigh_merge_kernel, dim3(grid), kWtKeys, 0, st, a, TPT, (const float*)part, (const WeighEnds*)ends, grid, status);
 }
 
-template <int VEC>
-static msa_status_t launch_keep(const KeepArgs& a, int64_t heads, int ctas, cudaStream_t st) {
+template <int VEC, int THREADS>
+static msa_status_t launch_keep(KeepArgs a, int64_t heads, int ctas, cudaStream_t st) {
     int* status = status_word();
     if (status == nullptr) return cuda_failed();
-    constexpr size_t kMost = sizeof(KeepSmem) + 49152 * sizeof(uint32_t);
-    static_assert(kMost <= 227 * 1024, "a CTA's shared memory");
+    // keys of a CTA in shared memory: all, as far as one CTA per SM has room, or two smaller ones
+    constexpr int kMost = THREADS == 1024 ? 49152 : 20480;
+    static_assert((sizeof(KeepSmem) + kMost * sizeof(uint32_t)) * (1024 / THREADS) <= 226 * 1024, "an SM's shared memory");
+    const int64_t cap = (int64_t)a.c.max_pages * a.c.page_size;
+    a.cached = (int)std::min<int64_t>((ceil_div64(cap, ctas) + 8191) / 4096 * 4096, kMost);
     static bool attr_set[64] = {false};  // per device
     const int dev = current_device();
     if (!attr_set[dev]) {
-        if (cudaFuncSetAttribute(paged_keep_kernel<VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMost) != cudaSuccess) return cuda_failed();
+        if (cudaFuncSetAttribute(paged_keep_kernel<VEC, THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                 (int)(sizeof(KeepSmem) + kMost * sizeof(uint32_t))) != cudaSuccess)
+            return cuda_failed();
         attr_set[dev] = true;
     }
     cudaLaunchAttribute attr;
@@ -395,13 +400,13 @@ static msa_status_t launch_keep(const KeepArgs& a, int64_t heads, int ctas, cuda
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(heads * ctas));
-    cfg.blockDim = dim3(kKeepThreads);
+    cfg.blockDim = dim3(THREADS);
     cfg.dynamicSmemBytes = sizeof(KeepSmem) + a.cached * sizeof(uint32_t);
     cfg.stream = st;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     StageScope sc(kStageNone, st);
-    return cudaLaunchKernelEx(&cfg, paged_keep_kernel<VEC>, a, status) == cudaSuccess ? MSA_OK : cuda_failed();
+    return cudaLaunchKernelEx(&cfg, paged_keep_kernel<VEC, THREADS>, a, status) == cudaSuccess ? MSA_OK : cuda_failed();
 }
 
 // What a call on the cache's places needs of it (no new tokens, maybe no keys).
@@ -680,15 +685,15 @@ msa_status_t msa_paged_keep(const msa_paged_cache_t* cache, const float* weights
     if (cache->batch == 0) return MSA_OK;
     if (keep == nullptr || !aligned_to(keep, 4) || !aligned_to(new_lens, 4)) return MSA_ERR_INVALID_ARG;
     if (cache->n_pages > 0 && (weights == nullptr || !aligned_to(weights, 4))) return MSA_ERR_INVALID_ARG;
-    // CTAs of a (sequence, head): as many as are resident at once (one per SM), each with some 8K places or more of the longest.
+    // CTAs of a (sequence, head): as many as are resident at once, each with some 8K places or more of the longest.  Many
+    // (sequence, head): CTAs of 512 threads, two per SM.
     const int64_t heads = (int64_t)cache->batch * cache->n_kv_heads, cap = (int64_t)cache->max_pages * cache->page_size;
     const int ctas = (int)std::max<int64_t>(1, std::min<int64_t>({kKeepCtas, sm_count() / heads, cap / 8192}));
-    if (heads * ctas > 2147483647LL) return MSA_ERR_UNSUPPORTED;
-    KeepArgs a{view, weights, keep, new_lens, budget, sinks, recent, 0};
-    a.cached = (int)std::min<int64_t>((ceil_div64(cap, ctas) + 8191) / 4096 * 4096, 49152);
-    const bool wide = cache->page_size % 4 == 0 && aligned_to(weights, 16);
+    const KeepArgs a{view, weights, keep, new_lens, budget, sinks, recent, 0};
+    const bool wide = cache->page_size % 4 == 0 && aligned_to(weights, 16), many = heads > sm_count();
     cudaStream_t st = (cudaStream_t)stream;
-    return wide ? launch_keep<4>(a, heads, ctas, st) : launch_keep<1>(a, heads, ctas, st);
+    if (many) return wide ? launch_keep<4, 512>(a, heads, ctas, st) : launch_keep<1, 512>(a, heads, ctas, st);
+    return wide ? launch_keep<4, 1024>(a, heads, ctas, st) : launch_keep<1, 1024>(a, heads, ctas, st);
 }
 
 msa_status_t msa_paged_compact(const msa_paged_cache_t* cache, const int32_t* keep, int32_t width, float* weights,
@@ -702,17 +707,21 @@ msa_status_t msa_paged_compact(const msa_paged_cache_t* cache, const int32_t* ke
     if (cache->n_pages > 0 && (!cache->k || !aligned_to(cache->k, 16) || !aligned_to(cache->v, 16))) return MSA_ERR_INVALID_ARG;
     const int row = cache->head_dim * (cache->fp8 ? 1 : 2);
     CompactArgs a{view, {(uint8_t*)cache->k, (uint8_t*)cache->v}, weights, keep, width, row, row};
-    // Slices of a row (whole sectors) until the machine has four CTAs per SM.
+    // Slices of a row (whole sectors) until the machine has three CTAs per SM, of four that are resident.
     const int64_t heads = (int64_t)cache->batch * cache->n_kv_heads;
-    while (a.slice_bytes % 64 == 0 && heads * 2 * (row / a.slice_bytes) < 4LL * sm_count()) a.slice_bytes /= 2;
+    while (a.slice_bytes % 64 == 0 && heads * 2 * (row / a.slice_bytes) < 3LL * sm_count()) a.slice_bytes /= 2;
     const int slices = row / a.slice_bytes;
     int* status = status_word();
     if (status == nullptr) return cuda_failed();
-    const dim3 grid((unsigned)heads, 2 * slices + (weights != nullptr ? 1 : 0));
+    const dim3 grid((unsigned)heads, (cache->v != nullptr ? 2 : 1) * slices);
     cudaStream_t st = (cudaStream_t)stream;
     StageScope sc(kStageNone, st);
-    if (a.slice_bytes % 16 == 0) paged_compact_kernel<uint4><<<grid, kCompactThreads, 0, st>>>(a, slices, status);
-    else paged_compact_kernel<uint2><<<grid, kCompactThreads, 0, st>>>(a, slices, status);
+    // (1024 threads look up and move as many rows at a time: 8 heads of one sequence, 4096 tokens, 31 us with 256, COMPACT1 with 1024)
+    const bool wide = a.slice_bytes % 16 == 0, few = (int64_t)grid.x * grid.y <= sm_count();
+    if (wide && few) paged_compact_kernel<uint4, 1024><<<grid, 1024, 0, st>>>(a, slices, status);
+    else if (wide) paged_compact_kernel<uint4, 256><<<grid, 256, 0, st>>>(a, slices, status);
+    else if (few) paged_compact_kernel<uint2, 1024><<<grid, 1024, 0, st>>>(a, slices, status);
+    else paged_compact_kernel<uint2, 256><<<grid, 256, 0, st>>>(a, slices, status);
     return launch_status();
 }
 
