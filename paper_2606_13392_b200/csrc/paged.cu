@@ -325,6 +325,23 @@ static PagedFew weigh_few(const WeighArgs& a, const msa_paged_cache_t& c) {
     return PagedFew{0, false};
 }
 
+template <int NT, bool F8>
+static msa_status_t launch_weigh_few(const WeighArgs& a, int grid, cudaStream_t st) {
+    constexpr size_t smem = weigh_few_smem(F8);
+    static_assert(smem <= 113 * 1024, "two CTAs per SM");
+    if constexpr (smem > 0) {
+        static bool attr_set[64] = {false};  // per device
+        const int dev = current_device();
+        if (!attr_set[dev]) {
+            if (cudaFuncSetAttribute(weigh_few_kernel<NT, F8>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return cuda_failed();
+            attr_set[dev] = true;
+        }
+    }
+    StageScope sc(kStageNone, st);
+    weigh_few_kernel<NT, F8><<<grid, kWeighWarps * 32, smem, st>>>(a, 1.0 / grid, status_word());
+    return launch_status();
+}
+
 template <bool F8>
 static msa_status_t launch_weigh(WeighArgs a, const msa_paged_cache_t& c, void* workspace, cudaStream_t st) {
     int* status = status_word();
@@ -343,13 +360,7 @@ static msa_status_t launch_weigh(WeighArgs a, const msa_paged_cache_t& c, void* 
         // rows of a sequence if all have as many: eight, sixteen or more of them stay in registers
         const int64_t rows = std::min<int64_t>(ceil_div64(a.n_tokens, c.batch), few.tokens) * a.G;
         const int grid = (rows <= 16 ? 2 : 1) * sm_count();
-        {
-            StageScope sc(kStageNone, st);
-            if (rows <= 8) weigh_few_kernel<1, F8><<<grid, kWeighWarps * 32, 0, st>>>(f, 1.0 / grid, status);
-            else if (rows <= 16) weigh_few_kernel<2, F8><<<grid, kWeighWarps * 32, 0, st>>>(f, 1.0 / grid, status);
-            else weigh_few_kernel<4, F8><<<grid, kWeighWarps * 32, 0, st>>>(f, 1.0 / grid, status);
-        }
-        const msa_status_t s = launch_status();
+        const msa_status_t s = rows <= 8 ? launch_weigh_few<1, F8>(f, grid, st) : (rows <= 16 ? launch_weigh_few<2, F8>(f, grid, st) : launch_weigh_few<4, F8>(f, grid, st));
         if (few.alone || s != MSA_OK) return s;
     }
     const int TPT = 128 / a.G, grid = sm_count();

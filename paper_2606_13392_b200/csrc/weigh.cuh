@@ -120,6 +120,16 @@ __device__ __forceinline__ uint32_t weigh_f16x2(float a, float b) {
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
+// fp8 keys are half the bytes a tile: five tiles of a warp are on their way through shared memory instead, each lane's 16-byte
+// pieces to places of its own, so that nothing is exchanged (32 sequences of 4K - 32K tokens, 64/4 heads: WEIGH8).
+constexpr int kWeighStages = 5;
+struct WeighSlot {
+    uint4 k[4][32];
+    int64_t w[32];
+    float old[32];
+};
+constexpr size_t weigh_few_smem(bool f8) { return f8 ? sizeof(WeighSlot) * kWeighStages * kWeighWarps : 0; }
+
 template <int NT, bool F8>
 __global__ void __launch_bounds__(kWeighWarps * 32, NT <= 2 ? 2 : 1)
 weigh_few_kernel(const WeighArgs a, double inv_grid, int* status) {
@@ -288,18 +298,65 @@ weigh_few_kernel(const WeighArgs a, double inv_grid, int* status) {
         };
 
         Place p = places_of(t);
-        Tile x, y;
-        fetch(p, t, x);
-        p = places_of(t + kWeighWarps);
-        if (rows <= 8 * NT) load_q(0);
-        for (; t < hi; t += 2 * kWeighWarps) {  // two tiles in registers, taken in turn
-            fetch(p, t + kWeighWarps, y);
-            p = places_of(t + 2 * kWeighWarps);
-            finish(t, x);
-            if (t + kWeighWarps >= hi) break;
-            fetch(p, t + 2 * kWeighWarps, x);
-            p = places_of(t + 3 * kWeighWarps);
-            finish(t + kWeighWarps, y);
+        if constexpr (F8) {
+            extern __shared__ __align__(16) uint8_t weigh_few_raw[];
+            WeighSlot* slots = reinterpret_cast<WeighSlot*>(weigh_few_raw) + warp * kWeighStages;
+            auto send = [&](int tile, int stage) {
+                WeighSlot& x = slots[stage];
+                const int r0 = __shfl_sync(0xffffffffu, p.row, g), r1 = __shfl_sync(0xffffffffu, p.row, 8 + g);
+                const int off = __shfl_sync(0xffffffffu, p.off, (t4 & 1) * 8 + g);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int row = i == 0 ? r0 : r1;
+                    const uint4* from = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(a.k) + ((int64_t)max(row, 0) * a.c.H_kv + head) * 128) + t4;
+#pragma unroll
+                    for (int j = 0; j < LD; ++j)
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(&x.k[i * LD + j][lane])), "l"(from + 4 * j), "r"(row >= 0 ? 16 : 0)
+                                     : "memory");
+                }
+                const int key = tile * kWeighKeys + (t4 & 1) * 8 + g, mine = t4 == 0 ? r0 : r1;
+                const int64_t w = t4 < 2 && mine >= 0 ? (int64_t)(mine - off) * a.c.H_kv + (int64_t)head * a.c.page_size + off : -1;
+                const bool was = w >= 0 && a.decay != 0.f && key < sq.base;
+                x.w[lane] = w;
+                asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(&x.old[lane])), "l"(a.w + (was ? w : 0)), "r"(was ? 4 : 0) : "memory");
+                asm volatile("cp.async.commit_group;" ::: "memory");
+            };
+#pragma unroll
+            for (int i = 0; i < kWeighStages - 1; ++i) {  // (tiles beyond the end: nowhere, nothing)
+                send(t + i * kWeighWarps, i);
+                p = places_of(t + (i + 1) * kWeighWarps);
+            }
+            if (rows <= 8 * NT) load_q(0);
+            for (int stage = 0; t < hi; t += kWeighWarps) {
+                const int ahead = stage == 0 ? kWeighStages - 1 : stage - 1;
+                send(t + (kWeighStages - 1) * kWeighWarps, ahead);
+                p = places_of(t + kWeighStages * kWeighWarps);
+                asm volatile("cp.async.wait_group %0;" ::"n"(kWeighStages - 1) : "memory");
+                Tile x;
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < LD; ++j) x.k[i][j] = slots[stage].k[i * LD + j][lane];
+                x.w = slots[stage].w[lane];
+                x.old = a.decay * slots[stage].old[lane];
+                finish(t, x);
+                stage = stage + 1 == kWeighStages ? 0 : stage + 1;
+            }
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+        } else {
+            Tile x, y;
+            fetch(p, t, x);
+            p = places_of(t + kWeighWarps);
+            if (rows <= 8 * NT) load_q(0);
+            for (; t < hi; t += 2 * kWeighWarps) {  // two tiles in registers, taken in turn
+                fetch(p, t + kWeighWarps, y);
+                p = places_of(t + 2 * kWeighWarps);
+                finish(t, x);
+                if (t + kWeighWarps >= hi) break;
+                fetch(p, t + 2 * kWeighWarps, x);
+                p = places_of(t + 3 * kWeighWarps);
+                finish(t + kWeighWarps, y);
+            }
         }
     }
 }
