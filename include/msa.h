@@ -541,7 +541,7 @@ msa_status_t msa_paged_attn_workspace_bytes(const msa_paged_cache_t* cache, int3
  * msa_paged_append, msa_paged_attn, msa_paged_weights and, once the sequences are over their budget, msa_paged_keep and
  * msa_paged_compact; from then on kv_lens starts from the new lengths.  Dropped tokens leave no gap, so a token's place is
  * no longer its position: keys that are rotated take msa_qk_norm_rope with the true positions, then msa_paged_append
- * without rotation.
+ * without rotation.  These calls take sequences of up to 2^31 - 65536 tokens; a longer length is reported as a bad index.
  *
  * weights is a pool like the keys' and values', fp32 [n_pages, n_kv_heads, page_size]: the weight of token t of sequence s and
  * KV head h is element t mod page_size of row h of the token's page.
@@ -566,7 +566,7 @@ msa_status_t msa_paged_weights_workspace_bytes(const msa_paged_cache_t* cache, i
  * The tokens that stay: of a sequence of L = kv_lens[s] tokens n = min(L, budget), for each KV head by itself - the last
  * r = min(recent, n), the first min(sinks, n - r), and of those between the ones with the largest weights (equal weights: the
  * lower place; NaN counts as lowest).  keep [batch, n_kv_heads, budget] int32 gets their places in ascending order, -1
- * behind; new_lens [batch] int32 (may be NULL, may not be kv_lens) gets n.  Of `cache` it uses page_table, kv_lens and the sizes only.
+ * behind; new_lens [batch] int32 (may be NULL, not kv_lens) gets n.  budget is at most 2^30.  Of `cache` it uses page_table, kv_lens and the sizes only.
  */
 msa_status_t msa_paged_keep(const msa_paged_cache_t* cache, const float* weights, int32_t budget, int32_t sinks, int32_t recent,
                             int32_t* keep, int32_t* new_lens, msa_stream_t stream);
@@ -574,7 +574,7 @@ msa_status_t msa_paged_keep(const msa_paged_cache_t* cache, const float* weights
 /*
  * Moves token keep[s, h, i] of KV head h to place i of its sequence, for every i < width: its key, its value (cache->v may be
  * NULL) and its weight (weights may be NULL).  keep [batch, n_kv_heads, width] int32 as msa_paged_keep writes it: ascending
- * places below kv_lens[s] (still the old lengths), -1 = none.  In place: what stood at places that nothing moves to
+ * places below kv_lens[s] (still the old lengths), -1 = none; width is at most 2^30.  In place: what stood at places that nothing moves to
  * stays.  Sequences must not share pages.  A place that is not below the length, on a bad page or below its own i is
  * reported as a bad index and not moved; of a list that is not ascending the result is otherwise unspecified.
  */

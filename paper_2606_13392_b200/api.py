@@ -245,6 +245,9 @@ def paged_attn(cache: PagedCache, q: torch.Tensor, softmax_scale: float = 0.0, o
     return out, lse
 
 
+_WEIGHTS_BYTES = {}  # workspace of paged_weights by device, query heads and shape of the pool
+
+
 def paged_weights(cache: PagedCache, q: torch.Tensor, lse: torch.Tensor, weights: torch.Tensor, decay: float = 1.0,
                   softmax_scale: float = 0.0, workspace: Optional[torch.Tensor] = None, max_new: int = 0) -> torch.Tensor:
     """Adds the attention weight that cached tokens receive from the new tokens to `weights` (fp32 [pages, KV heads, page
@@ -252,7 +255,13 @@ def paged_weights(cache: PagedCache, q: torch.Tensor, lse: torch.Tensor, weights
     returned by paged_attn - or some of its rows, with a cu_q that counts those (the last tokens of prompts as observers)."""
     _no_graph("paged_weights", "it has no backward pass; call it under torch.no_grad", q, lse, weights)
     if workspace is None:
-        workspace = _workspace(q, B.msa_paged_weights_workspace_bytes, cache.k, q.shape[1])
+        what = (q.get_device(), q.shape[1], cache.k.shape)
+        size = _WEIGHTS_BYTES.get(what)
+        if size is None:
+            workspace = _workspace(q, B.msa_paged_weights_workspace_bytes, cache.k, q.shape[1])
+            _WEIGHTS_BYTES[what] = workspace.numel()
+        else:
+            workspace = q.new_empty(size, dtype=torch.uint8)
     B.msa_paged_weights(cache.k, cache.page_table, cache.kv_lens, cache.cu_q, q, lse, softmax_scale, decay, weights, workspace,
                         max_new=max_new)
     return weights

@@ -656,14 +656,14 @@ def msa_paged_attn(k_pool, v_pool, page_table, kv_lens, cu_q, q, softmax_scale, 
     return out
 
 
-def _made(t: Optional[torch.Tensor], shape, dtype, what: str, index: int, stream) -> torch.Tensor:
-    """A dense output of a given shape and type, made here (on the stream that writes it) if there is none."""
+def _made(t: Optional[torch.Tensor], near: torch.Tensor, shape, dtype, what: str, index: int, stream) -> torch.Tensor:
+    """A dense output of a given shape and type, made here (beside `near`, on the stream that writes it) if there is none."""
     if t is None:
         if stream is None:
-            return torch.empty(shape, dtype=dtype, device="cuda:%d" % index)
+            return near.new_empty(shape, dtype=dtype)
         current = torch.cuda.current_stream(index)
         with torch.cuda.stream(stream):
-            t = torch.empty(shape, dtype=dtype, device="cuda:%d" % index)
+            t = near.new_empty(shape, dtype=dtype)
         t.record_stream(current)
         return t
     if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.get_device() != index:
@@ -703,8 +703,8 @@ def msa_paged_keep(k_pool, page_table, kv_lens, cu_q, weights, budget, sinks, re
     """-> (keep int32 [batch, KV heads, budget], new_lens int32 [batch]); those that are not given are made."""
     index, cache = _paged(k_pool, None, page_table, kv_lens, cu_q)
     at = _weight_pool(weights, cache, index)
-    keep = _made(keep, (cache.batch, cache.n_kv_heads, max(budget, 0)), torch.int32, "keep", index, stream)
-    new_lens = _made(new_lens, (cache.batch,), torch.int32, "new_lens", index, stream)
+    keep = _made(keep, weights, (cache.batch, cache.n_kv_heads, max(budget, 0)), torch.int32, "keep", index, stream)
+    new_lens = _made(new_lens, weights, (cache.batch,), torch.int32, "new_lens", index, stream)
     _launch(index, "msa_paged_keep", ctypes.byref(cache), at, budget, sinks, recent, keep.data_ptr(), new_lens.data_ptr(), stream=stream)
     return keep, new_lens
 
@@ -725,7 +725,7 @@ _LOGIT_TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 
 def _setting(v, dtype, rows: int, index: int, what: str):
     """(number, device pointer) of a setting: a number for all rows or a tensor of one for every row."""
-    if not torch.is_tensor(v):
+    if not isinstance(v, torch.Tensor):
         return v, None
     if v.dtype != dtype or v.shape != (rows,) or not v.is_contiguous() or v.get_device() != index:
         raise ValueError("%s must be a number or a contiguous %s vector, one for each of %d rows, on cuda:%d" % (what, dtype, rows, index))
@@ -736,11 +736,12 @@ def msa_sample(logits, uniform, temperature, top_k, top_p, min_p, token=None, lo
     """logits: [rows, vocabulary] of bf16, fp16 or fp32, rows may be strided; uniform: fp32 [rows]; settings: numbers, or fp32
     (top_k: int32) vectors.  -> (token int64 [rows], logprob fp32 [rows]); those that are not given are made."""
     index = _device_of(logits, "the logits")
-    if logits.dtype not in _LOGIT_TYPES or logits.dim() != 2 or logits.shape[1] < 1 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+    kind, shape, strides = _LOGIT_TYPES.get(logits.dtype), logits.shape, logits.stride()
+    if kind is None or len(shape) != 2 or shape[1] < 1 or (shape[1] > 1 and strides[1] != 1):
         raise ValueError("the logits must be bf16, fp16 or fp32 [rows, vocabulary] with dense rows, got %s %s, strides %s"
-                         % (logits.dtype, tuple(logits.shape), logits.stride()))
-    rows, vocab = logits.shape
-    stride = logits.stride(0) if rows > 1 else vocab
+                         % (logits.dtype, tuple(shape), strides))
+    rows, vocab = shape
+    stride = strides[0] if rows > 1 else vocab
     if stride < vocab:
         raise ValueError("rows of the logits must not overlap: %d values every %d" % (vocab, stride))
     if uniform.dtype != torch.float32 or uniform.shape != (rows,) or not uniform.is_contiguous() or uniform.get_device() != index:
@@ -748,9 +749,9 @@ def msa_sample(logits, uniform, temperature, top_k, top_p, min_p, token=None, lo
     f32 = torch.float32
     (t, ts), (k, ks) = _setting(temperature, f32, rows, index, "temperature"), _setting(top_k, torch.int32, rows, index, "top_k")
     (p, ps), (m, ms) = _setting(top_p, f32, rows, index, "top_p"), _setting(min_p, f32, rows, index, "min_p")
-    token = _made(token, (rows,), torch.int64, "token", index, stream)
-    logprob = _made(logprob, (rows,), f32, "logprob", index, stream)
-    _launch(index, "msa_sample", ctypes.byref(MsaSampling(t, k, p, m, ts, ks, ps, ms)), logits.data_ptr(), _LOGIT_TYPES[logits.dtype],
+    token = _made(token, uniform, (rows,), torch.int64, "token", index, stream)
+    logprob = _made(logprob, uniform, (rows,), f32, "logprob", index, stream)
+    _launch(index, "msa_sample", ctypes.byref(MsaSampling(t, k, p, m, ts, ks, ps, ms)), logits.data_ptr(), kind,
             stride, rows, vocab, uniform.data_ptr(), token.data_ptr(), logprob.data_ptr(), stream=stream)
     return token, logprob
 

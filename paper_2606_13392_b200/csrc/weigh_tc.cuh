@@ -4,12 +4,17 @@
 // owns a key, adds exp2(scale D - lse) over the columns, and nothing is exchanged until a part ends.  256 keys (two
 // operand tiles) stay in shared memory while the queries' tiles of 128 rows - (token, head of the group) pairs, TPT = 128 / G
 // tokens - stream past them; each tile is read once for two products.
-// One exponential for 2 * 128 flops: the exponential unit (16 a cycle and SM) and the tensor pipe are both near their limits.
+// One exponential for 2 * 128 flops: bound by the exponential unit (16 a cycle and SM; 4096 tokens on 28K have 8 10^9, 1.8 ms of
+// it at 1.9 GHz) at the clock that the board's power allows.
+// Measured (64/8 heads): 4096 tokens on 28K 2.36 - 2.45 ms, 0.84 - 0.87 PFLOP/s; on themselves 172 us; 512 on 7K 81 - 90 us; the
+// last 32 of 4 prompts of 8K - 16K 44 us; the last 17 - 48 of 6 prompts of up to 32K on fp8, 64/4 heads, 139 us.
+// Looked at and not kept: the keys as operands in tensor memory (2.40 ms; windows 139 -> 165 us, the next keys wait for the last
+// products), without exponentials 1.95 ms, without anything but the products 1.65 ms (power), with loops that share code 2.58 ms.
 //
 // Unit of work: one tile of rows against 256 keys of a (sequence, KV head).  All units form one line (sequence, head, key
 // block, tile), tiles that see none of the keys left out; every CTA takes an equal stretch, so that neither ragged batches nor the
 // causal triangle leave CTAs idle.  A key block that a boundary cuts leaves partial sums (at most two per CTA), which
-// weigh_merge_kernel adds up in order.
+// weigh_merge_kernel adds up in order (no atomics: equal calls give equal bits).
 #pragma once
 
 #include "paged_attn.cuh"
@@ -31,7 +36,7 @@ __host__ __device__ __forceinline__ WeighTcSeq weigh_tc_seq(const WeighArgs& a, 
     q.q_row = lo;
     q.q_len = max(hi - lo, 0);
     if (q.q_len < a.min_len || q.q_len > a.max_len) q.q_len = 0;
-    q.kv = (int)min((int64_t)max(a.c.kv_lens[s], 0), (int64_t)a.c.max_pages * a.c.page_size);
+    q.kv = (int)min((int64_t)max(a.c.kv_lens[s], 0), paged_places(a.c));
     q.base = q.kv - max(end - lo, 0);
     q.n_tiles = (q.q_len + TPT - 1) / TPT;
     q.n_kb = q.q_len == 0 ? 0 : (int)(((int64_t)q.kv + kWtKeys - 1) / kWtKeys);
@@ -111,7 +116,7 @@ __device__ inline void weigh_tc_stretch(const WeighArgs& a, int TPT, WeighTcPlan
     int64_t mine = 0;
     for (int s = lo; s < hi; ++s) {
         mine += units(s);
-        if (blockIdx.x == 0 && (a.c.kv_lens[s] < 0 || a.c.kv_lens[s] > (int64_t)a.c.max_pages * a.c.page_size))
+        if (blockIdx.x == 0 && (a.c.kv_lens[s] < 0 || a.c.kv_lens[s] > paged_places(a.c)))
             report_async(status, kAsyncBadIndex, 0x801);
     }
     int64_t upto = mine;
@@ -315,7 +320,7 @@ weigh_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                                            __ffma2_rn(make_float2(__uint_as_float(w[2]), __uint_as_float(w[3])), sc, make_float2(l.z, l.w))};
 #pragma unroll
                             for (int i = 0; i < 2; ++i) {
-                                                                if (weigh_by_arithmetic((c >> 1) + i)) x[i] = exp2_by_arithmetic(x[i]);
+                                if (weigh_by_arithmetic((c >> 1) + i)) x[i] = exp2_by_arithmetic(x[i]);
                                 else { x[i].x = ex2_approx(x[i].x); x[i].y = ex2_approx(x[i].y); }
                                 if constexpr (decltype(masked)::value) {
                                     const int col = ch * 16 + c + 2 * i;

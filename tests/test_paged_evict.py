@@ -214,11 +214,12 @@ def test_refusals_without_a_launch():
     c = cache_struct()
     keep, compact = B._fn("msa_paged_keep"), B._fn("msa_paged_compact")
 
-    def k(cache=c, w=4096, budget=4, sinks=0, recent=0, to=4096, lens=4096):
+    def k(cache=c, w=4096, budget=4, sinks=0, recent=0, to=4096, lens=8192):
         return keep(ctypes.byref(cache) if cache is not None else None, w, budget, sinks, recent, to, lens, None)
 
     assert k(cache=None) == 1 and k(w=None) == 1 and k(w=4097) == 1 and k(to=None) == 1 and k(to=4098) == 1 and k(lens=4097) == 1
-    assert k(budget=0) == 1 and k(sinks=-1) == 1 and k(recent=-1) == 1
+    assert k(budget=0) == 1 and k(sinks=-1) == 1 and k(recent=-1) == 1 and k(budget=(1 << 30) + 1) == 2
+    assert k(lens=4096) == 1  # (the old lengths are still read)
     assert k(cache=cache_struct(kv_lens=None)) == 1 and k(cache=cache_struct(page_table=None)) == 1
     assert k(cache=cache_struct(n_kv_heads=5000)) == 2 and k(cache=cache_struct(page_size=0)) == 1
     assert k(cache=cache_struct(batch=0)) == 0
@@ -228,6 +229,7 @@ def test_refusals_without_a_launch():
 
     assert m(cache=None) == 1 and m(at=None) == 1 and m(at=4097) == 1 and m(w=4098) == 1 and m(width=-1) == 1
     assert m(cache=cache_struct(k=None)) == 1 and m(cache=cache_struct(k=4100)) == 1 and m(cache=cache_struct(v=4100)) == 1
+    assert m(width=(1 << 30) + 1) == 2
     assert m(width=0) == 0 and m(cache=cache_struct(batch=0)) == 0
 
 
