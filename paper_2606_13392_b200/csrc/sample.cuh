@@ -183,10 +183,13 @@ struct SampleScale {
         const bool some = __double2hiint(t) == 0x43380000 && (uint32_t)k < (uint32_t)(kSampleReach * kSampleTable);
         return power(k, fma(x, -c, fma(t - kFront, -1.0 / kSampleTable, tc)), some);
     }
+    // Distance to the top in 32 bits, in units of the bins' axis (log2 of the weight).  Its operations, and those that make bins of it,
+    // are named: contracted in one pass over the row and not in another, a logit would change its bin.
+    __device__ __forceinline__ float distance(float v) const { return __fmul_rn(__fsub_rn(top, v), c32); }
     // Bin of a logit, larger logits in lower bins; kSampleBins: its weight is 0.
     __device__ __forceinline__ int bin(float v) const {
-        const float z = (top - v) * c32;
-        return z < kSampleReach ? min((int)(z * (kSampleBins / kSampleReach)), kSampleBins - 1) : kSampleBins;
+        const float z = distance(v);
+        return z < kSampleReach ? min((int)__fmul_rn(z, kSampleBins / kSampleReach), kSampleBins - 1) : kSampleBins;
     }
 };
 
@@ -558,7 +561,7 @@ sample_kernel(const SampleArgs a) {
     float from = 0.f, to = INFINITY, finer = 0.f;
     int end = 0;
     uint64_t whole = 0, above = 0;      // weight of the row, of what comes before the list
-    auto distance = [&](float v) { return (sc.top - v) * sc.c32; };
+    auto finer_bin = [&](float z) { return min((int)__fmul_rn(__fsub_rn(z, from), finer), kSampleBins - 1); };
     constexpr float kWidth = kSampleReach / kSampleBins;
     // Twice as many threads as k, at least, or most of what they would list is not wanted.
     bool by_maxima = by_k && tame && (int64_t)k * 2 <= (int64_t)ctas * kSampleThreads;
@@ -619,11 +622,11 @@ sample_kernel(const SampleArgs a) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     const uint64_t w = sc.weight_of(v[e]);
-                    const float z = distance(v[e]);
+                    const float z = sc.distance(v[e]);
                     total += w;
                     if (z < from) earlier += w;
                     else if (z < to && w > 0) {
-                        const int b = min((int)((z - from) * finer), kSampleBins - 1);
+                        const int b = finer_bin(z);
                         const uint32_t old = atomicAdd(&sm.mass_lo[b], (uint32_t)w);
                         const uint32_t up = (uint32_t)(w >> 32) + (old + (uint32_t)w < old ? 1u : 0u);
                         if (up != 0) atomicAdd(&sm.mass_hi[b], up);
@@ -691,8 +694,8 @@ sample_kernel(const SampleArgs a) {
         uint64_t* mine = cluster.map_shared_rank(sm.list, 0) + rank * part;
         auto wanted = [&](float v) {
             if (by_k) return sc.bin(v) <= end;
-            const float z = distance(v);
-            const int b = z < from ? -1 : (z < to ? min((int)((z - from) * finer), kSampleBins - 1) : kSampleBins);
+            const float z = sc.distance(v);
+            const int b = z < from ? -1 : (z < to ? finer_bin(z) : kSampleBins);
             return mode == kBin ? b == end : b <= end;
         };
         // (logits at the far end of what is wanted, or a little below: most pieces have none)

@@ -244,3 +244,42 @@ def test_refusals_of_tensors():
             api.sample(x, u, **{name: math.nan})
     with pytest.raises(ValueError):
         api.sample(x.requires_grad_(), u)
+
+
+def pick_all(x, u, t, k, p, m):
+    """pick() of many rows at once on the device -> (tokens, rows that are clear)."""
+    x, u = x.double(), u.double()[:, None]
+    t, p, m = [float(torch.tensor(v, dtype=torch.float32)) for v in (t, p, m)]
+    z, index = x.sort(dim=-1, descending=True, stable=True)
+    z = (z - z[:, :1]) / t
+    w = z.exp()
+    if 0 < k < x.shape[1]:
+        w[:, k:] = 0
+    clear = torch.ones(len(x), dtype=torch.bool, device=x.device)
+    if p < 1:
+        mass = w.cumsum(-1)
+        goal = p * mass[:, -1:]
+        clear &= ((mass - goal).abs() > NEAR * mass[:, -1:]).all(-1)
+        w = torch.where(mass - w >= goal, 0.0, w)
+    if m > 0:
+        clear &= ((z - math.log(m)).abs() > NEAR).all(-1)
+        w = torch.where(z < math.log(m), 0.0, w)
+    w = torch.zeros_like(w).scatter_(1, index, w)
+    upto = w.cumsum(-1)
+    total = upto[:, -1:]
+    clear &= ((upto - u * total).abs() > NEAR * total).all(-1)
+    return (upto <= u * total).sum(-1), clear
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("vocab,spread,t,k,p,m", [(1159, 3.0, 1.5, 0, 0.99, 0.0), (4120, 2.0, 0.9, 0, 0.9, 0.0), (1500, 1.0, 1.0, 0, 0.5, 0.0),
+                                                  (2001, 2.0, 1.0, 300, 0.9, 0.0), (1000, 2.0, 0.7, 20, 1.0, 0.05), (900, 2.5, 1.0, 0, 1.0, 0.0)])
+def test_many_rows(kind, vocab, spread, t, k, p, m):
+    """Enough rows that a token lost at the edge of a bin shows."""
+    for seed in range(4):
+        logits, u = made(8000, vocab, kind, spread, 50 + seed)
+        token, _ = api.sample(logits, u, t, k, p, m)
+        want, clear = pick_all(logits, u, t, k, p, m)
+        assert clear.float().mean() > 0.99
+        assert torch.equal(token[clear], want[clear]), (seed, (token != want)[clear].sum())
