@@ -606,10 +606,11 @@ enum { MSA_BF16 = 0, MSA_FP16 = 1, MSA_FP32 = 2 };
 /*
  * For every row: p = softmax(logits / T), what the settings keep of it, and with uniform[row] = u in [0, 1) the first token
  * index at which the running sum of the kept probabilities exceeds u times their sum -> token[row]; logprob[row] (logprob may
- * be NULL) is the natural log of its probability among the kept.  Sums are exact to 2^-42 of the largest probability for each
- * token, in any order: equal calls choose equal tokens.  A logit of -infinity is never chosen; if there are logits of
- * +infinity, one of them is.  A row with nothing to choose from (all -infinity) or with a NaN (logits, u or T) gives
- * -1 and NaN.  Rows of `vocab` (at most 2^21) values of logits_type start every `stride` elements.
+ * be NULL) is the natural log of its probability among the kept.  Probabilities count in whole numbers of 2^-42 of the largest
+ * (one of less than 2^-43 is never chosen) and are added as such, in any order: equal calls choose equal tokens.  A logit of
+ * -infinity is never chosen; if there are logits of +infinity, one of them is.  A row with nothing to choose from (all
+ * -infinity) or with a NaN (logits, u or T) gives -1 and NaN.  Rows of `vocab` (at most 2^21) values of logits_type start every
+ * `stride` elements.
  */
 msa_status_t msa_sample(const msa_sampling_t* settings, const void* logits, int32_t logits_type, int64_t stride, int64_t n_rows,
                         int32_t vocab, const float* uniform, int64_t* token, float* logprob, msa_stream_t stream);
