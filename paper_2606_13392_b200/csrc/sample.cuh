@@ -165,9 +165,9 @@ struct SampleScale {
     __device__ __forceinline__ uint64_t power(int k, double r, bool some) const {
         constexpr double L = -0.69314718055994530942;
         const double p = fma(r, fma(r, fma(r, L * L * L / 6, L * L / 2), L), 1.0);
-        const double w = table[k & (kSampleTable - 1)] * p;
-        const double scaled = __hiloint2double(__double2hiint(w) + ((kSampleBits - (k >> 10)) << 20), __double2loint(w));
-        const uint64_t whole = (uint64_t)__double_as_longlong(scaled + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
+        const double root = table[k & (kSampleTable - 1)];
+        const double scaled = __hiloint2double(__double2hiint(root) + ((kSampleBits - (k >> 10)) << 20), __double2loint(root));
+        const uint64_t whole = (uint64_t)__double_as_longlong(fma(scaled, p, 4503599627370496.0)) & 0xFFFFFFFFFFFFFull;
         return some ? whole : 0;  // (no branch: what is computed beyond the reach is not used)
     }
     // Weight at a distance d >= 0 of the top: z = d c = k / 1024 + r.  From z = 43 on (infinity, too; NaN): 0.
@@ -465,7 +465,7 @@ __device__ __noinline__ void sample_slow(const SampleArgs a, int64_t row_number,
 // Measured: one row of 131072 with top_k and top_p 11 us (five meetings of the cluster and a short list, 4 - 6 thousand cycles each);
 // 512 of 65536 with both 39 us; 96 of 100003 whose settings differ 55 - 58 us (the few without top_k); a flat nucleus of
 // 33 rows of 50001 41 us; 256 whole rows of 131072 in fp32 97 us (the row is read twice, and 64-bit arithmetic).
-// Where the cycles go, long rows: 30 instructions of 9 in 64 bits a weight, two passes of weights for a nucleus.  Loops that unroll
+// Where the cycles go, long rows: 30 instructions, 8 of them in 64 bits, a weight, two passes of weights for a nucleus.  Loops that unroll
 // more than a piece of 16 bytes leave the instruction cache (512 rows of 65536: 55 us with four).
 template <class T>
 __global__ void __launch_bounds__(kSampleThreads, 2)
