@@ -117,27 +117,35 @@ struct SampleRow {
 };
 
 // Pieces [lo, hi) of a warp: a run of the row, lanes side by side, U in flight (few where f is long: a loop that does not fit the
-// instruction cache is what slows these passes most).  f(piece, index of its first value) is called by
+// instruction cache is what slows these passes most); U = 0: one, while the next two are on their way.  f(piece, index of its first value) is called by
 // all lanes of the warp (beyond the run: with -infinities).
 template <int U, class T, class F>
 __device__ __forceinline__ void sample_pieces(const SampleRow<T>& row, int lo, int hi, F f) {
     const int lane = threadIdx.x & 31;
-    for (int p0 = lo; p0 < hi; p0 += 32 * U) {
-        uint4 raw[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int p = p0 + u * 32 + lane;
-            raw[u] = p < hi ? row.load(p) : SampleRow<T>::nothing();
+    auto load = [&](int p) { return p < hi ? row.load(p) : SampleRow<T>::nothing(); };
+    if constexpr (U == 0) {
+        uint4 next[2] = {load(lo + lane), load(lo + 32 + lane)};
+        for (int p0 = lo; p0 < hi; p0 += 32) {
+            const uint4 raw = next[0];
+            next[0] = next[1];
+            next[1] = load(p0 + 64 + lane);
+            f(raw, row.index(p0 + lane));
         }
+    } else {
+        for (int p0 = lo; p0 < hi; p0 += 32 * U) {
+            uint4 raw[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (p0 + u * 32 < hi) f(raw[u], row.index(p0 + u * 32 + lane));
+            for (int u = 0; u < U; ++u) raw[u] = load(p0 + u * 32 + lane);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (p0 + u * 32 < hi) f(raw[u], row.index(p0 + u * 32 + lane));
+        }
     }
 }
 // The same with the values as floats.
-template <class T, class F>
+template <int U = 1, class T, class F>
 __device__ __forceinline__ void sample_run(const SampleRow<T>& row, int lo, int hi, F f) {
-    sample_pieces<1>(row, lo, hi, [&](const uint4& raw, int at) {
+    sample_pieces<U>(row, lo, hi, [&](const uint4& raw, int at) {
         float v[SampleRow<T>::E];
         Logits<T>::widen(raw, v);
         f(v, at);
@@ -464,7 +472,7 @@ __device__ __noinline__ void sample_slow(const SampleArgs a, int64_t row_number,
 //   no filters: every warp adds up its run, and the one that the target falls into finds the token.
 // Measured: one row of 131072 with top_k and top_p 11 us (five meetings of the cluster and a short list, 4 - 6 thousand cycles each);
 // 512 of 65536 with both 39 us; 96 of 100003 whose settings differ 55 - 58 us (the few without top_k); a flat nucleus of
-// 33 rows of 50001 41 us; 256 whole rows of 131072 in fp32 97 us (the row is read twice, and 64-bit arithmetic).
+// 33 rows of 50001 41 us; 256 whole rows of 131072 in fp32 91 us (the row is read twice, and 64-bit arithmetic).
 // Where the cycles go, long rows: 30 instructions, 8 of them in 64 bits, a weight, two passes of weights for a nucleus.  Loops that unroll
 // more than a piece of 16 bytes leave the instruction cache (512 rows of 65536: 55 us with four).
 template <class T>
@@ -877,7 +885,7 @@ sample_kernel(const SampleArgs a) {
     };
     uint64_t mine = 0;
     if (mode == kAll && least == INFINITY) {
-        sample_run(row, run_lo, run_hi, [&](const float (&v)[E], int) {
+        sample_run<0>(row, run_lo, run_hi, [&](const float (&v)[E], int) {
 #pragma unroll
             for (int e = 0; e < E; ++e) mine += sc.weight_of(v[e]);
         });
