@@ -1,0 +1,100 @@
+"""Choices of the next token at the edges: few tokens allowed, settings out of the ordinary, rows anywhere.  The reference, its
+tolerances and when a row is not compared are those of test_sample.py."""
+
+import math
+
+import pytest
+import torch
+
+from paper_2606_13392_b200 import api
+from paper_2606_13392_b200 import binding as B
+from test_sample import made, pick
+
+DEV = "cuda"
+
+
+def check_written(x, u, t, k, p, m=0.0, unclear=0):
+    """As check() there, into given outputs that hold something else before."""
+    token = torch.full((len(x),), -9, device=DEV)
+    logprob = torch.full((len(x),), 99.0, device=DEV)
+    B.msa_sample(x, u, t, k, p, m, token, logprob)
+    skipped, rows, us = 0, x.cpu(), u.tolist()
+    for r in range(len(x)):
+        want, lp, clear = pick(rows[r], us[r], t, k, p, m)
+        if not clear:
+            skipped += 1
+            continue
+        assert int(token[r]) == want, (r, int(token[r]), want)
+        got = float(logprob[r])
+        assert (got != got and lp != lp) or abs(got - lp) <= 2.0 ** -24 * abs(lp) + 1e-9, (r, got, lp)
+    assert skipped <= unclear
+
+
+def leave_traces(kind):
+    """Calls that leave counts, digits and sums of their own in the SMs' shared memory."""
+    x, u = made(300, 3000, kind, 3.0, 5)
+    api.sample(x, u)
+    api.sample(x, u, 1.0, 0, 0.9)
+    api.sample(x * 1e4, u, 1e-5, 100, 0.9)
+    api.sample(-x.abs() * 1e4 - 1e4, u, 1e-5, 2900)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("k", [50, 1000])
+@pytest.mark.parametrize("p", [1.0, 0.9])
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float16, torch.float32])
+def test_fewer_tokens_allowed_than_top_k_asks_for_at_low_temperatures(kind, k, p):
+    vocab, allowed = 6000, [1, 2, 3, 10, 49, 50, 51, 200, 600, 999]
+    x, u = made(len(allowed), vocab, kind, 3.0, k)
+    g = torch.Generator().manual_seed(7)
+    y = torch.full_like(x, -math.inf)
+    for r, n in enumerate(allowed):
+        places = torch.randperm(vocab, generator=g)[:n].to(DEV)
+        y[r, places] = x[r, places]
+        y[r, places[:2]] = -30.0 if r % 2 else 30.0  # (the largest is far from zero, or near it, of either sign)
+        if r % 3 == 0:
+            y[r, places] = -y[r, places].abs() - 9
+    for t in (1e-6, 1e-5):
+        for z in (y, -40 + y):
+            leave_traces(kind)
+            check_written(z, u, t, k, p)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("at", [1e6, -2e6])
+@pytest.mark.parametrize("k,p,m", [(50, 1.0, 0.0), (1000, 1.0, 0.0), (1000, 0.9, 0.0), (700, 0.5, 0.01)])
+def test_fewer_tokens_allowed_than_top_k_asks_for_far_from_zero(at, k, p, m):
+    """Logits so far from zero that 32-bit steps between them are counted one by one; several of them weigh something."""
+    vocab = 5000
+    x, u = made(24, vocab, torch.float32, 3.0, 3)
+    g = torch.Generator().manual_seed(8)
+    y = torch.full_like(x, -math.inf)
+    for r in range(24):
+        places = torch.randperm(vocab, generator=g)[:3 + 25 * r].to(DEV)
+        y[r, places] = at + x[r, places]
+    leave_traces(torch.float32)
+    check_written(y, u, 1.0, k, p, m, unclear=1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float16, torch.float32])
+def test_one_infinite_logit_and_nothing_else(kind):
+    x, u = made(4, 3000, kind, 1.0, 1)
+    x.fill_(-math.inf)
+    x[:, 1717] = math.inf
+    for t, k, p, m in ((1.0, 50, 1.0, 0.0), (0.7, 2, 0.9, 0.0), (1.0, 2999, 0.5, 0.1), (1.0, 0, 0.9, 0.0), (0.0, 50, 0.9, 0.0)):
+        leave_traces(kind)
+        check_written(x, u, t, k, p, m)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows", [2, 400])
+def test_more_equal_logits_than_a_list_holds_and_fewer_than_top_k(kind, rows):
+    vocab = 20000
+    x = torch.full((rows, vocab), -math.inf, dtype=kind, device=DEV)
+    x[:, 100:19000:6] = -1.5  # 3150 of them
+    u = made(rows, 1, kind, 1.0, rows)[1]
+    for k, p in ((5000, 0.9), (3151, 0.5), (3150, 0.9), (3149, 0.9), (5000, 1.0)):
+        leave_traces(kind)
+        check_written(x, u, 0.8, k, p, unclear=2)
