@@ -185,23 +185,31 @@ struct WeighTcSmem {
 };
 static_assert(sizeof(WeighTcSmem) <= 227 * 1024, "a CTA's shared memory");
 
+// Clamps that let a NaN through.
+__device__ __forceinline__ float clamp_nan(float x, float lo, float hi) {
+    float d;
+    asm("{\n\t.reg .f32 a;\n\tmax.NaN.f32 a, %1, %2;\n\tmin.NaN.f32 %0, a, %3;\n\t}" : "=f"(d) : "f"(x), "f"(lo), "f"(hi));
+    return d;
+}
+
 // 2^x by arithmetic, two at a time: x = n + f with n the nearest whole number, |f| <= 1/2; 2^f = 1 + f r(f) with r of degree 4
-// fitted to the least relative error (1.6e-7 with fp32 roundings); n goes to the exponent's place.  Below 2^-126 the result is a
-// part of the smallest numbers, at -127 zero; from 128 on infinity.
+// fitted to the least relative error (1.6e-7 with fp32 roundings); twice that times 2^(n-1), a product, so that a NaN stays one (n
+// added in the exponent's place would make a number of it).  From 128 on infinity; below -125.5, where 2^(n-1) is no normal
+// number, zero.
 __device__ __forceinline__ float2 exp2_by_arithmetic(float2 x) {
     constexpr float M = 12582912.f;  // 1.5 * 2^23: a sum with it has the whole number in its last bits
-    x.x = fminf(fmaxf(x.x, -127.f), 128.f);
-    x.y = fminf(fmaxf(x.y, -127.f), 128.f);
+    x.x = clamp_nan(x.x, -126.f, 128.f);
+    x.y = clamp_nan(x.y, -126.f, 128.f);
     const float2 t = __fadd2_rn(x, make_float2(M, M));
     const float2 n = __fadd2_rn(t, make_float2(-M, -M));
     const float2 f = __ffma2_rn(n, make_float2(-1.f, -1.f), x);
-    float2 r = __ffma2_rn(make_float2(1.326466561295092e-3f, 1.326466561295092e-3f), f, make_float2(9.671512991189957e-3f, 9.671512991189957e-3f));
-    r = __ffma2_rn(r, f, make_float2(5.550733953714371e-2f, 5.550733953714371e-2f));
-    r = __ffma2_rn(r, f, make_float2(0.24022242426872253f, 0.24022242426872253f));
-    r = __ffma2_rn(r, f, make_float2(0.6931470036506653f, 0.6931470036506653f));
-    r = __ffma2_rn(r, f, make_float2(1.f, 1.f));
-    return make_float2(__int_as_float(__float_as_int(r.x) + (__float_as_int(t.x) << 23)),
-                       __int_as_float(__float_as_int(r.y) + (__float_as_int(t.y) << 23)));
+    auto both = [](float c) { return make_float2(2.f * c, 2.f * c); };
+    float2 r = __ffma2_rn(both(1.326466561295092e-3f), f, both(9.671512991189957e-3f));
+    r = __ffma2_rn(r, f, both(5.550733953714371e-2f));
+    r = __ffma2_rn(r, f, both(0.24022242426872253f));
+    r = __ffma2_rn(r, f, both(0.6931470036506653f));
+    r = __ffma2_rn(r, f, both(1.f));
+    return __fmul2_rn(r, make_float2(__int_as_float((__float_as_int(t.x) << 23) + 0x3F000000), __int_as_float((__float_as_int(t.y) << 23) + 0x3F000000)));
 }
 
 // Waits for this thread's loads from tensor memory; the registers are named so that nothing reads them earlier.

@@ -1,0 +1,69 @@
+"""The calls of a bounded cache at their edges: what is not a number, waits that run out, bad lengths and pages, settings out of
+the ordinary.  References and tolerances are those of test_paged_weights.py."""
+
+import math
+
+import pytest
+import torch
+
+from paper_2606_13392_b200 import api
+from paper_2606_13392_b200 import binding as B
+from test_paged_append import batch
+from test_paged_weights import filled, queries, reference
+
+DEV = "cuda"
+KERNELS = [  # new tokens, head size, fp8: single tokens, a few, many (tensor memory), head sizes without tensor cores
+    (1, 128, False), (1, 128, True), (3, 128, False), (3, 128, True), (200, 128, False), (200, 128, True), (20, 64, False)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("new,d,fp8", KERNELS)
+@pytest.mark.parametrize("what", ["lse", "q"])
+def test_a_row_that_is_not_a_number_shows_wherever_it_stands(new, d, fp8, what):
+    """Token and head of every column that a product of rows has: the places that the token sees get no number, the rest stay right."""
+    cache = filled(batch([(new, 300)], 16, 1, d, fp8, values=False))
+    q = queries(cache, 8)
+    start = torch.rand(cache.k.shape[0], 1, 16, device=DEV)
+    want, tol, lse = reference(cache, q, None, start, 0.5)
+    place = torch.arange(new + 300, device=DEV)
+    at = (cache.page_table[0].long()[place // 16], 0, place % 16)
+    for tok in sorted({0, 1, 2, 15, 16, 31, 100, new - 1} & set(range(new))):
+        for head in range(8):
+            q2, lse2 = q.clone(), lse.clone()
+            if what == "q":
+                q2[tok, head, 5] = math.nan
+            else:
+                lse2[tok, head] = math.nan
+            got = api.paged_weights(cache, q2, lse2, start.clone(), 0.5)[at].double()
+            sees = place <= 300 + tok
+            assert got[sees].isnan().all(), (tok, head, int((~got[sees].isnan()).sum()))
+            assert (got - want[at])[~sees].abs().le(tol[at][~sees]).all()
+    assert B.check_async_status() == (0, 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("new", [1, 200])
+def test_scores_far_above_the_lse_overflow(new):
+    """2^x of any size, by whatever way: finite as long as it is, infinite beyond, nothing at minus infinity."""
+    cache = filled(batch([(new, 40)], 16, 1, 128, False, values=False))
+    q = queries(cache, 8)
+    q.zero_()
+    for x in (126.5, 127.25, 127.75, 200.0, math.inf, -126.0, -130.0, -200.0, -math.inf):
+        lse = torch.full((new, 8), -x * math.log(2.0), device=DEV)
+        if x == -math.inf:
+            lse.fill_(math.inf)
+        if x == math.inf:
+            lse.fill_(-1e30)  # (minus infinity itself gives nothing)
+        for head in range(8):
+            one = torch.full_like(lse, math.inf)
+            one[0, head] = lse[0, head]
+            got = api.paged_weights(cache, q, one, torch.zeros(cache.k.shape[0], 1, 16, device=DEV), 1.0)
+            value = got[int(cache.page_table[0, 0]), 0, 0].double().item()
+            # x is made of two products in 32 bits: off by 2^-22 of itself, its power by as much again; below 2^-126 anything down to 0
+            size = 2.0 ** x if abs(x) < 1000 else (math.inf if x > 0 else 0.0)
+            if x >= 200:
+                assert value == math.inf
+            elif x <= -126:
+                assert 0 <= value <= 2.0 ** -125
+            else:
+                assert abs(value / size - 1) < 1e-4, (x, head, value)
