@@ -198,7 +198,7 @@ weigh_few_kernel(const WeighArgs a, double inv_grid, int* status) {
         // ---- 8 NT rows of queries
         uint32_t qf[NT][8][2];
         float nl[NT][2], sc[NT][2];
-        int lim[NT][2];  // last visible place of the row, -1 for rows that are not there
+        int lim[NT][2];  // last visible place of the row, -1 for rows that are not there or are to give nothing
         auto load_q = [&](int first) {
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
@@ -247,8 +247,8 @@ weigh_few_kernel(const WeighArgs a, double inv_grid, int* status) {
                     const bool there = tc < sq.q_len;
                     const float l = there ? __ldg(a.lse + (int64_t)(sq.q_row + tc) * H_q + head * a.G + hc) : INFINITY;
                     sc[n][i] = F8 ? __shfl_sync(0xffffffffu, scale, (2 * t4 + i) * 4) : scale;
-                    nl[n][i] = l == -INFINITY ? -INFINITY : -l * 1.4426950408889634f;  // (a row that saw nothing gives nothing)
-                    lim[n][i] = there ? sq.base + tc : -1;
+                    nl[n][i] = -l * 1.4426950408889634f;
+                    lim[n][i] = there && l != -INFINITY ? sq.base + tc : -1;  // (a row that saw nothing gives nothing, whatever it holds)
                 }
             }
         };
@@ -393,11 +393,11 @@ weigh_generic_kernel(const WeighArgs a, int d, int* status) {
                     __syncthreads();
                     for (int c = threadIdx.x; c < d; c += 128) qs[c] = __bfloat162float(a.q[at * d + c]);
                     __syncthreads();
-                    if (p.row < 0 || key > (int64_t)sq.base + tok) continue;
+                    const float l = a.lse[at];
+                    if (p.row < 0 || key > (int64_t)sq.base + tok || l == -INFINITY) continue;  // (a row that saw nothing gives nothing)
                     float x = 0.f;
                     for (int c = 0; c < d; ++c) x = fmaf(qs[c], idx_elem<F8>(row, c), x);
-                    const float l = a.lse[at];
-                    sum += exp2f(fmaf(x, a.scale_log2e, l == -INFINITY ? -INFINITY : -l * 1.4426950408889634f));
+                    sum += exp2f(fmaf(x, a.scale_log2e, -l * 1.4426950408889634f));
                 }
             }
             if (p.row >= 0) a.w[p.w] = weigh_old(a, p.w, (int)key, sq.base) + sum;

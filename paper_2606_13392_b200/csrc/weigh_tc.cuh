@@ -174,6 +174,7 @@ struct WeighTcSmem {
     alignas(1024) uint8_t k[2][2][128 * 256];  // [buffer][128 keys]: [8 keys][d half][key][64 bf16], 128-byte swizzle
     alignas(1024) uint8_t q[kWtStages][128 * 256];  // [d half][row][64 bf16]
     float nl[kWtStages][128];                  // -lse of the tile's rows, base two
+    alignas(16) uint32_t live[kWtStages][4];   // a bit for each row: clear where it gives nothing, whatever it holds (lse -infinity)
     union {
         float join[kWtKeys];                   // the second half of the columns' sums on their way to the first's threads
         WeighTcPlan plan;
@@ -305,14 +306,21 @@ weigh_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             for (int t = p.lo; ok && t < p.hi; ++t, ++T) {
                 const int st = T % kWtStages, buf = T & 1;
                 if (!mbar_wait(&sm.l_full[st], (T / kWtStages) & 1, abort)) { ok = false; break; }
-                // visible columns [c_lo, c_hi) of this thread's key; all of them for all keys of the warp: no masks
+                // visible columns [c_lo, c_hi) of this thread's key; all of them for all keys of the warp, and no row that gives
+                // nothing: no masks
+                const uint2 live = *reinterpret_cast<const uint2*>(&sm.live[st][half * 2]);
                 const int tok0 = t * TPT;
                 const int c_hi = min(TPT, p.q_len - tok0) * a.G - half * 64;
                 const int c_lo = min(max(first_tok - tok0, 0), 256) * a.G - half * 64;
-                const bool all = c_hi >= 64 && __all_sync(0xffffffffu, c_lo <= 0);
+                const bool all = c_hi >= 64 && (live.x & live.y) == 0xFFFFFFFFu && __all_sync(0xffffffffu, c_lo <= 0);
                 const float* nl = sm.nl[st] + half * 64;
                 float2 s2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
                 auto add = [&](auto masked) {  // (two loops: with the masks in one the selects bound it)
+                    uint32_t seen[2];  // a bit for each column
+                    for (int w = 0; w < 2; ++w) {
+                        const int lo = min(max(c_lo - 32 * w, 0), 32), hi = min(max(c_hi - 32 * w, 0), 32);
+                        seen[w] = (w == 0 ? live.x : live.y) & (lo < hi ? (0xFFFFFFFFu << lo) & (0xFFFFFFFFu >> (32 - hi)) : 0u);
+                    }
 #pragma unroll
                     for (int ch = 0; ch < 4; ++ch) {
                         const bool more = ch < 3 || t + 1 < p.hi;
@@ -332,8 +340,8 @@ weigh_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                                 else { x[i].x = ex2_approx(x[i].x); x[i].y = ex2_approx(x[i].y); }
                                 if constexpr (decltype(masked)::value) {
                                     const int col = ch * 16 + c + 2 * i;
-                                    x[i].x = col >= c_lo && col < c_hi ? x[i].x : 0.f;
-                                    x[i].y = col + 1 >= c_lo && col + 1 < c_hi ? x[i].y : 0.f;
+                                    x[i].x = (seen[col >> 5] & 1u << (col & 31)) != 0 ? x[i].x : 0.f;
+                                    x[i].y = (seen[col >> 5] & 2u << (col & 31)) != 0 ? x[i].y : 0.f;
                                 }
                                 s2[i] = __fadd2_rn(s2[i], x[i]);
                             }
@@ -431,11 +439,11 @@ weigh_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             }
         }
     } else if (warp == 18) {
-        // ---------------- lse of the rows, four a lane, a tile ahead
+        // ---------------- lse of the rows, four a lane, a tile ahead; which of them give nothing
         int tok[4], at[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int r = lane * 4 + i;
+            const int r = i * 32 + lane;
             tok[i] = r < TPT * a.G ? r / a.G : 1 << 30;
             at[i] = r / a.G * H_q + r % a.G;
         }
@@ -453,14 +461,18 @@ weigh_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
 #pragma unroll
                 for (int i = 0; i < 4; ++i) l[i] = ahead[i];
                 fetch(t + 1, ahead);
-                if (T >= kWtStages && !mbar_wait(&sm.l_empty[st], (T / kWtStages - 1) & 1, abort)) {
+                if (T >= kWtStages && !__all_sync(0xffffffffu, mbar_wait(&sm.l_empty[st], (T / kWtStages - 1) & 1, abort))) {
                     if (lane == 0) report_async(status, kAsyncTimeout, 0x826);
                     ok = false;
                     break;
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) l[i] = l[i] == -INFINITY ? -INFINITY : -l[i] * 1.4426950408889634f;
-                *reinterpret_cast<float4*>(sm.nl[st] + lane * 4) = make_float4(l[0], l[1], l[2], l[3]);
+                for (int i = 0; i < 4; ++i) {
+                    const bool out = l[i] == -INFINITY;
+                    const uint32_t live = ~__ballot_sync(0xffffffffu, out);
+                    if (lane == 0) sm.live[st][i] = live;
+                    sm.nl[st][i * 32 + lane] = out ? -INFINITY : -l[i] * 1.4426950408889634f;
+                }
                 mbar_arrive(&sm.l_full[st]);
             }
         }

@@ -67,3 +67,24 @@ def test_scores_far_above_the_lse_overflow(new):
                 assert 0 <= value <= 2.0 ** -125
             else:
                 assert abs(value / size - 1) < 1e-4, (x, head, value)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("new,d,fp8", KERNELS)
+def test_a_row_whose_lse_is_minus_infinity_gives_nothing_whatever_it_holds(new, d, fp8):
+    """Rows that are to be left out: their queries need not be numbers."""
+    cache = filled(batch([(new, 300), (1, 40)], 16, 2, d, fp8, values=False))
+    q = queries(cache, 16)
+    start = torch.rand(cache.k.shape[0], 2, 16, device=DEV)
+    _, _, lse = reference(cache, q, None, start, 0.5)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    out = torch.rand(lse.shape, generator=g, device=DEV) < 0.3
+    out[0, 3] = out[new - 1, :9] = True
+    lse[out] = -math.inf
+    want, tol, _ = reference(cache, q, lse, start, 0.5)
+    for value in (math.nan, math.inf, -math.inf, 3e38):
+        bad = q.clone()
+        bad[out] = value
+        got = api.paged_weights(cache, bad, lse, start.clone(), 0.5)
+        assert (got.double() - want).abs().le(tol + 1e-9).all(), value
+    assert B.check_async_status() == (0, 0)
