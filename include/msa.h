@@ -554,7 +554,8 @@ msa_status_t msa_paged_attn_workspace_bytes(const msa_paged_cache_t* cache, int3
  * softmax_scale and max_new as in msa_paged_attn.  The rows may be some of the queries only (cu_q counts those given): the
  * last tokens of a prompt as observers of all of it, say - they are the last tokens of kv_lens[s], and what comes before them
  * counts as old.  Sums are fp32 in a fixed order: equal calls give equal bits.  Sequences must not share pages (their weights
- * would).  Places on bad pages are reported and left out.  head_dim = 128 runs on the tensor cores, other sizes on a generic kernel.
+ * would).  Places on bad pages are reported and left out.  Where a device-side wait runs out (MSA_ERR_TIMEOUT), every weight has its
+ * old value or its new one.  head_dim = 128 runs on the tensor cores, other sizes on a generic kernel.
  * workspace (256-byte aligned; may be NULL where it has 0 bytes) >= msa_paged_weights_workspace_bytes.
  */
 msa_status_t msa_paged_weights(const msa_paged_cache_t* cache, const void* q, int32_t n_q_heads, const float* lse,

@@ -166,8 +166,9 @@ __device__ inline void weigh_tc_stretch(const WeighArgs& a, int TPT, WeighTcPlan
 }
 
 // What weigh_merge_kernel has to know about a CTA: first 0 no part; 1 its first block came from an earlier CTA and goes on in a
-// later one; 2 came from an earlier one and ends here; 3 begins here.  open: its last block begins here and ends later.
-struct WeighEnds { int first, open, seq, head, kb, pad[3]; };
+// later one; 2 came from an earlier one and ends here; 3 begins here.  open: its last block begins here and ends later.  failed: a
+// wait ran out, so that its sums may lack something and its parts are not all there.
+struct WeighEnds { int first, open, seq, head, kb, failed, pad[2]; };
 static_assert(sizeof(WeighEnds) == 32, "two int4");
 
 struct WeighTcSmem {
@@ -238,7 +239,7 @@ weigh_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     if ((smem_u32(weigh_smem) & 1023) != 0) {  // swizzled tiles need it; the same for every thread
         if (threadIdx.x == 0) {
             report_async(status, kAsyncBadIndex, 0x8FF);
-            ends[blockIdx.x] = WeighEnds{};
+            ends[blockIdx.x] = WeighEnds{0, 0, 0, 0, 0, 1, {}};
         }
         return;
     }
@@ -364,7 +365,7 @@ weigh_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
             // the two halves of the columns, then the key's place (or this CTA's partial sums)
             if (half == 1) {
                 ok = ok && (n == 0 || mbar_wait(&sm.j_empty[dd], (n - 1) & 1, abort));
-                sm.join[in_block] = total;
+                if (ok) sm.join[in_block] = total;  // (else the sums before it may still be read)
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sm.j_full[dd]);
             } else {
@@ -373,7 +374,11 @@ weigh_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sm.j_empty[dd]);
                 const int which = p.lo > p.t0 ? 0 : 1;
-                if (p.whole()) {
+                // (the other half's wait may have run out where this one's has not: it says so before it hands over its sum)
+                ok = ok && *abort == 0;
+                if (!ok) {
+                    // what stands in the pool stays: it is the sum of many steps
+                } else if (p.whole()) {
                     if (w >= 0) a.w[w] = old + total;
                 } else {
                     part[((int64_t)blockIdx.x * 2 + which) * kWtKeys + in_block] = total;
@@ -553,6 +558,7 @@ weigh_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
     }
     tc_fence_before();
     __syncthreads();
+    if (threadIdx.x == 0 && *abort != 0) ends[blockIdx.x].failed = 1;
     if (warp == 16) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
@@ -565,10 +571,11 @@ weigh_merge_kernel(const WeighArgs a, int TPT, const float* part, const WeighEnd
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int c = blockIdx.x;
     const WeighEnds e = ends[c];
-    if (e.open == 0) return;
+    if (e.open == 0 || e.failed != 0) return;
     float sum = part[((int64_t)c * 2 + 1) * kWtKeys + threadIdx.x];
     for (int i = c + 1; i < n_ctas; ++i) {
         const int first = ends[i].first;
+        if (ends[i].failed != 0) return;
         if (first == 3) break;
         if (first == 0) continue;
         sum += part[(int64_t)i * 2 * kWtKeys + threadIdx.x];

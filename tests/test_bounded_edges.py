@@ -88,3 +88,25 @@ def test_a_row_whose_lse_is_minus_infinity_gives_nothing_whatever_it_holds(new, 
         got = api.paged_weights(cache, bad, lse, start.clone(), 0.5)
         assert (got.double() - want).abs().le(tol + 1e-9).all(), value
     assert B.check_async_status() == (0, 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("lens", [[(70, 700), (100, 90)], [(300, 5000), (1, 40), (64, 3000)]])
+def test_a_wait_that_runs_out_leaves_weights_old_or_new(lens, fp8):
+    """The pool holds sums of many steps: nothing half added is written to it."""
+    cache = filled(batch(lens, 16, 2, 128, fp8, values=False))
+    q = queries(cache, 16)
+    start = torch.rand(cache.k.shape[0], 2, 16, device=DEV)
+    _, _, lse = reference(cache, q, None, start, 1.0)
+    want = api.paged_weights(cache, q, lse, start.clone(), 0.9)
+    assert B.check_async_status() == (0, 0)
+    try:
+        B.msa_debug_set_wait(20000, 2000000)  # 10 us against a copy role that is 1 ms late
+        got = api.paged_weights(cache, q, lse, start.clone(), 0.9)
+        assert B.check_async_status()[0] == 5
+    finally:
+        B.msa_debug_set_wait(0, 0)
+    assert ((got == start) | (got == want)).all()
+    assert torch.equal(api.paged_weights(cache, q, lse, start.clone(), 0.9), want)
+    assert B.check_async_status() == (0, 0)
