@@ -271,7 +271,7 @@ paged_compact_kernel(const CompactArgs a, int slices, int* status) {
     const int s = blockIdx.x / a.c.H_kv, head = blockIdx.x - s * a.c.H_kv, tid = threadIdx.x;
     const int32_t* keep = a.keep + (int64_t)blockIdx.x * a.width;
     const int32_t* table = a.c.table + (int64_t)s * a.c.max_pages;
-    const int len = (int)min((int64_t)max(a.c.kv_lens[s], 0), paged_places(a.c));
+    const int said = a.c.kv_lens[s], len = (int)min((int64_t)max(said, 0), paged_places(a.c));
     const bool values = (int)blockIdx.y >= slices, weights = blockIdx.y == 0 && a.w != nullptr;
     uint8_t* pool = a.pool[values];
     const int slice = values ? blockIdx.y - slices : blockIdx.y;
@@ -293,7 +293,8 @@ paged_compact_kernel(const CompactArgs a, int slices, int* status) {
         place = place_next;
         page_from = page_to = -2;
         if (place >= 0 && place < i) report_async(status, kAsyncBadIndex, 0xA03);  // (not ascending from 0)
-        if (place >= len) report_async(status, kAsyncBadIndex, 0xA01);
+        // (a bad length is reported where a place beyond it would be: a branch of its own cost 4 - 12 % by the code around it)
+        if (place >= len || (r == 0 && said != len)) report_async(status, kAsyncBadIndex, 0xA01);
         if (place > i && place < len) {
             page_from = table[(uint32_t)place / size];
             page_to = table[(uint32_t)i / size];

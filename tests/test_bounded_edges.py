@@ -110,3 +110,29 @@ def test_a_wait_that_runs_out_leaves_weights_old_or_new(lens, fp8):
     assert ((got == start) | (got == want)).all()
     assert torch.equal(api.paged_weights(cache, q, lse, start.clone(), 0.9), want)
     assert B.check_async_status() == (0, 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("heads", [1, 5])
+@pytest.mark.parametrize("length", [-4, 97, 10 ** 8])
+def test_compact_reports_bad_lengths(heads, length):
+    """Pages hold 96 places: a length beyond is cut down to them, one below zero to nothing."""
+    cache = batch([(0, 96), (0, 70)], 16, heads, 128, False)
+    lens = cache.kv_lens.clone()
+    lens[0] = length
+    keep = torch.full((2, heads, 4), -1, dtype=torch.int32, device=DEV)
+    before = cache.k.view(torch.int16).clone()
+    for places in ([], [2, 50, 95]):  # nothing to move, something
+        for i, p in enumerate(places):
+            keep[0, :, i] = p
+        cache.k.view(torch.int16).copy_(before)
+        api.paged_compact(cache._replace(kv_lens=lens), keep)
+        torch.cuda.synchronize()
+        assert B.check_async_status()[0] != 0, places
+        want, table = before.clone(), cache.page_table[0].long()
+        for i, p in enumerate(places if length > 0 else []):
+            want[table[0], i] = before[table[p // 16], p % 16]
+        assert torch.equal(cache.k.view(torch.int16), want)
+    lens[0] = 96
+    api.paged_compact(cache._replace(kv_lens=lens), keep)
+    assert B.check_async_status() == (0, 0)
