@@ -291,18 +291,19 @@ paged_compact_kernel(const CompactArgs a, int slices, int* status) {
     auto load_pages = [&](int r) {
         const int i = r * run + tid;
         place = place_next;
-        page_from = page_to = -2;
         if (place >= 0 && place < i) report_async(status, kAsyncBadIndex, 0xA03);  // (not ascending from 0)
         // (a bad length is reported where a place beyond it would be: a branch of its own cost 4 - 12 % by the code around it)
         if (place >= len || (r == 0 && said != len)) report_async(status, kAsyncBadIndex, 0xA01);
         if (place > i && place < len) {
             page_from = table[(uint32_t)place / size];
             page_to = table[(uint32_t)i / size];
+        } else {
+            place = -1;  // (it does not move)
         }
     };
     auto set_rows = [&](int r) {
         const int i = r * run + tid;
-        const bool moves = page_from != -2, good = page_from >= 0 && page_from < a.c.n_pages && page_to >= 0 && page_to < a.c.n_pages;
+        const bool moves = place >= 0, good = page_from >= 0 && page_from < a.c.n_pages && page_to >= 0 && page_to < a.c.n_pages;
         if (moves && !good) report_async(status, kAsyncBadIndex, 0xA02);
         s_from[r % 3][tid] = moves && good ? (int64_t)page_from * size + (uint32_t)place % size : 0;
         s_to[r % 3][tid] = moves && good ? (int64_t)page_to * size + (uint32_t)i % size : -1;

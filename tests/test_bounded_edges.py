@@ -136,3 +136,24 @@ def test_compact_reports_bad_lengths(heads, length):
     lens[0] = 96
     api.paged_compact(cache._replace(kv_lens=lens), keep)
     assert B.check_async_status() == (0, 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("entry", [-1, -2, -3, -2147483648, 2147483647])
+@pytest.mark.parametrize("which", [0, 3])
+def test_compact_reports_every_bad_page(entry, which):
+    """The page that a token comes from, or goes to, whatever number stands there."""
+    cache = batch([(0, 100)], 16, 2, 128, False)
+    before = [p.view(torch.int16).clone() for p in (cache.k, cache.v)]
+    bad = cache.page_table.clone()
+    bad[0, which] = entry
+    keep = torch.tensor([[[7, 50]] * 2], dtype=torch.int32, device=DEV)
+    api.paged_compact(cache._replace(page_table=bad), keep)
+    torch.cuda.synchronize()
+    assert B.check_async_status()[0] != 0
+    table = cache.page_table[0].long()
+    for p, b in zip((cache.k, cache.v), before):
+        want = b.clone()
+        if which == 3:
+            want[table[0], 0] = b[table[0], 7]
+        assert torch.equal(p.view(torch.int16), want)
