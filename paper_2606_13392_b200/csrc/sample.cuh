@@ -105,7 +105,7 @@ struct SampleRow {
     __device__ __forceinline__ uint4 load(int piece) const {
         const int at = index(piece);
         if (at >= 0 && at + E <= vocab) return __ldg(reinterpret_cast<const uint4*>(x + at));
-        T v[E];
+        alignas(16) T v[E];  // (read as one below)
 #pragma unroll
         for (int e = 0; e < E; ++e) v[e] = at + e >= 0 && at + e < vocab ? __ldg(x + at + e) : T(-INFINITY);
         return *reinterpret_cast<const uint4*>(v);

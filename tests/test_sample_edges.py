@@ -98,3 +98,14 @@ def test_more_equal_logits_than_a_list_holds_and_fewer_than_top_k(kind, rows):
     for k, p in ((5000, 0.9), (3151, 0.5), (3150, 0.9), (3149, 0.9), (5000, 1.0)):
         leave_traces(kind)
         check_written(x, u, 0.8, k, p, unclear=2)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float16, torch.float32])
+def test_rows_that_begin_and_end_anywhere(kind):
+    """Every place of the first and the last value in 16 bytes, rows of a piece or less among them."""
+    for vocab in (1, 3, 5, 7, 8, 9, 15, 17, 23, 1001):
+        wide, u = made(4, vocab + 16, kind, 3.0, vocab)
+        for lo in range(9):
+            for s in ((1.0, 0, 1.0, 0.0), (0.9, 4, 0.9, 0.0), (1.0, 0, 0.8, 0.0), (0.0, 0, 1.0, 0.0)):
+                check_written(wide[:, lo:lo + vocab], u, *s, unclear=1)
