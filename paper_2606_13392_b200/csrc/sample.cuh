@@ -323,7 +323,7 @@ __device__ __noinline__ void sample_slow(const SampleArgs a, int64_t row_number,
     };
     auto below = [&](float v) { return v == sc.top ? 0.0 : sc.below(v); };  // (the top may be infinite)
     auto weight_of = [&](float v) { return sc.weight(below(v)); };
-    // (all of what is kept where that is no more than `target`: a row may have fewer logits to choose from than top_k)
+    // (the target is at most all that there is: a row may have fewer logits to choose from than top_k)
     auto narrow = [&](bool by_mass, uint64_t target) {
         uint32_t prefix = 0;
         uint64_t want = target;
@@ -356,7 +356,7 @@ __device__ __noinline__ void sample_slow(const SampleArgs a, int64_t row_number,
                 mine += c[j];
             }
             uint64_t above = block_upto64(mine, sm.sums) - mine;
-            if (round == 0 && sm.sums[kSampleWarps] <= target) return;
+            if (round == 0) want = min(want, sm.sums[kSampleWarps]);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 if (above < want && above + c[j] >= want) { sm.found32[0] = d - j; sm.found64[0] = want - above; }  // (one thread)
