@@ -590,6 +590,7 @@ msa_status_t msa_paged_compact(const msa_paged_cache_t* cache, const int32_t* ke
  *   top_p        of these, largest first, the shortest run whose probabilities reach top_p of their sum stays (at least
  *                one token); 1 or more: all
  *   min_p        of these stay the ones whose probability is at least min_p times the largest; 0 or less: all
+ * A number that is NaN is an invalid argument; a NaN in a vector takes its row (below).
  */
 typedef struct {
     float temperature;
@@ -610,8 +611,8 @@ enum { MSA_BF16 = 0, MSA_FP16 = 1, MSA_FP32 = 2 };
  * be NULL) is the natural log of its probability among the kept.  Probabilities count in whole numbers of 2^-42 of the largest
  * (one of less than 2^-43 is never chosen) and are added as such, in any order: equal calls choose equal tokens.  A logit of
  * -infinity is never chosen; if there are logits of +infinity, one of them is.  A row with nothing to choose from (all
- * -infinity) or with a NaN (logits, u or T) gives -1 and NaN.  Rows of `vocab` (at most 2^21) values of logits_type start every
- * `stride` elements.
+ * -infinity) or with a NaN (logits, u, T, or - T above 0 - top_p or min_p) gives -1 and NaN.  Rows of `vocab` (at most 2^21) values
+ * of logits_type start every `stride` elements.
  */
 msa_status_t msa_sample(const msa_sampling_t* settings, const void* logits, int32_t logits_type, int64_t stride, int64_t n_rows,
                         int32_t vocab, const float* uniform, int64_t* token, float* logprob, msa_stream_t stream);

@@ -523,7 +523,8 @@ sample_kernel(const SampleArgs a) {
             top = warp_max(other->said.top);
             nan = __any_sync(0xffffffffu, other->said.nan != 0);
         }
-        nan |= !(temperature == temperature) || !(u == u);
+        // (a filter that is not a number filters nothing that could be meant; the largest logit asks for none)
+        nan |= !(temperature == temperature) || !(u == u) || (temperature > 0.f && !(top_p == top_p && min_p == min_p));
         if (nan || top == -INFINITY) {  // nothing to choose from
             if (threadIdx.x == 0 && rank == 0) {
                 a.token[r] = -1;

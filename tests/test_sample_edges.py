@@ -109,3 +109,31 @@ def test_rows_that_begin_and_end_anywhere(kind):
         for lo in range(9):
             for s in ((1.0, 0, 1.0, 0.0), (0.9, 4, 0.9, 0.0), (1.0, 0, 0.8, 0.0), (0.0, 0, 1.0, 0.0)):
                 check_written(wide[:, lo:lo + vocab], u, *s, unclear=1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", ["temperature", "top_p", "min_p"])
+def test_a_setting_that_is_not_a_number_takes_its_row(name):
+    """In a vector as in a number, which is refused: no filter is silently left out."""
+    rows = 12
+    x, u = made(rows, 4000, torch.bfloat16, 3.0, 2)
+    settings = dict(temperature=torch.full((rows,), 0.8, device=DEV), top_k=torch.full((rows,), 30, dtype=torch.int32, device=DEV),
+                    top_p=torch.full((rows,), 0.9, device=DEV), min_p=torch.full((rows,), 0.02, device=DEV))
+    settings["top_k"][::2] = 0
+    settings["min_p"][::3] = 0
+    want = [t.clone() for t in api.sample(x, u, **settings)]
+    assert (want[0] >= 0).all()
+    settings[name] = settings[name].clone()
+    settings[name][[1, 4, 6]] = math.nan
+    token, logprob = api.sample(x, u, **settings)
+    for r in range(rows):
+        if r in (1, 4, 6):
+            assert token[r] == -1 and logprob[r].isnan()
+        else:
+            assert token[r] == want[0][r] and logprob[r] == want[1][r]
+    if name != "temperature":  # the largest logit, whatever the rest says
+        settings["temperature"][:] = 0
+        token, logprob = api.sample(x, u, **settings)
+        assert torch.equal(token, x.float().argmax(1)) and (logprob == 0).all()
+    with pytest.raises(B.MsaError):
+        api.sample(x, u, **{name: math.nan})
