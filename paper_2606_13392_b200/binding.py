@@ -679,6 +679,11 @@ def _weight_pool(t: torch.Tensor, cache: MsaPagedCache, index: int) -> int:
     return t.data_ptr()
 
 
+def _int32(v: int) -> int:
+    """The nearest 32-bit number, for whole numbers that only bound something (ctypes would take the lowest 32 bits)."""
+    return v if -0x80000000 <= v <= 0x7FFFFFFF else (0x7FFFFFFF if v > 0 else -0x80000000)
+
+
 def msa_paged_weights_workspace_bytes(k_pool, n_q_heads: int) -> int:
     pages, size, heads, d = k_pool.shape
     cache = MsaPagedCache(n_pages=pages, page_size=size, n_kv_heads=heads, head_dim=d, fp8=0 if k_pool.dtype == torch.bfloat16 else 1)
@@ -703,9 +708,10 @@ def msa_paged_keep(k_pool, page_table, kv_lens, cu_q, weights, budget, sinks, re
     """-> (keep int32 [batch, KV heads, budget], new_lens int32 [batch]); those that are not given are made."""
     index, cache = _paged(k_pool, None, page_table, kv_lens, cu_q)
     at = _weight_pool(weights, cache, index)
+    sinks, recent = _int32(sinks), _int32(recent)
     keep = _made(keep, weights, (cache.batch, cache.n_kv_heads, max(budget, 0)), torch.int32, "keep", index, stream)
     new_lens = _made(new_lens, weights, (cache.batch,), torch.int32, "new_lens", index, stream)
-    _launch(index, "msa_paged_keep", ctypes.byref(cache), at, budget, sinks, recent, keep.data_ptr(), new_lens.data_ptr(), stream=stream)
+    _launch(index, "msa_paged_keep", ctypes.byref(cache), at, _int32(budget), sinks, recent, keep.data_ptr(), new_lens.data_ptr(), stream=stream)
     return keep, new_lens
 
 
@@ -726,7 +732,7 @@ _LOGIT_TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 def _setting(v, dtype, rows: int, index: int, what: str):
     """(number, device pointer) of a setting: a number for all rows or a tensor of one for every row."""
     if not isinstance(v, torch.Tensor):
-        return v, None
+        return (_int32(v) if dtype == torch.int32 else v), None
     if v.dtype != dtype or v.shape != (rows,) or not v.is_contiguous() or v.get_device() != index:
         raise ValueError("%s must be a number or a contiguous %s vector, one for each of %d rows, on cuda:%d" % (what, dtype, rows, index))
     return 0, v.data_ptr()

@@ -157,3 +157,16 @@ def test_compact_reports_every_bad_page(entry, which):
         if which == 3:
             want[table[0], 0] = b[table[0], 7]
         assert torch.equal(p.view(torch.int16), want)
+
+
+@pytest.mark.gpu
+def test_whole_numbers_beyond_32_bits_mean_what_they_say():
+    cache = batch([(0, 100), (0, 30)], 16, 2, 128, False, values=False)
+    w = torch.rand(cache.k.shape[0], 2, 16, device=DEV)
+    for many in (1 << 31, (1 << 32) + 3, 1 << 62):
+        for sinks, recent in ((many, 4), (0, many), (many, many)):
+            got, want = api.paged_keep(cache, w, 40, sinks, recent), api.paged_keep(cache, w, 40, min(sinks, 1000), min(recent, 1000))
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+        for bad in (dict(sinks=-many), dict(recent=-many), dict(budget=-many)):
+            with pytest.raises(B.MsaError):
+                api.paged_keep(cache, w, **(dict(budget=40) | bad))

@@ -137,3 +137,11 @@ def test_a_setting_that_is_not_a_number_takes_its_row(name):
         assert torch.equal(token, x.float().argmax(1)) and (logprob == 0).all()
     with pytest.raises(B.MsaError):
         api.sample(x, u, **{name: math.nan})
+
+
+@pytest.mark.gpu
+def test_whole_numbers_beyond_32_bits_mean_what_they_say():
+    x, u = made(40, 3000, torch.float32, 3.0, 9)
+    want = [t.clone() for t in api.sample(x, u)]
+    for k in (1 << 31, (1 << 32) + 5, (1 << 40) + 1, -(1 << 32) + 5, -(1 << 31) - 1):  # more than there are, or no limit
+        assert all(torch.equal(a, b) for a, b in zip(api.sample(x, u, top_k=k), want)), k
