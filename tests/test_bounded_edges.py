@@ -170,3 +170,47 @@ def test_whole_numbers_beyond_32_bits_mean_what_they_say():
         for bad in (dict(sinks=-many), dict(recent=-many), dict(budget=-many)):
             with pytest.raises(B.MsaError):
                 api.paged_keep(cache, w, **(dict(budget=40) | bad))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("hint", [1, 2, 5])
+def test_a_hint_below_the_longest_changes_little(hint, fp8):
+    cache = filled(batch([(1, 300), (45, 200), (6, 20), (0, 50)], 16, 2, 128, fp8, values=False))
+    q = queries(cache, 16)
+    start = torch.rand(cache.k.shape[0], 2, 16, device=DEV)
+    want, tol, lse = reference(cache, q, None, start, 0.7)
+    got = api.paged_weights(cache, q, lse, start.clone(), 0.7, max_new=hint)
+    assert (got.double() - want).abs().le(tol + 1e-9).all() and B.check_async_status() == (0, 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens", [[(1, 900), (1, 3000)], [(70, 700), (100, 90)]])
+def test_weights_and_moves_on_a_given_stream(lens):
+    """Their results, and that they run there: work that is queued on that stream comes first."""
+    cache = filled(batch(lens, 16, 2, 128, False), 1)
+    q = queries(cache, 16)
+    start = torch.rand(cache.k.shape[0], 2, 16, device=DEV)
+    _, _, lse = reference(cache, q, None, start, 0.7)
+    places = (cache.page_table, cache.kv_lens, cache.cu_q)
+    ws = B.alloc_workspace(B.msa_paged_weights_workspace_bytes(cache.k, 16), DEV)
+    weights = api.paged_weights(cache, q, lse, start.clone(), 0.7)
+    keep, _ = api.paged_keep(cache, weights, 64, 4, 8)
+    k, v, w = cache.k.clone(), cache.v.clone(), weights.clone()
+    api.paged_compact(cache._replace(k=k, v=v), keep, w)
+    side = torch.cuda.Stream()
+    late = [torch.zeros_like(t) for t in (start, cache.k, cache.v)]  # filled on the side stream, behind a long wait
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(40_000_000)
+        for t, source in zip(late, (start, cache.k, cache.v)):
+            t.view(torch.uint8).copy_(source.view(torch.uint8))
+    B.msa_paged_weights(late[1], *places, q, lse, 0.0, 0.7, late[0], ws, stream=side)
+    with torch.cuda.stream(side):
+        seen = late[0].clone()
+    B.msa_paged_compact(late[1], late[2], *places, keep, late[0], stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(seen, weights)
+    for a, b in zip(late, (w, k, v)):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    assert B.check_async_status() == (0, 0)
