@@ -164,7 +164,7 @@ struct SampleScale {
         c32 = fminf((float)c, 3e38f);
         tc = (double)top * c;
         ct = c * kSampleTable;
-        tct = (double)top * ct + kFront;
+        tct = fma((double)top, ct, kFront);  // (rounded once, or the top itself could come out half a step before itself)
     }
     // Distance to the top (in 32 bits it would be rounded); a top of infinity comes with sample_slow only.
     __device__ __forceinline__ double below(float v) const { return (double)top - (double)v; }

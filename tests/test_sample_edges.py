@@ -145,3 +145,16 @@ def test_whole_numbers_beyond_32_bits_mean_what_they_say():
     want = [t.clone() for t in api.sample(x, u)]
     for k in (1 << 31, (1 << 32) + 5, (1 << 40) + 1, -(1 << 32) + 5, -(1 << 31) - 1):  # more than there are, or no limit
         assert all(torch.equal(a, b) for a, b in zip(api.sample(x, u, top_k=k), want)), k
+
+
+@pytest.mark.gpu
+def test_the_largest_logit_is_at_no_distance_of_itself():
+    """Logits and temperatures whose product, rounded once more than it has to be, falls on the other side of a half: the largest
+    logit's place would come out in front of the first, where nothing weighs anything."""
+    pairs = [(352947.40625, 0.8524332046508789), (694587.375, 1.1001274585723877), (386510.59375, 0.8756565451622009),
+             (613832.8125, 0.9162696003913879), (497531.15625, 0.7205303907394409), (645018.25, 0.9723894000053406)]
+    for top, t in pairs:
+        x = torch.full((3, 2000), top - 80.0, device=DEV)
+        x[0, 1234] = x[1, 0] = x[2, [3, 1999]] = top
+        for k, p in ((0, 1.0), (50, 1.0), (0, 0.9), (20, 0.9)):
+            check_written(x, torch.full((3,), 0.6, device=DEV), t, k, p)
