@@ -214,6 +214,13 @@ __device__ __forceinline__ float2 exp2_by_arithmetic(float2 x) {
     return __fmul2_rn(r, make_float2(__int_as_float((__float_as_int(t.x) << 23) + 0x3F000000), __int_as_float((__float_as_int(t.y) << 23) + 0x3F000000)));
 }
 
+// n bits from bit `first` on, as far as 32 bits go.
+__device__ __forceinline__ uint32_t bits_from(uint32_t first, uint32_t n) {
+    uint32_t m;
+    asm("bmsk.clamp.b32 %0, %1, %2;" : "=r"(m) : "r"(first), "r"(n));
+    return m;
+}
+
 // Waits for this thread's loads from tensor memory; the registers are named so that nothing reads them earlier.
 __device__ __forceinline__ void tmem_landed(uint32_t (&r)[16]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;"
@@ -319,8 +326,8 @@ weigh_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 auto add = [&](auto masked) {  // (two loops: with the masks in one the selects bound it)
                     uint32_t seen[2];  // a bit for each column
                     for (int w = 0; w < 2; ++w) {
-                        const int lo = min(max(c_lo - 32 * w, 0), 32), hi = min(max(c_hi - 32 * w, 0), 32);
-                        seen[w] = (w == 0 ? live.x : live.y) & (lo < hi ? (0xFFFFFFFFu << lo) & (0xFFFFFFFFu >> (32 - hi)) : 0u);
+                        const int lo = max(c_lo - 32 * w, 0);
+                        seen[w] = (w == 0 ? live.x : live.y) & bits_from(lo, max(c_hi - 32 * w - lo, 0));
                     }
 #pragma unroll
                     for (int ch = 0; ch < 4; ++ch) {
@@ -370,12 +377,13 @@ weigh_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant_
                 if (lane == 0) mbar_arrive(&sm.j_full[dd]);
             } else {
                 ok = ok && mbar_wait(&sm.j_full[dd], n & 1, abort);
+                // (the other half's wait may have run out where this one's has not: it says so before it hands over its sum)
+                const int gone = *abort;
                 total += sm.join[in_block];
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&sm.j_empty[dd]);
                 const int which = p.lo > p.t0 ? 0 : 1;
-                // (the other half's wait may have run out where this one's has not: it says so before it hands over its sum)
-                ok = ok && *abort == 0;
+                ok = ok && gone == 0;
                 if (!ok) {
                     // what stands in the pool stays: it is the sum of many steps
                 } else if (p.whole()) {
