@@ -576,8 +576,8 @@ msa_status_t msa_paged_keep(const msa_paged_cache_t* cache, const float* weights
  * Moves token keep[s, h, i] of KV head h to place i of its sequence, for every i < width: its key, its value (cache->v may be
  * NULL) and its weight (weights may be NULL).  keep [batch, n_kv_heads, width] int32 as msa_paged_keep writes it: ascending
  * places below kv_lens[s] (still the old lengths), -1 = none; width is at most 2^30.  In place: what stood at places that nothing moves to
- * stays.  Sequences must not share pages.  A place that is not below the length, on a bad page or below its own i is
- * reported as a bad index and not moved; of a list that is not ascending the result is otherwise unspecified.
+ * stays.  Sequences must not share pages.  A place that is not below the length, below its own i, or - where it moves - on a bad
+ * page or to one is reported as a bad index and not moved; of a list that is not ascending the result is otherwise unspecified.
  */
 msa_status_t msa_paged_compact(const msa_paged_cache_t* cache, const int32_t* keep, int32_t width, float* weights,
                                msa_stream_t stream);

@@ -15,8 +15,8 @@ namespace msa {
 // to the lower place.  A cluster of CTAs per (sequence, head), each with a run of the middle whose keys it holds in shared memory,
 // finds the need-th largest by its bits, 11, 11 and 10 at a time: a count of the values of each digit, then the digit in which the
 // need-th falls.  Two more passes count and write the places in order: a warp owns a run, so only totals are exchanged.
-// Measured (8 heads): 4160 tokens of 32 sequences to 4096 13 us, bound by the rounds' latencies (some 1.5 us each of ten); 60000 -
-// 262144 of 3 prompts to 2048 38 us, a million of one to 4096 130 us (five passes over what a CTA holds, instructions).
+// Measured (8 heads): 4160 tokens of 32 sequences to 4096 13 - 15 us, bound by the rounds' latencies (some 1.5 us each of ten); 60000 -
+// 262144 of 3 prompts to 2048 38 - 44 us, a million of one to 4096 130 us (five passes over what a CTA holds, instructions).
 struct KeepArgs {
     PagedView c;
     const float* w;     // [n_pages, H_kv, page_size]
@@ -248,8 +248,8 @@ paged_keep_kernel(const KeepArgs a, int* status) {
 // keep is ascending: sources of a run of places lie behind the sources of the runs before and not before the run itself.
 // So a CTA that goes through the places in order, reading a run before writing it, is safe - and the slices of a row are
 // independent of each other, which is where the parallelism comes from: a CTA per (sequence, head, pool, slice of a row).
-// Measured (8 heads of 128): 4096 of 4160 tokens of 32 sequences 202 us, 81 % of the copy bandwidth; of one sequence of 8192 18 us;
-// 2048 of 30000 - 65536 of 3 prompts on fp8 20 us (bound by the chain place -> page -> row of two runs, and by launch).
+// Measured (8 heads of 128): 4096 of 4160 tokens of 32 sequences 203 us, 80 % of the copy bandwidth; of one sequence of 8192 18 us;
+// 2048 of 30000 - 65536 of 3 prompts on fp8 21 us (bound by the chain place -> page -> row of two runs, and by launch).
 struct CompactArgs {
     PagedView c;
     uint8_t* pool[2];     // keys and values; a null one is not moved

@@ -65,7 +65,7 @@ __device__ __forceinline__ float weigh_old(const WeighArgs& a, int64_t at, int k
 // element of the contraction a register holds is free, as long as the query fragments hold the same), 8 NT rows of
 // queries (token, head of the group) are its second.  A key's sum is then spread over four lanes.  The next tile's loads
 // are in flight meanwhile.  All tiles of all (sequence, head) form one line, of which every CTA takes an equal stretch.
-// Measured (64/8 heads): 64 sequences of one token on up to 32K 386 - 394 us, 97 - 99 % of the copy bandwidth; on up to 1000
+// Measured (64/8 heads): 64 sequences of one token on up to 32K 386 - 405 us, 94 - 99 % of the copy bandwidth; on up to 1000
 // 20 us; one token on 2K 4.8 us (latency: the stretch, places, keys, sums, one after the other).
 constexpr int kWeighFewRows = 32;
 constexpr int kWeighKeys = 16, kWeighWarps = 8, kWeighSegCost = 8;  // tiles' worth of a (sequence, head)'s beginning

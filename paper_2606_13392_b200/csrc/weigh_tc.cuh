@@ -6,8 +6,8 @@
 // tokens - stream past them; each tile is read once for two products.
 // One exponential for 2 * 128 flops: bound by the exponential unit (16 a cycle and SM; 4096 tokens on 28K have 8 10^9, 1.8 ms of
 // it at 1.9 GHz) at the clock that the board's power allows.
-// Measured (64/8 heads): 4096 tokens on 28K 2.36 - 2.45 ms, 0.84 - 0.87 PFLOP/s; on themselves 172 us; 512 on 7K 81 - 90 us; the
-// last 32 of 4 prompts of 8K - 16K 44 us; the last 17 - 48 of 6 prompts of up to 32K on fp8, 64/4 heads, 139 us.
+// Measured (64/8 heads): 4096 tokens on 28K 2.36 - 2.46 ms, 0.84 - 0.87 PFLOP/s; on themselves 170 us; 512 on 7K 80 - 90 us; the
+// last 32 of 4 prompts of 8K - 16K 45 us; the last 17 - 48 of 6 prompts of up to 32K on fp8, 64/4 heads, 139 us.
 // Looked at and not kept: the keys as operands in tensor memory (2.40 ms; windows 139 -> 165 us, the next keys wait for the last
 // products), without exponentials 1.95 ms, without anything but the products 1.65 ms (power), with loops that share code 2.58 ms.
 //
@@ -230,8 +230,8 @@ __device__ __forceinline__ void tmem_landed(uint32_t (&r)[16]) {
                  : "memory");
 }
 
-// One of eight pairs of columns takes its exponentials by arithmetic (4096 tokens on 28K: none 2.47 ms, one 2.36, two 2.42, three
-// 2.56: the exponential unit is relieved, but arithmetic costs issue slots and power).
+// One of eight pairs of columns takes its exponentials by arithmetic (4096 tokens on 28K: none 2.42 ms, one 2.38, two 2.43, three
+// 2.55: the exponential unit is relieved, but arithmetic costs issue slots and power).
 __host__ __device__ constexpr bool weigh_by_arithmetic(int pair) { return pair % 8 == 0; }
 template <bool V> struct Flag { static constexpr bool value = V; };
 
