@@ -537,7 +537,8 @@ sample_kernel(const SampleArgs a) {
     const bool greedy = !(temperature > 0.f);
     const double T_ = greedy ? 1.0 : (double)temperature;
     const SampleScale sc(top, T_, sm.table);
-    const double least = !greedy && min_p > 0.f ? fmax(0.0, -log((double)min_p) * T_) : INFINITY;
+    // (at an infinite T a min_p of one asks for zero times infinity: all are as likely as the largest)
+    const double least = !greedy && min_p > 0.f && (min_p != 1.f || T_ < INFINITY) ? fmax(0.0, -log((double)min_p) * T_) : INFINITY;
     const int k = greedy ? 1 : top_k;
     bool by_k = k > 0 && k < a.vocab;
     const bool by_p = !greedy && top_p < 1.f;

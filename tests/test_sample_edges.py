@@ -158,3 +158,19 @@ def test_the_largest_logit_is_at_no_distance_of_itself():
         x[0, 1234] = x[1, 0] = x[2, [3, 1999]] = top
         for k, p in ((0, 1.0), (50, 1.0), (0, 0.9), (20, 0.9)):
             check_written(x, torch.full((3,), 0.6, device=DEV), t, k, p)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kind", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("vocab", [400, 3000, 60000])
+def test_min_p_of_a_flat_distribution(kind, vocab):
+    """At an infinite temperature every logit is as likely as the largest, and at least once as likely."""
+    x, _ = made(5, vocab, kind, 3.0, 4)
+    u = torch.tensor([0.0, 0.2, 0.4, 0.7, 0.96], device=DEV)
+    for m in (1.0, 0.5, 0.0):
+        token, logprob = api.sample(x, u, math.inf, 0, 1.0, m)
+        assert token.tolist() == [int(float(v) * vocab) for v in u], m  # (sums of ones are exact)
+        assert torch.equal(logprob, torch.full((5,), -math.log(vocab), device=DEV))
+        order = x.float().argsort(dim=1, descending=True, stable=True)[:, :64].sort(dim=1).values
+        token, _ = api.sample(x, u, math.inf, 64, 1.0, m)
+        assert token.tolist() == [int(order[r, int(float(u[r]) * 64)]) for r in range(5)], m
